@@ -335,6 +335,155 @@ kvr_status kvr_gather_noalloc(const void *device_pool, const kvr_geometry *g, in
                               void *dst_device, void *stream);
 
 /*
+ * Operators over the paged cache (no counterpart in the paper, whose serving engine brings its own): what writes a
+ * token into the blocks this library hands out, what answers with them, what reads them back, and what keeps the
+ * accepted ones of drafted tokens.  They work on a pool in the layout above, take the engine's DEVICE arrays as they
+ * are, allocate nothing, enqueue on the given stream and return (they may be captured in a CUDA graph).  They run on
+ * the current device, which must be the stream's.  Ordering against this library's own moves is the caller's: kvr_wait()
+ * on a request before its blocks are read or written here, and a stream or event wait before it is suspended.
+ *
+ * A cache holds 16-bit elements as they are, or 8-bit codes with one fp32 scale per token, head and plane.  A token's
+ * row is then [kv_heads][head_dim] codes, the scales of all heads, unused bytes up to a multiple of 16: the scales lie in
+ * the row, so a move of valid rows takes them along, and a suspended request is half as large.  kvr_cache_geometry()
+ * gives the pool geometry of a cache.
+ *   E4M3 : scale = max(largest |x| * (1/448), 2^-126), code = x / scale rounded to the nearest e4m3 (ties to even)
+ *   INT8 : scale = max(largest |x| * (1/127), 2^-126), code = x / scale rounded to the nearest integer (ties to even)
+ * (all in fp32; the constant is rounded to fp32, and a code that this would push past 448 or 127 stays there).
+ * A head with an element that is not finite gets scale NaN: all of it reads back as NaN.
+ */
+enum { KVR_BF16 = 0, KVR_F16 = 1, KVR_F32 = 2 };                                             /* kvr_rows.type */
+enum { KVR_CACHE_BF16 = 0, KVR_CACHE_F16 = 1, KVR_CACHE_E4M3 = 2, KVR_CACHE_INT8 = 3 };     /* kvr_cache_spec.format */
+enum { KVR_ROPE_HALF = 0, KVR_ROPE_INTERLEAVED = 1 };                                       /* kvr_rope.style */
+
+typedef struct {
+  int32_t layers, kv_heads;
+  int32_t head_dim;          /* multiple of 16, at most 256 */
+  int32_t block_size, num_blocks;
+  int32_t format;            /* KVR_CACHE_* */
+  int32_t layout;            /* KVR_LAYER_MAJOR or KVR_BLOCK_MAJOR */
+} kvr_cache_spec;
+
+/* Rows of a DEVICE tensor [tokens][heads][head_dim]: strides in elements, the last dimension contiguous; data 16-byte
+ * aligned and both strides multiples of 16 bytes.  A projection's output holding q, k and v side by side is three of these. */
+typedef struct {
+  void *data;
+  int64_t token_stride, head_stride;
+  int32_t heads, type;       /* type: KVR_BF16, KVR_F16 or KVR_F32 */
+} kvr_rows;
+
+/*
+ * One step's requests.  Request r has context[r] tokens in the cache and new tokens token_start[r] .. token_start[r+1]-1
+ * (rows of q, k, v, out); its new token i is logical token context[r] + i, in slot j % block_size of block
+ * tables[r * table_stride + j / block_size].  All four arrays are DEVICE int32 and are read on the device only, so a
+ * captured graph follows them; max_new and max_tokens are bounds the caller knows on the host (they choose launch
+ * shapes; a request beyond them is an error the device reports).
+ * What the host cannot see is checked on the device: a request or token that does not fit (more than max_new new tokens,
+ * more than max_tokens or table_stride * block_size tokens in all, a token_start that goes backwards, a position outside
+ * the rotary table) is left out, a block id outside [0, num_blocks) is never addressed, and *status, if given, becomes
+ * one of KVR_DEV_*.  Outputs of what was left out are not written.
+ */
+#define KVR_DEV_BAD_BLOCK 3
+#define KVR_DEV_BAD_LENGTH 4
+#define KVR_DEV_BAD_POSITION 5
+#define KVR_DEV_BAD_INDEX 6
+typedef struct {
+  int32_t n_req, n_tokens;           /* n_tokens = token_start[n_req] */
+  int32_t max_new, max_tokens;       /* bounds of one request: new tokens, and context + new tokens */
+  int32_t table_stride;
+  const int32_t *token_start;        /* DEVICE [n_req + 1] */
+  const int32_t *context;            /* DEVICE [n_req] */
+  const int32_t *tables;             /* DEVICE [n_req][table_stride] */
+  int32_t *status;                   /* DEVICE or mapped HOST word, or NULL; only ever set, never cleared */
+} kvr_batch;
+
+/* Rotary positions: pair p of a head is turned by the angle whose (cos, sin) is table[position][p]. */
+typedef struct {
+  const float *table;                /* DEVICE [positions][rot_dim / 2][2], 16-byte aligned */
+  int32_t positions, rot_dim;        /* rot_dim: even, at most head_dim; channels beyond it pass unchanged */
+  int32_t style;                     /* KVR_ROPE_HALF: pairs (p, p + rot_dim/2); KVR_ROPE_INTERLEAVED: (2p, 2p + 1) */
+  int32_t inverse;                   /* != 0: turn back (the transpose) */
+} kvr_rope;
+
+/*
+ * Frequencies for contexts longer than the model was trained on.  theta_p = base^(-2p / rot_dim) becomes, with
+ * wavelength w = 2 pi / theta and the factor s:
+ *   KVR_SCALE_NONE    theta
+ *   KVR_SCALE_LINEAR  theta / s                                                    (position interpolation)
+ *   KVR_SCALE_BASE    base * s^(rot_dim / (rot_dim - 2)) in place of base          (rot_dim >= 4)
+ *   KVR_SCALE_BANDS   theta if w < original / high; theta / s if w > original / low; in between a blend that is linear
+ *                     in original / w: t = (original / w - low) / (high - low), theta * (t + (1 - t) / s)
+ *   KVR_SCALE_RAMP    a blend linear in p: with c(x) = rot_dim * ln(original / (2 pi x)) / (2 ln base),
+ *                     a = max(floor(c(high)), 0), b = min(ceil(c(low)), rot_dim - 1),
+ *                     t = 1 - clamp((p - a) / max(b - a, 0.001), 0, 1): theta * (t + (1 - t) / s); cos and sin are
+ *                     also multiplied by 0.1 ln(s) + 1 (s > 1)
+ * low and high count turns within the original context (BANDS: usually 1 and 4; RAMP: 1 and 32).
+ */
+enum { KVR_SCALE_NONE = 0, KVR_SCALE_LINEAR = 1, KVR_SCALE_BASE = 2, KVR_SCALE_BANDS = 3, KVR_SCALE_RAMP = 4 };
+typedef struct {
+  double base;                       /* > 1 */
+  double factor;                     /* s >= 1; not read with KVR_SCALE_NONE */
+  double low, high;                  /* 0 < low < high; BANDS and RAMP */
+  int32_t original;                  /* original context, > 0; BANDS and RAMP */
+  int32_t kind;                      /* KVR_SCALE_* */
+} kvr_rope_scaling;
+
+/* The pool geometry of a cache, for kvr_pool_create (a quantised row is given as one head of row bytes).
+ * KVR_ERR_INVALID_ARG (NULL), KVR_ERR_GEOMETRY. */
+kvr_status kvr_cache_geometry(const kvr_cache_spec *spec, kvr_geometry *out);
+
+/* rot_dim / 2 frequencies (HOST out) and the factor on cos and sin (may be NULL). */
+kvr_status kvr_rope_frequencies(const kvr_rope_scaling *s, int32_t rot_dim, double *freq, double *magnitude);
+/* Fill table_device [positions][rot_dim / 2][2] with the cos and sin of first .. first + positions - 1; angles are
+ * computed in fp64 and rounded once. */
+kvr_status kvr_rope_table(const kvr_rope_scaling *s, int32_t rot_dim, int32_t first, int32_t positions, float *table_device,
+                          void *stream);
+
+/*
+ * Write the new tokens of a step into one layer of the cache and turn q.  q, k, v: [n_tokens] rows of one type; k and v
+ * have kv_heads heads and go to the cache (k turned, v as it is); q, of any number of heads, goes turned to q_out (same
+ * type and heads; q_out may be q).  q with q_out, k and v may each be NULL; so may rope (nothing is turned).  positions:
+ * DEVICE int32 [n_tokens], or NULL: a token's position is its logical index.  Products and sums of a rotation are fp32,
+ * each rounded on its own; the result is rounded once to the output's type, or quantised as above.
+ */
+kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch,
+                            const kvr_rows *q, const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out,
+                            const kvr_rope *rope, const int32_t *positions, void *stream);
+
+/*
+ * Read tokens back: row token_start[r] + i of k and v (either may be NULL; any type) becomes logical token context[r] + i
+ * of request r, code times scale in fp32, rounded once.  With context 0 and token_start the lengths' sums these are whole requests.
+ */
+kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, int32_t layer, const kvr_batch *batch,
+                          const kvr_rows *k, const kvr_rows *v, void *stream);
+
+/*
+ * Attention of the new tokens over the cache (their own K and V are in it already).  Query head h reads KV head
+ * h / (q heads / kv_heads).  Row i of request r attends to all context[r] tokens and to those new tokens j of its request
+ * with bit j % 64 of mask[(token_start[r] + i) * mask_words + j / 64] set: the tree of drafted tokens, ancestors and
+ * itself; without a mask to j <= i.  mask: DEVICE, 64 * mask_words >= max_new.
+ *   out = softmax(scale * q K^T) V,  lse (DEVICE fp32 [n_tokens][q heads] or NULL) = ln of the sum of exponentials
+ * A row that attends to nothing gives out 0 and lse -infinity; what a row does not attend to has no influence on it,
+ * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
+ * the cache's type.  Scores, sums and accumulators are fp32; probabilities are rounded to the 16-bit type of the product with V.
+ * workspace: DEVICE, kvr_attend_workspace(spec) bytes, 256-byte aligned; its content is of no interest before or after,
+ * calls that may overlap need their own.
+ */
+uint64_t kvr_attend_workspace(const kvr_cache_spec *spec);
+kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *device_pool, int32_t layer, const kvr_batch *batch,
+                            const kvr_rows *q, const kvr_rows *out, float *lse, const uint64_t *mask, int32_t mask_words,
+                            float scale, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Keep the accepted ones of the new tokens, in all layers: for i < count[r] the row of new token index[r * index_stride + i]
+ * of request r moves, K and V, to new token i's place; the indices ascend and lie in [0, new tokens).  Afterwards the
+ * request has context[r] + count[r] tokens.  A request whose list is not like that is left as it was
+ * (KVR_DEV_BAD_INDEX).  Positions do not change: a drafted token is written with the position of its depth.
+ * index, count: DEVICE int32.
+ */
+kvr_status kvr_cache_keep(const kvr_cache_spec *spec, void *device_pool, const kvr_batch *batch, const int32_t *index,
+                          int32_t index_stride, const int32_t *count, void *stream);
+
+/*
  * Observe one request.  Any out pointer may be NULL.  blocks (cap entries) is
  * written for requests that hold blocks; host_image is a borrowed pointer into
  * the arena, valid while the request stays in HOST; arena_offset is its offset.

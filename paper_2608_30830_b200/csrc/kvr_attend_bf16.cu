@@ -1,0 +1,6 @@
+// The row kernel of attention over bf16 caches.
+#include "kvr_attend_rows.cuh"
+
+namespace kvr {
+cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, cudaStream_t s) { return launch_rows<KVR_CACHE_BF16>(a, tiles, slices, s); }
+}  // namespace kvr

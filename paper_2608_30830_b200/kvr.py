@@ -1,5 +1,6 @@
 """ctypes binding of libkvr.so: same names as the C ABI (include/kvr.h), argument marshalling only."""
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -18,6 +19,11 @@ FAIL_CUDA, FAIL_ALLOC = 0, 1
 LAYER_MAJOR, BLOCK_MAJOR = 0, 1
 KERNEL_WARP, KERNEL_BULK = 1, 2
 ALL = 2**64 - 1
+BF16, F16, F32 = 0, 1, 2
+CACHE_BF16, CACHE_F16, CACHE_E4M3, CACHE_INT8 = 0, 1, 2, 3
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_BANDS, SCALE_RAMP = 0, 1, 2, 3, 4
+DEV_BAD_BLOCK, DEV_BAD_LENGTH, DEV_BAD_POSITION, DEV_BAD_INDEX = 3, 4, 5, 6
 
 
 class KvrError(RuntimeError):
@@ -74,6 +80,28 @@ class Stats(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class CacheSpec(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layers", "kv_heads", "head_dim", "block_size", "num_blocks", "format", "layout")]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("heads", C.c_int32),
+                ("type", C.c_int32)]
+
+
+class BatchStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_req", "n_tokens", "max_new", "max_tokens", "table_stride")] + \
+               [(n, C.c_void_p) for n in ("token_start", "context", "tables", "status")]
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [("table", C.c_void_p)] + [(n, C.c_int32) for n in ("positions", "rot_dim", "style", "inverse")]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("base", "factor", "low", "high")] + [("original", C.c_int32), ("kind", C.c_int32)]
+
+
 EXPORTS = [
     "kvr_bytes_per_token", "kvr_pool_create", "kvr_pool_destroy", "kvr_request_admit", "kvr_request_admit_into", "kvr_request_release",
     "kvr_request_admit_sharing", "kvr_request_admit_sharing_into", "kvr_request_sharing", "kvr_block_refcount", "kvr_test_fail_nth", "kvr_test_points", "kvr_test_plan",
@@ -85,6 +113,8 @@ EXPORTS = [
     "kvr_policy_break_evens", "kvr_policy_host_ttl", "kvr_policy_replay", "kvr_policy_select",
     "kvr_controller_create", "kvr_controller_destroy", "kvr_controller_calibrate", "kvr_controller_suspend",
     "kvr_controller_advance", "kvr_controller_resume", "kvr_controller_get_stats",
+    "kvr_cache_geometry", "kvr_rope_frequencies", "kvr_rope_table", "kvr_cache_append", "kvr_cache_read",
+    "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep",
 ]
 
 _lib = None
@@ -200,6 +230,23 @@ def lib():
     L.kvr_read_load.argtypes = [vp, u64, i32, vp, vp]
     L.kvr_gather_noalloc.restype = i32
     L.kvr_gather_noalloc.argtypes = [vp, C.POINTER(Geometry), i32, pi32, i32, i64, vp, vp]
+    spec, batch, rows = C.POINTER(CacheSpec), C.POINTER(BatchStruct), C.POINTER(Rows)
+    L.kvr_cache_geometry.restype = i32
+    L.kvr_cache_geometry.argtypes = [spec, C.POINTER(Geometry)]
+    L.kvr_rope_frequencies.restype = i32
+    L.kvr_rope_frequencies.argtypes = [C.POINTER(RopeScaling), i32, pd, pd]
+    L.kvr_rope_table.restype = i32
+    L.kvr_rope_table.argtypes = [C.POINTER(RopeScaling), i32, i32, i32, vp, vp]
+    L.kvr_cache_append.restype = i32
+    L.kvr_cache_append.argtypes = [spec, vp, i32, batch, rows, rows, rows, rows, C.POINTER(RopeStruct), vp, vp]
+    L.kvr_cache_read.restype = i32
+    L.kvr_cache_read.argtypes = [spec, vp, i32, batch, rows, rows, vp]
+    L.kvr_attend_workspace.restype = u64
+    L.kvr_attend_workspace.argtypes = [spec]
+    L.kvr_cache_attend.restype = i32
+    L.kvr_cache_attend.argtypes = [spec, vp, i32, batch, rows, rows, vp, vp, i32, C.c_float, vp, u64, vp]
+    L.kvr_cache_keep.restype = i32
+    L.kvr_cache_keep.argtypes = [spec, vp, batch, vp, i32, vp, vp]
     _lib = L
     return L
 
@@ -560,3 +607,187 @@ class Pool:
     @property
     def host_arena_ptr(self):
         return lib().kvr_pool_host_arena(self._h)
+
+
+# ---- operators over the cache -------------------------------------------------------
+
+_FORMATS = {"bf16": CACHE_BF16, "f16": CACHE_F16, "e4m3": CACHE_E4M3, "int8": CACHE_INT8}
+_STYLES = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
+_torch = None        # the module, imported by the first call that is given a tensor
+_types = {}          # torch dtype -> kvr_rows.type
+_ref = C.byref
+
+
+def _use_torch():
+    global _torch
+    import torch
+    _types.update({torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32})
+    _torch = torch
+    return torch
+
+
+def _device():
+    """The current device's ordinal: every tensor of a call lies there."""
+    return (_torch or _use_torch()).cuda.current_device()
+
+
+def _array(t, what, dtype, dims, device):
+    """Device pointer of a dense array."""
+    if t.dtype is not dtype or t.dim() != dims or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("%s must be a contiguous %d-d tensor of %s on the current CUDA device" % (what, dims, dtype))
+    return t.data_ptr()
+
+
+def rows(t, head_dim=None, what="rows", device=None):
+    """kvr_rows of a torch tensor [tokens, heads, head_dim] (a view into a projection's output is fine)."""
+    if device is None:
+        device = _device()
+    stride, kind = t.stride(), _types.get(t.dtype)
+    if len(stride) != 3 or stride[2] != 1 or (head_dim is not None and t.shape[2] != head_dim):
+        raise ValueError("%s must be [tokens, heads, head_dim%s] with a dense last dimension" % (what, "" if head_dim is None else "=%d" % head_dim))
+    if kind is None or t.get_device() != device:
+        raise ValueError("%s must be bfloat16, float16 or float32 on the current CUDA device" % what)
+    return Rows(t.data_ptr(), stride[0], stride[1], t.shape[1], kind)
+
+
+def _stream(stream, device):
+    """A cudaStream_t; None is torch's current stream, which is also the one a graph is captured on."""
+    return _torch._C._cuda_getCurrentRawStream(device) if stream is None else stream
+
+
+def rope_frequencies(rot_dim, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0, high=4.0, original=0):
+    """kvr_rope_frequencies: (rot_dim / 2 frequencies, factor on cos and sin)."""
+    sc = RopeScaling(base, factor, low, high, original, kind)
+    f, m = np.zeros(max(rot_dim // 2, 1)), C.c_double()
+    _check(lib().kvr_rope_frequencies(C.byref(sc), rot_dim, _f64p(f), C.byref(m)))
+    return f, m.value
+
+
+def rope_table(out, first=0, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0, high=4.0, original=0, stream=None):
+    """kvr_rope_table into a float32 CUDA tensor [positions, rot_dim / 2, 2]."""
+    sc = RopeScaling(base, factor, low, high, original, kind)
+    dev = _device()
+    _check(lib().kvr_rope_table(C.byref(sc), 2 * out.shape[1], first, out.shape[0], _array(out, "out", _torch.float32, 3, dev),
+                                _stream(stream, dev)))
+
+
+class Rope:
+    """kvr_rope over a table of rope_table()."""
+
+    def __init__(self, table, rot_dim, style="half", inverse=False):
+        dev, shape = _device(), table.shape
+        if len(shape) != 3 or 2 * shape[1] != rot_dim or shape[2] != 2:
+            raise ValueError("table must be [positions, rot_dim / 2, 2]")
+        self.struct = RopeStruct(_array(table, "table", _torch.float32, 3, dev), shape[0], rot_dim, _STYLES[style], inverse)
+        self.table = table          # kept alive
+
+
+class Batch:
+    """kvr_batch over int32 CUDA tensors: token_start [n_req + 1], context [n_req], tables [n_req, blocks]; max_new and
+    max_tokens bound one request's new tokens and its tokens in all; status: an int32 CUDA tensor of one element, or None."""
+
+    def __init__(self, token_start, context, tables, max_new, max_tokens, status=None):
+        dev = _device()
+        i32, n, shape, stride = _torch.int32, context.shape[0], tables.shape, tables.stride()
+        if token_start.shape[0] != n + 1 or len(shape) != 2 or shape[0] != n:
+            raise ValueError("token_start has n_req + 1 entries, context n_req, tables n_req rows")
+        if tables.dtype is not i32 or tables.get_device() != dev or (shape[1] > 1 and stride[1] != 1) or (n > 1 and stride[0] < shape[1]):
+            raise ValueError("tables must be of int32 on the current CUDA device, with dense rows that do not overlap")
+        # a row's entries are counted by the stride: with one request, or rows cut from wider ones, by the shape alone
+        self.struct = BatchStruct(n, 0, max_new, max_tokens, stride[0] if n > 1 else shape[1],
+                                  _array(token_start, "token_start", i32, 1, dev), _array(context, "context", i32, 1, dev),
+                                  tables.data_ptr(), None if status is None else _array(status, "status", i32, 1, dev))
+        self.arrays = (token_start, context, tables, status)          # kept alive
+        self._ref = _ref(self.struct)
+
+    def of(self, n_tokens):
+        self.struct.n_tokens = n_tokens
+        return self._ref
+
+
+class Cache:
+    """A paged cache as the operators see it: its description only; the pool (device pointer or CUDA tensor) is given to
+    each call.  Errors raise KvrError, malformed tensors ValueError."""
+
+    def __init__(self, layers, kv_heads, head_dim, block_size, num_blocks, fmt="bf16", layout=LAYER_MAJOR):
+        self.spec = CacheSpec(layers, kv_heads, head_dim, block_size, num_blocks, _FORMATS.get(fmt, fmt), layout)
+        g = Geometry()
+        _check(lib().kvr_cache_geometry(C.byref(self.spec), C.byref(g)))
+        self.geometry = tuple(getattr(g, n) for n, _ in Geometry._fields_)         # for Pool(*geometry, num_blocks, ...)
+        self.row_bytes = g.kv_heads * g.head_dim * g.dtype_bytes                    # one token, one layer, K or V
+        self.pool_bytes = 2 * layers * num_blocks * block_size * self.row_bytes
+        self.head_dim = head_dim
+        self._spec = _ref(self.spec)
+        self._scale = 1.0 / math.sqrt(head_dim)
+        self._workspace = int(lib().kvr_attend_workspace(self._spec))
+
+    def _pool(self, pool, device):
+        if isinstance(pool, int):
+            return pool
+        if pool.numel() * pool.element_size() < self.pool_bytes or not pool.is_contiguous() or pool.get_device() != device:
+            raise ValueError("pool must be contiguous, of %d bytes at least, on the current CUDA device" % self.pool_bytes)
+        return pool.data_ptr()
+
+    def _rows(self, t, n, what, device):
+        if t is None:
+            return None
+        if t.shape[0] != n:
+            raise ValueError("%s must have %d tokens" % (what, n))
+        return _ref(rows(t, self.head_dim, what, device))
+
+    def append(self, pool, layer, batch, q=None, k=None, v=None, q_out=None, rope=None, positions=None, stream=None):
+        """kvr_cache_append: write k (turned) and v of the step's tokens into the cache, q turned to q_out."""
+        dev = _device()
+        n = (q if q is not None else k if k is not None else v).shape[0]
+        if positions is not None and positions.shape[0] != n:
+            raise ValueError("positions must have %d entries" % n)
+        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(q, n, "q", dev),
+                                   self._rows(k, n, "k", dev), self._rows(v, n, "v", dev), self._rows(q_out, n, "q_out", dev),
+                                   None if rope is None else _ref(rope.struct),
+                                   None if positions is None else _array(positions, "positions", _torch.int32, 1, dev), _stream(stream, dev))
+        if st:
+            _check(st)
+
+    def read(self, pool, layer, batch, k=None, v=None, stream=None):
+        """kvr_cache_read: the tokens [context, context + new) of each request into k and v."""
+        dev = _device()
+        n = (k if k is not None else v).shape[0]
+        st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(k, n, "k", dev),
+                                 self._rows(v, n, "v", dev), _stream(stream, dev))
+        if st:
+            _check(st)
+
+    def workspace_bytes(self):
+        """Bytes of attend()'s workspace."""
+        return self._workspace
+
+    def attend(self, pool, layer, batch, q, out, workspace, lse=None, mask=None, scale=None, stream=None):
+        """kvr_cache_attend: attention of the step's tokens over the cache.  mask: int64 [tokens, words], bit j of a row
+        set where the token looks at new token j of its request; None is causal.  scale: 1 / sqrt(head_dim) if None."""
+        dev = _device()
+        n, heads, _ = q.shape
+        if lse is not None and lse.shape != (n, heads):
+            raise ValueError("lse must be [tokens, query heads]")
+        if mask is not None and mask.shape[0] != n:
+            raise ValueError("mask must be [tokens, words]")
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+        st = _lib.kvr_cache_attend(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(q, n, "q", dev),
+                                   self._rows(out, n, "out", dev), None if lse is None else _array(lse, "lse", _torch.float32, 2, dev),
+                                   None if mask is None else _array(mask, "mask", _torch.int64, 2, dev),
+                                   0 if mask is None else mask.shape[1], self._scale if scale is None else scale,
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream, dev))
+        if st:
+            _check(st)
+
+    def keep(self, pool, batch, index, count, stream=None):
+        """kvr_cache_keep: the accepted ones of the step's tokens (index [n_req, n], ascending; count [n_req]) move to the
+        front, in all layers."""
+        dev, b = _device(), batch.struct
+        if index.shape[0] != b.n_req or count.shape[0] != b.n_req:
+            raise ValueError("index and count must have a row for each request")
+        st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(min(b.n_req * b.max_new, 2**31 - 1)),
+                                 _array(index, "index", _torch.int32, 2, dev), index.shape[1],
+                                 _array(count, "count", _torch.int32, 1, dev), _stream(stream, dev))
+        if st:
+            _check(st)
