@@ -382,6 +382,7 @@ typedef struct {
  * the rotary table) is left out, a block id outside [0, num_blocks) is never addressed, and *status, if given, becomes
  * one of KVR_DEV_*.  Outputs of what was left out are not written.
  */
+#define KVR_DEV_GAVE_UP 1        /* a bounded wait inside a kernel ran out: the call's outputs are not complete */
 #define KVR_DEV_BAD_BLOCK 3
 #define KVR_DEV_BAD_LENGTH 4
 #define KVR_DEV_BAD_POSITION 5

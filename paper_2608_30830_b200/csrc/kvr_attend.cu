@@ -143,9 +143,18 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   a.group_heads = (spec->kv_heads + a.head_groups - 1) / a.head_groups;
   const int slices = warps / a.group_heads;
   const int64_t rows = (int64_t)batch->max_new * group;
-  const int tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
-  a.row_tile = tiles * 8;
-  a.unit_keys = 16 * slices;
+  int tiles = 0;
+  if (rows > 32 && padded <= 128) {
+    // more rows than the row kernel keeps in registers
+    a.head_groups = spec->kv_heads;
+    a.group_heads = 1;
+    a.row_tile = rows <= 128 ? 128 : 256;
+    a.unit_keys = rows <= 128 ? 128 : 64;
+  } else {
+    tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
+    a.row_tile = tiles * 8;
+    a.unit_keys = 16 * slices;
+  }
   a.ctas = sms;
   a.part_ml = static_cast<float2 *>(workspace);
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)kMaxSms * 2 * kPartRows * 8);

@@ -120,8 +120,8 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int 
 // warps of a CTA of the row kernel: KV heads of a group x slices of the keys
 __host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim == 256 ? 4 : 8; }
 
-// The row kernel by cache format, one translation unit each (kvr_attend_<format>.cu); tiles: query rows of a segment / 8,
-// 1, 2 or 4 (at most 2 above 128 channels).
+// By cache format, one translation unit each (kvr_attend_<format>.cu).  tiles: of the row kernel, query rows of a segment / 8,
+// 1, 2 or 4 (at most 2 above 128 channels); 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment.
 cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
 cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
 cudaError_t launch_attend_e4m3(const AttendArgs &a, int tiles, int slices, cudaStream_t s);

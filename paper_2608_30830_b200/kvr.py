@@ -23,7 +23,7 @@ BF16, F16, F32 = 0, 1, 2
 CACHE_BF16, CACHE_F16, CACHE_E4M3, CACHE_INT8 = 0, 1, 2, 3
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_BANDS, SCALE_RAMP = 0, 1, 2, 3, 4
-DEV_BAD_BLOCK, DEV_BAD_LENGTH, DEV_BAD_POSITION, DEV_BAD_INDEX = 3, 4, 5, 6
+DEV_GAVE_UP, DEV_BAD_BLOCK, DEV_BAD_LENGTH, DEV_BAD_POSITION, DEV_BAD_INDEX = 1, 3, 4, 5, 6
 
 
 class KvrError(RuntimeError):
