@@ -466,7 +466,7 @@ kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, i
  * A row that attends to nothing gives out 0 and lse -infinity; what a row does not attend to has no influence on it,
  * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
  * the cache's type.  Scores, sums and accumulators are fp32; probabilities are rounded to the 16-bit type of the product with V.
- * workspace: DEVICE, kvr_attend_workspace(spec) bytes, 256-byte aligned; its content is of no interest before or after,
+ * At most 2^30 tokens in one request.  workspace: DEVICE, kvr_attend_workspace(spec) bytes, 256-byte aligned; its content is of no interest before or after,
  * calls that may overlap need their own.
  */
 uint64_t kvr_attend_workspace(const kvr_cache_spec *spec);

@@ -92,6 +92,27 @@ int sm_count() {
   return counts[dev];
 }
 
+// The layer's planes as [plane][block][token][head][channel]: boxes are `box_rows` tokens of one head, 128 bytes wide (128-byte
+// swizzle, the products' operand layout) or a whole 8-bit head; channels beyond head_dim read as zero.
+bool layer_map(const kvr_cache_spec *s, const CacheView &c, int padded, int box_rows, CUtensorMap *map) {
+  typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void *f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return false;
+  const bool quant = quantised(s->format);
+  const cuuint64_t element = quant ? 1 : 2;
+  const cuuint64_t dims[5] = {(cuuint64_t)s->head_dim, (cuuint64_t)s->kv_heads, (cuuint64_t)s->block_size, (cuuint64_t)s->num_blocks, 2};
+  const cuuint64_t strides[4] = {s->head_dim * element, (cuuint64_t)c.row_bytes, (cuuint64_t)c.block_stride, (cuuint64_t)c.v_offset};
+  const cuuint32_t box[5] = {(cuuint32_t)(quant ? padded : 64), 1, (cuuint32_t)box_rows, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+  return encode(map, quant ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, c.base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                quant ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 }  // namespace kvr
 
@@ -118,6 +139,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   if (q->heads % spec->kv_heads) return fail_cache(KVR_ERR_INVALID_ARG, "q's heads must be a multiple of kv_heads");
   const int group = q->heads / spec->kv_heads;
   if ((int64_t)batch->max_new * group > (1 << 28)) return fail_cache(KVR_ERR_INVALID_ARG, "too many new tokens in one request");
+  if (batch->max_tokens > (1 << 30)) return fail_cache(KVR_ERR_INVALID_ARG, "at most 2^30 tokens in one request");
   if (!std::isfinite(scale)) return fail_cache(KVR_ERR_INVALID_ARG, "scale must be finite");
   if (mask && (mask_words < 1 || (int64_t)mask_words * 64 < batch->max_new || ((uintptr_t)mask & 7)))
     return fail_cache(KVR_ERR_INVALID_ARG, "mask must be 8-byte aligned and have a bit for each of max_new tokens");
@@ -144,12 +166,15 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   const int slices = warps / a.group_heads;
   const int64_t rows = (int64_t)batch->max_new * group;
   int tiles = 0;
+  CUtensorMap map{};
   if (rows > 32 && padded <= 128) {
     // more rows than the row kernel keeps in registers
     a.head_groups = spec->kv_heads;
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
     a.unit_keys = rows <= 128 ? 128 : 64;
+    a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
+    if (a.box_rows && !layer_map(spec, a.c, padded, a.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
   } else {
     tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
     a.row_tile = tiles * 8;
@@ -161,10 +186,10 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   switch (spec->format) {
-    case KVR_CACHE_BF16: e = launch_attend_bf16(a, tiles, slices, s); break;
-    case KVR_CACHE_F16: e = launch_attend_f16(a, tiles, slices, s); break;
-    case KVR_CACHE_E4M3: e = launch_attend_e4m3(a, tiles, slices, s); break;
-    default: e = launch_attend_int8(a, tiles, slices, s);
+    case KVR_CACHE_BF16: e = launch_attend_bf16(a, tiles, slices, map, s); break;
+    case KVR_CACHE_F16: e = launch_attend_f16(a, tiles, slices, map, s); break;
+    case KVR_CACHE_E4M3: e = launch_attend_e4m3(a, tiles, slices, map, s); break;
+    default: e = launch_attend_int8(a, tiles, slices, map, s);
   }
   if (e != cudaSuccess) return fail_cache(KVR_ERR_CUDA, cudaGetErrorString(e));
   const long long joins = ((long long)batch->n_tokens * q->heads + kJoinThreads / 32 - 1) / (kJoinThreads / 32);

@@ -7,6 +7,8 @@
 // grid's size.  A CTA that holds a whole segment writes its result; the pieces of a cut segment go to the workspace as
 // (maximum, sum, accumulator) and are joined in the order of their keys, so results do not depend on timing.
 #pragma once
+#include <cuda.h>
+
 #include "kvr_cache.cuh"
 
 namespace kvr {
@@ -24,6 +26,7 @@ struct AttendArgs {
   int head_groups, group_heads;      // KV heads are taken group_heads at a time
   int row_tile;              // query rows of a segment
   int unit_keys;
+  int box_rows;              // tokens of a TMA box (tile kernel): 8 or 16, 0: the block size does not allow one
   int ctas;                  // the grid of the main kernel
   float *part_o;             // [ctas][2][group_heads][row_tile][head_dim]
   float2 *part_ml;           // [ctas][2][group_heads][row_tile]: maximum (log2), sum
@@ -121,10 +124,11 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int 
 __host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim == 256 ? 4 : 8; }
 
 // By cache format, one translation unit each (kvr_attend_<format>.cu).  tiles: of the row kernel, query rows of a segment / 8,
-// 1, 2 or 4 (at most 2 above 128 channels); 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment.
-cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
-cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
-cudaError_t launch_attend_e4m3(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
-cudaError_t launch_attend_int8(const AttendArgs &a, int tiles, int slices, cudaStream_t s);
+// 1, 2 or 4 (at most 2 above 128 channels); 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment, with its map of
+// the layer's K and V planes.
+cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
+cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
+cudaError_t launch_attend_e4m3(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
+cudaError_t launch_attend_int8(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
 
 }  // namespace kvr

@@ -3,7 +3,7 @@
 #include "kvr_attend_tiles.cuh"
 
 namespace kvr {
-cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, cudaStream_t s) {
-  return tiles ? launch_rows<KVR_CACHE_F16>(a, tiles, slices, s) : launch_tiles<KVR_CACHE_F16>(a, s);
+cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s) {
+  return tiles ? launch_rows<KVR_CACHE_F16>(a, tiles, slices, s) : launch_tiles<KVR_CACHE_F16>(a, map, s);
 }
 }  // namespace kvr

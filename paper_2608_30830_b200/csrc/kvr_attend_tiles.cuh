@@ -11,9 +11,10 @@
 // sums at the end of a piece.  S is double-buffered for each warpgroup, so the products of the next tile run under the
 // exponentials of this one.  Tensor memory: 2 x O (128 columns), 2 x 2 x S (64).
 //
-// 128 threads load.  16-bit caches: asynchronous copies into the ring, kLag tiles in flight.  8-bit caches: copies into
-// a private staging area (a thread widens what it copied itself), then to f16 in the ring, exactly; scales multiply scores
-// and probabilities as in the row kernel.
+// Loading: three warps bring the tiles in turn.  Where blocks are a multiple of 8 tokens a tile is a few TMA boxes (rows of one
+// head out of a block, swizzled on the way); the ragged end of a request, new tokens whose V has to be looked through, and
+// other block sizes go through 16-byte asynchronous copies.  8-bit codes land in a staging area that belongs to the warp, which
+// widens them to f16 into the ring, exactly.  Scales multiply scores and probabilities as in the row kernel.
 //
 // Every wait is bounded.  One that runs out sets a flag which all roles see, and the kernel ends in the ordinary way (copies
 // drained, products drained, tensor memory freed) with the status word set.
@@ -24,23 +25,27 @@ namespace kvr {
 namespace {
 
 constexpr int kTileKeys = 64;
-constexpr int kLoaders = 128, kSoftmax = 256, kTileThreads = kSoftmax + kLoaders + 32;
-constexpr unsigned kTileSpin = 1u << 20, kTileNap = 1000;               // tries, and nanoseconds that one may sleep
+constexpr int kSoftmax = 256;
+constexpr unsigned kTileSpin = 1u << 24;
 
 // ---- barriers, fences, tensor memory
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
+__device__ __forceinline__ bool bar_test(unsigned bar, unsigned parity) {
   unsigned ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity), "r"(kTileNap) : "memory");
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// false: the limit ran out here, or another role has given up
+// false: the limit ran out here, or another role has given up.  (try_wait, which may sleep, costs 250 clocks more than a test
+// on a barrier that is complete already: too much for the thread that issues the products.)
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *gave_up) {
   for (unsigned spin = 0; spin < kTileSpin; ++spin) {
-    if (bar_try(bar, parity)) return true;
-    if ((spin & 15) == 15 && *gave_up) return false;
+    if (bar_test(bar, parity)) return true;
+    if ((spin & 63) == 63) {
+      if (*gave_up) return false;
+      if (spin > 1024) __nanosleep(64);
+    }
   }
   *gave_up = 1;
   return false;
@@ -48,16 +53,33 @@ __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(unsigned bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The issuing warp runs in step, so that addresses stay in uniform registers; `leader` (one lane) is a predicate of the
+// instruction itself.
+__device__ __forceinline__ unsigned elect_one() {
+  unsigned r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
-__device__ __forceinline__ void tc_product_ss(unsigned d, unsigned long long a, unsigned long long b, unsigned desc, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((unsigned)add) : "memory");
+__device__ __forceinline__ void tc_commit(unsigned bar, unsigned leader) {
+  asm volatile("{\n\t.reg .pred l;\n\tsetp.ne.u32 l, %1, 0;\n\t"
+               "@l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void tc_product_ts(unsigned d, unsigned a, unsigned long long b, unsigned desc, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((unsigned)add) : "memory");
+// Shared-memory operand: rows of 128 bytes, 16-byte columns xor-ed with the row's number mod 8, 1024-byte groups of 8 rows
+// one after the other; `stride` bytes from one group of 64 elements of the other dimension to the next (unused along k).
+// The high word is the same for all: 1024 bytes between groups, descriptor version 1, 128-byte swizzle.
+constexpr unsigned kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ unsigned operand(unsigned addr, unsigned stride) { return (addr & 0x3ffffu) >> 4 | (stride >> 4) << 16; }
+
+// operands in shared memory are given by the low words of their descriptors
+__device__ __forceinline__ void tc_product_ss(unsigned d, unsigned a, unsigned b, unsigned desc, unsigned add, unsigned leader) {
+  asm volatile("{\n\t.reg .pred p, l;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 l, %6, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+               "@l tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(add), "n"(kOperandHigh), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void tc_product_ts(unsigned d, unsigned a, unsigned b, unsigned desc, unsigned add, unsigned leader) {
+  asm volatile("{\n\t.reg .pred p, l;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 l, %6, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+               "@l tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "r"(b), "r"(desc), "r"(add), "n"(kOperandHigh), "r"(leader) : "memory");
 }
 #define KVR_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define KVR_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -78,35 +100,71 @@ __device__ __forceinline__ void tm_store1(unsigned at, unsigned x) { asm volatil
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared-memory operand: rows of 128 bytes, 16-byte columns xor-ed with the row's number mod 8, 1024-byte groups of 8 rows
-// one after the other; `stride` bytes from one group of 64 elements of the other dimension to the next (unused along k).
-__device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned stride) {
-  return (unsigned long long)((addr & 0x3ffffu) >> 4) | (unsigned long long)(stride >> 4) << 16 | (unsigned long long)(1024 >> 4) << 32 |
-         1ull << 46 | 2ull << 61;
+__device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void box_load(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int head, int row, int block, int plane) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(head), "r"(row), "r"(block), "r"(plane) : "memory");
+}
+
+// pairs of fp32 in one 64-bit register
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float a, float b) { Pair r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpair(Pair v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
 template <int FMT, int DP>
 struct TileShape {
   static constexpr bool kQuant = quantised(FMT);
   static constexpr int kBlocks = DP / 64;                                // 128-byte columns of a row
+  static constexpr int kLoaders = 3, kProducts = 8 + kLoaders;           // loading warps; the warp that issues the products
+  static constexpr int kThreads = 384;
   static constexpr int kQBytes = 2 * 128 * DP * 2;                       // two tiles of 128 rows
   static constexpr int kBuffer = kTileKeys * DP * 2;                     // K or V of a tile, 16 bits
-  static constexpr int kRing = kQuant ? 6 : 9;
-  static constexpr int kLag = kQuant ? 6 : 5;                            // loads in flight, in buffers
+  static constexpr int kRing = kQuant ? 5 : 9;
   static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
-  static constexpr int kRawRing = kQuant ? kLag + 1 : 0;
+  static constexpr int kRawRing = kQuant ? 3 : 0;                        // for each loader
   static constexpr int kScaleSlots = kQuant ? 8 : 0;                     // 64 scales of K, 64 of V
-  static constexpr int kScaleRaw = kQuant ? kRawRing * kLoaders * 4 : 0;
-  static constexpr int kBytes = kQBytes + kRing * kBuffer + kRawRing * kRaw + kScaleSlots * 512 + kScaleRaw + 1024;
+  static constexpr int kBytes = kQBytes + kRing * kBuffer + kLoaders * kRawRing * (kRaw + kTileKeys * 4) + kScaleSlots * 512 + 1024;
 };
 
 struct TileBars {
   unsigned long long full[9], empty[9];
   unsigned long long s_full[2][2], p_full[2][2], pv_done[2][2], q_full, join, scale_full[8], drained;
+  unsigned long long raw_full[3][3];
+};
+
+// The order in which tiles are loaded and used: of a piece of n tiles K 0 .. ahead-1, then V t, K t + ahead, ...
+template <int AHEAD>
+struct TileWalk {
+  Piece p;
+  int t0, n, k, v, step, tiles;          // step and tiles (of K): since the CTA's start
+  bool more;
+  __device__ __forceinline__ void open(const AttendArgs &a, int unit_tiles) {
+    t0 = p.begin * unit_tiles;
+    n = min(p.end * unit_tiles, (p.len.keys + kTileKeys - 1) / kTileKeys) - t0;
+    k = v = 0;
+  }
+  __device__ __forceinline__ bool is_k() const { return k < n && k < v + AHEAD; }
+  __device__ __forceinline__ int tile() const { return t0 + (is_k() ? k : v); }
+  __device__ __forceinline__ int slot() const { return (is_k() ? tiles : tiles - (k - v)) & 7; }     // of the tile's scales
+  __device__ __forceinline__ void advance(const AttendArgs &a, int unit_tiles, long long last) {
+    ++step;
+    if (is_k()) { ++k; ++tiles; } else ++v;
+    if (v == n) {
+      more = next_piece(a, p, last);
+      if (more) open(a, unit_tiles);
+    }
+  }
 };
 
 template <int FMT, int DP, bool TWO>
-__global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(TileShape<FMT, DP>::kThreads, 1)
+attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
   using S = TileShape<FMT, DP>;
   constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
   constexpr int kAhead = TWO ? 2 : 4;            // key tiles whose scores are made before the first is used
@@ -118,10 +176,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
   __shared__ int gave_up_word;
   __shared__ unsigned long long odd_keys[9];     // by ring slot: keys of a V tile with elements that are not finite
   __shared__ float join_ml[128][2];
+  __shared__ int box_ids[3][64];                 // by loader: block ids of the boxes around its step
   volatile int *gave_up = &gave_up_word;
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   unsigned char *q_tile = smem, *ring = q_tile + S::kQBytes, *raw = ring + S::kRing * S::kBuffer;
-  float *scales = reinterpret_cast<float *>(raw + S::kRawRing * S::kRaw);
+  float *scales = reinterpret_cast<float *>(raw + S::kLoaders * S::kRawRing * S::kRaw);
   float *scale_raw = scales + S::kScaleSlots * 128;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -140,17 +199,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
 
   if (threadIdx.x == 0) {
     gave_up_word = 0;
-    for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), 4); bar_init(shared_at(&bars.empty[i]), 1); }
+    for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), 1); bar_init(shared_at(&bars.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) {
       for (int b = 0; b < 2; ++b) { bar_init(shared_at(&bars.s_full[w][b]), 1); bar_init(shared_at(&bars.p_full[w][b]), 4); bar_init(shared_at(&bars.pv_done[w][b]), 1); }
     }
     bar_init(shared_at(&bars.q_full), 8);
     bar_init(shared_at(&bars.join), 8);
     bar_init(shared_at(&bars.drained), 1);
-    for (int i = 0; i < 8; ++i) bar_init(shared_at(&bars.scale_full[i]), 4);
+    for (int i = 0; i < 8; ++i) {
+      bar_init(shared_at(&bars.scale_full[i]), 2);       // K's scales and V's
+      for (int k = 0; i < 3 && k < 3; ++k) bar_init(shared_at(&bars.raw_full[i][k]), 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == S::kProducts) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_at(&tm_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -161,214 +223,270 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
   const unsigned tm_o[2] = {tm, tm + 128};
   auto tm_s = [&](int w, int b) { return tm + 256 + (w * 2 + b) * 64; };
 
-  if (warp >= 8 && warp < 12) {
-    // ---- loaders: 16 keys of a tile a warp; K and V tiles in the order in which the products take them
-    const int w16 = (warp - 8) * 16, tid = threadIdx.x - kSoftmax;
-    constexpr int kChunks = DP * (kQuant ? 1 : 2) / 16, kAtOnce = 32 / kChunks, kCopies = 16 / kAtOnce;
+  if (warp >= 8 && warp < S::kProducts) {
+    // ---- loaders: a step (K or V of a tile) each
+    const int me = warp - 8;
+    constexpr int kElement = kQuant ? 1 : 2, kChunks = DP * kElement / 16, kAtOnce = 32 / kChunks;
     const int chunk = lane % kChunks, sub = lane / kChunks;
-    const int used = a.c.head_dim * (kQuant ? 1 : 2) / 16;
-    const int element = kQuant ? 1 : 2;
-    // the order within a piece of n tiles: K 0 .. ahead-1, then V t, K t + ahead, ...
-    struct Step { Piece p; int t0, n, k, v; bool more; } st;
-    st.p = piece; st.t0 = first_tile(piece); st.n = last_tile(piece) - st.t0; st.k = st.v = 0; st.more = true;
-    auto is_k = [&]() { return st.k < st.n && st.k < st.v + kAhead; };
-    auto advance = [&]() {
-      if (is_k()) ++st.k; else ++st.v;
-      if (st.v == st.n) {
-        st.more = next_piece(a, st.p, last);
-        if (st.more) { st.t0 = first_tile(st.p); st.n = last_tile(st.p) - st.t0; st.k = st.v = 0; }
-      }
-    };
-    // what the next copies need, fetched one step ahead
-    int next_id = 0, next_j = 0;
-    bool next_in = false;
+    const int used = a.c.head_dim * kElement / 16;
+    TileWalk<kAhead> at;
+    at.p = piece; at.step = at.tiles = 0; at.more = true;
+    at.open(a, unit_tiles);
+
+    // Ids of the blocks that the boxes of a piece lie in, 32 boxes at a time, a batch ahead of its use: V's steps are at most four
+    // tiles (32 boxes of 8 tokens) behind K's, so both find theirs among the last 64.
+    int *ids = box_ids[me];
+    const int per_tile = a.box_rows ? kTileKeys / a.box_rows : 0;
+    int box_next = 0, fetched = 0;       // first box of the batch in `fetched`
+    long long at_unit = -1;
     auto fetch = [&]() {
-      if (!st.more) return;
-      next_j = (st.t0 + (is_k() ? st.k : st.v)) * kTileKeys + w16 + (lane & 15);
-      next_in = next_j < st.p.len.keys;
-      next_id = next_in ? __ldg(a.b.tables + (long long)st.p.r * a.b.table_stride + a.bs.div(next_j)) : 0;
+      const int token = (box_next + lane) * a.box_rows;
+      fetched = token < at.p.len.keys ? __ldg(a.b.tables + (long long)at.p.r * a.b.table_stride + a.bs.div(token)) : -1;
     };
-    // of a step whose copies are under way: is it V, the tile's number in the call's order, does it hold new tokens
-    int issued = 0, done = 0, tiles_k = 0;
-    unsigned char kind[8];               // by step mod 8: bit 0 V, bit 1 look for odd values, bits 2..4 scale slot
-    bool ok = true;
-    auto issue = [&]() {                 // copies of the next step, if there is one
-      if (st.more) {
-        const bool v = !is_k();
-        const bool known = (unsigned)next_id < (unsigned)a.c.num_blocks, in = next_in && known;
-        if (!known) report(a.b.status, KVR_DEV_BAD_BLOCK);
-        const int within = next_j - (int)a.bs.div(next_j) * (int)a.bs.d;
-        const long long offset = in ? (long long)next_id * a.c.block_stride + (long long)within * a.c.row_bytes : 0;
-        const unsigned valid = __ballot_sync(0xffffffffu, in);
-        const char *plane = a.c.base + (v ? a.c.v_offset : 0);
-        const char *base = plane + st.p.head_group * a.c.head_dim * element;
-        unsigned dst;
-        if constexpr (kQuant) dst = shared_at(raw + (issued % S::kRawRing) * S::kRaw + tid * 16);
-        else dst = shared_at(ring + (issued % S::kRing) * S::kBuffer);
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int key = i * kAtOnce + sub;
-          const long long off = __shfl_sync(0xffffffffu, offset, key);
-          const bool got = (valid >> key & 1) && chunk < used;
-          const char *src = base + off + (got ? chunk * 16 : 0);
-          if constexpr (kQuant) copy16(dst + i * (kLoaders * 16), src, got);
-          else copy16(dst + (chunk >> 3) * (kTileKeys * 128) + (w16 + key) * 128 + (((chunk & 7) ^ (key & 7)) << 4), src, got);
-        }
-        if constexpr (kQuant) {
-          // lanes 0..15 of a warp bring its keys' scales
-          if (lane < 16) copy4(shared_at(scale_raw + (issued % S::kRawRing) * kLoaders + w16 + lane), plane + offset + (in ? a.c.scale_offset + 4 * st.p.head_group : 0), in);
-        }
-        const int slot = (v ? tiles_k - (st.k - st.v) : tiles_k) & 7;
-        const bool look = !kQuant && v && (st.t0 + st.v + 1) * kTileKeys > st.p.len.context && (st.p.len.fresh > 1 || a.mask);
-        kind[issued & 7] = (unsigned char)((v ? 1 : 0) | (look ? 2 : 0) | slot << 2);
-        if (!v) ++tiles_k;
-        ++issued;
-        advance();
+    auto have_ids = [&](int tile) {
+      if (at.p.unit != at_unit) {
+        at_unit = at.p.unit;
+        box_next = at.t0 * per_tile;
         fetch();
       }
-      copy_commit();
-    };
-    fetch();
-    auto slot_free = [&](int step) {     // has the buffer's previous tenant been used up?
-      if (step < S::kRing) return true;
-      bool good = true;
-      if (lane == 0) good = bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up);
-      return __shfl_sync(0xffffffffu, (int)good, 0) != 0;
-    };
-    // kLag - 1 steps ahead
-    for (int i = 0; i < S::kLag - 1; ++i) issue();       // kLag - 1 < kRing: these buffers are fresh
-    while (ok && (st.more || done < issued)) {
-      if constexpr (!kQuant) { if (st.more) ok = slot_free(issued); }
-      if (!ok) break;
-      issue();
-      copy_wait<S::kLag - 1>();
-      const int what = kind[done & 7];
-      unsigned char *buf = ring + (done % S::kRing) * S::kBuffer;
-      if constexpr (!kQuant) {
-        if (what & 2) {
-          // Elements of V that are not finite must not meet the zero probabilities of rows that do not see their key: they
-          // are set to zero here and added by the softmax threads, row by row.  A thread looks at what it copied.
-          unsigned odd = 0;
-          constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
-#pragma unroll
-          for (int i = 0; i < kCopies; ++i) {
-            const int key = i * kAtOnce + sub;
-            uint4 *at = reinterpret_cast<uint4 *>(buf + (chunk >> 3) * (kTileKeys * 128) + (w16 + key) * 128 + (((chunk & 7) ^ (key & 7)) << 4));
-            uint4 x = *at;
-            unsigned *e = reinterpret_cast<unsigned *>(&x);
-            bool any = false;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if ((e[j] & kExp) == kExp) { e[j] &= 0xffff0000u; any = true; }
-              if ((e[j] >> 16 & kExp) == kExp) { e[j] &= 0xffffu; any = true; }
-            }
-            if (any) { *at = x; odd |= 1u << key; }
-          }
-          odd = __reduce_or_sync(0xffffffffu, odd);
-          if (lane == 0) reinterpret_cast<unsigned short *>(&odd_keys[done % S::kRing])[warp - 8] = (unsigned short)odd;
-        } else if ((what & 1) && lane == 0) {
-          reinterpret_cast<unsigned short *>(&odd_keys[done % S::kRing])[warp - 8] = 0;
-        }
-      } else {
-        ok = slot_free(done);
-        if (!ok) break;
-        const unsigned char *mine = raw + (done % S::kRawRing) * S::kRaw + tid * 16;
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int key = i * kAtOnce + sub;
-          const uint4 x = *reinterpret_cast<const uint4 *>(mine + i * (kLoaders * 16));
-          // 16 channels, 32 bytes: two neighbouring 16-byte columns
-          unsigned char *row = buf + (chunk >> 2) * (kTileKeys * 128) + (w16 + key) * 128;
-          const int c0 = (chunk & 3) * 2;
-          *reinterpret_cast<uint4 *>(row + ((c0 ^ (key & 7)) << 4)) =
-              make_uint4(widen<FMT, false>(x.x), widen<FMT, true>(x.x), widen<FMT, false>(x.y), widen<FMT, true>(x.y));
-          *reinterpret_cast<uint4 *>(row + (((c0 + 1) ^ (key & 7)) << 4)) =
-              make_uint4(widen<FMT, false>(x.z), widen<FMT, true>(x.z), widen<FMT, false>(x.w), widen<FMT, true>(x.w));
-        }
-        if (lane < 16) scales[(what >> 2) * 128 + (what & 1) * 64 + w16 + lane] = scale_raw[(done % S::kRawRing) * kLoaders + w16 + lane];
+      while (box_next < (tile + 1) * per_tile) {
+        ids[(box_next + lane) & 63] = fetched;
+        box_next += 32;
+        fetch();
       }
-      fence_async();
       __syncwarp();
-      if (lane == 0) {
-        bar_arrive(shared_at(&bars.full[done % S::kRing]));
-        if (kQuant && (what & 1)) bar_arrive(shared_at(&bars.scale_full[what >> 2]));
-      }
-      ++done;
-    }
-    copy_wait<0>();
-  } else if (warp == 12) {
-    // ---- products, issued by one thread
-    if (lane == 0) {
-      constexpr unsigned kType = kBf16 ? 1u : 0u;
-      constexpr unsigned kS = 1u << 4 | kType << 7 | kType << 10 | (kTileKeys / 8) << 17 | (128 / 16) << 24;
-      constexpr unsigned kO = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
-      const unsigned q_at = shared_at(q_tile), ring_at = shared_at(ring);
-      int step = 0, jobs_s[2] = {0, 0}, jobs_p[2] = {0, 0}, pieces = 0;
-      bool ok = true, again = true;
-      auto take = [&]() { return bar_wait(shared_at(&bars.full[step % S::kRing]), (step / S::kRing) & 1, gave_up); };
-      auto scores = [&](int w) {                 // of the K tile in the current step's buffer
-        const unsigned k_at = ring_at + (step % S::kRing) * S::kBuffer, q = q_at + (TWO ? w : 0) * (128 * DP * 2);
-        const unsigned d = tm_s(w, jobs_s[w] & 1);
-#pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          tc_product_ss(d, operand(q + (k >> 2) * (128 * 128) + (k & 3) * 32, 16), operand(k_at + (k >> 2) * (kTileKeys * 128) + (k & 3) * 32, 16), kS, k > 0);
-        tc_commit(shared_at(&bars.s_full[w][jobs_s[w] & 1]));
-        ++jobs_s[w];
-      };
-      while (ok && again) {
-        const int n = last_tile(piece) - first_tile(piece);
-        int fresh[2] = {1, 1};                   // the first product of a piece overwrites O
-        ok = bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
-        ++pieces;
-        tc_after();
-        for (int t = 0; ok && t < min(kAhead, n); ++t) {
-          if (!(ok = take())) break;
-          tc_after();
-          if (TWO) { scores(0); scores(1); } else scores(t & 1);
-          tc_commit(shared_at(&bars.empty[step % S::kRing]));
-          ++step;
+    };
+    // K or V of a tile to dst, rows of 64 keys: boxes that complete on bar (true), or copies by this warp's lanes (false)
+    auto bring = [&](unsigned char *dst, unsigned long long *bar, bool v, int tile, bool look) {
+      const int key0 = tile * kTileKeys;
+      if (a.box_rows && !look && key0 + kTileKeys <= at.p.len.keys) {
+        have_ids(tile);
+        // a lane a box; 16-bit heads of 128 channels take two, side by side
+        constexpr int kWide = kQuant ? 1 : S::kBlocks;
+        const int box = lane / kWide, part = lane % kWide;
+        const int id = box < per_tile ? ids[(tile * per_tile + box) & 63] : 0;
+        if (__all_sync(0xffffffffu, (unsigned)id < (unsigned)a.c.num_blocks)) {
+          if (lane == 0) bar_expect(shared_at(bar), kTileKeys * DP * kElement);
+          __syncwarp();
+          if (box < per_tile) {
+            const int token = key0 + box * a.box_rows, row = token - (int)a.bs.div(token) * (int)a.bs.d;
+            unsigned char *to = kQuant ? dst + box * a.box_rows * DP : dst + part * (kTileKeys * 128) + box * a.box_rows * 128;
+            box_load(shared_at(to), &map, shared_at(bar), part * 64, at.p.head_group, row, id, v);
+          }
+          __syncwarp();
+          return true;
         }
-        for (int t = 0; ok && t < n; ++t) {
-          if (!(ok = take())) break;             // V of tile t
-          const unsigned v_at = ring_at + (step % S::kRing) * S::kBuffer;
-          const int v_slot = step % S::kRing;
-          ++step;
-          const bool next = t + kAhead < n;
-          bool have_next = false;
+      }
+      const char *base = a.c.base + (v ? a.c.v_offset : 0) + at.p.head_group * a.c.head_dim * kElement;
+#pragma unroll 1
+      for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+        const int key = i * kAtOnce + sub, j = key0 + key;
+        const long long off = j < at.p.len.keys ? token_offset(a.b, a.c, a.bs, at.p.r, j) : -1;
+        if (off < 0 && j < at.p.len.keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
+        const bool got = off >= 0 && chunk < used;
+        const char *src = got ? base + off + chunk * 16 : a.c.base;
+        if constexpr (kQuant) copy16(shared_at(dst + key * DP + chunk * 16), src, got);
+        else copy16(shared_at(dst + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4)), src, got);
+      }
+      return false;
+    };
+    bool ok = true;
+    auto slot_free = [&](int step) {     // has the buffer's previous tenant been used up?
+      return step < S::kRing || __all_sync(0xffffffffu, bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up));
+    };
+    auto mine = [&]() { while (at.more && at.step % S::kLoaders != me) at.advance(a, unit_tiles, last); };
+    mine();
+    if constexpr (!kQuant) {
+      while (at.more) {
+        const int slot = at.step % S::kRing, tile = at.tile();
+        const bool v = !at.is_k();
+        const bool look = v && (tile + 1) * kTileKeys > at.p.len.context && (at.p.len.fresh > 1 || a.mask);
+        if (!(ok = slot_free(at.step))) break;
+        unsigned char *buf = ring + slot * S::kBuffer;
+        if (!bring(buf, &bars.full[slot], v, tile, look)) {
+          copy_commit();
+          copy_wait<0>();
+          if (look) {
+            // Elements of V that are not finite must not meet the zero probabilities of rows that do not see their key: they
+            // are set to zero here and added by the softmax threads, row by row.  A thread looks at what it copied.
+            unsigned long long odd = 0;
+            constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
+#pragma unroll 1
+            for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+              const int key = i * kAtOnce + sub;
+              uint4 *x_at = reinterpret_cast<uint4 *>(buf + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4));
+              uint4 x = *x_at;
+              unsigned *e = reinterpret_cast<unsigned *>(&x);
+              bool any = false;
 #pragma unroll
-          for (int i = 0; i < (TWO ? 2 : 1); ++i) {
-            const int w = TWO ? i : t & 1, b = jobs_p[w] & 1;
-            if (!(ok = bar_wait(shared_at(&bars.p_full[w][b]), (jobs_p[w] >> 1) & 1, gave_up))) break;
-            tc_after();
-#pragma unroll
-            for (int k = 0; k < kTileKeys / 16; ++k)
-              tc_product_ts(tm_o[w], tm_s(w, b) + k * 8, operand(v_at + k * (16 * 128), kTileKeys * 128), kO, !fresh[w] || k > 0);
-            fresh[w] = 0;
-            tc_commit(shared_at(&bars.pv_done[w][b]));
-            ++jobs_p[w];
-            if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]));
-            if (next) {
-              if (!have_next) {
-                if (!(ok = take())) break;
-                tc_after();
-                have_next = true;
+              for (int q = 0; q < 4; ++q) {
+                if ((e[q] & kExp) == kExp) { e[q] &= 0xffff0000u; any = true; }
+                if ((e[q] >> 16 & kExp) == kExp) { e[q] &= 0xffffu; any = true; }
               }
-              scores(w);
+              if (any) { *x_at = x; odd |= 1ull << key; }
             }
+            const unsigned lo = __reduce_or_sync(0xffffffffu, (unsigned)odd), hi = __reduce_or_sync(0xffffffffu, (unsigned)(odd >> 32));
+            if (lane == 0) odd_keys[slot] = (unsigned long long)hi << 32 | lo;
           }
-          if (ok && next) {
-            tc_commit(shared_at(&bars.empty[step % S::kRing]));
-            ++step;
+          fence_async();
+          __syncwarp();
+          if (lane == 0) bar_arrive(shared_at(&bars.full[slot]));
+        }
+        at.advance(a, unit_tiles, last);
+        mine();
+      }
+    } else {
+      // this warp's steps: staged kRawRing - 1 ahead, then widened
+      unsigned char *stage = raw + (me * S::kRawRing) * S::kRaw;
+      float *scale_stage = scale_raw + (me * S::kRawRing) * kTileKeys;
+      int steps[S::kRawRing], kinds[S::kRawRing];        // by place: step, (V, boxes, scale slot)
+      int issued = 0, done = 0;
+      auto issue = [&](int place) {
+        if (at.more) {
+          const bool v = !at.is_k();
+          const int tile = at.tile();
+          const bool boxes = bring(stage + place * S::kRaw, &bars.raw_full[me][place], v, tile, false);
+#pragma unroll
+          for (int h = 0; h < kTileKeys; h += 32) {
+            const int j = tile * kTileKeys + h + lane;
+            long long off = -1;
+            if (boxes) {                 // all keys are there, their blocks' ids at hand
+              const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
+              off = (long long)ids[(a.box_rows == 16 ? j >> 4 : j >> 3) & 63] * a.c.block_stride + (long long)row * a.c.row_bytes;
+            } else if (j < at.p.len.keys) {
+              off = token_offset(a.b, a.c, a.bs, at.p.r, j);
+            }
+            const char *src = a.c.base + (v ? a.c.v_offset : 0) + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
+            copy4(shared_at(scale_stage + place * kTileKeys + h + lane), src, off >= 0);
+          }
+          steps[place] = at.step;
+          kinds[place] = (v ? 1 : 0) | (boxes ? 2 : 0) | at.slot() << 2;
+          ++issued;
+          at.advance(a, unit_tiles, last);
+          mine();
+        }
+        copy_commit();
+      };
+      unsigned phases = 0;               // of raw_full, by place
+#pragma unroll
+      for (int i = 0; i < S::kRawRing - 1; ++i) issue(i);
+      while (ok && (at.more || done < issued)) {
+#pragma unroll
+        for (int place = 0; place < S::kRawRing; ++place) {
+          if (!ok || !(at.more || done < issued)) break;
+          issue((place + S::kRawRing - 1) % S::kRawRing);
+          if (done >= issued) break;
+          copy_wait<S::kRawRing - 1>();
+          const int step = steps[place], kind = kinds[place], slot = step % S::kRing;
+          if (kind & 2) {
+            ok = __all_sync(0xffffffffu, bar_wait(shared_at(&bars.raw_full[me][place]), phases >> place & 1, gave_up));
+            phases ^= 1u << place;
+          }
+          __syncwarp();
+          ok = ok && slot_free(step);
+          if (!ok) break;
+          const unsigned char *src = stage + place * S::kRaw + sub * DP + chunk * 16;
+          // 16 channels of a key are two neighbouring 16-byte columns; which goes first alternates, so that the lanes of a
+          // quarter warp store to all banks
+          const int c0 = (chunk & 3) * 2, swap = (chunk >> 2) & 1;
+          unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + sub * 128;
+#pragma unroll 4
+          for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+            const int key = i * kAtOnce + sub;
+            const uint4 x = *reinterpret_cast<const uint4 *>(src + i * (kAtOnce * DP));
+            const uint4 lo = make_uint4(widen<FMT, false>(x.x), widen<FMT, true>(x.x), widen<FMT, false>(x.y), widen<FMT, true>(x.y));
+            const uint4 hi = make_uint4(widen<FMT, false>(x.z), widen<FMT, true>(x.z), widen<FMT, false>(x.w), widen<FMT, true>(x.w));
+            unsigned char *to = row + i * (kAtOnce * 128);
+            *reinterpret_cast<uint4 *>(to + (((c0 + swap) ^ (key & 7)) << 4)) = swap ? hi : lo;
+            *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) = swap ? lo : hi;
+          }
+          scales[(kind >> 2) * 128 + (kind & 1) * 64 + lane] = scale_stage[place * kTileKeys + lane];
+          scales[(kind >> 2) * 128 + (kind & 1) * 64 + 32 + lane] = scale_stage[place * kTileKeys + 32 + lane];
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            bar_arrive(shared_at(&bars.full[slot]));
+            bar_arrive(shared_at(&bars.scale_full[kind >> 2]));
+          }
+          ++done;
+        }
+      }
+      copy_wait<0>();
+      // boxes that a run given up left under way still write to shared memory: they end before the CTA does
+      for (int place = 0; !ok && place < S::kRawRing; ++place)
+        for (unsigned spin = 0; spin < 100000 && !bar_test(shared_at(&bars.raw_full[me][place]), phases >> place & 1); ++spin) {}
+    }
+  } else if (warp == S::kProducts) {
+    // ---- products: the warp runs in step, one lane issues
+    const unsigned leader = elect_one();
+    constexpr unsigned kType = kBf16 ? 1u : 0u;
+    constexpr unsigned kS = 1u << 4 | kType << 7 | kType << 10 | (kTileKeys / 8) << 17 | (128 / 16) << 24;
+    constexpr unsigned kO = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
+    const unsigned q_low = operand(shared_at(q_tile), 16), k_low = operand(shared_at(ring), 16), v_low = operand(shared_at(ring), kTileKeys * 128);
+    int slot = 0, round = 0;               // of the step: place in the ring, and how often it has come by
+    int jobs_s[2] = {0, 0}, jobs_p[2] = {0, 0}, pieces = 0;
+    bool ok = true, again = true;
+    auto take = [&]() { return bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); };
+    auto step_on = [&]() { if (++slot == S::kRing) { slot = 0; ++round; } };
+    auto scores = [&](int w) {                 // of the K tile in the current step's buffer
+      const unsigned k_at = k_low + slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16), d = tm_s(w, jobs_s[w] & 1);
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k)        // 16 channels: 32 bytes of a row; 64: the next 128-byte column
+        tc_product_ss(d, q + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, k_at + (k >> 2) * (kTileKeys * 128 / 16) + (k & 3) * 2, kS, k > 0, leader);
+      tc_commit(shared_at(&bars.s_full[w][jobs_s[w] & 1]), leader);
+      ++jobs_s[w];
+    };
+    while (ok && again) {
+      const int n = last_tile(piece) - first_tile(piece);
+      unsigned old[2] = {0, 0};                // the first product of a piece overwrites O
+      ok = bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
+      ++pieces;
+      tc_after();
+      for (int t = 0; ok && t < min(kAhead, n); ++t) {
+        if (!(ok = take())) break;
+        tc_after();
+        if (TWO) { scores(0); scores(1); } else scores(t & 1);
+        tc_commit(shared_at(&bars.empty[slot]), leader);
+        step_on();
+      }
+      for (int t = 0; ok && t < n; ++t) {
+        if (!(ok = take())) break;             // V of tile t
+        const int v_slot = slot;
+        const unsigned v_at = v_low + v_slot * (S::kBuffer / 16);
+        step_on();
+        const bool next = t + kAhead < n;
+#pragma unroll
+        for (int i = 0; i < (TWO ? 2 : 1); ++i) {
+          const int w = TWO ? i : t & 1, b = jobs_p[w] & 1;
+          if (!(ok = bar_wait(shared_at(&bars.p_full[w][b]), (jobs_p[w] >> 1) & 1, gave_up))) break;
+          tc_after();
+#pragma unroll
+          for (int k = 0; k < kTileKeys / 16; ++k)
+            tc_product_ts(tm_o[w], tm_s(w, b) + k * 8, v_at + k * (16 * 128 / 16), kO, k > 0 ? 1u : old[w], leader);
+          old[w] = 1;
+          tc_commit(shared_at(&bars.pv_done[w][b]), leader);
+          ++jobs_p[w];
+          if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]), leader);
+          if (next) {
+            if (i == 0) {
+              if (!(ok = take())) break;
+              tc_after();
+            }
+            scores(w);
           }
         }
-        again = next_piece(a, piece, last);
+        if (ok && next) {
+          tc_commit(shared_at(&bars.empty[slot]), leader);
+          step_on();
+        }
       }
-      // all products have ended before tensor memory is given back
-      tc_commit(shared_at(&bars.drained));
-      for (unsigned spin = 0; spin < kTileSpin && !bar_try(shared_at(&bars.drained), 0); ++spin) {}
+      again = next_piece(a, piece, last);
     }
+    // all products have ended before tensor memory is given back
+    tc_commit(shared_at(&bars.drained), leader);
+    for (unsigned spin = 0; spin < kTileSpin && !bar_test(shared_at(&bars.drained), 0); ++spin) {}
     __syncwarp();
-  } else {
+  } else if (warp < 8) {
     // ---- softmax: warpgroup w, thread = row
     const int w = warp >> 2, tid = threadIdx.x & 127;
     const unsigned lanes = (unsigned)(warp & 3) << 21;   // this warp's 32 lanes of tensor memory
@@ -455,8 +573,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
           if (!(ok = wait_all(&bars.scale_full[slot], (tile >> 3) & 1))) break;
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
-            const float4 k4 = *reinterpret_cast<const float4 *>(ks + i);
-            s[i] *= k4.x; s[i + 1] *= k4.y; s[i + 2] *= k4.z; s[i + 3] *= k4.w;
+            const ulonglong2 k4 = *reinterpret_cast<const ulonglong2 *>(ks + i);
+            const float2 x = unpair(mul2(pair(s[i], s[i + 1]), k4.x)), y = unpair(mul2(pair(s[i + 2], s[i + 3]), k4.y));
+            s[i] = x.x; s[i + 1] = x.y; s[i + 2] = y.x; s[i + 3] = y.y;
           }
         }
         const bool edge = key0 + kTileKeys > len.context;
@@ -485,10 +604,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
 #pragma unroll
           for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
         }
-        float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
+        float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
 #pragma unroll
-        for (int i = 4; i < 64; i += 4) { m0 = fmaxf(m0, s[i]); m1 = fmaxf(m1, s[i + 1]); m2 = fmaxf(m2, s[i + 2]); m3 = fmaxf(m3, s[i + 3]); }
-        m0 = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+        for (int i = 4; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
+        m0 = fmaxf(m0, m1);
         const float best = m0 == -INFINITY ? m0 : m0 * scale;
         float f = 1.f, f_unit = 1.f;     // of the sum, and of O's unit
         if (best > top + kLazy) {
@@ -525,19 +644,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
           tm_stored();
         }
         const float base = top == -INFINITY ? 0.f : top;
-        float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+        const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base);
+        Pair sum0 = 0, sum1 = 0;
 #pragma unroll
         for (int i = 0; i < 64; i += 4) {
-          s[i] = exp2_fast(fmaf(s[i], scale, -base)); s[i + 1] = exp2_fast(fmaf(s[i + 1], scale, -base));
-          s[i + 2] = exp2_fast(fmaf(s[i + 2], scale, -base)); s[i + 3] = exp2_fast(fmaf(s[i + 3], scale, -base));
-          a0 += s[i]; a1 += s[i + 1]; a2 += s[i + 2]; a3 += s[i + 3];
+          const float2 x = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), y = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
+          s[i] = exp2_fast(x.x); s[i + 1] = exp2_fast(x.y); s[i + 2] = exp2_fast(y.x); s[i + 3] = exp2_fast(y.y);
+          sum0 = add2(sum0, pair(s[i], s[i + 1]));
+          sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
         }
-        sum = sum * f + ((a0 + a1) + (a2 + a3));
+        const float2 sums = unpair(add2(sum0, sum1));
+        sum = sum * f + (sums.x + sums.y);
         if constexpr (kQuant) {
+          const Pair unit2 = pair(v_unit, v_unit);
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
-            const float4 v4 = *reinterpret_cast<const float4 *>(vs + i);
-            s[i] *= v4.x * v_unit; s[i + 1] *= v4.y * v_unit; s[i + 2] *= v4.z * v_unit; s[i + 3] *= v4.w * v_unit;
+            const ulonglong2 v4 = *reinterpret_cast<const ulonglong2 *>(vs + i);
+            const float2 x = unpair(mul2(pair(s[i], s[i + 1]), mul2(v4.x, unit2))), y = unpair(mul2(pair(s[i + 2], s[i + 3]), mul2(v4.y, unit2)));
+            s[i] = x.x; s[i + 1] = x.y; s[i + 2] = y.x; s[i + 3] = y.y;
           }
           if (edge) {                    // a scale that is not finite, at a key that the row does not see
 #pragma unroll
@@ -661,21 +785,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tiles_kernel(const __g
   tc_before();
   __syncthreads();
   tc_after();
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
+  if (warp == S::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
   if (threadIdx.x == 0 && gave_up_word) report(a.b.status, KVR_DEV_GAVE_UP);
 }
 
 template <int FMT, int DP, bool TWO>
-cudaError_t launch_tiles(const AttendArgs &a, cudaStream_t s) {
-  static const cudaError_t set = cudaFuncSetAttribute(attend_tiles_kernel<FMT, DP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<FMT, DP>::kBytes);
+cudaError_t launch_tiles(const AttendArgs &a, const CUtensorMap &map, cudaStream_t s) {
+  using S = TileShape<FMT, DP>;
+  const auto kernel = attend_tiles_kernel<FMT, DP, TWO>;
+  static const cudaError_t set = [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+  }();
   if (set != cudaSuccess) return set;
-  attend_tiles_kernel<FMT, DP, TWO><<<a.ctas, kTileThreads, TileShape<FMT, DP>::kBytes, s>>>(a);
+  kernel<<<a.ctas, S::kThreads, S::kBytes, s>>>(a, map);
   return cudaGetLastError();
 }
 template <int FMT>
-cudaError_t launch_tiles(const AttendArgs &a, cudaStream_t s) {
-  if (a.c.head_dim <= 64) return a.row_tile > 128 ? launch_tiles<FMT, 64, true>(a, s) : launch_tiles<FMT, 64, false>(a, s);
-  return a.row_tile > 128 ? launch_tiles<FMT, 128, true>(a, s) : launch_tiles<FMT, 128, false>(a, s);
+cudaError_t launch_tiles(const AttendArgs &a, const CUtensorMap &map, cudaStream_t s) {
+  if (a.c.head_dim <= 64) return a.row_tile > 128 ? launch_tiles<FMT, 64, true>(a, map, s) : launch_tiles<FMT, 64, false>(a, map, s);
+  return a.row_tile > 128 ? launch_tiles<FMT, 128, true>(a, map, s) : launch_tiles<FMT, 128, false>(a, map, s);
 }
 
 }  // namespace
