@@ -54,10 +54,11 @@ struct Piece {
   Lengths len;
 };
 __device__ __forceinline__ void open_piece(const AttendArgs &a, Piece &p, long long last) {
-  // requests without units are passed over
+  // requests without units are passed over (the bound on r cannot be met while p.unit is below the call's units)
   while (p.len.segments == 0 || p.unit - p.base >= (long long)p.len.units * p.len.segments) {
     p.base = p.unit;
-    p.len = attend_lengths(a, ++p.r);
+    if (++p.r >= a.b.n_req) { p.r = a.b.n_req - 1; p.len = Lengths{0, 0, 0, 0, 1, 1}; break; }
+    p.len = attend_lengths(a, p.r);
   }
   const int offset = (int)((p.unit - p.base) / p.len.units);
   p.begin = (int)((p.unit - p.base) - (long long)offset * p.len.units);

@@ -11,10 +11,14 @@
 // sums at the end of a piece.  S is double-buffered for each warpgroup, so the products of the next tile run under the
 // exponentials of this one.  Tensor memory: 2 x O (128 columns), 2 x 2 x S (64).
 //
-// Loading: three warps bring the tiles in turn.  Where blocks are a multiple of 8 tokens a tile is a few TMA boxes (rows of one
-// head out of a block, swizzled on the way); the ragged end of a request, new tokens whose V has to be looked through, and
+// Exponentials do not wait for their tile's maximum: they are taken against the maximum known before; only a row whose new
+// maximum is more than 2^kLazy higher (rare after the first tile) makes its warp rescale O and take them again.
+//
+// Loading: warps of their own bring the tiles in turn.  Where blocks are a multiple of 8 tokens a tile is a few TMA boxes (rows of
+// one head out of a block, swizzled on the way); the ragged end of a request, new tokens whose V has to be looked through, and
 // other block sizes go through 16-byte asynchronous copies.  8-bit codes land in a staging area that belongs to the warp, which
-// widens them to f16 into the ring, exactly.  Scales multiply scores and probabilities as in the row kernel.
+// widens them to f16 into the ring, exactly (six such warps, against three).  Scales multiply scores and probabilities as in
+// the row kernel.
 //
 // Every wait is bounded.  One that runs out sets a flag which all roles see, and the kernel ends in the ordinary way (copies
 // drained, products drained, tensor memory freed) with the status word set.
@@ -26,29 +30,32 @@ namespace {
 
 constexpr int kTileKeys = 64;
 constexpr int kSoftmax = 256;
-constexpr unsigned kTileSpin = 1u << 24;
+constexpr unsigned kTileSpin = 1u << 23;
 
 // ---- barriers, fences, tensor memory
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_test(unsigned bar, unsigned parity) {
+__device__ __forceinline__ bool bar_test(unsigned bar, unsigned parity, bool ask = true) {
   unsigned ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  asm volatile("{\n\t.reg .pred p, l;\n\tsetp.ne.u32 l, %3, 0;\n\tsetp.ne.u32 p, %3, %3;\n\t@l mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity), "r"((unsigned)ask) : "memory");
   return ok != 0;
 }
-// false: the limit ran out here, or another role has given up.  (try_wait, which may sleep, costs 250 clocks more than a test
-// on a barrier that is complete already: too much for the thread that issues the products.)
-__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *gave_up) {
+// A warp's wait.  Lane 0 asks for all: 32 lanes testing one barrier are served one after the other (200 to 400 clocks, and
+// try_wait, which may sleep, costs 250 even on a barrier that is complete).  The warp stays in step: the test is predicated and
+// its answer voted on, because what follows are instructions of the whole warp whose operands lie in uniform registers.
+// A wait that runs out, here or in another role, sets the flag and goes on like one that did not, on whatever is there: all
+// addresses stay in bounds, later waits give up at once, and the roles look at the flag once a step.
+__device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *gave_up) {
+  const bool ask = (threadIdx.x & 31) == 0;
   for (unsigned spin = 0; spin < kTileSpin; ++spin) {
-    if (bar_test(bar, parity)) return true;
-    if ((spin & 63) == 63) {
-      if (*gave_up) return false;
-      if (spin > 1024) __nanosleep(64);
+    if (__any_sync(0xffffffffu, bar_test(bar, parity, ask))) {
+      __syncwarp();                    // what lane 0 has been shown by the barrier all lanes see
+      return;
     }
+    if ((spin & 63) == 63 && __any_sync(0xffffffffu, *gave_up != 0)) return;
   }
   *gave_up = 1;
-  return false;
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -121,21 +128,23 @@ template <int FMT, int DP>
 struct TileShape {
   static constexpr bool kQuant = quantised(FMT);
   static constexpr int kBlocks = DP / 64;                                // 128-byte columns of a row
-  static constexpr int kLoaders = 3, kProducts = 8 + kLoaders;           // loading warps; the warp that issues the products
-  static constexpr int kThreads = 384;
+  // Loading warps (no more than buffers: a loader waits for step s - kRing to be used up having filled step s - kLoaders, and
+  // a barrier's parity is clear only if step s - 2 kRing is known to be over); the warp that issues the products.
+  static constexpr int kLoaders = kQuant ? 6 : 3, kProducts = 8 + kLoaders;
+  static constexpr int kThreads = kQuant ? 512 : 384;                    // whole warpgroups: registers are dealt out to those
   static constexpr int kQBytes = 2 * 128 * DP * 2;                       // two tiles of 128 rows
   static constexpr int kBuffer = kTileKeys * DP * 2;                     // K or V of a tile, 16 bits
-  static constexpr int kRing = kQuant ? 5 : 9;
+  static constexpr int kRing = kQuant ? 6 : 9;
+  static_assert(kLoaders <= kRing, "");
   static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
-  static constexpr int kRawRing = kQuant ? 3 : 0;                        // for each loader
   static constexpr int kScaleSlots = kQuant ? 8 : 0;                     // 64 scales of K, 64 of V
-  static constexpr int kBytes = kQBytes + kRing * kBuffer + kLoaders * kRawRing * (kRaw + kTileKeys * 4) + kScaleSlots * 512 + 1024;
+  static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? kLoaders : 0) * (kRaw + kTileKeys * 4) + kScaleSlots * 512 + 1024;
 };
 
 struct TileBars {
   unsigned long long full[9], empty[9];
   unsigned long long s_full[2][2], p_full[2][2], pv_done[2][2], q_full, join, scale_full[8], drained;
-  unsigned long long raw_full[3][3];
+  unsigned long long raw_full[6];
 };
 
 // The order in which tiles are loaded and used: of a piece of n tiles K 0 .. ahead-1, then V t, K t + ahead, ...
@@ -162,13 +171,38 @@ struct TileWalk {
   }
 };
 
+// Which of the keys key0 .. key0 + 63 a row sees: bit i is key0 + i.  The context, then the row's own bits, nothing behind the
+// request's last new token.  For tiles that reach beyond the context (key0 + 64 > context).
+__device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const Lengths &len, int key0, bool have, int t_row) {
+  const int off = key0 - len.context;
+  unsigned long long vis = 0;
+  if (off < 0) vis = ~0ull >> (64 + off);                       // -off low bits (off > -64)
+  if (have) {
+    unsigned long long fresh = 0;                                // bit i: new token off + i
+    if (a.mask) {
+      const unsigned long long *m = a.mask + (long long)(len.first + t_row) * a.mask_words;
+      const int lo = off >> 6, sh = off & 63;                    // floor, also for negative off
+      const unsigned long long w0 = lo >= 0 && lo < a.mask_words ? __ldg(m + lo) : 0ull;
+      const unsigned long long w1 = lo + 1 >= 0 && lo + 1 < a.mask_words ? __ldg(m + lo + 1) : 0ull;
+      fresh = sh ? w0 >> sh | w1 << (64 - sh) : w0;
+    } else {
+      const int upto = t_row - off + 1;                          // tokens off .. t_row
+      fresh = upto <= 0 ? 0ull : upto >= 64 ? ~0ull : ~0ull >> (64 - upto);
+    }
+    const int room = len.fresh - off;                            // tokens there are from off on
+    if (room <= 0) fresh = 0; else if (room < 64) fresh &= ~0ull >> (64 - room);
+    vis |= off < 0 ? fresh & ~(~0ull >> (64 + off)) : fresh;
+  }
+  return vis;
+}
+
 template <int FMT, int DP, bool TWO>
 __global__ void __launch_bounds__(TileShape<FMT, DP>::kThreads, 1)
 attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
   using S = TileShape<FMT, DP>;
   constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
   constexpr int kAhead = TWO ? 2 : 4;            // key tiles whose scores are made before the first is used
-  constexpr float kLazy = 4.f;
+  constexpr float kLazy = kQuant ? 4.f : 8.f;    // 8-bit: leaves room for V's scale, see the row kernel
   extern __shared__ unsigned char raw_smem[];
   __shared__ long long scratch[34];
   __shared__ __align__(8) TileBars bars;
@@ -176,13 +210,18 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ int gave_up_word;
   __shared__ unsigned long long odd_keys[9];     // by ring slot: keys of a V tile with elements that are not finite
   __shared__ float join_ml[128][2];
-  __shared__ int box_ids[3][64];                 // by loader: block ids of the boxes around its step
+  __shared__ int box_ids[S::kLoaders][64];                 // by loader: block ids of the boxes around its step
   volatile int *gave_up = &gave_up_word;
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   unsigned char *q_tile = smem, *ring = q_tile + S::kQBytes, *raw = ring + S::kRing * S::kBuffer;
-  float *scales = reinterpret_cast<float *>(raw + S::kLoaders * S::kRawRing * S::kRaw);
+  float *scales = reinterpret_cast<float *>(raw + (kQuant ? S::kLoaders : 0) * S::kRaw);
   float *scale_raw = scales + S::kScaleSlots * 128;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // Roles: 0..7 softmax, 8.. loaders, then the products.  The scheduler prefers older warps, and the short chains of the products
+  // and the loaders must not queue behind exponentials: they are the CTA's first warps.
+  constexpr int kOthers = S::kThreads / 32 - 8;
+  const int lane = threadIdx.x & 31, first_warps = (int)(threadIdx.x >> 5);
+  const int warp = first_warps >= kOthers ? first_warps - kOthers : first_warps == 0 ? S::kProducts :
+                   first_warps <= S::kLoaders ? 7 + first_warps : S::kProducts + 1;      // the last has no role
 
   const long long total = total_units(a, scratch);
   const int ctas = (int)min((long long)a.ctas, total);
@@ -208,7 +247,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     bar_init(shared_at(&bars.drained), 1);
     for (int i = 0; i < 8; ++i) {
       bar_init(shared_at(&bars.scale_full[i]), 2);       // K's scales and V's
-      for (int k = 0; i < 3 && k < 3; ++k) bar_init(shared_at(&bars.raw_full[i][k]), 1);
+      if (i < 6) bar_init(shared_at(&bars.raw_full[i]), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -292,7 +331,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     };
     bool ok = true;
     auto slot_free = [&](int step) {     // has the buffer's previous tenant been used up?
-      return step < S::kRing || __all_sync(0xffffffffu, bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up));
+      if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up);
+      return __any_sync(0xffffffffu, *gave_up != 0) == 0;
     };
     auto mine = [&]() { while (at.more && at.step % S::kLoaders != me) at.advance(a, unit_tiles, last); };
     mine();
@@ -336,85 +376,64 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         mine();
       }
     } else {
-      // this warp's steps: staged kRawRing - 1 ahead, then widened
-      unsigned char *stage = raw + (me * S::kRawRing) * S::kRaw;
-      float *scale_stage = scale_raw + (me * S::kRawRing) * kTileKeys;
-      int steps[S::kRawRing], kinds[S::kRawRing];        // by place: step, (V, boxes, scale slot)
-      int issued = 0, done = 0;
-      auto issue = [&](int place) {
-        if (at.more) {
-          const bool v = !at.is_k();
-          const int tile = at.tile();
-          const bool boxes = bring(stage + place * S::kRaw, &bars.raw_full[me][place], v, tile, false);
+      // a step's codes and scales come to this warp's stage and are widened into the ring
+      unsigned char *stage = raw + me * S::kRaw;
+      float *scale_stage = scale_raw + me * kTileKeys;
+      unsigned phase = 0;                // of raw_full
+      while (at.more) {
+        const bool v = !at.is_k();
+        const int tile = at.tile(), slot = at.step % S::kRing, scale_slot = at.slot();
+        const bool boxes = bring(stage, &bars.raw_full[me], v, tile, false);
 #pragma unroll
-          for (int h = 0; h < kTileKeys; h += 32) {
-            const int j = tile * kTileKeys + h + lane;
-            long long off = -1;
-            if (boxes) {                 // all keys are there, their blocks' ids at hand
-              const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
-              off = (long long)ids[(a.box_rows == 16 ? j >> 4 : j >> 3) & 63] * a.c.block_stride + (long long)row * a.c.row_bytes;
-            } else if (j < at.p.len.keys) {
-              off = token_offset(a.b, a.c, a.bs, at.p.r, j);
-            }
-            const char *src = a.c.base + (v ? a.c.v_offset : 0) + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
-            copy4(shared_at(scale_stage + place * kTileKeys + h + lane), src, off >= 0);
+        for (int h = 0; h < kTileKeys; h += 32) {
+          const int j = tile * kTileKeys + h + lane;
+          long long off = -1;
+          if (boxes) {                   // all keys are there, their blocks' ids at hand
+            const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
+            off = (long long)ids[(a.box_rows == 16 ? j >> 4 : j >> 3) & 63] * a.c.block_stride + (long long)row * a.c.row_bytes;
+          } else if (j < at.p.len.keys) {
+            off = token_offset(a.b, a.c, a.bs, at.p.r, j);
           }
-          steps[place] = at.step;
-          kinds[place] = (v ? 1 : 0) | (boxes ? 2 : 0) | at.slot() << 2;
-          ++issued;
-          at.advance(a, unit_tiles, last);
-          mine();
+          const char *src = a.c.base + (v ? a.c.v_offset : 0) + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
+          copy4(shared_at(scale_stage + h + lane), src, off >= 0);
         }
         copy_commit();
-      };
-      unsigned phases = 0;               // of raw_full, by place
-#pragma unroll
-      for (int i = 0; i < S::kRawRing - 1; ++i) issue(i);
-      while (ok && (at.more || done < issued)) {
-#pragma unroll
-        for (int place = 0; place < S::kRawRing; ++place) {
-          if (!ok || !(at.more || done < issued)) break;
-          issue((place + S::kRawRing - 1) % S::kRawRing);
-          if (done >= issued) break;
-          copy_wait<S::kRawRing - 1>();
-          const int step = steps[place], kind = kinds[place], slot = step % S::kRing;
-          if (kind & 2) {
-            ok = __all_sync(0xffffffffu, bar_wait(shared_at(&bars.raw_full[me][place]), phases >> place & 1, gave_up));
-            phases ^= 1u << place;
-          }
-          __syncwarp();
-          ok = ok && slot_free(step);
-          if (!ok) break;
-          const unsigned char *src = stage + place * S::kRaw + sub * DP + chunk * 16;
-          // 16 channels of a key are two neighbouring 16-byte columns; which goes first alternates, so that the lanes of a
-          // quarter warp store to all banks
-          const int c0 = (chunk & 3) * 2, swap = (chunk >> 2) & 1;
-          unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + sub * 128;
-#pragma unroll 4
-          for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
-            const int key = i * kAtOnce + sub;
-            const uint4 x = *reinterpret_cast<const uint4 *>(src + i * (kAtOnce * DP));
-            const uint4 lo = make_uint4(widen<FMT, false>(x.x), widen<FMT, true>(x.x), widen<FMT, false>(x.y), widen<FMT, true>(x.y));
-            const uint4 hi = make_uint4(widen<FMT, false>(x.z), widen<FMT, true>(x.z), widen<FMT, false>(x.w), widen<FMT, true>(x.w));
-            unsigned char *to = row + i * (kAtOnce * 128);
-            *reinterpret_cast<uint4 *>(to + (((c0 + swap) ^ (key & 7)) << 4)) = swap ? hi : lo;
-            *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) = swap ? lo : hi;
-          }
-          scales[(kind >> 2) * 128 + (kind & 1) * 64 + lane] = scale_stage[place * kTileKeys + lane];
-          scales[(kind >> 2) * 128 + (kind & 1) * 64 + 32 + lane] = scale_stage[place * kTileKeys + 32 + lane];
-          fence_async();
-          __syncwarp();
-          if (lane == 0) {
-            bar_arrive(shared_at(&bars.full[slot]));
-            bar_arrive(shared_at(&bars.scale_full[kind >> 2]));
-          }
-          ++done;
+        ok = slot_free(at.step);
+        copy_wait<0>();
+        if (boxes) {
+          bar_wait(shared_at(&bars.raw_full[me]), phase, gave_up);
+          ok = __any_sync(0xffffffffu, *gave_up != 0) == 0 && ok;
+          phase ^= 1;
         }
+        __syncwarp();
+        if (!ok) break;
+        // 16 channels of a key are two neighbouring 16-byte columns.  Which goes first alternates with the half of the row and
+        // with the key, so that 8-byte reads of 16 lanes and 16-byte writes of 8 lanes fall into different banks.
+        const int c0 = (chunk & 3) * 2, swap = ((chunk >> 2) ^ sub) & 1;
+        const unsigned char *src = stage + sub * DP + chunk * 16;
+        unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + sub * 128;
+#pragma unroll 4
+        for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+          const int key = i * kAtOnce + sub;             // kAtOnce is even: the key's parity is sub's
+          const uint2 x = *reinterpret_cast<const uint2 *>(src + i * (kAtOnce * DP) + swap * 8), y = *reinterpret_cast<const uint2 *>(src + i * (kAtOnce * DP) + 8 - swap * 8);
+          unsigned char *to = row + i * (kAtOnce * 128);
+          *reinterpret_cast<uint4 *>(to + (((c0 + swap) ^ (key & 7)) << 4)) =
+              make_uint4(widen<FMT, false>(x.x), widen<FMT, true>(x.x), widen<FMT, false>(x.y), widen<FMT, true>(x.y));
+          *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) =
+              make_uint4(widen<FMT, false>(y.x), widen<FMT, true>(y.x), widen<FMT, false>(y.y), widen<FMT, true>(y.y));
+        }
+        scales[scale_slot * 128 + v * 64 + lane] = scale_stage[lane];
+        scales[scale_slot * 128 + v * 64 + 32 + lane] = scale_stage[32 + lane];
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+          bar_arrive(shared_at(&bars.full[slot]));
+          bar_arrive(shared_at(&bars.scale_full[scale_slot]));
+        }
+        at.advance(a, unit_tiles, last);
+        mine();
       }
       copy_wait<0>();
-      // boxes that a run given up left under way still write to shared memory: they end before the CTA does
-      for (int place = 0; !ok && place < S::kRawRing; ++place)
-        for (unsigned spin = 0; spin < 100000 && !bar_test(shared_at(&bars.raw_full[me][place]), phases >> place & 1); ++spin) {}
     }
   } else if (warp == S::kProducts) {
     // ---- products: the warp runs in step, one lane issues
@@ -425,8 +444,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     const unsigned q_low = operand(shared_at(q_tile), 16), k_low = operand(shared_at(ring), 16), v_low = operand(shared_at(ring), kTileKeys * 128);
     int slot = 0, round = 0;               // of the step: place in the ring, and how often it has come by
     int jobs_s[2] = {0, 0}, jobs_p[2] = {0, 0}, pieces = 0;
-    bool ok = true, again = true;
-    auto take = [&]() { return bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); };
+    bool again = true;
+    auto take = [&]() { bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); };
     auto step_on = [&]() { if (++slot == S::kRing) { slot = 0; ++round; } };
     auto scores = [&](int w) {                 // of the K tile in the current step's buffer
       const unsigned k_at = k_low + slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16), d = tm_s(w, jobs_s[w] & 1);
@@ -436,21 +455,21 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       tc_commit(shared_at(&bars.s_full[w][jobs_s[w] & 1]), leader);
       ++jobs_s[w];
     };
-    while (ok && again) {
+    while (again) {
       const int n = last_tile(piece) - first_tile(piece);
       unsigned old[2] = {0, 0};                // the first product of a piece overwrites O
-      ok = bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
+      bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
       ++pieces;
       tc_after();
-      for (int t = 0; ok && t < min(kAhead, n); ++t) {
-        if (!(ok = take())) break;
+      for (int t = 0; t < min(kAhead, n); ++t) {
+        take();
         tc_after();
         if (TWO) { scores(0); scores(1); } else scores(t & 1);
         tc_commit(shared_at(&bars.empty[slot]), leader);
         step_on();
       }
-      for (int t = 0; ok && t < n; ++t) {
-        if (!(ok = take())) break;             // V of tile t
+      for (int t = 0; t < n; ++t) {
+        take();                                // V of tile t
         const int v_slot = slot;
         const unsigned v_at = v_low + v_slot * (S::kBuffer / 16);
         step_on();
@@ -458,7 +477,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 #pragma unroll
         for (int i = 0; i < (TWO ? 2 : 1); ++i) {
           const int w = TWO ? i : t & 1, b = jobs_p[w] & 1;
-          if (!(ok = bar_wait(shared_at(&bars.p_full[w][b]), (jobs_p[w] >> 1) & 1, gave_up))) break;
+          bar_wait(shared_at(&bars.p_full[w][b]), (jobs_p[w] >> 1) & 1, gave_up);
           tc_after();
 #pragma unroll
           for (int k = 0; k < kTileKeys / 16; ++k)
@@ -469,47 +488,46 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]), leader);
           if (next) {
             if (i == 0) {
-              if (!(ok = take())) break;
+              take();
               tc_after();
             }
             scores(w);
           }
         }
-        if (ok && next) {
+        if (next) {
           tc_commit(shared_at(&bars.empty[slot]), leader);
           step_on();
         }
+        if (__any_sync(0xffffffffu, *gave_up != 0)) break;
       }
-      again = next_piece(a, piece, last);
+      again = next_piece(a, piece, last) && !__any_sync(0xffffffffu, *gave_up != 0);
     }
     // all products have ended before tensor memory is given back
     tc_commit(shared_at(&bars.drained), leader);
-    for (unsigned spin = 0; spin < kTileSpin && !bar_test(shared_at(&bars.drained), 0); ++spin) {}
-    __syncwarp();
+    bar_wait(shared_at(&bars.drained), 0, gave_up);
   } else if (warp < 8) {
     // ---- softmax: warpgroup w, thread = row
     const int w = warp >> 2, tid = threadIdx.x & 127;
     const unsigned lanes = (unsigned)(warp & 3) << 21;   // this warp's 32 lanes of tensor memory
     int jobs = 0, joins = 0, tiles_before = 0, steps_before = 0;
     bool ok = true, again = true;
-    auto wait_all = [&](unsigned long long *bar, unsigned parity) {      // the same answer for the whole warp
-      return __all_sync(0xffffffffu, bar_wait(shared_at(bar), parity, gave_up)) != 0;
-    };
+    // A wait that runs out goes on like one that did not, on whatever is there; the flag is looked at once a tile.
+    auto wait = [&](unsigned long long *bar, unsigned parity) { bar_wait(shared_at(bar), parity, gave_up); };
     // The product of job j with V.  One barrier for even and one for odd jobs: that of job j - 2 is known to have ended (the
     // scores of job j, which this warpgroup has seen, were issued behind it), so the parity tells job j from it.
-    auto wait_product = [&](int j) { return wait_all(&bars.pv_done[w][j & 1], (j >> 1) & 1); };
+    auto wait_product = [&](int j) { wait(&bars.pv_done[w][j & 1], (j >> 1) & 1); };
     auto join = [&]() {
       __syncwarp();
       if (lane == 0) bar_arrive(shared_at(&bars.join));
-      const bool r = wait_all(&bars.join, joins & 1);
+      wait(&bars.join, joins & 1);
       ++joins;
-      return r;
+      return __all_sync(0xffffffffu, !*gave_up) != 0;
     };
     while (ok && again) {
       const Lengths len = piece.len;
       const int head = piece.head_group, t0 = first_tile(piece), n = last_tile(piece) - t0;
       const int row = piece.row0 + (TWO ? w * 128 : 0) + tid;
-      const bool have = row < len.fresh * (int)a.group.d && (TWO ? w * 128 : 0) + tid < a.row_tile;
+      const bool have = row < len.fresh * (int)a.group.d && (TWO ? w * 128 : 0) + tid < a.row_tile && head < a.c.kv_heads;
       const int t_row = have ? (int)a.group.div(row) : 0, q_head = head * (int)a.group.d + (have ? row - t_row * (int)a.group.d : 0);
       // the row of Q, to the operand layout
       float scale = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);     // a scale of zero: Q is zero instead
@@ -556,65 +574,61 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       int v_exp = -1000, mine = 0;       // mine: jobs of this warpgroup in this piece
       for (int t = TWO ? 0 : w; t < n; t += TWO ? 1 : 2) {
         const int b = jobs & 1, key0 = (t0 + t) * kTileKeys;
-        if (!(ok = wait_all(&bars.s_full[w][b], (jobs >> 1) & 1))) break;
+        const int tile = tiles_before + t, slot = tile & 7;
+        const float *ks = scales + slot * 128, *vs = ks + 64;
+        const unsigned s_at = tm_s(w, b) + lanes;
+        wait(&bars.s_full[w][b], (jobs >> 1) & 1);
         tc_after();
+        if constexpr (kQuant) wait(&bars.scale_full[slot], (tile >> 3) & 1);
+        const bool edge = key0 + kTileKeys > len.context;
+        unsigned long long vis = ~0ull;
+        if (edge) vis = visible(a, len, key0, have, t_row);
         float s[64];
-        {
+        auto load_scores = [&]() {
           unsigned x[32], y[32];
-          tm_load32(x, tm_s(w, b) + lanes);
-          tm_load32(y, tm_s(w, b) + lanes + 32);
+          __syncwarp();
+          tm_load32(x, s_at);
+          tm_load32(y, s_at + 32);
           tm_loaded();
 #pragma unroll
           for (int i = 0; i < 32; ++i) { s[i] = __uint_as_float(x[i]); s[32 + i] = __uint_as_float(y[i]); }
-        }
-        const int tile = tiles_before + t, slot = tile & 7;
-        const float *ks = scales + slot * 128, *vs = ks + 64;
-        if constexpr (kQuant) {
-          if (!(ok = wait_all(&bars.scale_full[slot], (tile >> 3) & 1))) break;
+          if constexpr (kQuant) {
+#pragma unroll
+            for (int i = 0; i < 64; i += 4) {
+              const ulonglong2 k4 = *reinterpret_cast<const ulonglong2 *>(ks + i);
+              const float2 p = unpair(mul2(pair(s[i], s[i + 1]), k4.x)), q = unpair(mul2(pair(s[i + 2], s[i + 3]), k4.y));
+              s[i] = p.x; s[i + 1] = p.y; s[i + 2] = q.x; s[i + 3] = q.y;
+            }
+          }
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
+          }
+        };
+        float sums;
+        auto exponentials = [&]() {      // s to probabilities against `top`, and their sum
+          const float base = top == -INFINITY ? 0.f : top;
+          const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base);
+          Pair sum0 = 0, sum1 = 0;
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
-            const ulonglong2 k4 = *reinterpret_cast<const ulonglong2 *>(ks + i);
-            const float2 x = unpair(mul2(pair(s[i], s[i + 1]), k4.x)), y = unpair(mul2(pair(s[i + 2], s[i + 3]), k4.y));
-            s[i] = x.x; s[i + 1] = x.y; s[i + 2] = y.x; s[i + 3] = y.y;
+            const float2 p = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), q = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
+            s[i] = exp2_fast(p.x); s[i + 1] = exp2_fast(p.y); s[i + 2] = exp2_fast(q.x); s[i + 3] = exp2_fast(q.y);
+            sum0 = add2(sum0, pair(s[i], s[i + 1]));
+            sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
           }
-        }
-        const bool edge = key0 + kTileKeys > len.context;
-        unsigned long long vis = ~0ull;
-        if (edge) {
-          // bit i: key0 + i.  Context below, then the row's own bits, nothing behind the last new token
-          const int off = key0 - len.context;
-          vis = 0;
-          if (off < 0) vis = ~0ull >> (64 + off);                       // -off low bits (off > -64)
-          if (have) {
-            unsigned long long fresh = 0;                                // bit i: new token off + i
-            if (a.mask) {
-              const unsigned long long *m = a.mask + (long long)(len.first + t_row) * a.mask_words;
-              const int lo = off >> 6, sh = off & 63;                    // floor, also for negative off
-              const unsigned long long w0 = lo >= 0 && lo < a.mask_words ? __ldg(m + lo) : 0ull;
-              const unsigned long long w1 = lo + 1 >= 0 && lo + 1 < a.mask_words ? __ldg(m + lo + 1) : 0ull;
-              fresh = sh ? w0 >> sh | w1 << (64 - sh) : w0;
-            } else {
-              const int upto = t_row - off + 1;                          // tokens off .. t_row
-              fresh = upto <= 0 ? 0ull : upto >= 64 ? ~0ull : ~0ull >> (64 - upto);
-            }
-            const int room = len.fresh - off;                            // tokens there are from off on
-            if (room <= 0) fresh = 0; else if (room < 64) fresh &= ~0ull >> (64 - room);
-            vis |= off < 0 ? fresh & ~(~0ull >> (64 + off)) : fresh;
-          }
-#pragma unroll
-          for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
-        }
+          const float2 x = unpair(add2(sum0, sum1));
+          sums = x.x + x.y;
+        };
+        load_scores();
         float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
 #pragma unroll
         for (int i = 4; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
         m0 = fmaxf(m0, m1);
+        exponentials();                  // (of a piece's first tile: taken again below)
         const float best = m0 == -INFINITY ? m0 : m0 * scale;
-        float f = 1.f, f_unit = 1.f;     // of the sum, and of O's unit
-        if (best > top + kLazy) {
-          f = top == -INFINITY ? 0.f : exp2_fast(top - best);
-          top = best;
-        }
-        float v_unit = 1.f;
+        const bool higher = best > top + kLazy;
+        float v_unit = 1.f, f_unit = 1.f;        // V's scales' unit, and what its change does to O
         if constexpr (kQuant) {
           // the row kernel's rule for V's scales
           float big = fmaxf(vs[lane], vs[lane + 32]);
@@ -628,40 +642,39 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
           if (v_exp != -1000) v_unit = power2(-v_exp);
         }
-        const float f_o = f * f_unit;
-        if (mine > 0 && __any_sync(0xffffffffu, f_o != 1.f)) {
-          if (!(ok = wait_product(jobs - 1))) break;
-          tc_after();
-#pragma unroll 1
-          for (int c = 0; c < DP; c += 32) {
-            unsigned x[32];
-            tm_load32(x, tm_o[w] + lanes + c);
-            tm_loaded();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f_o);
-            tm_store32(tm_o[w] + lanes + c, x);
+        if (__any_sync(0xffffffffu, higher || f_unit != 1.f) || mine == 0) {
+          float f = 1.f;
+          if (higher) {
+            f = top == -INFINITY ? 0.f : exp2_fast(top - best);
+            top = best;
           }
-          tm_stored();
-        }
-        const float base = top == -INFINITY ? 0.f : top;
-        const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base);
-        Pair sum0 = 0, sum1 = 0;
+          sum *= f;
+          if (mine > 0) {
+            wait_product(jobs - 1);
+            tc_after();
+            const float f_o = f * f_unit;
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+              unsigned x[32];
+              tm_load32(x, tm_o[w] + lanes + c);
+              tm_loaded();
 #pragma unroll
-        for (int i = 0; i < 64; i += 4) {
-          const float2 x = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), y = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
-          s[i] = exp2_fast(x.x); s[i + 1] = exp2_fast(x.y); s[i + 2] = exp2_fast(y.x); s[i + 3] = exp2_fast(y.y);
-          sum0 = add2(sum0, pair(s[i], s[i + 1]));
-          sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
+              for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f_o);
+              tm_store32(tm_o[w] + lanes + c, x);
+            }
+            tm_stored();
+          }
+          load_scores();                 // S is still there: the probabilities have not been written yet
+          exponentials();
         }
-        const float2 sums = unpair(add2(sum0, sum1));
-        sum = sum * f + (sums.x + sums.y);
+        sum += sums;
         if constexpr (kQuant) {
           const Pair unit2 = pair(v_unit, v_unit);
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
             const ulonglong2 v4 = *reinterpret_cast<const ulonglong2 *>(vs + i);
-            const float2 x = unpair(mul2(pair(s[i], s[i + 1]), mul2(v4.x, unit2))), y = unpair(mul2(pair(s[i + 2], s[i + 3]), mul2(v4.y, unit2)));
-            s[i] = x.x; s[i + 1] = x.y; s[i + 2] = y.x; s[i + 3] = y.y;
+            const float2 p = unpair(mul2(pair(s[i], s[i + 1]), mul2(v4.x, unit2))), q = unpair(mul2(pair(s[i + 2], s[i + 3]), mul2(v4.y, unit2)));
+            s[i] = p.x; s[i + 1] = p.y; s[i + 2] = q.x; s[i + 3] = q.y;
           }
           if (edge) {                    // a scale that is not finite, at a key that the row does not see
 #pragma unroll
@@ -673,7 +686,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         if (look) {
           // V's tile is in its buffer and stays there until this warpgroup has handed over its probabilities
           const int at = steps_before + min(kAhead, n) + t + min(t, max(n - kAhead, 0)), slot_v = at % S::kRing;
-          if (!(ok = wait_all(&bars.full[slot_v], (at / S::kRing) & 1))) break;
+          wait(&bars.full[slot_v], (at / S::kRing) & 1);
           odd = *reinterpret_cast<volatile unsigned long long *>(&odd_keys[slot_v]);
         }
         __syncwarp();
@@ -681,7 +694,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           unsigned p[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) p[i] = kBf16 ? pack_bf16(s[2 * i], s[2 * i + 1]) : pack_f16(s[2 * i], s[2 * i + 1]);
-          tm_store32(tm_s(w, b) + lanes, p);
+          tm_store32(s_at, p);
         }
         tm_stored();
         tc_before();
@@ -689,7 +702,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         if (lane == 0) bar_arrive(shared_at(&bars.p_full[w][b]));
         if (odd) {
           // infinite or NaN elements of V: added as they are to the rows that see their key (the probability is positive)
-          if (!(ok = wait_product(jobs))) break;
+          wait_product(jobs);
           tc_after();
           while (odd) {
             const int i = __ffsll((long long)odd) - 1;
@@ -710,9 +723,10 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         }
         ++jobs;
         ++mine;
+        if (__any_sync(0xffffffffu, *gave_up != 0)) break;
       }
-      if (ok && mine > 0) ok = wait_product(jobs - 1);
-      if (!ok) break;
+      if (mine > 0) wait_product(jobs - 1);
+      if (!(ok = __all_sync(0xffffffffu, !*gave_up))) break;
       tc_after();
       tiles_before += n;
       steps_before += 2 * n;
@@ -785,6 +799,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   tc_before();
   __syncthreads();
   tc_after();
+  if (gave_up_word) {
+    // boxes that were under way when a wait ran out still land in shared memory: a fifth of a millisecond is ample
+    for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
+    __syncthreads();
+  }
   if (warp == S::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
   if (threadIdx.x == 0 && gave_up_word) report(a.b.status, KVR_DEV_GAVE_UP);
 }

@@ -82,6 +82,7 @@ __device__ __forceinline__ bool request_lengths(const Batch &b, int block_size, 
 // Offset of logical token j of request r inside a plane; -1 where its block id is out of range.
 __device__ __forceinline__ long long token_offset(const Batch &b, const CacheView &c, const FastDiv &bs, int r, int j) {
   const unsigned blk = bs.div((unsigned)j);
+  if (blk >= (unsigned)b.table_stride) return -1;
   const int id = __ldg(b.tables + (long long)r * b.table_stride + blk);
   if ((unsigned)id >= (unsigned)c.num_blocks) return -1;
   return (long long)id * c.block_stride + (long long)(j - blk * bs.d) * c.row_bytes;
