@@ -172,7 +172,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     a.head_groups = spec->kv_heads;
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
-    a.unit_keys = rows <= 128 ? 128 : 64;
+    a.unit_keys = 128;
     a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
     if (a.box_rows && !layer_map(spec, a.c, padded, a.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
   } else {

@@ -1,23 +1,20 @@
 // Attention for many query rows a KV head (trees of drafted tokens, chunks): both products on tcgen05.
 //
-// A CTA streams 64 keys of one KV head at a time past its query rows.  S[128 rows x 64 keys] = Q K^T goes to tensor memory;
+// A CTA streams 128 keys of one KV head at a time past its query rows.  S[128 rows x 128 keys] = Q K^T goes to tensor memory;
 // a warpgroup reads it (a thread is a row: maximum and sum need no shuffle), writes the probabilities back over it in 16
 // bits, and O[128 x channels] += P V takes them from there.  K and V lie in shared memory as they are in the cache, rows of
 // 128 bytes swizzled: K is the right operand with its channels along k, V the right operand with its keys along k, so
 // one layout serves both and nothing is transposed.
 //
-// Two warpgroups work at a time.  TWO: up to 256 rows, each warpgroup has 128 of them and every K and V tile is used twice.
-// Otherwise (up to 128 rows, bound by the stream): the warpgroups take alternate key tiles of the same rows and join their
-// sums at the end of a piece.  S is double-buffered for each warpgroup, so the products of the next tile run under the
-// exponentials of this one.  Tensor memory: 2 x O (128 columns), 2 x 2 x S (64).
-//
-// Exponentials do not wait for their tile's maximum: they are taken against the maximum known before; only a row whose new
-// maximum is more than 2^kLazy higher (rare after the first tile) makes its warp rescale O and take them again.
+// Two such jobs run at a time, a warpgroup each, so that the products of one run under the exponentials of the other.  TWO: up to
+// 256 rows, a job for each 128 of them and every K and V tile used twice.  Otherwise (up to 128 rows, bound by the stream): the
+// jobs take alternate key tiles of the same rows and join their sums at the end of a piece.  Tensor memory: 2 x O and 2 x S, 128
+// columns each.  A row's maximum moves only when a score passes it by 2^kLazy (rare after the first tile): O is rescaled then.
 //
 // Loading: warps of their own bring the tiles in turn.  Where blocks are a multiple of 8 tokens a tile is a few TMA boxes (rows of
 // one head out of a block, swizzled on the way); the ragged end of a request, new tokens whose V has to be looked through, and
 // other block sizes go through 16-byte asynchronous copies.  8-bit codes land in a staging area that belongs to the warp, which
-// widens them to f16 into the ring, exactly (six such warps, against three).  Scales multiply scores and probabilities as in
+// widens them to f16 into the ring, exactly (three pairs of such warps, against three).  Scales multiply scores and probabilities as in
 // the row kernel.
 //
 // Every wait is bounded.  One that runs out sets a flag which all roles see, and the kernel ends in the ordinary way (copies
@@ -28,34 +25,29 @@
 namespace kvr {
 namespace {
 
-constexpr int kTileKeys = 64;
+constexpr int kTileKeys = 128;
 constexpr int kSoftmax = 256;
-constexpr unsigned kTileSpin = 1u << 23;
+constexpr unsigned kTileSpin = 1u << 18;
 
 // ---- barriers, fences, tensor memory
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_test(unsigned bar, unsigned parity, bool ask = true) {
+__device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
   unsigned ok;
-  asm volatile("{\n\t.reg .pred p, l;\n\tsetp.ne.u32 l, %3, 0;\n\tsetp.ne.u32 p, %3, %3;\n\t@l mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity), "r"((unsigned)ask) : "memory");
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// A warp's wait.  Lane 0 asks for all: 32 lanes testing one barrier are served one after the other (200 to 400 clocks, and
-// try_wait, which may sleep, costs 250 even on a barrier that is complete).  The warp stays in step: the test is predicated and
-// its answer voted on, because what follows are instructions of the whole warp whose operands lie in uniform registers.
-// A wait that runs out, here or in another role, sets the flag and goes on like one that did not, on whatever is there: all
+// A warp's wait, by all of its lanes (95 clocks on a barrier that is complete; one lane's loop with the others waiting for it
+// takes 170).  One that runs out, here or in another role, sets the flag and goes on like one that did not, on whatever is there: all
 // addresses stay in bounds, later waits give up at once, and the roles look at the flag once a step.
 __device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *gave_up) {
-  const bool ask = (threadIdx.x & 31) == 0;
-  for (unsigned spin = 0; spin < kTileSpin; ++spin) {
-    if (__any_sync(0xffffffffu, bar_test(bar, parity, ask))) {
-      __syncwarp();                    // what lane 0 has been shown by the barrier all lanes see
-      return;
-    }
-    if ((spin & 63) == 63 && __any_sync(0xffffffffu, *gave_up != 0)) return;
+  unsigned spin = 0;
+  while (!bar_try(bar, parity)) {
+    if (++spin == kTileSpin) *gave_up = 1;
+    if ((spin & 15) == 0 && *gave_up) break;
   }
-  *gave_up = 1;
+  __syncwarp();
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -124,26 +116,28 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair r; asm("add.rn.f32x2
 __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
-template <int FMT, int DP>
+template <int FMT, int DP, bool TWO>
 struct TileShape {
   static constexpr bool kQuant = quantised(FMT);
   static constexpr int kBlocks = DP / 64;                                // 128-byte columns of a row
-  // Loading warps (no more than buffers: a loader waits for step s - kRing to be used up having filled step s - kLoaders, and
-  // a barrier's parity is clear only if step s - 2 kRing is known to be over); the warp that issues the products.
-  static constexpr int kLoaders = kQuant ? 6 : 3, kProducts = 8 + kLoaders;
+  static constexpr int kPerStep = kQuant ? 2 : 1;                        // loading warps of a step; three steps at a time
+  static constexpr int kLoaders = 3 * kPerStep, kSpan = kTileKeys / kPerStep;      // a warp's keys of a step
+  static constexpr int kProducts = 8 + kLoaders;                         // the warp that issues the products
   static constexpr int kThreads = kQuant ? 512 : 384;                    // whole warpgroups: registers are dealt out to those
   static constexpr int kQBytes = 2 * 128 * DP * 2;                       // two tiles of 128 rows
   static constexpr int kBuffer = kTileKeys * DP * 2;                     // K or V of a tile, 16 bits
-  static constexpr int kRing = kQuant ? 6 : 9;
-  static_assert(kLoaders <= kRing, "");
+  // Buffers: what shared memory holds.  No fewer than the steps loaded at a time: a loader waits for step s - kRing to be used up
+  // having filled step s - 3, and a barrier's parity is clear only if step s - 2 kRing is known to be over.
+  static constexpr int kRing = kQuant ? 3 : TWO ? 5 : 4;
+  static_assert(kRing >= 3, "");
   static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
-  static constexpr int kScaleSlots = kQuant ? 8 : 0;                     // 64 scales of K, 64 of V
-  static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? kLoaders : 0) * (kRaw + kTileKeys * 4) + kScaleSlots * 512 + 1024;
+  static constexpr int kScaleSlots = kQuant ? 4 : 0;                     // 128 scales of K, 128 of V
+  static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? 3 * (kRaw + kTileKeys * 4) : 0) + kScaleSlots * 1024 + 1024;
 };
 
 struct TileBars {
-  unsigned long long full[9], empty[9];
-  unsigned long long s_full[2][2], p_full[2][2], pv_done[2][2], q_full, join, scale_full[8], drained;
+  unsigned long long full[5], empty[5];
+  unsigned long long s_full[2], p_full[2], pv_done[2], q_full, join, scale_full[4], drained;
   unsigned long long raw_full[6];
 };
 
@@ -160,7 +154,7 @@ struct TileWalk {
   }
   __device__ __forceinline__ bool is_k() const { return k < n && k < v + AHEAD; }
   __device__ __forceinline__ int tile() const { return t0 + (is_k() ? k : v); }
-  __device__ __forceinline__ int slot() const { return (is_k() ? tiles : tiles - (k - v)) & 7; }     // of the tile's scales
+  __device__ __forceinline__ int slot() const { return (is_k() ? tiles : tiles - (k - v)) & 3; }     // of the tile's scales
   __device__ __forceinline__ void advance(const AttendArgs &a, int unit_tiles, long long last) {
     ++step;
     if (is_k()) { ++k; ++tiles; } else ++v;
@@ -172,9 +166,10 @@ struct TileWalk {
 };
 
 // Which of the keys key0 .. key0 + 63 a row sees: bit i is key0 + i.  The context, then the row's own bits, nothing behind the
-// request's last new token.  For tiles that reach beyond the context (key0 + 64 > context).
+// request's last new token.
 __device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const Lengths &len, int key0, bool have, int t_row) {
   const int off = key0 - len.context;
+  if (off <= -64) return ~0ull;
   unsigned long long vis = 0;
   if (off < 0) vis = ~0ull >> (64 + off);                       // -off low bits (off > -64)
   if (have) {
@@ -197,31 +192,26 @@ __device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const
 }
 
 template <int FMT, int DP, bool TWO>
-__global__ void __launch_bounds__(TileShape<FMT, DP>::kThreads, 1)
+__global__ void __launch_bounds__(TileShape<FMT, DP, TWO>::kThreads, 1)
 attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
-  using S = TileShape<FMT, DP>;
+  using S = TileShape<FMT, DP, TWO>;
   constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
-  constexpr int kAhead = TWO ? 2 : 4;            // key tiles whose scores are made before the first is used
+  constexpr int kAhead = TWO ? 1 : 2;            // key tiles whose scores are made before the first is used
   constexpr float kLazy = kQuant ? 4.f : 8.f;    // 8-bit: leaves room for V's scale, see the row kernel
   extern __shared__ unsigned char raw_smem[];
   __shared__ long long scratch[34];
   __shared__ __align__(8) TileBars bars;
   __shared__ unsigned tm_slot;
   __shared__ int gave_up_word;
-  __shared__ unsigned long long odd_keys[9];     // by ring slot: keys of a V tile with elements that are not finite
+  __shared__ unsigned long long odd_keys[5][2];  // by ring slot: keys of a V tile with elements that are not finite
   __shared__ float join_ml[128][2];
   __shared__ int box_ids[S::kLoaders][64];                 // by loader: block ids of the boxes around its step
   volatile int *gave_up = &gave_up_word;
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   unsigned char *q_tile = smem, *ring = q_tile + S::kQBytes, *raw = ring + S::kRing * S::kBuffer;
-  float *scales = reinterpret_cast<float *>(raw + (kQuant ? S::kLoaders : 0) * S::kRaw);
-  float *scale_raw = scales + S::kScaleSlots * 128;
-  // Roles: 0..7 softmax, 8.. loaders, then the products.  The scheduler prefers older warps, and the short chains of the products
-  // and the loaders must not queue behind exponentials: they are the CTA's first warps.
-  constexpr int kOthers = S::kThreads / 32 - 8;
-  const int lane = threadIdx.x & 31, first_warps = (int)(threadIdx.x >> 5);
-  const int warp = first_warps >= kOthers ? first_warps - kOthers : first_warps == 0 ? S::kProducts :
-                   first_warps <= S::kLoaders ? 7 + first_warps : S::kProducts + 1;      // the last has no role
+  float *scales = reinterpret_cast<float *>(raw + (kQuant ? 3 : 0) * S::kRaw);
+  float *scale_raw = scales + S::kScaleSlots * 256;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   const long long total = total_units(a, scratch);
   const int ctas = (int)min((long long)a.ctas, total);
@@ -238,17 +228,13 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 
   if (threadIdx.x == 0) {
     gave_up_word = 0;
-    for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), 1); bar_init(shared_at(&bars.empty[i]), 1); }
-    for (int w = 0; w < 2; ++w) {
-      for (int b = 0; b < 2; ++b) { bar_init(shared_at(&bars.s_full[w][b]), 1); bar_init(shared_at(&bars.p_full[w][b]), 4); bar_init(shared_at(&bars.pv_done[w][b]), 1); }
-    }
+    for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), S::kPerStep); bar_init(shared_at(&bars.empty[i]), 1); }
+    for (int w = 0; w < 2; ++w) { bar_init(shared_at(&bars.s_full[w]), 1); bar_init(shared_at(&bars.p_full[w]), 4); bar_init(shared_at(&bars.pv_done[w]), 1); }
     bar_init(shared_at(&bars.q_full), 8);
     bar_init(shared_at(&bars.join), 8);
     bar_init(shared_at(&bars.drained), 1);
-    for (int i = 0; i < 8; ++i) {
-      bar_init(shared_at(&bars.scale_full[i]), 2);       // K's scales and V's
-      if (i < 6) bar_init(shared_at(&bars.raw_full[i]), 1);
-    }
+    for (int i = 0; i < 4; ++i) bar_init(shared_at(&bars.scale_full[i]), 4);       // K's scales and V's, two warps each
+    for (int i = 0; i < 6; ++i) bar_init(shared_at(&bars.raw_full[i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == S::kProducts) {
@@ -260,11 +246,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   tc_after();
   const unsigned tm = *reinterpret_cast<volatile unsigned *>(&tm_slot);
   const unsigned tm_o[2] = {tm, tm + 128};
-  auto tm_s = [&](int w, int b) { return tm + 256 + (w * 2 + b) * 64; };
+  auto tm_s = [&](int w) { return tm + 256 + w * 128; };
 
   if (warp >= 8 && warp < S::kProducts) {
-    // ---- loaders: a step (K or V of a tile) each
-    const int me = warp - 8;
+    // ---- loaders: a step (K or V of a tile) for each, or for a pair
+    const int me = warp - 8, group = me / S::kPerStep, span0 = (me % S::kPerStep) * S::kSpan;
     constexpr int kElement = kQuant ? 1 : 2, kChunks = DP * kElement / 16, kAtOnce = 32 / kChunks;
     const int chunk = lane % kChunks, sub = lane / kChunks;
     const int used = a.c.head_dim * kElement / 16;
@@ -272,8 +258,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     at.p = piece; at.step = at.tiles = 0; at.more = true;
     at.open(a, unit_tiles);
 
-    // Ids of the blocks that the boxes of a piece lie in, 32 boxes at a time, a batch ahead of its use: V's steps are at most four
-    // tiles (32 boxes of 8 tokens) behind K's, so both find theirs among the last 64.
+    // Ids of the blocks that the boxes of a piece lie in, 32 boxes at a time, a batch ahead of its use: V's steps are at most one
+    // tile (16 boxes of 8 tokens) behind K's, so both find theirs among the last 64.
     int *ids = box_ids[me];
     const int per_tile = a.box_rows ? kTileKeys / a.box_rows : 0;
     int box_next = 0, fetched = 0;       // first box of the batch in `fetched`
@@ -295,19 +281,19 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       }
       __syncwarp();
     };
-    // K or V of a tile to dst, rows of 64 keys: boxes that complete on bar (true), or copies by this warp's lanes (false)
+    // This warp's keys of K or V of a tile, to dst (the tile's first row of them): boxes that complete on bar (true), or copies by this warp's lanes (false)
     auto bring = [&](unsigned char *dst, unsigned long long *bar, bool v, int tile, bool look) {
-      const int key0 = tile * kTileKeys;
-      if (a.box_rows && !look && key0 + kTileKeys <= at.p.len.keys) {
+      const int key0 = tile * kTileKeys + span0;
+      if (a.box_rows && !look && key0 + S::kSpan <= at.p.len.keys) {
         have_ids(tile);
         // a lane a box; 16-bit heads of 128 channels take two, side by side
         constexpr int kWide = kQuant ? 1 : S::kBlocks;
-        const int box = lane / kWide, part = lane % kWide;
-        const int id = box < per_tile ? ids[(tile * per_tile + box) & 63] : 0;
+        const int box = lane / kWide, part = lane % kWide, boxes = per_tile / S::kPerStep;
+        const int id = box < boxes ? ids[(key0 / a.box_rows + box) & 63] : 0;
         if (__all_sync(0xffffffffu, (unsigned)id < (unsigned)a.c.num_blocks)) {
-          if (lane == 0) bar_expect(shared_at(bar), kTileKeys * DP * kElement);
+          if (lane == 0) bar_expect(shared_at(bar), S::kSpan * DP * kElement);
           __syncwarp();
-          if (box < per_tile) {
+          if (box < boxes) {
             const int token = key0 + box * a.box_rows, row = token - (int)a.bs.div(token) * (int)a.bs.d;
             unsigned char *to = kQuant ? dst + box * a.box_rows * DP : dst + part * (kTileKeys * 128) + box * a.box_rows * 128;
             box_load(shared_at(to), &map, shared_at(bar), part * 64, at.p.head_group, row, id, v);
@@ -318,7 +304,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       }
       const char *base = a.c.base + (v ? a.c.v_offset : 0) + at.p.head_group * a.c.head_dim * kElement;
 #pragma unroll 1
-      for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+      for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
         const int key = i * kAtOnce + sub, j = key0 + key;
         const long long off = j < at.p.len.keys ? token_offset(a.b, a.c, a.bs, at.p.r, j) : -1;
         if (off < 0 && j < at.p.len.keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
@@ -334,7 +320,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up);
       return __any_sync(0xffffffffu, *gave_up != 0) == 0;
     };
-    auto mine = [&]() { while (at.more && at.step % S::kLoaders != me) at.advance(a, unit_tiles, last); };
+    auto mine = [&]() { while (at.more && at.step % 3 != group) at.advance(a, unit_tiles, last); };
     mine();
     if constexpr (!kQuant) {
       while (at.more) {
@@ -349,7 +335,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           if (look) {
             // Elements of V that are not finite must not meet the zero probabilities of rows that do not see their key: they
             // are set to zero here and added by the softmax threads, row by row.  A thread looks at what it copied.
-            unsigned long long odd = 0;
+            unsigned long long odd[2] = {0, 0};
             constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
 #pragma unroll 1
             for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
@@ -363,10 +349,13 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
                 if ((e[q] & kExp) == kExp) { e[q] &= 0xffff0000u; any = true; }
                 if ((e[q] >> 16 & kExp) == kExp) { e[q] &= 0xffffu; any = true; }
               }
-              if (any) { *x_at = x; odd |= 1ull << key; }
+              if (any) { *x_at = x; if (key < 64) odd[0] |= 1ull << key; else odd[1] |= 1ull << (key - 64); }
             }
-            const unsigned lo = __reduce_or_sync(0xffffffffu, (unsigned)odd), hi = __reduce_or_sync(0xffffffffu, (unsigned)(odd >> 32));
-            if (lane == 0) odd_keys[slot] = (unsigned long long)hi << 32 | lo;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const unsigned lo = __reduce_or_sync(0xffffffffu, (unsigned)odd[h]), hi = __reduce_or_sync(0xffffffffu, (unsigned)(odd[h] >> 32));
+              if (lane == 0) odd_keys[slot][h] = (unsigned long long)hi << 32 | lo;
+            }
           }
           fence_async();
           __syncwarp();
@@ -377,16 +366,16 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       }
     } else {
       // a step's codes and scales come to this warp's stage and are widened into the ring
-      unsigned char *stage = raw + me * S::kRaw;
-      float *scale_stage = scale_raw + me * kTileKeys;
+      unsigned char *stage = raw + group * S::kRaw + span0 * DP;
+      float *scale_stage = scale_raw + group * kTileKeys + span0;
       unsigned phase = 0;                // of raw_full
       while (at.more) {
         const bool v = !at.is_k();
         const int tile = at.tile(), slot = at.step % S::kRing, scale_slot = at.slot();
         const bool boxes = bring(stage, &bars.raw_full[me], v, tile, false);
 #pragma unroll
-        for (int h = 0; h < kTileKeys; h += 32) {
-          const int j = tile * kTileKeys + h + lane;
+        for (int h = 0; h < S::kSpan; h += 32) {
+          const int j = tile * kTileKeys + span0 + h + lane;
           long long off = -1;
           if (boxes) {                   // all keys are there, their blocks' ids at hand
             const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
@@ -411,9 +400,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // with the key, so that 8-byte reads of 16 lanes and 16-byte writes of 8 lanes fall into different banks.
         const int c0 = (chunk & 3) * 2, swap = ((chunk >> 2) ^ sub) & 1;
         const unsigned char *src = stage + sub * DP + chunk * 16;
-        unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + sub * 128;
+        unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + (span0 + sub) * 128;
 #pragma unroll 4
-        for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+        for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
           const int key = i * kAtOnce + sub;             // kAtOnce is even: the key's parity is sub's
           const uint2 x = *reinterpret_cast<const uint2 *>(src + i * (kAtOnce * DP) + swap * 8), y = *reinterpret_cast<const uint2 *>(src + i * (kAtOnce * DP) + 8 - swap * 8);
           unsigned char *to = row + i * (kAtOnce * 128);
@@ -422,8 +411,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) =
               make_uint4(widen<FMT, false>(y.x), widen<FMT, true>(y.x), widen<FMT, false>(y.y), widen<FMT, true>(y.y));
         }
-        scales[scale_slot * 128 + v * 64 + lane] = scale_stage[lane];
-        scales[scale_slot * 128 + v * 64 + 32 + lane] = scale_stage[32 + lane];
+#pragma unroll
+        for (int h = 0; h < S::kSpan; h += 32) scales[scale_slot * 256 + v * 128 + span0 + h + lane] = scale_stage[h + lane];
         fence_async();
         __syncwarp();
         if (lane == 0) {
@@ -443,58 +432,51 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     constexpr unsigned kO = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
     const unsigned q_low = operand(shared_at(q_tile), 16), k_low = operand(shared_at(ring), 16), v_low = operand(shared_at(ring), kTileKeys * 128);
     int slot = 0, round = 0;               // of the step: place in the ring, and how often it has come by
-    int jobs_s[2] = {0, 0}, jobs_p[2] = {0, 0}, pieces = 0;
+    int used[2] = {0, 0}, pieces = 0;      // jobs whose product with V is issued
     bool again = true;
-    auto take = [&]() { bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); };
+    auto take = [&]() { bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); tc_after(); };
     auto step_on = [&]() { if (++slot == S::kRing) { slot = 0; ++round; } };
     auto scores = [&](int w) {                 // of the K tile in the current step's buffer
-      const unsigned k_at = k_low + slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16), d = tm_s(w, jobs_s[w] & 1);
+      const unsigned k_at = k_low + slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16);
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k)        // 16 channels: 32 bytes of a row; 64: the next 128-byte column
-        tc_product_ss(d, q + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, k_at + (k >> 2) * (kTileKeys * 128 / 16) + (k & 3) * 2, kS, k > 0, leader);
-      tc_commit(shared_at(&bars.s_full[w][jobs_s[w] & 1]), leader);
-      ++jobs_s[w];
+        tc_product_ss(tm_s(w), q + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, k_at + (k >> 2) * (kTileKeys * 128 / 16) + (k & 3) * 2, kS, k > 0, leader);
+      tc_commit(shared_at(&bars.s_full[w]), leader);
     };
     while (again) {
       const int n = last_tile(piece) - first_tile(piece);
-      unsigned old[2] = {0, 0};                // the first product of a piece overwrites O
       bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
       ++pieces;
       tc_after();
-      for (int t = 0; t < min(kAhead, n); ++t) {
-        take();
-        tc_after();
-        if (TWO) { scores(0); scores(1); } else scores(t & 1);
-        tc_commit(shared_at(&bars.empty[slot]), leader);
-        step_on();
-      }
-      for (int t = 0; t < n; ++t) {
-        take();                                // V of tile t
+      // t < 0: scores of the first kAhead tiles; then V product of tile t, scores of tile t + kAhead
+#pragma unroll 1
+      for (int t = -min(kAhead, n); t < n; ++t) {
+        const bool v = t >= 0, k = !v || t + kAhead < n;
         const int v_slot = slot;
-        const unsigned v_at = v_low + v_slot * (S::kBuffer / 16);
-        step_on();
-        const bool next = t + kAhead < n;
-#pragma unroll
+        if (v) { take(); step_on(); }
+#pragma unroll 1
         for (int i = 0; i < (TWO ? 2 : 1); ++i) {
-          const int w = TWO ? i : t & 1, b = jobs_p[w] & 1;
-          bar_wait(shared_at(&bars.p_full[w][b]), (jobs_p[w] >> 1) & 1, gave_up);
-          tc_after();
+          const int w = TWO ? i : (v ? t : t + min(kAhead, n)) & 1;      // !TWO: kAhead is even, tile t + kAhead is the same job's
+          if (v) {
+            const int job = w ? used[1] : used[0];
+            bar_wait(shared_at(&bars.p_full[w]), job & 1, gave_up);
+            tc_after();
+            const unsigned v_at = v_low + v_slot * (S::kBuffer / 16);
+            const unsigned old = t >= (TWO ? 1 : 2);           // a job's first product of a piece overwrites O
 #pragma unroll
-          for (int k = 0; k < kTileKeys / 16; ++k)
-            tc_product_ts(tm_o[w], tm_s(w, b) + k * 8, v_at + k * (16 * 128 / 16), kO, k > 0 ? 1u : old[w], leader);
-          old[w] = 1;
-          tc_commit(shared_at(&bars.pv_done[w][b]), leader);
-          ++jobs_p[w];
-          if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]), leader);
-          if (next) {
-            if (i == 0) {
-              take();
-              tc_after();
-            }
+            for (int s = 0; s < kTileKeys / 16; ++s)
+              tc_product_ts(tm + w * 128, tm_s(w) + s * 8, v_at + s * (16 * 128 / 16), kO, s > 0 ? 1u : old, leader);
+            tc_commit(shared_at(&bars.pv_done[w]), leader);
+            used[0] += 1 - w;
+            used[1] += w;
+            if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]), leader);
+          }
+          if (k) {
+            if (i == 0) take();
             scores(w);
           }
         }
-        if (next) {
+        if (k) {
           tc_commit(shared_at(&bars.empty[slot]), leader);
           step_on();
         }
@@ -513,9 +495,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     bool ok = true, again = true;
     // A wait that runs out goes on like one that did not, on whatever is there; the flag is looked at once a tile.
     auto wait = [&](unsigned long long *bar, unsigned parity) { bar_wait(shared_at(bar), parity, gave_up); };
-    // The product of job j with V.  One barrier for even and one for odd jobs: that of job j - 2 is known to have ended (the
-    // scores of job j, which this warpgroup has seen, were issued behind it), so the parity tells job j from it.
-    auto wait_product = [&](int j) { wait(&bars.pv_done[w][j & 1], (j >> 1) & 1); };
+    // The product of job j with V.  That of job j - 1 has ended when the scores of job j are there, which were issued behind it.
+    auto wait_product = [&](int j) { wait(&bars.pv_done[w], j & 1); };
     auto join = [&]() {
       __syncwarp();
       if (lane == 0) bar_arrive(shared_at(&bars.join));
@@ -572,66 +553,59 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       }
       float top = -INFINITY, sum = 0.f;  // top: of scaled scores
       int v_exp = -1000, mine = 0;       // mine: jobs of this warpgroup in this piece
+#pragma unroll 1
       for (int t = TWO ? 0 : w; t < n; t += TWO ? 1 : 2) {
-        const int b = jobs & 1, key0 = (t0 + t) * kTileKeys;
-        const int tile = tiles_before + t, slot = tile & 7;
-        const float *ks = scales + slot * 128, *vs = ks + 64;
-        const unsigned s_at = tm_s(w, b) + lanes;
-        wait(&bars.s_full[w][b], (jobs >> 1) & 1);
+        const int key0 = (t0 + t) * kTileKeys, tile = tiles_before + t;
+        const float *ks = scales + (tile & 3) * 256;     // K's scales, then V's
+        const unsigned s_at = tm_s(w) + lanes;
+        wait(&bars.s_full[w], jobs & 1);
         tc_after();
-        if constexpr (kQuant) wait(&bars.scale_full[slot], (tile >> 3) & 1);
+        if constexpr (kQuant) wait(&bars.scale_full[tile & 3], (tile >> 2) & 1);
         const bool edge = key0 + kTileKeys > len.context;
-        unsigned long long vis = ~0ull;
-        if (edge) vis = visible(a, len, key0, have, t_row);
         float s[64];
-        auto load_scores = [&]() {
-          unsigned x[32], y[32];
-          __syncwarp();
-          tm_load32(x, s_at);
-          tm_load32(y, s_at + 32);
-          tm_loaded();
+        auto load_scores = [&](int h) {          // keys 64 h .. 64 h + 63
+          {
+            unsigned x[32], y[32];
+            tm_load32(x, s_at + h * 64);
+            tm_load32(y, s_at + h * 64 + 32);
+            tm_loaded();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) { s[i] = __uint_as_float(x[i]); s[32 + i] = __uint_as_float(y[i]); }
+            for (int i = 0; i < 32; ++i) { s[i] = __uint_as_float(x[i]); s[32 + i] = __uint_as_float(y[i]); }
+          }
           if constexpr (kQuant) {
+            const float *k_scale = ks + h * 64;
 #pragma unroll
             for (int i = 0; i < 64; i += 4) {
-              const ulonglong2 k4 = *reinterpret_cast<const ulonglong2 *>(ks + i);
+              const ulonglong2 k4 = *reinterpret_cast<const ulonglong2 *>(k_scale + i);
               const float2 p = unpair(mul2(pair(s[i], s[i + 1]), k4.x)), q = unpair(mul2(pair(s[i + 2], s[i + 3]), k4.y));
               s[i] = p.x; s[i + 1] = p.y; s[i + 2] = q.x; s[i + 3] = q.y;
             }
           }
-          if (edge) {
+        };
+        float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          load_scores(h);
+          if (__builtin_expect(edge, 0)) {
+            const unsigned long long vis = visible(a, len, key0 + h * 64, have, t_row);
 #pragma unroll
             for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
           }
-        };
-        float sums;
-        auto exponentials = [&]() {      // s to probabilities against `top`, and their sum
-          const float base = top == -INFINITY ? 0.f : top;
-          const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base);
-          Pair sum0 = 0, sum1 = 0;
 #pragma unroll
-          for (int i = 0; i < 64; i += 4) {
-            const float2 p = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), q = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
-            s[i] = exp2_fast(p.x); s[i + 1] = exp2_fast(p.y); s[i + 2] = exp2_fast(q.x); s[i + 3] = exp2_fast(q.y);
-            sum0 = add2(sum0, pair(s[i], s[i + 1]));
-            sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
-          }
-          const float2 x = unpair(add2(sum0, sum1));
-          sums = x.x + x.y;
-        };
-        load_scores();
-        float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
-#pragma unroll
-        for (int i = 4; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
+          for (int i = 0; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
+          __syncwarp();
+        }
         m0 = fmaxf(m0, m1);
-        exponentials();                  // (of a piece's first tile: taken again below)
         const float best = m0 == -INFINITY ? m0 : m0 * scale;
-        const bool higher = best > top + kLazy;
-        float v_unit = 1.f, f_unit = 1.f;        // V's scales' unit, and what its change does to O
+        float f = 1.f, f_unit = 1.f, v_unit = 1.f;       // of the sum; of O's unit; V's scales' unit
+        if (best > top + kLazy) {
+          f = top == -INFINITY ? 0.f : exp2_fast(top - best);
+          top = best;
+        }
         if constexpr (kQuant) {
           // the row kernel's rule for V's scales
-          float big = fmaxf(vs[lane], vs[lane + 32]);
+          const float *vs = ks + 128;
+          float big = fmaxf(fmaxf(vs[lane], vs[lane + 32]), fmaxf(vs[lane + 64], vs[lane + 96]));
 #pragma unroll
           for (int d = 16; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
           const int e = (int)(__float_as_uint(big) >> 23) - 127;
@@ -642,17 +616,10 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
           if (v_exp != -1000) v_unit = power2(-v_exp);
         }
-        if (__any_sync(0xffffffffu, higher || f_unit != 1.f) || mine == 0) {
-          float f = 1.f;
-          if (higher) {
-            f = top == -INFINITY ? 0.f : exp2_fast(top - best);
-            top = best;
-          }
+        const float f_o = f * f_unit;
+        if (__builtin_expect(__any_sync(0xffffffffu, f_o != 1.f), 0)) {
           sum *= f;
-          if (mine > 0) {
-            wait_product(jobs - 1);
-            tc_after();
-            const float f_o = f * f_unit;
+          if (mine > 0) {                // the last product is over: these scores were issued behind it
 #pragma unroll 1
             for (int c = 0; c < DP; c += 32) {
               unsigned x[32];
@@ -664,58 +631,78 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             }
             tm_stored();
           }
-          load_scores();                 // S is still there: the probabilities have not been written yet
-          exponentials();
         }
-        sum += sums;
-        if constexpr (kQuant) {
-          const Pair unit2 = pair(v_unit, v_unit);
+        const float base = top == -INFINITY ? 0.f : top;
+        const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base), unit2 = pair(v_unit, v_unit);
+        Pair sum0 = 0, sum1 = 0;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          load_scores(h);
+          unsigned long long vis = ~0ull;
+          if (__builtin_expect(edge, 0)) {
+            vis = visible(a, len, key0 + h * 64, have, t_row);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
+          }
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
-            const ulonglong2 v4 = *reinterpret_cast<const ulonglong2 *>(vs + i);
-            const float2 p = unpair(mul2(pair(s[i], s[i + 1]), mul2(v4.x, unit2))), q = unpair(mul2(pair(s[i + 2], s[i + 3]), mul2(v4.y, unit2)));
-            s[i] = p.x; s[i + 1] = p.y; s[i + 2] = q.x; s[i + 3] = q.y;
+            const float2 p = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), q = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
+            s[i] = exp2_fast(p.x); s[i + 1] = exp2_fast(p.y); s[i + 2] = exp2_fast(q.x); s[i + 3] = exp2_fast(q.y);
+            sum0 = add2(sum0, pair(s[i], s[i + 1]));
+            sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
           }
-          if (edge) {                    // a scale that is not finite, at a key that the row does not see
+          if constexpr (kQuant) {
+            const float *v_scale = ks + 128 + h * 64;
 #pragma unroll
-            for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = 0.f;
+            for (int i = 0; i < 64; i += 4) {
+              const ulonglong2 v4 = *reinterpret_cast<const ulonglong2 *>(v_scale + i);
+              const float2 p = unpair(mul2(pair(s[i], s[i + 1]), mul2(v4.x, unit2))), q = unpair(mul2(pair(s[i + 2], s[i + 3]), mul2(v4.y, unit2)));
+              s[i] = p.x; s[i + 1] = p.y; s[i + 2] = q.x; s[i + 3] = q.y;
+            }
+            if (__builtin_expect(edge, 0)) {     // a scale that is not finite, at a key that the row does not see
+#pragma unroll
+              for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = 0.f;
+            }
           }
-        }
-        const bool look = !kQuant && edge && (len.fresh > 1 || a.mask);
-        unsigned long long odd = 0;
-        if (look) {
-          // V's tile is in its buffer and stays there until this warpgroup has handed over its probabilities
-          const int at = steps_before + min(kAhead, n) + t + min(t, max(n - kAhead, 0)), slot_v = at % S::kRing;
-          wait(&bars.full[slot_v], (at / S::kRing) & 1);
-          odd = *reinterpret_cast<volatile unsigned long long *>(&odd_keys[slot_v]);
-        }
-        __syncwarp();
-        {
           unsigned p[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) p[i] = kBf16 ? pack_bf16(s[2 * i], s[2 * i + 1]) : pack_f16(s[2 * i], s[2 * i + 1]);
-          tm_store32(s_at, p);
+          __syncwarp();
+          tm_store32(s_at + h * 32, p);  // over the scores of keys that are done with
+          tm_stored();
         }
-        tm_stored();
+        const float2 sums = unpair(add2(sum0, sum1));
+        sum += sums.x + sums.y;
+        const bool look = !kQuant && edge && (len.fresh > 1 || a.mask);
+        unsigned long long odd[2] = {0, 0};
+        if (__builtin_expect(look, 0)) {
+          // V's tile is in its buffer and stays there until this warpgroup has handed over its probabilities
+          const int at = steps_before + min(kAhead, n) + t + min(t, max(n - kAhead, 0)), slot_v = at % S::kRing;
+          wait(&bars.full[slot_v], (at / S::kRing) & 1);
+          odd[0] = *reinterpret_cast<volatile unsigned long long *>(&odd_keys[slot_v][0]);
+          odd[1] = *reinterpret_cast<volatile unsigned long long *>(&odd_keys[slot_v][1]);
+        }
         tc_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(shared_at(&bars.p_full[w][b]));
-        if (odd) {
+        if (lane == 0) bar_arrive(shared_at(&bars.p_full[w]));
+        if (__builtin_expect((odd[0] | odd[1]) != 0, 0)) {
           // infinite or NaN elements of V: added as they are to the rows that see their key (the probability is positive)
           wait_product(jobs);
           tc_after();
-          while (odd) {
-            const int i = __ffsll((long long)odd) - 1;
-            odd &= odd - 1;
+#pragma unroll 1
+          for (int i = 0; i < kTileKeys; ++i) {
+            if (!((i < 64 ? odd[0] >> i : odd[1] >> (i - 64)) & 1)) continue;
+            const bool sees_it = visible(a, len, key0 + (i & 64), have, t_row) >> (i & 63) & 1;
             const long long off = token_offset(a.b, a.c, a.bs, piece.r, key0 + i);
             if (off < 0) continue;
             const char *v = a.c.base + a.c.v_offset + off + (long long)head * a.c.head_dim * 2;
             for (int d = 0; d < a.c.head_dim; ++d) {
               const float x = load1<kBf16 ? KVR_BF16 : KVR_F16>(v + d * 2);
               if (!(fabsf(x) < INFINITY)) {
+                __syncwarp();
                 const float o = __uint_as_float(tm_load1(tm_o[w] + lanes + d));
                 tm_loaded();
-                tm_store1(tm_o[w] + lanes + d, __float_as_uint(vis >> i & 1 ? o + x : o));
+                tm_store1(tm_o[w] + lanes + d, __float_as_uint(sees_it ? o + x : o));
                 tm_stored();
               }
             }
@@ -810,7 +797,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 
 template <int FMT, int DP, bool TWO>
 cudaError_t launch_tiles(const AttendArgs &a, const CUtensorMap &map, cudaStream_t s) {
-  using S = TileShape<FMT, DP>;
+  using S = TileShape<FMT, DP, TWO>;
   const auto kernel = attend_tiles_kernel<FMT, DP, TWO>;
   static const cudaError_t set = [&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
