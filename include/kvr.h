@@ -466,8 +466,9 @@ kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, i
  * A row that attends to nothing gives out 0 and lse -infinity; what a row does not attend to has no influence on it,
  * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
  * the cache's type.  Scores, sums and accumulators are fp32; probabilities are rounded to the 16-bit type of the product with V.
- * At most 2^30 tokens in one request.  workspace: DEVICE, kvr_attend_workspace(spec) bytes, 256-byte aligned; its content is of no interest before or after,
- * calls that may overlap need their own.
+ * At most 2^30 tokens in one request.  workspace: DEVICE, kvr_attend_workspace(spec) bytes,
+ * 256-byte aligned, zeroed once before its first use (its first 4096 bytes are counters that each call leaves at zero; the rest is
+ * of no interest).  Calls that may overlap need their own; after KVR_DEV_GAVE_UP zero it again.
  */
 uint64_t kvr_attend_workspace(const kvr_cache_spec *spec);
 kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *device_pool, int32_t layer, const kvr_batch *batch,

@@ -1,84 +1,10 @@
-// kvr_cache_attend: argument checks, the choice of kernel, and the kernel that joins the pieces of cut segments.
+// kvr_cache_attend: argument checks and the choice of kernel.
 #include "kvr_attend.cuh"
 
 #include <cmath>
 
 namespace kvr {
 namespace {
-
-constexpr int kJoinThreads = 256;
-
-// One warp per (row, query head).  Most segments are whole and their rows are left at once; for a cut one the pieces'
-// maxima and sums are read side by side by the lanes, then the accumulators one after the other, in the order of keys.
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const __grid_constant__ AttendArgs a) {
-  const int lane = threadIdx.x & 31;
-  const long long at = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  if (at >= (long long)a.b.n_tokens * a.q_heads) return;
-  const int token = (int)(at / a.q_heads), q_head = (int)(at - (long long)token * a.q_heads);
-  const int r = find_request(a.b, token);
-  const Lengths len = attend_lengths(a, r);
-  if (token < len.first || token - len.first >= len.fresh) return;       // left out
-  long long base = 0, total = 0;
-  for (int i = lane; i < a.b.n_req; i += 32) {
-    const long long u = units_of(a, i);
-    total += u;
-    if (i < r) base += u;
-  }
-  base = warp_sum(base);
-  total = warp_sum(total);
-  const int ctas = (int)min((long long)a.ctas, total);
-  const int head = (int)a.group.div(q_head);
-  const long long row = (long long)(token - len.first) * (int)a.group.d + (q_head - head * (int)a.group.d);
-  const int head_group = head / a.group_heads, tile = (int)(row / a.row_tile), tiles = len.segments / a.head_groups;
-  const long long begin = base + (long long)(head_group * tiles + tile) * len.units, end = begin + len.units;
-  const int c0 = cta_of(total, ctas, begin), c1 = cta_of(total, ctas, end - 1);
-  if (c0 == c1) return;
-  const int local_head = head - head_group * a.group_heads, local_row = (int)(row - (long long)tile * a.row_tile);
-  const int which0 = first_unit(total, ctas, c0) == begin ? 0 : 1;
-  auto place = [&](int c) {
-    return (((long long)c * 2 + (c == c0 ? which0 : 0)) * a.group_heads + local_head) * a.row_tile + local_row;
-  };
-  float m = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[place(c)].x);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  float sum = 0.f, acc[2][4] = {};
-  for (int cb = c0; cb <= c1; cb += 32) {
-    const int n = min(32, c1 - cb + 1);
-    float f = 0.f;
-    if (lane < n) {
-      const float2 ml = a.part_ml[place(cb + lane)];
-      f = ml.x == m ? 1.f : exp2f(ml.x - m);                             // both -infinity: an empty piece of an empty row
-      sum += ml.y * f;
-    }
-    for (int i = 0; i < n; ++i) {
-      const float w = __shfl_sync(0xffffffffu, f, i);
-      const float *src = a.part_o + place(cb + i) * a.c.head_dim;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int d = h * 128 + lane * 4;
-        if (d < a.c.head_dim) {
-          const float4 x = *reinterpret_cast<const float4 *>(src + d);
-          acc[h][0] += x.x * w; acc[h][1] += x.y * w; acc[h][2] += x.z * w; acc[h][3] += x.w * w;
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
-  char *dst = a.out.data + (long long)token * a.out.token_stride + (long long)q_head * a.out.head_stride;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int d = h * 128 + lane * 4;
-    if (d >= a.c.head_dim) continue;
-    uint2 w;
-    if (a.out.type == KVR_BF16) w = make_uint2(pack_bf16(acc[h][0] * inv, acc[h][1] * inv), pack_bf16(acc[h][2] * inv, acc[h][3] * inv));
-    else w = make_uint2(pack_f16(acc[h][0] * inv, acc[h][1] * inv), pack_f16(acc[h][2] * inv, acc[h][3] * inv));
-    *reinterpret_cast<uint2 *>(dst + d * 2) = w;
-  }
-  if (a.lse && lane == 0) a.lse[(long long)token * a.q_heads + q_head] = sum == 0.f ? -INFINITY : m * 0.69314718f + logf(sum);
-}
 
 int sm_count() {
   static int counts[64];
@@ -120,7 +46,7 @@ using namespace kvr;
 
 extern "C" uint64_t kvr_attend_workspace(const kvr_cache_spec *spec) {
   if (check_spec(spec)) return 0;
-  return (uint64_t)kMaxSms * 2 * kPartRows * (spec->head_dim * 4ull + 8);
+  return kCounterBytes + (uint64_t)kMaxSms * 2 * kPartRows * (spec->head_dim * 4ull + 8);
 }
 
 extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *device_pool, int32_t layer, const kvr_batch *batch,
@@ -178,11 +104,12 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   } else {
     tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
     a.row_tile = tiles * 8;
-    a.unit_keys = 16 * slices;
+    a.unit_keys = slices < 4 ? (64 + 16 * slices - 1) / (16 * slices) * 16 * slices : 16 * slices;     // 64 or more: fewer pieces
   }
   a.ctas = sms;
-  a.part_ml = static_cast<float2 *>(workspace);
-  a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)kMaxSms * 2 * kPartRows * 8);
+  a.handed_in = static_cast<int *>(workspace);
+  a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + kCounterBytes);
+  a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + kCounterBytes + (size_t)kMaxSms * 2 * kPartRows * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   switch (spec->format) {
@@ -191,10 +118,5 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     case KVR_CACHE_E4M3: e = launch_attend_e4m3(a, tiles, slices, map, s); break;
     default: e = launch_attend_int8(a, tiles, slices, map, s);
   }
-  if (e != cudaSuccess) return fail_cache(KVR_ERR_CUDA, cudaGetErrorString(e));
-  const long long joins = ((long long)batch->n_tokens * q->heads + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
-  if (joins > INT32_MAX) return fail_cache(KVR_ERR_INVALID_ARG, "too many rows in one call");
-  attend_join_kernel<<<(unsigned)joins, kJoinThreads, 0, s>>>(a);
-  e = cudaGetLastError();
   return e == cudaSuccess ? KVR_OK : fail_cache(KVR_ERR_CUDA, cudaGetErrorString(e));
 }

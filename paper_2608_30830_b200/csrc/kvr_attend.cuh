@@ -5,7 +5,9 @@
 // other request by request, and the units of all of them are dealt out in equal runs, one to each CTA of a grid that
 // fills the GPU once: ragged requests keep all SMs busy to the end, and the cut needs nothing from the host but the
 // grid's size.  A CTA that holds a whole segment writes its result; the pieces of a cut segment go to the workspace as
-// (maximum, sum, accumulator) and are joined in the order of their keys, so results do not depend on timing.
+// (maximum, sum, accumulator), and the CTA that hands in the last one joins them.  More than 16 pieces are joined by groups of 16
+// first, so that one long request is not joined by one CTA.  Pieces are always taken in the order of their keys: results do not
+// depend on timing.
 #pragma once
 #include <cuda.h>
 
@@ -28,6 +30,7 @@ struct AttendArgs {
   int unit_keys;
   int box_rows;              // tokens of a TMA box (tile kernel): 8 or 16, 0: the block size does not allow one
   int ctas;                  // the grid of the main kernel
+  int *handed_in;            // [2][ctas][2]: pieces of a group, groups of a segment; zero between calls
   float *part_o;             // [ctas][2][group_heads][row_tile][head_dim]
   float2 *part_ml;           // [ctas][2][group_heads][row_tile]: maximum (log2), sum
 };
@@ -35,6 +38,9 @@ struct AttendArgs {
 // The workspace holds, for every SM, two pieces of this many rows (fp32 accumulators and a pair of statistics each).
 constexpr int kPartRows = 256;
 constexpr int kMaxSms = 160;
+constexpr int kCounterBytes = 4096;
+constexpr int kJoinAtOnce = 16;
+static_assert(kMaxSms * 4 * 4 <= kCounterBytes, "");
 
 #ifdef __CUDACC__
 struct Lengths {

@@ -74,5 +74,137 @@ __device__ __forceinline__ bool next_piece(const AttendArgs &a, Piece &p, long l
   return true;
 }
 
+struct Cut {
+  int c0, c1, which0;        // the CTAs of the segment; which of the first one's two pieces it is
+};
+// The rows of a segment from its pieces of `n` <= 32 CTAs c, c + step, ...: to the output, or (fold) to the first one's place.
+// A lane has 4 channels of a 128-channel slab; what costs is latency, so kRows rows and kAhead pieces are read at once.
+template <int SLABS>
+__device__ __forceinline__ void join_pieces(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int rows, int heads, int warps, int warp, int lane) {
+  constexpr int kRows = SLABS > 1 ? 2 : 4, kAhead = 4;
+  const int total = rows * heads;
+  const long long stride = (long long)step * 2 * a.group_heads * a.row_tile;     // rows from one piece to the next
+  // the first CTA of a segment may hold it as its second piece, all others as their first
+  auto first_row = [&](int lh, int row) { return ((long long)c * 2 * a.group_heads + lh) * a.row_tile + row; };
+  const long long second = c == cut.c0 && cut.which0 ? (long long)a.group_heads * a.row_tile : 0;
+#pragma unroll 1
+  for (int i0 = warp * kRows; i0 < total; i0 += warps * kRows) {
+    float f[kRows], m[kRows], l[kRows], o[kRows][SLABS][4];
+    long long at[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int i = min(i0 + u, total - 1), lh = i / rows;
+      at[u] = first_row(lh, i - lh * rows);
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < n) ml = __ldcg(a.part_ml + at[u] + lane * stride + (lane == 0 ? second : 0));
+      f[u] = m[u] = ml.x;
+      l[u] = ml.y;
+#pragma unroll
+      for (int h = 0; h < SLABS; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[u][h][e] = 0.f;
+    }
+    float4 x[kAhead][kRows][SLABS];
+    auto read = [&](int k, float4 (&to)[kRows][SLABS]) {
+#pragma unroll
+      for (int u = 0; u < kRows; ++u)
+#pragma unroll
+        for (int h = 0; h < SLABS; ++h) {
+          const int d = h * 128 + lane * 4;
+          to[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k < n && d < a.c.head_dim) to[u][h] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (at[u] + k * stride + (k == 0 ? second : 0)) * a.c.head_dim + d));
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) read(k, x[k]);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xffffffffu, m[u], d));
+      f[u] = lane >= n ? 0.f : f[u] == m[u] ? 1.f : exp2_fast(f[u] - m[u]);        // both -infinity: a piece of an empty row
+      l[u] *= f[u];
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) l[u] += __shfl_xor_sync(0xffffffffu, l[u], d);
+    }
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+          const float w = __shfl_sync(0xffffffffu, f[u], (k0 + k) & 31);           // 0 beyond the last
+#pragma unroll
+          for (int h = 0; h < SLABS; ++h) {
+            if (k0 + k >= n) continue;
+            o[u][h][0] += x[k][u][h].x * w; o[u][h][1] += x[k][u][h].y * w; o[u][h][2] += x[k][u][h].z * w; o[u][h][3] += x[k][u][h].w * w;
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) read(k0 + kAhead + k, x[k]);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      if (i0 + u >= total) break;
+      const int lh = (i0 + u) / rows, row = i0 + u - lh * rows;
+      if (fold) {
+#pragma unroll
+        for (int h = 0; h < SLABS; ++h) {
+          const int d = h * 128 + lane * 4;
+          if (d < a.c.head_dim) *reinterpret_cast<float4 *>(a.part_o + (at[u] + second) * a.c.head_dim + d) = make_float4(o[u][h][0], o[u][h][1], o[u][h][2], o[u][h][3]);
+        }
+        if (lane == 0) a.part_ml[at[u] + second] = make_float2(m[u], l[u]);
+        continue;
+      }
+      const float inv = l[u] > 0.f ? 1.f / l[u] : l[u] == 0.f ? 0.f : NAN;
+      const int t = (int)a.group.div(p.row0 + row), q_head = (p.head_group * a.group_heads + lh) * (int)a.group.d + (p.row0 + row - t * (int)a.group.d);
+      char *dst = a.out.data + (long long)(p.len.first + t) * a.out.token_stride + (long long)q_head * a.out.head_stride;
+#pragma unroll
+      for (int h = 0; h < SLABS; ++h) {
+        const int d = h * 128 + lane * 4;
+        if (d >= a.c.head_dim) continue;
+        uint2 w;
+        if (a.out.type == KVR_BF16) w = make_uint2(pack_bf16(o[u][h][0] * inv, o[u][h][1] * inv), pack_bf16(o[u][h][2] * inv, o[u][h][3] * inv));
+        else w = make_uint2(pack_f16(o[u][h][0] * inv, o[u][h][1] * inv), pack_f16(o[u][h][2] * inv, o[u][h][3] * inv));
+        *reinterpret_cast<uint2 *>(dst + d * 2) = w;
+      }
+      if (a.lse && lane == 0) a.lse[(long long)(p.len.first + t) * a.q_heads + q_head] = l[u] == 0.f ? -INFINITY : m[u] * 0.69314718f + logf(l[u]);
+    }
+    __syncwarp();
+  }
+}
+
+// After this CTA's piece of a cut segment has been stored: joins the segment's pieces if it was the last to come in.  sync() is
+// a barrier of the `warps` warps that call this (false: given up); `last` is shared memory.
+template <int SLABS, class Sync>
+__device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, long long total, int ctas, int rows, int heads, int warps, int warp, int lane, Sync sync, volatile int *last) {
+  const long long begin = p.unit - p.begin;
+  Cut cut;
+  cut.c0 = cta_of(total, ctas, begin);
+  cut.c1 = cta_of(total, ctas, begin + p.len.units - 1);
+  cut.which0 = first_unit(total, ctas, cut.c0) == begin ? 0 : 1;
+  const int all = cut.c1 - cut.c0 + 1, groups = (all + kJoinAtOnce - 1) / kJoinAtOnce;
+  const int group = ((int)blockIdx.x - cut.c0) / kJoinAtOnce, leader = cut.c0 + group * kJoinAtOnce, n = min(kJoinAtOnce, cut.c1 - leader + 1);
+  auto come_in = [&](int *counter, int of) {
+    if (!sync()) return false;
+    if (warp == 0 && lane == 0) {
+      __threadfence();                   // what the barrier has shown this thread goes before the count
+      const bool is_last = atomicAdd(counter, 1) == of - 1;
+      if (is_last) atomicExch(counter, 0);
+      __threadfence();
+      *last = is_last;
+    }
+    return (bool)sync();
+  };
+  if (!come_in(a.handed_in + leader * 2 + (leader == cut.c0 ? cut.which0 : 0), n)) return false;
+  if (!*last) return true;
+  join_pieces<SLABS>(a, p, cut, leader, 1, n, groups > 1, rows, heads, warps, warp, lane);
+  if (groups == 1) return true;
+  if (!come_in(a.handed_in + (a.ctas + cut.c0) * 2 + cut.which0, groups)) return false;
+  if (!*last) return true;
+  join_pieces<SLABS>(a, p, cut, cut.c0, kJoinAtOnce, groups, false, rows, heads, warps, warp, lane);
+  return true;
+}
+
 }  // namespace
 }  // namespace kvr

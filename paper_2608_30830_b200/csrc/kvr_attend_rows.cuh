@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
   __shared__ long long scratch[34];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const int local_head = warp / slices, slice = warp - local_head * slices;
+  __shared__ int last_in;
 
   const long long total = total_units(a, scratch);
   const int ctas = (int)min((long long)a.ctas, total);
@@ -530,6 +531,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
             if (gid == 0) a.part_ml[slot * a.row_tile + row] = make_float2(top[n][e], sum[n][e]);
           }
         }
+    }
+    if (piece.begin != 0 || piece.end != len.units) {
+      const int heads = min(a.group_heads, a.c.kv_heads - piece.head_group * a.group_heads);
+      hand_in<DP / 128 + DP % 128 / 64>(a, piece, total, ctas, rows, heads, (int)blockDim.x / 32, warp, lane, [] { __syncthreads(); return true; }, &last_in);
     }
     again = next_piece(a, piece, last);
   }

@@ -202,7 +202,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ long long scratch[34];
   __shared__ __align__(8) TileBars bars;
   __shared__ unsigned tm_slot;
-  __shared__ int gave_up_word;
+  __shared__ int gave_up_word, last_in;
   __shared__ unsigned long long odd_keys[5][2];  // by ring slot: keys of a V tile with elements that are not finite
   __shared__ float join_ml[128][2];
   __shared__ int box_ids[S::kLoaders][64];                 // by loader: block ids of the boxes around its step
@@ -779,7 +779,10 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum == 0.f ? -INFINITY : top * 0.69314718f + logf(sum);
         }
       }
-      if (!TWO) ok = join();             // the exchange has been read: Q's place may be written again
+      if (piece.begin != 0 || piece.end != len.units)
+        ok = hand_in<1>(a, piece, total, ctas, min(a.row_tile, len.fresh * (int)a.group.d - piece.row0), 1, 8, warp, lane, join, &last_in);
+      else if (!TWO)
+        ok = join();                     // the exchange has been read: Q's place may be written again
       again = next_piece(a, piece, last);
     }
   }

@@ -758,7 +758,7 @@ class Cache:
             _check(st)
 
     def workspace_bytes(self):
-        """Bytes of attend()'s workspace."""
+        """Bytes of attend()'s workspace (uint8, zeroed once before its first use)."""
         return self._workspace
 
     def attend(self, pool, layer, batch, q, out, workspace, lse=None, mask=None, scale=None, stream=None):

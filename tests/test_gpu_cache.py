@@ -324,7 +324,8 @@ def check_attend(s, q_heads, dtype, mask=None, seen=None, scale=None, layer=0, s
     else:
         q, out = rand(s, s.tokens, q_heads, s.dim, dtype=kind), torch.full((s.tokens, q_heads, s.dim), 9.0, dtype=kind, device="cuda")
     lse = torch.full((s.tokens, q_heads), 9.0, device="cuda")
-    ws = torch.full((s.cache.workspace_bytes(),), 0xff, dtype=torch.uint8, device="cuda")           # its content is of no interest
+    ws = torch.full((s.cache.workspace_bytes(),), 0xff, dtype=torch.uint8, device="cuda")           # of no interest, but for
+    ws[:4096] = 0                                                                                    # the counters
     s.cache.attend(s.pool, layer, s.batch, q, out, ws, lse=lse, mask=mask, scale=scale)
     s.ok()
     want, want_lse, mag = attend64(s, q, k, v, scale, causal(s) if seen is None else seen)
@@ -339,6 +340,7 @@ def check_attend(s, q_heads, dtype, mask=None, seen=None, scale=None, layer=0, s
     again = torch.zeros_like(out)
     s.cache.attend(s.pool, layer, s.batch, q, again, ws, mask=mask, scale=scale)                     # no lse; the same bits
     assert torch.equal(again.view(torch.int16), out.contiguous().view(torch.int16))
+    assert not ws[:4096].any()
     return out, lse, q
 
 
