@@ -79,8 +79,9 @@ struct Cut {
 };
 // The rows of a segment from its pieces of `n` <= 32 CTAs c, c + step, ...: to the output, or (fold) to the first one's place.
 // A lane has 4 channels of a 128-channel slab; what costs is latency, so kRows rows and kAhead pieces are read at once.
+// Out of line: the kernels' own loops need the registers.
 template <int SLABS>
-__device__ __forceinline__ void join_pieces(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int rows, int heads, int warps, int warp, int lane) {
+__device__ __noinline__ void join_pieces(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int rows, int heads, int warps, int warp, int lane) {
   constexpr int kRows = SLABS > 1 ? 2 : 4, kAhead = 4;
   const int total = rows * heads;
   const long long stride = (long long)step * 2 * a.group_heads * a.row_tile;     // rows from one piece to the next
@@ -198,11 +199,12 @@ __device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, lon
   };
   if (!come_in(a.handed_in + leader * 2 + (leader == cut.c0 ? cut.which0 : 0), n)) return false;
   if (!*last) return true;
-  join_pieces<SLABS>(a, p, cut, leader, 1, n, groups > 1, rows, heads, warps, warp, lane);
+  const Piece copy = p;                  // what the call is shown lies in memory
+  join_pieces<SLABS>(a, copy, cut, leader, 1, n, groups > 1, rows, heads, warps, warp, lane);
   if (groups == 1) return true;
   if (!come_in(a.handed_in + (a.ctas + cut.c0) * 2 + cut.which0, groups)) return false;
   if (!*last) return true;
-  join_pieces<SLABS>(a, p, cut, cut.c0, kJoinAtOnce, groups, false, rows, heads, warps, warp, lane);
+  join_pieces<SLABS>(a, copy, cut, cut.c0, kJoinAtOnce, groups, false, rows, heads, warps, warp, lane);
   return true;
 }
 

@@ -9,7 +9,11 @@
 // Two such jobs run at a time, a warpgroup each, so that the products of one run under the exponentials of the other.  TWO: up to
 // 256 rows, a job for each 128 of them and every K and V tile used twice.  Otherwise (up to 128 rows, bound by the stream): the
 // jobs take alternate key tiles of the same rows and join their sums at the end of a piece.  Tensor memory: 2 x O and 2 x S, 128
-// columns each.  A row's maximum moves only when a score passes it by 2^kLazy (rare after the first tile): O is rescaled then.
+// columns each.  One warp issues both jobs' products in turn, which keeps the warpgroups half a tile apart: in step (a warp for
+// each job) they would share the exponential units and then both wait for the products (249 against 293 us).
+//
+// Exponentials do not wait for their tile's maximum: they are taken, 64 keys at a time, against the maximum known before; only
+// a row whose new maximum is more than 2^kLazy higher (rare after the first tile) makes its warp rescale what it has and take them again.
 //
 // Loading: warps of their own bring the tiles in turn.  Where blocks are a multiple of 8 tokens a tile is a few TMA boxes (rows of
 // one head out of a block, swizzled on the way); the ragged end of a request, new tokens whose V has to be looked through, and
@@ -120,19 +124,19 @@ template <int FMT, int DP, bool TWO>
 struct TileShape {
   static constexpr bool kQuant = quantised(FMT);
   static constexpr int kBlocks = DP / 64;                                // 128-byte columns of a row
-  static constexpr int kPerStep = kQuant ? 2 : 1;                        // loading warps of a step; three steps at a time
-  static constexpr int kLoaders = 3 * kPerStep, kSpan = kTileKeys / kPerStep;      // a warp's keys of a step
-  static constexpr int kProducts = 8 + kLoaders;                         // the warp that issues the products
-  static constexpr int kThreads = kQuant ? 512 : 384;                    // whole warpgroups: registers are dealt out to those
+  // Warps: 0..7 softmax, 8 issues the products, the others load.  Whole warpgroups: registers are dealt to those.
+  static constexpr int kSteps = 3, kPerStep = kQuant ? 2 : 1;         // steps loaded at a time, warps of a step
+  static constexpr int kLoaders = kSteps * kPerStep, kSpan = kTileKeys / kPerStep; // a warp's keys of a step
+  static constexpr int kThreads = kQuant ? 512 : 384;
   static constexpr int kQBytes = 2 * 128 * DP * 2;                       // two tiles of 128 rows
   static constexpr int kBuffer = kTileKeys * DP * 2;                     // K or V of a tile, 16 bits
   // Buffers: what shared memory holds.  No fewer than the steps loaded at a time: a loader waits for step s - kRing to be used up
-  // having filled step s - 3, and a barrier's parity is clear only if step s - 2 kRing is known to be over.
+  // having filled step s - kSteps, and a barrier's parity is clear only if step s - 2 kRing is known to be over.
   static constexpr int kRing = kQuant ? 3 : TWO ? 5 : 4;
-  static_assert(kRing >= 3, "");
+  static_assert(kRing >= kSteps, "");
   static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
   static constexpr int kScaleSlots = kQuant ? 4 : 0;                     // 128 scales of K, 128 of V
-  static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? 3 * (kRaw + kTileKeys * 4) : 0) + kScaleSlots * 1024 + 1024;
+  static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? kSteps * (kRaw + 2 * kTileKeys * 4) : 0) + kScaleSlots * 1024 + 1024;
 };
 
 struct TileBars {
@@ -209,7 +213,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   volatile int *gave_up = &gave_up_word;
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   unsigned char *q_tile = smem, *ring = q_tile + S::kQBytes, *raw = ring + S::kRing * S::kBuffer;
-  float *scales = reinterpret_cast<float *>(raw + (kQuant ? 3 : 0) * S::kRaw);
+  float *scales = reinterpret_cast<float *>(raw + (kQuant ? S::kSteps : 0) * S::kRaw);
   float *scale_raw = scales + S::kScaleSlots * 256;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -233,11 +237,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     bar_init(shared_at(&bars.q_full), 8);
     bar_init(shared_at(&bars.join), 8);
     bar_init(shared_at(&bars.drained), 1);
-    for (int i = 0; i < 4; ++i) bar_init(shared_at(&bars.scale_full[i]), 4);       // K's scales and V's, two warps each
+    for (int i = 0; i < 4; ++i) bar_init(shared_at(&bars.scale_full[i]), 2);       // brought with K by two warps
     for (int i = 0; i < 6; ++i) bar_init(shared_at(&bars.raw_full[i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == S::kProducts) {
+  if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_at(&tm_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -248,9 +252,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   const unsigned tm_o[2] = {tm, tm + 128};
   auto tm_s = [&](int w) { return tm + 256 + w * 128; };
 
-  if (warp >= 8 && warp < S::kProducts) {
+  if (warp >= 9 && warp < 9 + S::kLoaders) {
     // ---- loaders: a step (K or V of a tile) for each, or for a pair
-    const int me = warp - 8, group = me / S::kPerStep, span0 = (me % S::kPerStep) * S::kSpan;
+    const int me = warp - 9, group = me / S::kPerStep, span0 = (me % S::kPerStep) * S::kSpan;
     constexpr int kElement = kQuant ? 1 : 2, kChunks = DP * kElement / 16, kAtOnce = 32 / kChunks;
     const int chunk = lane % kChunks, sub = lane / kChunks;
     const int used = a.c.head_dim * kElement / 16;
@@ -320,7 +324,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up);
       return __any_sync(0xffffffffu, *gave_up != 0) == 0;
     };
-    auto mine = [&]() { while (at.more && at.step % 3 != group) at.advance(a, unit_tiles, last); };
+    auto mine = [&]() { while (at.more && at.step % S::kSteps != group) at.advance(a, unit_tiles, last); };
     mine();
     if constexpr (!kQuant) {
       while (at.more) {
@@ -367,24 +371,28 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     } else {
       // a step's codes and scales come to this warp's stage and are widened into the ring
       unsigned char *stage = raw + group * S::kRaw + span0 * DP;
-      float *scale_stage = scale_raw + group * kTileKeys + span0;
+      float *scale_stage = scale_raw + group * 2 * kTileKeys + span0;
       unsigned phase = 0;                // of raw_full
       while (at.more) {
         const bool v = !at.is_k();
         const int tile = at.tile(), slot = at.step % S::kRing, scale_slot = at.slot();
         const bool boxes = bring(stage, &bars.raw_full[me], v, tile, false);
+        if (!v) {
+          // the scales of K and of V: scores must not wait for V's codes to be widened
 #pragma unroll
-        for (int h = 0; h < S::kSpan; h += 32) {
-          const int j = tile * kTileKeys + span0 + h + lane;
-          long long off = -1;
-          if (boxes) {                   // all keys are there, their blocks' ids at hand
-            const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
-            off = (long long)ids[(a.box_rows == 16 ? j >> 4 : j >> 3) & 63] * a.c.block_stride + (long long)row * a.c.row_bytes;
-          } else if (j < at.p.len.keys) {
-            off = token_offset(a.b, a.c, a.bs, at.p.r, j);
+          for (int h = 0; h < S::kSpan; h += 32) {
+            const int j = tile * kTileKeys + span0 + h + lane;
+            long long off = -1;
+            if (boxes) {                 // all keys are there, their blocks' ids at hand
+              const int row = j - (int)a.bs.div(j) * (int)a.bs.d;
+              off = (long long)ids[(a.box_rows == 16 ? j >> 4 : j >> 3) & 63] * a.c.block_stride + (long long)row * a.c.row_bytes;
+            } else if (j < at.p.len.keys) {
+              off = token_offset(a.b, a.c, a.bs, at.p.r, j);
+            }
+            const char *src = a.c.base + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
+            copy4(shared_at(scale_stage + h + lane), src, off >= 0);
+            copy4(shared_at(scale_stage + kTileKeys + h + lane), src + (off >= 0 ? a.c.v_offset : 0), off >= 0);
           }
-          const char *src = a.c.base + (v ? a.c.v_offset : 0) + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
-          copy4(shared_at(scale_stage + h + lane), src, off >= 0);
         }
         copy_commit();
         ok = slot_free(at.step);
@@ -411,75 +419,77 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) =
               make_uint4(widen<FMT, false>(y.x), widen<FMT, true>(y.x), widen<FMT, false>(y.y), widen<FMT, true>(y.y));
         }
+        if (!v) {
 #pragma unroll
-        for (int h = 0; h < S::kSpan; h += 32) scales[scale_slot * 256 + v * 128 + span0 + h + lane] = scale_stage[h + lane];
+          for (int h = 0; h < S::kSpan; h += 32) {
+            scales[scale_slot * 256 + span0 + h + lane] = scale_stage[h + lane];
+            scales[scale_slot * 256 + 128 + span0 + h + lane] = scale_stage[kTileKeys + h + lane];
+          }
+        }
         fence_async();
         __syncwarp();
         if (lane == 0) {
           bar_arrive(shared_at(&bars.full[slot]));
-          bar_arrive(shared_at(&bars.scale_full[scale_slot]));
+          if (!v) bar_arrive(shared_at(&bars.scale_full[scale_slot]));
         }
         at.advance(a, unit_tiles, last);
         mine();
       }
       copy_wait<0>();
     }
-  } else if (warp == S::kProducts) {
+  } else if (warp == 8) {
     // ---- products: the warp runs in step, one lane issues
     const unsigned leader = elect_one();
     constexpr unsigned kType = kBf16 ? 1u : 0u;
     constexpr unsigned kS = 1u << 4 | kType << 7 | kType << 10 | (kTileKeys / 8) << 17 | (128 / 16) << 24;
     constexpr unsigned kO = 1u << 4 | kType << 7 | kType << 10 | 1u << 16 | (DP / 8) << 17 | (128 / 16) << 24;
     const unsigned q_low = operand(shared_at(q_tile), 16), k_low = operand(shared_at(ring), 16), v_low = operand(shared_at(ring), kTileKeys * 128);
-    int slot = 0, round = 0;               // of the step: place in the ring, and how often it has come by
-    int used[2] = {0, 0}, pieces = 0;      // jobs whose product with V is issued
+    int used[2] = {0, 0}, pieces = 0, slot = 0, round = 0;     // jobs whose product with V is issued; the step's place in the ring
     bool again = true;
-    auto take = [&]() { bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up); tc_after(); };
-    auto step_on = [&]() { if (++slot == S::kRing) { slot = 0; ++round; } };
-    auto scores = [&](int w) {                 // of the K tile in the current step's buffer
-      const unsigned k_at = k_low + slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16);
+    auto take = [&]() {                        // the next step's buffer, when it is full
+      bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up);
+      const int s = slot;
+      if (++slot == S::kRing) { slot = 0; ++round; }
+      return s;
+    };
+    auto scores = [&](int w, int k_slot) {
+      const unsigned k_at = k_low + k_slot * (S::kBuffer / 16), q = q_low + (TWO ? w : 0) * (128 * DP * 2 / 16);
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k)        // 16 channels: 32 bytes of a row; 64: the next 128-byte column
         tc_product_ss(tm_s(w), q + (k >> 2) * (128 * 128 / 16) + (k & 3) * 2, k_at + (k >> 2) * (kTileKeys * 128 / 16) + (k & 3) * 2, kS, k > 0, leader);
       tc_commit(shared_at(&bars.s_full[w]), leader);
     };
     while (again) {
-      const int n = last_tile(piece) - first_tile(piece);
+      const int n = last_tile(piece) - first_tile(piece), head_start = min(kAhead, n);
       bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
       ++pieces;
-      tc_after();
-      // t < 0: scores of the first kAhead tiles; then V product of tile t, scores of tile t + kAhead
+      for (int t = 0; t < head_start; ++t) {
+        const int k_slot = take();
+        tc_after();
+        scores(TWO ? 0 : t & 1, k_slot);
+        if (TWO) scores(1, k_slot);
+        tc_commit(shared_at(&bars.empty[k_slot]), leader);
+      }
 #pragma unroll 1
-      for (int t = -min(kAhead, n); t < n; ++t) {
-        const bool v = t >= 0, k = !v || t + kAhead < n;
-        const int v_slot = slot;
-        if (v) { take(); step_on(); }
+      for (int t = 0; t < n; ++t) {
+        const bool next = t + kAhead < n;      // scores of tile t + kAhead follow (!TWO: kAhead is even, the same job's)
+        const int v_slot = take(), k_slot = next ? take() : 0;
+        const unsigned v_at = v_low + v_slot * (S::kBuffer / 16), old = t >= (TWO ? 1 : 2);    // a job's first product overwrites O
 #pragma unroll 1
         for (int i = 0; i < (TWO ? 2 : 1); ++i) {
-          const int w = TWO ? i : (v ? t : t + min(kAhead, n)) & 1;      // !TWO: kAhead is even, tile t + kAhead is the same job's
-          if (v) {
-            const int job = w ? used[1] : used[0];
-            bar_wait(shared_at(&bars.p_full[w]), job & 1, gave_up);
-            tc_after();
-            const unsigned v_at = v_low + v_slot * (S::kBuffer / 16);
-            const unsigned old = t >= (TWO ? 1 : 2);           // a job's first product of a piece overwrites O
+          const int w = TWO ? i : t & 1;
+          bar_wait(shared_at(&bars.p_full[w]), (w ? used[1] : used[0]) & 1, gave_up);
+          tc_after();
 #pragma unroll
-            for (int s = 0; s < kTileKeys / 16; ++s)
-              tc_product_ts(tm + w * 128, tm_s(w) + s * 8, v_at + s * (16 * 128 / 16), kO, s > 0 ? 1u : old, leader);
-            tc_commit(shared_at(&bars.pv_done[w]), leader);
-            used[0] += 1 - w;
-            used[1] += w;
-            if (i == (TWO ? 1 : 0)) tc_commit(shared_at(&bars.empty[v_slot]), leader);
-          }
-          if (k) {
-            if (i == 0) take();
-            scores(w);
-          }
+          for (int s = 0; s < kTileKeys / 16; ++s)
+            tc_product_ts(tm + w * 128, tm_s(w) + s * 8, v_at + s * (16 * 128 / 16), kO, s > 0 ? 1u : old, leader);
+          used[0] += 1 - w;
+          used[1] += w;
+          if (next) scores(w, k_slot);
+          tc_commit(shared_at(&bars.pv_done[w]), leader);      // (read at a piece's end and where V is not finite)
         }
-        if (k) {
-          tc_commit(shared_at(&bars.empty[slot]), leader);
-          step_on();
-        }
+        tc_commit(shared_at(&bars.empty[v_slot]), leader);
+        if (next) tc_commit(shared_at(&bars.empty[k_slot]), leader);
         if (__any_sync(0xffffffffu, *gave_up != 0)) break;
       }
       again = next_piece(a, piece, last) && !__any_sync(0xffffffffu, *gave_up != 0);
@@ -582,26 +592,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             }
           }
         };
-        float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          load_scores(h);
-          if (__builtin_expect(edge, 0)) {
-            const unsigned long long vis = visible(a, len, key0 + h * 64, have, t_row);
-#pragma unroll
-            for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
-          }
-#pragma unroll
-          for (int i = 0; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
-          __syncwarp();
-        }
-        m0 = fmaxf(m0, m1);
-        const float best = m0 == -INFINITY ? m0 : m0 * scale;
-        float f = 1.f, f_unit = 1.f, v_unit = 1.f;       // of the sum; of O's unit; V's scales' unit
-        if (best > top + kLazy) {
-          f = top == -INFINITY ? 0.f : exp2_fast(top - best);
-          top = best;
-        }
+        float v_unit = 1.f, f_unit = 1.f;        // V's scales' unit, and what its change does to O
         if constexpr (kQuant) {
           // the row kernel's rule for V's scales
           const float *vs = ks + 128;
@@ -616,27 +607,9 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
           if (v_exp != -1000) v_unit = power2(-v_exp);
         }
-        const float f_o = f * f_unit;
-        if (__builtin_expect(__any_sync(0xffffffffu, f_o != 1.f), 0)) {
-          sum *= f;
-          if (mine > 0) {                // the last product is over: these scores were issued behind it
+        const Pair scale2 = pair(scale, scale), unit2 = pair(v_unit, v_unit);
 #pragma unroll 1
-            for (int c = 0; c < DP; c += 32) {
-              unsigned x[32];
-              tm_load32(x, tm_o[w] + lanes + c);
-              tm_loaded();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f_o);
-              tm_store32(tm_o[w] + lanes + c, x);
-            }
-            tm_stored();
-          }
-        }
-        const float base = top == -INFINITY ? 0.f : top;
-        const Pair scale2 = pair(scale, scale), base2 = pair(-base, -base), unit2 = pair(v_unit, v_unit);
-        Pair sum0 = 0, sum1 = 0;
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2;) {
           load_scores(h);
           unsigned long long vis = ~0ull;
           if (__builtin_expect(edge, 0)) {
@@ -644,6 +617,13 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 #pragma unroll
             for (int i = 0; i < 64; ++i) if (!(vis >> i & 1)) s[i] = -INFINITY;
           }
+          float m0 = fmaxf(s[0], s[1]), m1 = fmaxf(s[2], s[3]);
+#pragma unroll
+          for (int i = 4; i < 64; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
+          m0 = fmaxf(m0, m1);
+          const float base = top == -INFINITY ? 0.f : top;
+          const Pair base2 = pair(-base, -base);
+          Pair sum0 = 0, sum1 = 0;
 #pragma unroll
           for (int i = 0; i < 64; i += 4) {
             const float2 p = unpair(fma2(pair(s[i], s[i + 1]), scale2, base2)), q = unpair(fma2(pair(s[i + 2], s[i + 3]), scale2, base2));
@@ -651,6 +631,51 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             sum0 = add2(sum0, pair(s[i], s[i + 1]));
             sum1 = add2(sum1, pair(s[i + 2], s[i + 3]));
           }
+          const float best = m0 == -INFINITY ? m0 : m0 * scale;
+          const bool higher = best > top + kLazy;
+          if (__builtin_expect(__any_sync(0xffffffffu, higher || f_unit != 1.f), 0)) {
+            // O, the sum and the probabilities that are already there go down; then the same 64 keys again: their scores
+            // have not been written over yet
+            float f = 1.f;
+            if (higher) {
+              f = top == -INFINITY ? 0.f : exp2_fast(top - best);
+              top = best;
+            }
+            sum *= f;
+            const float f_o = f * f_unit;
+            f_unit = 1.f;
+            if (mine > 0) {              // the last product is over: these scores were issued behind it
+#pragma unroll 1
+              for (int c = 0; c < DP; c += 32) {
+                unsigned x[32];
+                tm_load32(x, tm_o[w] + lanes + c);
+                tm_loaded();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f_o);
+                tm_store32(tm_o[w] + lanes + c, x);
+              }
+              tm_stored();
+            }
+            if (h == 1) {                // (V's unit moves before the first half only: f alone)
+              unsigned x[32];
+              tm_load32(x, s_at);
+              tm_loaded();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                if constexpr (kBf16) {
+                  x[i] = pack_bf16(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xffff0000u) * f);
+                } else {
+                  const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&x[i]));
+                  x[i] = pack_f16(p.x * f, p.y * f);
+                }
+              }
+              tm_store32(s_at, x);
+              tm_stored();
+            }
+            continue;
+          }
+          const float2 sums = unpair(add2(sum0, sum1));
+          sum += sums.x + sums.y;
           if constexpr (kQuant) {
             const float *v_scale = ks + 128 + h * 64;
 #pragma unroll
@@ -670,9 +695,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           __syncwarp();
           tm_store32(s_at + h * 32, p);  // over the scores of keys that are done with
           tm_stored();
+          ++h;
         }
-        const float2 sums = unpair(add2(sum0, sum1));
-        sum += sums.x + sums.y;
         const bool look = !kQuant && edge && (len.fresh > 1 || a.mask);
         unsigned long long odd[2] = {0, 0};
         if (__builtin_expect(look, 0)) {
@@ -794,7 +818,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
     __syncthreads();
   }
-  if (warp == S::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
   if (threadIdx.x == 0 && gave_up_word) report(a.b.status, KVR_DEV_GAVE_UP);
 }
 
