@@ -98,14 +98,18 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     a.head_groups = spec->kv_heads;
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
-    a.unit_keys = 128;
+    a.unit = FastDiv(128);
     a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
     if (a.box_rows && !layer_map(spec, a.c, padded, a.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
   } else {
     tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
     a.row_tile = tiles * 8;
-    a.unit_keys = slices < 4 ? (64 + 16 * slices - 1) / (16 * slices) * 16 * slices : 16 * slices;     // 64 or more: fewer pieces
+    a.unit = FastDiv(slices < 4 ? (64 + 16 * slices - 1) / (16 * slices) * 16 * slices : 16 * slices);       // 64 or more: fewer pieces
   }
+  while ((1 << a.row_shift) < a.row_tile) ++a.row_shift;
+  // units are numbered in 32 bits; a bound that the lengths on the device keep, whatever they are
+  const double most = (double)batch->n_req * (((int64_t)batch->max_new * group + a.row_tile - 1) / a.row_tile) * a.head_groups * (batch->max_tokens / a.unit.d + 1.);
+  if (most >= INT32_MAX) return fail_cache(KVR_ERR_INVALID_ARG, "n_req, max_new and max_tokens are too large for one call");
   a.ctas = sms;
   a.handed_in = static_cast<int *>(workspace);
   a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + kCounterBytes);

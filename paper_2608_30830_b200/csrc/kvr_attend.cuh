@@ -1,7 +1,7 @@
 // Attention over the paged cache: how a call's work is cut up, and what its kernels share.
 //
 // Work is cut along the keys.  A segment is one request, one group of KV heads and one tile of its query rows (row =
-// new token x query heads of one KV head + query head); a unit is `unit_keys` keys of a segment.  Segments follow each
+// new token x query heads of one KV head + query head); a unit is a fixed number of keys of a segment.  Segments follow each
 // other request by request, and the units of all of them are dealt out in equal runs, one to each CTA of a grid that
 // fills the GPU once: ragged requests keep all SMs busy to the end, and the cut needs nothing from the host but the
 // grid's size.  A CTA that holds a whole segment writes its result; the pieces of a cut segment go to the workspace as
@@ -18,7 +18,7 @@ namespace kvr {
 struct AttendArgs {
   Batch b;
   CacheView c;
-  FastDiv bs, group;         // block size; query heads per KV head
+  FastDiv bs, group, unit;   // block size; query heads per KV head; keys of a unit
   Rows q, out;
   float *lse;                // or NULL
   const unsigned long long *mask;    // or NULL: causal
@@ -26,12 +26,11 @@ struct AttendArgs {
   float scale_log2;          // scale * log2(e)
   int q_heads;
   int head_groups, group_heads;      // KV heads are taken group_heads at a time
-  int row_tile;              // query rows of a segment
-  int unit_keys;
+  int row_tile, row_shift;   // query rows of a segment, 2^row_shift
   int box_rows;              // tokens of a TMA box (tile kernel): 8 or 16, 0: the block size does not allow one
   int ctas;                  // the grid of the main kernel
   int *handed_in;            // [2][ctas][2]: pieces of a group, groups of a segment; zero between calls
-  float *part_o;             // [ctas][2][group_heads][row_tile][head_dim]
+  float *part_o;             // [ctas][2][group_heads][row_tile][head_dim]; of the tile kernel [ctas][2][head_dim][row_tile]
   float2 *part_ml;           // [ctas][2][group_heads][row_tile]: maximum (log2), sum
 };
 
@@ -54,70 +53,82 @@ __device__ __forceinline__ Lengths attend_lengths(const AttendArgs &a, int r) {
   Lengths l;
   request_lengths(a.b, a.bs.d, r, l.first, l.context, l.fresh);
   l.keys = l.context + l.fresh;
-  l.units = (l.keys + a.unit_keys - 1) / a.unit_keys;
-  l.segments = l.fresh > 0 ? a.head_groups * (int)(((long long)l.fresh * (int)a.group.d + a.row_tile - 1) / a.row_tile) : 0;
+  l.units = (int)a.unit.div(l.keys + a.unit.d - 1);
+  l.segments = a.head_groups * ((l.fresh * (int)a.group.d + a.row_tile - 1) >> a.row_shift);
   return l;
 }
-__device__ __forceinline__ long long units_of(const AttendArgs &a, int r) {
-  const Lengths l = attend_lengths(a, r);
-  return (long long)l.units * l.segments;
-}
 
-// Both for a whole CTA; scratch: 34 words of shared memory.  total_units: of all requests.  find_unit: the request that
-// holds a unit (one below the total), and the number of its first unit.
-__device__ __forceinline__ long long warp_sum(long long v) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  return v;
-}
-__device__ __forceinline__ long long total_units(const AttendArgs &a, long long *scratch) {
-  long long mine = 0;
-  for (int r = threadIdx.x; r < a.b.n_req; r += blockDim.x) {
-    int first, context, fresh;
-    if (blockIdx.x == 0 && !request_lengths(a.b, a.bs.d, r, first, context, fresh)) report(a.b.status, KVR_DEV_BAD_LENGTH);
-    mine += units_of(a, r);
+// How the units of a call are dealt out: `ctas` runs, the first `rem` of them one unit longer.  (The host has seen to it that units
+// fit 32 bits.)
+struct Shares {
+  unsigned total, size, rem;
+  int ctas;
+  __device__ __forceinline__ unsigned first(int c) const { return size * c + min((unsigned)c, rem); }
+  __device__ __forceinline__ int cta_of(unsigned unit) const {
+    const unsigned longer = rem * (size + 1);
+    return (int)(unit < longer ? unit / (size + 1) : rem + (unit - longer) / size);
   }
-  mine = warp_sum(mine);
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = mine;
-  __syncthreads();
-  long long total = 0;
-  for (int w = 0; w < (int)(blockDim.x + 31) / 32; ++w) total += scratch[w];
-  __syncthreads();
-  return total;
-}
-__device__ __forceinline__ void find_unit(const AttendArgs &a, long long unit, long long *scratch, int &r_out, long long &base_out) {
-  long long carry = 0;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) / 32;
-  for (int r0 = 0; r0 < a.b.n_req; r0 += blockDim.x) {
+};
+
+// For a whole CTA: the shares of the call, and the request that this CTA's first unit belongs to with its lengths and the number of
+// its own first unit.  False where there is nothing for this CTA.  scratch: 39 words of shared memory.
+__device__ __forceinline__ bool find_share(const AttendArgs &a, unsigned *scratch, Shares &sh, int &r_out, unsigned &base_out, Lengths &len_out) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
+  const bool once = a.b.n_req <= (int)blockDim.x;
+  Lengths mine{};
+  unsigned units = 0, incl = 0, before = 0;
+  // units of request r0 + thread, of all requests up to it within this round (incl) and of the rounds' warps before (before)
+  auto scan = [&](int r0) {
     const int r = r0 + threadIdx.x;
-    const long long mine = r < a.b.n_req ? units_of(a, r) : 0;
-    long long incl = mine;
+    units = 0;
+    if (r < a.b.n_req) {
+      mine = attend_lengths(a, r);
+      units = (unsigned)mine.units * mine.segments;
+      int first, context, fresh;
+      if (blockIdx.x == 0 && !request_lengths(a.b, a.bs.d, r, first, context, fresh)) report(a.b.status, KVR_DEV_BAD_LENGTH);
+    }
+    incl = units;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+      const unsigned up = __shfl_up_sync(0xffffffffu, incl, d);
       if (lane >= d) incl += up;
     }
     if (lane == 31) scratch[warp] = incl;
     __syncthreads();
-    long long before = carry, all = carry;
+    unsigned all = 0;
+    before = 0;
     for (int w = 0; w < warps; ++w) {
       if (w < warp) before += scratch[w];
       all += scratch[w];
     }
-    const long long lo = before + incl - mine;
-    if (unit >= lo && unit < lo + mine) { scratch[32] = r; scratch[33] = lo; }
     __syncthreads();
-    if (unit < all) break;
-    carry = all;
+    return all;
+  };
+  sh.total = 0;
+  for (int r0 = 0; r0 < a.b.n_req; r0 += blockDim.x) sh.total += scan(r0);
+  sh.ctas = (int)min((unsigned)a.ctas, sh.total);
+  if ((int)blockIdx.x >= sh.ctas) return false;
+  sh.size = sh.total / sh.ctas;
+  sh.rem = sh.total - sh.size * sh.ctas;
+  const unsigned unit = sh.first(blockIdx.x);
+  unsigned carry = 0;
+  for (int r0 = 0; r0 < a.b.n_req; r0 += blockDim.x) {
+    const unsigned all = once ? sh.total : scan(r0);
+    const unsigned lo = carry + before + incl - units;
+    if (unit >= lo && unit - lo < units) {
+      scratch[32] = r0 + threadIdx.x; scratch[33] = lo;
+      scratch[34] = mine.first; scratch[35] = mine.context; scratch[36] = mine.fresh; scratch[37] = mine.units; scratch[38] = mine.segments;
+    }
+    carry += all;
+    if (unit < carry) break;
+    __syncthreads();
   }
+  __syncthreads();
   r_out = (int)scratch[32];
   base_out = scratch[33];
-  __syncthreads();
+  len_out = Lengths{(int)scratch[34], (int)scratch[35], (int)scratch[36], (int)(scratch[35] + scratch[36]), (int)scratch[37], (int)scratch[38]};
+  return true;
 }
-
-// units [first_unit(c), first_unit(c + 1)) belong to CTA c
-__device__ __forceinline__ long long first_unit(long long total, int ctas, int c) { return total * c / ctas; }
-__device__ __forceinline__ int cta_of(long long total, int ctas, long long unit) { return (int)(((unit + 1) * ctas + total - 1) / total) - 1; }
 
 // May row i of a request (of `fresh` new tokens) look at its new token j?
 __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int j) {

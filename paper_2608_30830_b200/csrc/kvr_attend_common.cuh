@@ -47,27 +47,31 @@ __device__ __forceinline__ unsigned widen(unsigned w) {
 
 // A CTA's walk over the pieces of segments in its run of units.
 struct Piece {
-  long long unit;            // first unit of the piece
-  long long base;            // first unit of its request
+  unsigned unit;             // first unit of the piece
+  unsigned base;             // first unit of its request
   int r, head_group, row0;   // request, group of KV heads, first query row
   int begin, end;            // units of the segment
   Lengths len;
 };
-__device__ __forceinline__ void open_piece(const AttendArgs &a, Piece &p, long long last) {
+__device__ __forceinline__ void open_piece(const AttendArgs &a, Piece &p, unsigned last) {
   // requests without units are passed over (the bound on r cannot be met while p.unit is below the call's units)
-  while (p.len.segments == 0 || p.unit - p.base >= (long long)p.len.units * p.len.segments) {
+  while (p.unit - p.base >= (unsigned)p.len.units * p.len.segments) {
     p.base = p.unit;
     if (++p.r >= a.b.n_req) { p.r = a.b.n_req - 1; p.len = Lengths{0, 0, 0, 0, 1, 1}; break; }
     p.len = attend_lengths(a, p.r);
   }
   const int offset = (int)((p.unit - p.base) / p.len.units);
-  p.begin = (int)((p.unit - p.base) - (long long)offset * p.len.units);
-  p.end = (int)min((long long)p.len.units, p.begin + (last - p.unit));
-  const int tiles = p.len.segments / a.head_groups;
-  p.head_group = offset / tiles;
-  p.row0 = (offset - p.head_group * tiles) * a.row_tile;
+  p.begin = (int)((p.unit - p.base) - offset * p.len.units);
+  p.end = (int)min((unsigned)p.len.units, p.begin + (last - p.unit));
+  p.head_group = 0;
+  p.row0 = offset << a.row_shift;
+  if (a.head_groups > 1) {
+    const int tiles = p.len.segments / a.head_groups;
+    p.head_group = offset / tiles;
+    p.row0 = (offset - p.head_group * tiles) << a.row_shift;
+  }
 }
-__device__ __forceinline__ bool next_piece(const AttendArgs &a, Piece &p, long long last) {
+__device__ __forceinline__ bool next_piece(const AttendArgs &a, Piece &p, unsigned last) {
   p.unit += p.end - p.begin;
   if (p.unit >= last) return false;
   open_piece(a, p, last);
@@ -76,6 +80,7 @@ __device__ __forceinline__ bool next_piece(const AttendArgs &a, Piece &p, long l
 
 struct Cut {
   int c0, c1, which0;        // the CTAs of the segment; which of the first one's two pieces it is
+  __device__ __forceinline__ int piece(int c) const { return c * 2 + (c == c0 ? which0 : 0); }
 };
 // The rows of a segment from its pieces of `n` <= 32 CTAs c, c + step, ...: to the output, or (fold) to the first one's place.
 // A lane has 4 channels of a 128-channel slab; what costs is latency, so kRows rows and kAhead pieces are read at once.
@@ -176,14 +181,15 @@ __device__ __noinline__ void join_pieces(const AttendArgs &a, const Piece &p, co
 }
 
 // After this CTA's piece of a cut segment has been stored: joins the segment's pieces if it was the last to come in.  sync() is
-// a barrier of the `warps` warps that call this (false: given up); `last` is shared memory.
-template <int SLABS, class Sync>
-__device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, long long total, int ctas, int rows, int heads, int warps, int warp, int lane, Sync sync, volatile int *last) {
-  const long long begin = p.unit - p.begin;
+// a barrier of the warps that call this (false: given up); `last` is shared memory; join(cut, c, step, n, fold) joins the pieces of
+// the n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.
+template <class Sync, class Join>
+__device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, const Shares &sh, Sync sync, volatile int *last, int warp, int lane, Join join) {
+  const unsigned begin = p.unit - p.begin;
   Cut cut;
-  cut.c0 = cta_of(total, ctas, begin);
-  cut.c1 = cta_of(total, ctas, begin + p.len.units - 1);
-  cut.which0 = first_unit(total, ctas, cut.c0) == begin ? 0 : 1;
+  cut.c0 = sh.cta_of(begin);
+  cut.c1 = sh.cta_of(begin + p.len.units - 1);
+  cut.which0 = sh.first(cut.c0) == begin ? 0 : 1;
   const int all = cut.c1 - cut.c0 + 1, groups = (all + kJoinAtOnce - 1) / kJoinAtOnce;
   const int group = ((int)blockIdx.x - cut.c0) / kJoinAtOnce, leader = cut.c0 + group * kJoinAtOnce, n = min(kJoinAtOnce, cut.c1 - leader + 1);
   auto come_in = [&](int *counter, int of) {
@@ -199,12 +205,11 @@ __device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, lon
   };
   if (!come_in(a.handed_in + leader * 2 + (leader == cut.c0 ? cut.which0 : 0), n)) return false;
   if (!*last) return true;
-  const Piece copy = p;                  // what the call is shown lies in memory
-  join_pieces<SLABS>(a, copy, cut, leader, 1, n, groups > 1, rows, heads, warps, warp, lane);
+  join(cut, leader, 1, n, groups > 1);
   if (groups == 1) return true;
   if (!come_in(a.handed_in + (a.ctas + cut.c0) * 2 + cut.which0, groups)) return false;
   if (!*last) return true;
-  join_pieces<SLABS>(a, copy, cut, cut.c0, kJoinAtOnce, groups, false, rows, heads, warps, warp, lane);
+  join(cut, cut.c0, kJoinAtOnce, groups, false);
   return true;
 }
 

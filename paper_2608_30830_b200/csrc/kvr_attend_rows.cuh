@@ -65,22 +65,19 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
   constexpr float kLazy = 4.f;         // a row's maximum moves only when a score passes it by 2^4: fewer rescales,
                                        // probabilities up to 16 (room in f16, see the scale of V below)
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ long long scratch[34];
+  __shared__ unsigned scratch[39];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const int local_head = warp / slices, slice = warp - local_head * slices;
   __shared__ int last_in;
 
-  const long long total = total_units(a, scratch);
-  const int ctas = (int)min((long long)a.ctas, total);
-  if ((int)blockIdx.x >= ctas) return;
-  const long long first = first_unit(total, ctas, blockIdx.x), last = first_unit(total, ctas, blockIdx.x + 1);
+  Shares shares;
   Piece piece;
-  find_unit(a, first, scratch, piece.r, piece.base);
+  if (!find_share(a, scratch, shares, piece.r, piece.base, piece.len)) return;
+  const unsigned first = shares.first(blockIdx.x), last = shares.first(blockIdx.x + 1);
   piece.unit = first;
-  piece.len = attend_lengths(a, piece.r);
   open_piece(a, piece, last);
 
-  const int unit_chunks = a.unit_keys / (16 * slices);       // of one warp
+  const int unit_chunks = (int)a.unit.d / (16 * slices);     // of one warp
   unsigned char *ring = smem + warp * (kStages * S::kStageBytes);
   float *merge = reinterpret_cast<float *>(smem + (blockDim.x >> 5) * (kStages * S::kStageBytes));
 
@@ -534,7 +531,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
     }
     if (piece.begin != 0 || piece.end != len.units) {
       const int heads = min(a.group_heads, a.c.kv_heads - piece.head_group * a.group_heads);
-      hand_in<DP / 128 + DP % 128 / 64>(a, piece, total, ctas, rows, heads, (int)blockDim.x / 32, warp, lane, [] { __syncthreads(); return true; }, &last_in);
+      hand_in(a, piece, shares, [] { __syncthreads(); return true; }, &last_in, warp, lane, [&](const Cut &cut, int c, int step, int n, bool fold) {
+        const Piece copy = piece;        // what the call is shown lies in memory
+        join_pieces<DP / 128 + DP % 128 / 64>(a, copy, cut, c, step, n, fold, rows, heads, (int)blockDim.x / 32, warp, lane);
+      });
     }
     again = next_piece(a, piece, last);
   }

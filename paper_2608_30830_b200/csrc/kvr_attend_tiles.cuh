@@ -159,7 +159,7 @@ struct TileWalk {
   __device__ __forceinline__ bool is_k() const { return k < n && k < v + AHEAD; }
   __device__ __forceinline__ int tile() const { return t0 + (is_k() ? k : v); }
   __device__ __forceinline__ int slot() const { return (is_k() ? tiles : tiles - (k - v)) & 3; }     // of the tile's scales
-  __device__ __forceinline__ void advance(const AttendArgs &a, int unit_tiles, long long last) {
+  __device__ __forceinline__ void advance(const AttendArgs &a, int unit_tiles, unsigned last) {
     ++step;
     if (is_k()) { ++k; ++tiles; } else ++v;
     if (v == n) {
@@ -195,6 +195,64 @@ __device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const
   return vis;
 }
 
+// The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  256 threads, a
+// row each (of 128 rows: half of a row's channels); pieces lie channel by channel, so the threads of a warp read side by side.
+__device__ __forceinline__ float2 row_statistics(const AttendArgs &a, const Cut &cut, int c, int step, int n, int row) {
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(a.part_ml + (long long)cut.piece(c + k * step) * a.row_tile + row).x);
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) {
+    const float2 ml = __ldcg(a.part_ml + (long long)cut.piece(c + k * step) * a.row_tile + row);
+    l += ml.y * (ml.x == m ? 1.f : exp2_fast(ml.x - m));                 // both -infinity: a piece of an empty row
+  }
+  return make_float2(m, l);
+}
+__device__ __forceinline__ void fold_statistics(const AttendArgs &a, const Cut &cut, int c, int step, int n, int thread) {
+  if (thread >= a.row_tile) return;
+  const float2 ml = row_statistics(a, cut, c, step, n, thread);
+  a.part_ml[(long long)cut.piece(c) * a.row_tile + thread] = ml;
+}
+__device__ __noinline__ void join_tiles(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int thread) {
+  const int row = thread & (a.row_tile - 1);
+  const int per = a.row_tile > 128 ? a.c.head_dim : a.c.head_dim / 2, d0 = (thread >> a.row_shift) * per;      // channels of this thread
+  if (p.row0 + row >= p.len.fresh * (int)a.group.d) return;
+  const float2 all = row_statistics(a, cut, c, step, n, row);
+  const float inv = all.y > 0.f ? 1.f / all.y : all.y == 0.f ? 0.f : NAN;
+  const int t = (int)a.group.div(p.row0 + row), q_head = p.head_group * (int)a.group.d + (p.row0 + row - t * (int)a.group.d);
+  char *dst = a.out.data + (long long)(p.len.first + t) * a.out.token_stride + (long long)q_head * a.out.head_stride;
+#pragma unroll 1
+  for (int d = d0; d < d0 + per; d += 32) {
+    const int channels = min(32, d0 + per - d);          // a multiple of 8
+    float o[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      const long long piece = cut.piece(c + k * step);
+      const float m = __ldcg(a.part_ml + piece * a.row_tile + row).x, f = m == all.x ? 1.f : exp2_fast(m - all.x);
+      const float *src = a.part_o + (piece * a.c.head_dim + d) * a.row_tile + row;
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = i < channels ? __ldcg(src + i * a.row_tile) : 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] += f * x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+      if (i >= channels) break;
+      if (fold) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a.part_o[((long long)cut.piece(c) * a.c.head_dim + d + i + e) * a.row_tile + row] = o[i + e];
+      } else {
+        const float y[8] = {o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv, o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv};
+        if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + (d + i) * 2, y); else store8<KVR_F16>(dst + (d + i) * 2, y);
+      }
+    }
+  }
+  if (!fold && a.lse && d0 == 0) a.lse[(long long)(p.len.first + t) * a.q_heads + q_head] = all.y == 0.f ? -INFINITY : all.x * 0.69314718f + logf(all.y);
+}
+
 template <int FMT, int DP, bool TWO>
 __global__ void __launch_bounds__(TileShape<FMT, DP, TWO>::kThreads, 1)
 attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
@@ -203,7 +261,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   constexpr int kAhead = TWO ? 1 : 2;            // key tiles whose scores are made before the first is used
   constexpr float kLazy = kQuant ? 4.f : 8.f;    // 8-bit: leaves room for V's scale, see the row kernel
   extern __shared__ unsigned char raw_smem[];
-  __shared__ long long scratch[34];
+  __shared__ unsigned scratch[39];
   __shared__ __align__(8) TileBars bars;
   __shared__ unsigned tm_slot;
   __shared__ int gave_up_word, last_in;
@@ -217,16 +275,13 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   float *scale_raw = scales + S::kScaleSlots * 256;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  const long long total = total_units(a, scratch);
-  const int ctas = (int)min((long long)a.ctas, total);
-  if ((int)blockIdx.x >= ctas) return;
-  const long long first = first_unit(total, ctas, blockIdx.x), last = first_unit(total, ctas, blockIdx.x + 1);
+  Shares shares;
   Piece piece;
-  find_unit(a, first, scratch, piece.r, piece.base);
+  if (!find_share(a, scratch, shares, piece.r, piece.base, piece.len)) return;
+  const unsigned first = shares.first(blockIdx.x), last = shares.first(blockIdx.x + 1);
   piece.unit = first;
-  piece.len = attend_lengths(a, piece.r);
   open_piece(a, piece, last);
-  const int unit_tiles = a.unit_keys / kTileKeys;
+  const int unit_tiles = (int)a.unit.d / kTileKeys;
   auto first_tile = [&](const Piece &p) { return p.begin * unit_tiles; };
   auto last_tile = [&](const Piece &p) { return min(p.end * unit_tiles, (p.len.keys + kTileKeys - 1) / kTileKeys); };
 
@@ -267,7 +322,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     int *ids = box_ids[me];
     const int per_tile = a.box_rows ? kTileKeys / a.box_rows : 0;
     int box_next = 0, fetched = 0;       // first box of the batch in `fetched`
-    long long at_unit = -1;
+    unsigned at_unit = ~0u;
     auto fetch = [&]() {
       const int token = (box_next + lane) * a.box_rows;
       fetched = token < at.p.len.keys ? __ldg(a.b.tables + (long long)at.p.r * a.b.table_stride + a.bs.div(token)) : -1;
@@ -526,36 +581,35 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         const char *src = a.q.data + (long long)(len.first + t_row) * a.q.token_stride + (long long)q_head * a.q.head_stride;
         unsigned char *dst = q_tile + (TWO ? w : 0) * (128 * DP * 2) + tid * 128;
         const unsigned flip = a.scale_log2 < 0 ? 0x80008000u : 0u;       // a negative one: Q's sign
-        float down = 1.f;
+        uint4 x[DP / 8];
+#pragma unroll
+        for (int c = 0; c < DP / 8; ++c) {
+          x[c] = make_uint4(0, 0, 0, 0);
+          if (have && c * 8 < a.c.head_dim && a.scale_log2 != 0.f) x[c] = *reinterpret_cast<const uint4 *>(src + c * 16);
+        }
         if constexpr (kQuant) {
-          float top = 0.f;
-#pragma unroll 4
+          float top = 0.f, down = 1.f;
+          const bool bf16 = a.q.type == KVR_BF16;
+#pragma unroll
           for (int c = 0; c < DP / 8; ++c) {
-            if (!have || c * 8 >= a.c.head_dim) break;
             float y[8];
-            if (a.q.type == KVR_BF16) load8<KVR_BF16>(src + c * 16, y); else load8<KVR_F16>(src + c * 16, y);
+            if (bf16) widen8<KVR_BF16>(x[c], y); else widen8<KVR_F16>(x[c], y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));
           }
           const unsigned e = __float_as_uint(top) >> 23;
           if (e >= 1 && e <= 253) { down = __uint_as_float((254u - e) << 23); scale *= __uint_as_float(e << 23); }
+#pragma unroll
+          for (int c = 0; c < DP / 8; ++c) {
+            float y[8];
+            if (bf16) widen8<KVR_BF16>(x[c], y); else widen8<KVR_F16>(x[c], y);
+            x[c] = make_uint4(pack_f16(y[0] * down, y[1] * down), pack_f16(y[2] * down, y[3] * down), pack_f16(y[4] * down, y[5] * down), pack_f16(y[6] * down, y[7] * down));
+          }
         }
         if (TWO || w == 0) {
-#pragma unroll 4
-          for (int c = 0; c < DP / 8; ++c) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (have && c * 8 < a.c.head_dim && a.scale_log2 != 0.f) {
-              if constexpr (!kQuant) {
-                x = *reinterpret_cast<const uint4 *>(src + c * 16);
-              } else {
-                float y[8];
-                if (a.q.type == KVR_BF16) load8<KVR_BF16>(src + c * 16, y); else load8<KVR_F16>(src + c * 16, y);
-                x = make_uint4(pack_f16(y[0] * down, y[1] * down), pack_f16(y[2] * down, y[3] * down), pack_f16(y[4] * down, y[5] * down), pack_f16(y[6] * down, y[7] * down));
-              }
-              x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
-            }
-            *reinterpret_cast<uint4 *>(dst + (c >> 3) * (128 * 128) + (((c & 7) ^ (tid & 7)) << 4)) = x;
-          }
+#pragma unroll
+          for (int c = 0; c < DP / 8; ++c)
+            *reinterpret_cast<uint4 *>(dst + (c >> 3) * (128 * 128) + (((c & 7) ^ (tid & 7)) << 4)) = make_uint4(x[c].x ^ flip, x[c].y ^ flip, x[c].z ^ flip, x[c].w ^ flip);
         }
         fence_async();
         __syncwarp();
@@ -770,7 +824,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         const bool whole = piece.begin == 0 && piece.end == len.units;
         const int local = (TWO ? w * 128 : 0) + tid;
         const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
-        const long long place = ((long long)blockIdx.x * 2 + (piece.unit == first ? 0 : 1)) * a.row_tile + local;
+        const long long slot = (long long)blockIdx.x * 2 + (piece.unit == first ? 0 : 1);
         char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
         const bool joined = !TWO && n > 1;
 #pragma unroll 1
@@ -792,19 +846,27 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
               const float y[8] = {o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv, o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv};
               if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + (c + i) * 2, y); else store8<KVR_F16>(dst + (c + i) * 2, y);
             } else {
-              const float y[8] = {o[i], o[i + 1], o[i + 2], o[i + 3], o[i + 4], o[i + 5], o[i + 6], o[i + 7]};
-              store8<KVR_F32>(reinterpret_cast<char *>(a.part_o + place * a.c.head_dim + c + i), y);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) a.part_o[(slot * a.c.head_dim + c + i + e) * a.row_tile + local] = o[i + e];
             }
           }
           __syncwarp();
         }
         if (have) {
-          if (!whole) a.part_ml[place] = make_float2(top, sum);
+          if (!whole) a.part_ml[slot * a.row_tile + local] = make_float2(top, sum);
           else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum == 0.f ? -INFINITY : top * 0.69314718f + logf(sum);
         }
       }
       if (piece.begin != 0 || piece.end != len.units)
-        ok = hand_in<1>(a, piece, total, ctas, min(a.row_tile, len.fresh * (int)a.group.d - piece.row0), 1, 8, warp, lane, join, &last_in);
+        ok = hand_in(a, piece, shares, join, &last_in, warp, lane, [&](const Cut &cut, int c, int step, int n, bool fold) {
+          const Piece copy = piece;      // what the call is shown lies in memory
+          join_tiles(a, copy, cut, c, step, n, fold, threadIdx.x);
+          if (fold) {
+            // the folded statistics go last: two threads of a row may have read them
+            join();
+            fold_statistics(a, cut, c, step, n, threadIdx.x);
+          }
+        });
       else if (!TWO)
         ok = join();                     // the exchange has been read: Q's place may be written again
       again = next_piece(a, piece, last);
