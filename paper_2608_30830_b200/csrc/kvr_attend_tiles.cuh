@@ -128,11 +128,14 @@ struct TileShape {
   static constexpr int kSteps = 3, kPerStep = kQuant ? 2 : 1;         // steps loaded at a time, warps of a step
   static constexpr int kLoaders = kSteps * kPerStep, kSpan = kTileKeys / kPerStep; // a warp's keys of a step
   static constexpr int kThreads = kQuant ? 512 : 384;
-  static constexpr int kQBytes = 2 * 128 * DP * 2;                       // two tiles of 128 rows
+  // Q, a tile or two of 128 rows.  At a piece's end the place holds what the warpgroups exchange, 32 channels each way, and the
+  // weights of a join (16 pieces).
+  static constexpr int kQBytes = TWO || DP < 128 ? 2 * 128 * DP * 2 : 128 * DP * 2;
+  static_assert(kQBytes >= 2 * 32 * 128 * 4 && kQBytes >= kJoinAtOnce * 256 * 4, "");
   static constexpr int kBuffer = kTileKeys * DP * 2;                     // K or V of a tile, 16 bits
   // Buffers: what shared memory holds.  No fewer than the steps loaded at a time: a loader waits for step s - kRing to be used up
   // having filled step s - kSteps, and a barrier's parity is clear only if step s - 2 kRing is known to be over.
-  static constexpr int kRing = kQuant ? 3 : TWO ? 5 : 4;
+  static constexpr int kRing = (kQuant ? 3 : 5) + (kQuant && !TWO ? 1 : 0);
   static_assert(kRing >= kSteps, "");
   static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
   static constexpr int kScaleSlots = kQuant ? 4 : 0;                     // 128 scales of K, 128 of V
@@ -195,62 +198,78 @@ __device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const
   return vis;
 }
 
-// The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  256 threads, a
-// row each (of 128 rows: half of a row's channels); pieces lie channel by channel, so the threads of a warp read side by side.
-__device__ __forceinline__ float2 row_statistics(const AttendArgs &a, const Cut &cut, int c, int step, int n, int row) {
+// The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  256 threads.
+// First, a thread a row, what each piece counts for (weights[piece][row]); then the sums, a thread four rows and 8 channels at a
+// time: pieces lie channel by channel, and 16 loads of 16 bytes are under way for each thread (a row a thread, 4 bytes at a time, took
+// 15 us longer for three pieces of 256 rows).
+__device__ __noinline__ void join_weights(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int row, float *weights) {
+  if (row >= a.row_tile || p.row0 + row >= p.len.fresh * (int)a.group.d) return;
+  float2 ml[kJoinAtOnce];
   float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) m = fmaxf(m, __ldcg(a.part_ml + (long long)cut.piece(c + k * step) * a.row_tile + row).x);
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) {
-    const float2 ml = __ldcg(a.part_ml + (long long)cut.piece(c + k * step) * a.row_tile + row);
-    l += ml.y * (ml.x == m ? 1.f : exp2_fast(ml.x - m));                 // both -infinity: a piece of an empty row
+#pragma unroll
+  for (int k = 0; k < kJoinAtOnce; ++k) {
+    ml[k] = make_float2(-INFINITY, 0.f);
+    if (k < n) ml[k] = __ldcg(a.part_ml + (long long)cut.piece(c + k * step) * a.row_tile + row);
+    m = fmaxf(m, ml[k].x);
   }
-  return make_float2(m, l);
+#pragma unroll
+  for (int k = 0; k < kJoinAtOnce; ++k) {
+    ml[k].x = ml[k].x == m ? 1.f : exp2_fast(ml[k].x - m);      // both -infinity: a piece of an empty row
+    l += ml[k].y * ml[k].x;
+  }
+  const float inv = fold ? 1.f : l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+#pragma unroll
+  for (int k = 0; k < kJoinAtOnce; ++k) if (k < n) weights[k * 256 + row] = ml[k].x * inv;
+  if (fold) {
+    a.part_ml[(long long)cut.piece(c) * a.row_tile + row] = make_float2(m, l);
+  } else if (a.lse) {
+    const int t = (int)a.group.div(p.row0 + row), q_head = p.head_group * (int)a.group.d + (p.row0 + row - t * (int)a.group.d);
+    a.lse[(long long)(p.len.first + t) * a.q_heads + q_head] = l == 0.f ? -INFINITY : m * 0.69314718f + logf(l);
+  }
 }
-__device__ __forceinline__ void fold_statistics(const AttendArgs &a, const Cut &cut, int c, int step, int n, int thread) {
-  if (thread >= a.row_tile) return;
-  const float2 ml = row_statistics(a, cut, c, step, n, thread);
-  a.part_ml[(long long)cut.piece(c) * a.row_tile + thread] = ml;
-}
-__device__ __noinline__ void join_tiles(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int thread) {
-  const int row = thread & (a.row_tile - 1);
-  const int per = a.row_tile > 128 ? a.c.head_dim : a.c.head_dim / 2, d0 = (thread >> a.row_shift) * per;      // channels of this thread
-  if (p.row0 + row >= p.len.fresh * (int)a.group.d) return;
-  const float2 all = row_statistics(a, cut, c, step, n, row);
-  const float inv = all.y > 0.f ? 1.f / all.y : all.y == 0.f ? 0.f : NAN;
-  const int t = (int)a.group.div(p.row0 + row), q_head = p.head_group * (int)a.group.d + (p.row0 + row - t * (int)a.group.d);
-  char *dst = a.out.data + (long long)(p.len.first + t) * a.out.token_stride + (long long)q_head * a.out.head_stride;
+__device__ __noinline__ void join_rows(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int thread, const float *weights) {
+  const int quads = a.row_tile / 4, row = (thread & (quads - 1)) * 4, rows = min(4, p.len.fresh * (int)a.group.d - p.row0 - row);
+  if (rows <= 0) return;
 #pragma unroll 1
-  for (int d = d0; d < d0 + per; d += 32) {
-    const int channels = min(32, d0 + per - d);          // a multiple of 8
-    float o[32];
+  for (int d = (thread >> (a.row_shift - 2)) * 8; d < a.c.head_dim; d += 256 / quads * 8) {
+    float4 o[8];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) o[i] = 0.f;
+    for (int i = 0; i < 8; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (int k = 0; k < n; ++k) {
-      const long long piece = cut.piece(c + k * step);
-      const float m = __ldcg(a.part_ml + piece * a.row_tile + row).x, f = m == all.x ? 1.f : exp2_fast(m - all.x);
-      const float *src = a.part_o + (piece * a.c.head_dim + d) * a.row_tile + row;
-      float x[32];
+    for (int k = 0; k < n; k += 2) {
+      float4 x[2][8];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = i < channels ? __ldcg(src + i * a.row_tile) : 0.f;
+      for (int e = 0; e < 2; ++e) {
+        const float *src = a.part_o + ((long long)cut.piece(c + min(k + e, n - 1) * step) * a.c.head_dim + d) * a.row_tile + row;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] += f * x[i];
-    }
+        for (int i = 0; i < 8; ++i) x[e][i] = __ldcg(reinterpret_cast<const float4 *>(src + i * a.row_tile));
+      }
 #pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-      if (i >= channels) break;
-      if (fold) {
+      for (int e = 0; e < 2; ++e) {
+        if (k + e == n) break;
+        const float4 f = *reinterpret_cast<const float4 *>(weights + (k + e) * 256 + row);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a.part_o[((long long)cut.piece(c) * a.c.head_dim + d + i + e) * a.row_tile + row] = o[i + e];
-      } else {
-        const float y[8] = {o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv, o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv};
-        if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + (d + i) * 2, y); else store8<KVR_F16>(dst + (d + i) * 2, y);
+        for (int i = 0; i < 8; ++i) {
+          o[i].x += f.x * x[e][i].x; o[i].y += f.y * x[e][i].y; o[i].z += f.z * x[e][i].z; o[i].w += f.w * x[e][i].w;
+        }
       }
     }
+    if (fold) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(a.part_o + ((long long)cut.piece(c) * a.c.head_dim + d + i) * a.row_tile + row) = o[i];
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= rows) break;
+      const int t = (int)a.group.div(p.row0 + row + e), q_head = p.head_group * (int)a.group.d + (p.row0 + row + e - t * (int)a.group.d);
+      char *dst = a.out.data + (long long)(p.len.first + t) * a.out.token_stride + (long long)q_head * a.out.head_stride + d * 2;
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = e == 0 ? o[i].x : e == 1 ? o[i].y : e == 2 ? o[i].z : o[i].w;
+      if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst, y); else store8<KVR_F16>(dst, y);
+    }
   }
-  if (!fold && a.lse && d0 == 0) a.lse[(long long)(p.len.first + t) * a.q_heads + q_head] = all.y == 0.f ? -INFINITY : all.x * 0.69314718f + logf(all.y);
 }
 
 template <int FMT, int DP, bool TWO>
@@ -266,7 +285,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ unsigned tm_slot;
   __shared__ int gave_up_word, last_in;
   __shared__ unsigned long long odd_keys[5][2];  // by ring slot: keys of a V tile with elements that are not finite
-  __shared__ float join_ml[128][2];
+  __shared__ float2 join_ml[2][128];
   __shared__ int box_ids[S::kLoaders][64];                 // by loader: block ids of the boxes around its step
   volatile int *gave_up = &gave_up_word;
   unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
@@ -575,41 +594,46 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       const int row = piece.row0 + (TWO ? w * 128 : 0) + tid;
       const bool have = row < len.fresh * (int)a.group.d && (TWO ? w * 128 : 0) + tid < a.row_tile && head < a.c.kv_heads;
       const int t_row = have ? (int)a.group.div(row) : 0, q_head = head * (int)a.group.d + (have ? row - t_row * (int)a.group.d : 0);
-      // the row of Q, to the operand layout
+      // Q to the operand layout.  The lanes of a warp stand side by side along a few of its 32 rows at a time.
       float scale = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);     // a scale of zero: Q is zero instead
       {
-        const char *src = a.q.data + (long long)(len.first + t_row) * a.q.token_stride + (long long)q_head * a.q.head_stride;
-        unsigned char *dst = q_tile + (TWO ? w : 0) * (128 * DP * 2) + tid * 128;
+        constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
+        const int c = lane % kLanes, row_base = (TWO ? w * 128 : 0) + (warp & 3) * 32;
         const unsigned flip = a.scale_log2 < 0 ? 0x80008000u : 0u;       // a negative one: Q's sign
-        uint4 x[DP / 8];
+        uint4 x[kLanes];
 #pragma unroll
-        for (int c = 0; c < DP / 8; ++c) {
-          x[c] = make_uint4(0, 0, 0, 0);
-          if (have && c * 8 < a.c.head_dim && a.scale_log2 != 0.f) x[c] = *reinterpret_cast<const uint4 *>(src + c * 16);
+        for (int i = 0; i < kLanes; ++i) {
+          const int local = row_base + i * kRows + lane / kLanes, at = piece.row0 + local, t_at = (int)a.group.div(at);
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (at < len.fresh * (int)a.group.d && local < a.row_tile && c * 8 < a.c.head_dim && a.scale_log2 != 0.f)
+            x[i] = *reinterpret_cast<const uint4 *>(a.q.data + (long long)(len.first + t_at) * a.q.token_stride +
+                                                    (long long)(head * (int)a.group.d + at - t_at * (int)a.group.d) * a.q.head_stride + c * 16);
         }
         if constexpr (kQuant) {
-          float top = 0.f, down = 1.f;
+          // f16 of rows that have been brought to [1, 2) by a power of two, which goes to the row's scale
           const bool bf16 = a.q.type == KVR_BF16;
 #pragma unroll
-          for (int c = 0; c < DP / 8; ++c) {
-            float y[8];
-            if (bf16) widen8<KVR_BF16>(x[c], y); else widen8<KVR_F16>(x[c], y);
+          for (int i = 0; i < kLanes; ++i) {
+            float y[8], most = 0.f, down = 1.f;
+            if (bf16) widen8<KVR_BF16>(x[i], y); else widen8<KVR_F16>(x[i], y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));
-          }
-          const unsigned e = __float_as_uint(top) >> 23;
-          if (e >= 1 && e <= 253) { down = __uint_as_float((254u - e) << 23); scale *= __uint_as_float(e << 23); }
+            for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(y[k]));
 #pragma unroll
-          for (int c = 0; c < DP / 8; ++c) {
-            float y[8];
-            if (bf16) widen8<KVR_BF16>(x[c], y); else widen8<KVR_F16>(x[c], y);
-            x[c] = make_uint4(pack_f16(y[0] * down, y[1] * down), pack_f16(y[2] * down, y[3] * down), pack_f16(y[4] * down, y[5] * down), pack_f16(y[6] * down, y[7] * down));
+            for (int d = kLanes / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const unsigned e = __float_as_uint(most) >> 23, up = e >= 1 && e <= 253 ? e << 23 : 127u << 23;
+            if (e >= 1 && e <= 253) down = __uint_as_float((254u - e) << 23);
+            const unsigned own = __shfl_sync(0xffffffffu, up, lane % kRows * kLanes);
+            if (lane / kRows == i) scale *= __uint_as_float(own);        // this thread's own row
+            x[i] = make_uint4(pack_f16(y[0] * down, y[1] * down), pack_f16(y[2] * down, y[3] * down), pack_f16(y[4] * down, y[5] * down), pack_f16(y[6] * down, y[7] * down));
           }
         }
         if (TWO || w == 0) {
+          unsigned char *dst = q_tile + (TWO ? w : 0) * (128 * DP * 2) + (c >> 3) * (128 * 128);
 #pragma unroll
-          for (int c = 0; c < DP / 8; ++c)
-            *reinterpret_cast<uint4 *>(dst + (c >> 3) * (128 * 128) + (((c & 7) ^ (tid & 7)) << 4)) = make_uint4(x[c].x ^ flip, x[c].y ^ flip, x[c].z ^ flip, x[c].w ^ flip);
+          for (int i = 0; i < kLanes; ++i) {
+            const int r = (warp & 3) * 32 + i * kRows + lane / kLanes;
+            *reinterpret_cast<uint4 *>(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(x[i].x ^ flip, x[i].y ^ flip, x[i].z ^ flip, x[i].w ^ flip);
+          }
         }
         fence_async();
         __syncwarp();
@@ -795,80 +819,80 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       tc_after();
       tiles_before += n;
       steps_before += 2 * n;
-      float unit = kQuant && v_exp != -1000 ? power2(v_exp) : 1.f, other = 0.f;
-      float *ex = reinterpret_cast<float *>(q_tile);     // [channel][row]: Q is used up when both warpgroups have joined
+      const float unit = kQuant && v_exp != -1000 ? power2(v_exp) : 1.f;
+      // The row's sums, to the output or to the workspace.  Not TWO: the warpgroups have sums of the same rows.  Each takes half of
+      // the channels, 32 at a time, and gives the other's half away.
+      constexpr int kOwn = TWO ? DP : DP / 2;
+      const int d_own = TWO ? 0 : w * kOwn, d_give = kOwn - d_own, local = (TWO ? w * 128 : 0) + tid;
+      float *ex = reinterpret_cast<float *>(q_tile);     // [warpgroup][channel][row]
+      float own = unit, other = 0.f;
+      const bool whole = piece.begin == 0 && piece.end == len.units;
+      const long long slot = (long long)blockIdx.x * 2 + (piece.unit == first ? 0 : 1);
+      char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
       if constexpr (!TWO) {
-        if (!(ok = join())) break;
-        if (w == 1 && mine > 0) {
+        join_ml[w][tid] = make_float2(top, sum);
+        if (!(ok = join())) break;       // Q is used up
+        const float2 theirs = join_ml[1 - w][tid];
+        const float m = fmaxf(top, theirs.x), f = top == m ? 1.f : exp2_fast(top - m);
+        other = theirs.x == -INFINITY ? 0.f : theirs.x == m ? 1.f : exp2_fast(theirs.x - m);
+        own = mine > 0 ? unit * f : 0.f;
+        sum = sum * f + theirs.y * other;
+        top = m;
+      }
+      const float inv = !whole ? 1.f : sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
 #pragma unroll 1
-          for (int c = 0; c < DP; c += 32) {
-            unsigned x[32];
-            tm_load32(x, tm_o[1] + lanes + c);
+      for (int c = 0; c < kOwn; c += 32) {
+        unsigned x[32];
+        if constexpr (!TWO) {
+          if (mine > 0) {
+            tm_load32(x, tm_o[w] + lanes + d_give + c);
             tm_loaded();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) ex[(c + i) * 128 + tid] = __uint_as_float(x[i]) * unit;
+            for (int i = 0; i < 32; ++i) ex[(w * 32 + i) * 128 + tid] = __uint_as_float(x[i]) * unit;
+          }
+          if (!(ok = join())) break;
+        }
+        tm_load32(x, tm_o[w] + lanes + d_own + c);
+        tm_loaded();
+        float o[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = !TWO && mine == 0 ? 0.f : __uint_as_float(x[i]) * own;
+        if constexpr (!TWO) {
+          if (other != 0.f) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] += ex[((1 - w) * 32 + i) * 128 + tid] * other;
           }
         }
-        if (w == 1) { join_ml[tid][0] = top; join_ml[tid][1] = sum; }
-        if (!(ok = join())) break;
-        if (w == 0 && n > 1) {
-          const float m2 = join_ml[tid][0], m = fmaxf(top, m2);
-          const float f = top == m ? 1.f : exp2_fast(top - m);
-          other = m2 == -INFINITY ? 0.f : m2 == m ? 1.f : exp2_fast(m2 - m);
-          sum = sum * f + join_ml[tid][1] * other;
-          top = m;
-          unit *= f;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          const int d = d_own + c + i;
+          if (!have || d >= a.c.head_dim) break;
+          if (whole) {
+            const float y[8] = {o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv, o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv};
+            if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + d * 2, y); else store8<KVR_F16>(dst + d * 2, y);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a.part_o[(slot * a.c.head_dim + d + e) * a.row_tile + local] = o[i + e];
+          }
+        }
+        __syncwarp();
+        if constexpr (!TWO) {
+          if (!(ok = join())) break;     // read: may be written again, with Q too
         }
       }
-      if (TWO || w == 0) {
-        const bool whole = piece.begin == 0 && piece.end == len.units;
-        const int local = (TWO ? w * 128 : 0) + tid;
-        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
-        const long long slot = (long long)blockIdx.x * 2 + (piece.unit == first ? 0 : 1);
-        char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
-        const bool joined = !TWO && n > 1;
-#pragma unroll 1
-        for (int c = 0; c < DP; c += 32) {
-          unsigned x[32];
-          tm_load32(x, tm_o[w] + lanes + c);
-          tm_loaded();
-          float o[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]) * unit;
-          if (joined && other != 0.f) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] += ex[(c + i) * 128 + tid] * other;
-          }
-#pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            if (!have || c + i >= a.c.head_dim) break;
-            if (whole) {
-              const float y[8] = {o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv, o[i + 4] * inv, o[i + 5] * inv, o[i + 6] * inv, o[i + 7] * inv};
-              if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + (c + i) * 2, y); else store8<KVR_F16>(dst + (c + i) * 2, y);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) a.part_o[(slot * a.c.head_dim + c + i + e) * a.row_tile + local] = o[i + e];
-            }
-          }
-          __syncwarp();
-        }
-        if (have) {
-          if (!whole) a.part_ml[slot * a.row_tile + local] = make_float2(top, sum);
-          else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum == 0.f ? -INFINITY : top * 0.69314718f + logf(sum);
-        }
+      if (!ok) break;
+      if (have && (TWO || w == 0)) {
+        if (!whole) a.part_ml[slot * a.row_tile + local] = make_float2(top, sum);
+        else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum == 0.f ? -INFINITY : top * 0.69314718f + logf(sum);
       }
-      if (piece.begin != 0 || piece.end != len.units)
+      if (!whole)
         ok = hand_in(a, piece, shares, join, &last_in, warp, lane, [&](const Cut &cut, int c, int step, int n, bool fold) {
           const Piece copy = piece;      // what the call is shown lies in memory
-          join_tiles(a, copy, cut, c, step, n, fold, threadIdx.x);
-          if (fold) {
-            // the folded statistics go last: two threads of a row may have read them
-            join();
-            fold_statistics(a, cut, c, step, n, threadIdx.x);
-          }
+          join_weights(a, copy, cut, c, step, n, fold, threadIdx.x, ex);
+          join();
+          join_rows(a, copy, cut, c, step, n, fold, threadIdx.x, ex);
+          join();                        // the weights have been read
         });
-      else if (!TWO)
-        ok = join();                     // the exchange has been read: Q's place may be written again
       again = next_piece(a, piece, last);
     }
   }
