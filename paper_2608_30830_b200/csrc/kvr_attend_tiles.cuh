@@ -382,14 +382,20 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       }
       const char *base = a.c.base + (v ? a.c.v_offset : 0) + at.p.head_group * a.c.head_dim * kElement;
 #pragma unroll 1
-      for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
-        const int key = i * kAtOnce + sub, j = key0 + key;
-        const long long off = j < at.p.len.keys ? token_offset(a.b, a.c, a.bs, at.p.r, j) : -1;
-        if (off < 0 && j < at.p.len.keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
-        const bool got = off >= 0 && chunk < used;
-        const char *src = got ? base + off + chunk * 16 : a.c.base;
-        if constexpr (kQuant) copy16(shared_at(dst + key * DP + chunk * 16), src, got);
-        else copy16(shared_at(dst + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4)), src, got);
+      for (int k0 = 0; k0 < S::kSpan; k0 += 32) {
+        // a lane finds a key; a wait for the table in every turn below came to 10 us a tile
+        const int j = key0 + k0 + lane;
+        const long long found = j < at.p.len.keys ? token_offset(a.b, a.c, a.bs, at.p.r, j) : -1;
+        if (found < 0 && j < at.p.len.keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
+#pragma unroll 4
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+          const int key = k0 + i * kAtOnce + sub;
+          const long long off = __shfl_sync(0xffffffffu, found, i * kAtOnce + sub);
+          const bool got = off >= 0 && chunk < used;
+          const char *src = got ? base + off + chunk * 16 : a.c.base;
+          if constexpr (kQuant) copy16(shared_at(dst + key * DP + chunk * 16), src, got);
+          else copy16(shared_at(dst + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4)), src, got);
+        }
       }
       return false;
     };
@@ -412,11 +418,12 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           copy_wait<0>();
           if (look) {
             // Elements of V that are not finite must not meet the zero probabilities of rows that do not see their key: they
-            // are set to zero here and added by the softmax threads, row by row.  A thread looks at what it copied.
+            // are set to zero here and added by the softmax threads, row by row.  A thread looks at what it copied (of new tokens:
+            // all rows see the context).
             unsigned long long odd[2] = {0, 0};
             constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
-#pragma unroll 1
-            for (int i = 0; i < kTileKeys / kAtOnce; ++i) {
+#pragma unroll 4
+            for (int i = max(at.p.len.context - tile * kTileKeys, 0) / kAtOnce; i < kTileKeys / kAtOnce; ++i) {
               const int key = i * kAtOnce + sub;
               uint4 *x_at = reinterpret_cast<uint4 *>(buf + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4));
               uint4 x = *x_at;
