@@ -55,6 +55,32 @@ __device__ __forceinline__ TokenAt locate_token(const Batch &b, const CacheView 
   return t;
 }
 
+// 8 channels as they lie in memory.
+template <int XT>
+struct Raw8 {
+  static constexpr int kWords = XT == KVR_F32 ? 8 : 4;
+  unsigned w[kWords];
+  __device__ __forceinline__ void load(const char *p) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(p + i * 4);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void widen(float (&x)[8]) const {
+    if constexpr (XT == KVR_F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    } else {
+      widen8<XT>(make_uint4(w[0], w[1], w[2], w[3]), x);
+    }
+  }
+};
+
 // The angles of 8 channels d0 .. d0 + 7 at one position, and the turn by them.  Products and sums are rounded one by
 // one, so the result does not depend on what a compiler contracts.
 //   rot % 16 == 0, halves: partners are whole lanes; 8 (cos, sin)
@@ -64,45 +90,49 @@ template <int XT>
 struct Angles {
   const RopeView &rp;
   const float *row;          // (cos, sin) of this position
-  float c[8], s[8];
-  bool low;
-  __device__ __forceinline__ Angles(const RopeView &rope, int position, int d0) : rp(rope), row(nullptr), low(false) {
+  Pair c[4], s[4];           // halves: the sine's sign is the channel's side
+  __device__ __forceinline__ Angles(const RopeView &rope, int position, int d0) : rp(rope), row(nullptr) {
     if (!rp.table) return;
     row = rp.table + (long long)position * rp.rot;
-    low = d0 < (rp.rot >> 1);
+    const bool low = d0 < (rp.rot >> 1);
     if ((rp.rot & 15) || d0 >= rp.rot) return;
     const bool halves = rp.style == KVR_ROPE_HALF;
     const float4 *t = reinterpret_cast<const float4 *>(row + (!halves ? d0 : 2 * (low ? d0 : d0 - (rp.rot >> 1))));
+    const float sign = halves && low ? -rp.sign : rp.sign;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i >= 2 && !halves) break;
       const float4 x = __ldg(t + i);
-      c[2 * i] = x.x; s[2 * i] = x.y * rp.sign;
-      c[2 * i + 1] = x.z; s[2 * i + 1] = x.w * rp.sign;
+      c[i] = pair(x.x, x.z);
+      s[i] = pair(x.y * sign, x.w * sign);
     }
   }
   // d0 >= rot: nothing of the lane's is turned (it still lends its channels to its partner)
   template <int LPH>
-  __device__ __forceinline__ void turn(float (&x)[8], const char *src, int d0) const {
+  __device__ __forceinline__ void turn(float (&x)[8], const Raw8<XT> &raw, const char *src, int d0) const {
     const int half = rp.rot >> 1;
     if ((rp.rot & 15) == 0) {
       if (rp.style == KVR_ROPE_HALF) {
         const int partner = (d0 < half ? d0 + half : d0 - half) >> 3;
-        float y[8];
+        Raw8<XT> theirs;               // as they were loaded: half the shuffles for 16-bit types
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], partner, LPH);
+        for (int i = 0; i < Raw8<XT>::kWords; ++i) theirs.w[i] = __shfl_sync(0xffffffffu, raw.w[i], partner, LPH);
+        float y[8];
+        theirs.widen(y);
         if (d0 >= rp.rot) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float xc = __fmul_rn(x[i], c[i]), ys = __fmul_rn(y[i], s[i]);
-          x[i] = low ? __fsub_rn(xc, ys) : __fadd_rn(ys, xc);
+        for (int i = 0; i < 4; ++i) {
+          const float2 r = unpair(add2(mul2(pair(x[2 * i], x[2 * i + 1]), c[i]), mul2(pair(y[2 * i], y[2 * i + 1]), s[i])));
+          x[2 * i] = r.x; x[2 * i + 1] = r.y;
         }
       } else if (d0 < rp.rot) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float u = x[2 * i], v = x[2 * i + 1];
-          x[2 * i] = __fsub_rn(__fmul_rn(u, c[i]), __fmul_rn(v, s[i]));
-          x[2 * i + 1] = __fadd_rn(__fmul_rn(u, s[i]), __fmul_rn(v, c[i]));
+          const float2 cs = unpair(c[i >> 1]), sn = unpair(s[i >> 1]);
+          const float ci = i & 1 ? cs.y : cs.x, si = i & 1 ? sn.y : sn.x;
+          x[2 * i] = __fsub_rn(__fmul_rn(u, ci), __fmul_rn(v, si));
+          x[2 * i + 1] = __fadd_rn(__fmul_rn(u, si), __fmul_rn(v, ci));
         }
       }
       return;
@@ -128,6 +158,21 @@ struct Angles {
   }
 };
 
+// x / scale, rounded once: the product with the correctly rounded reciprocal, corrected by its exact remainder (P. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000", 1990), two numbers to an instruction.  The remainder of
+// -0 is +0, hence the sign.
+__device__ __forceinline__ void quotients(float x, float y, float scale, float back, bool plain, float &a, float &b) {
+  if (!plain) {
+    a = __fdiv_rn(x, scale);
+    b = __fdiv_rn(y, scale);
+    return;
+  }
+  const Pair n = pair(x, y), r = pair(back, back), q = mul2(n, r);
+  const float2 v = unpair(fma2(fma2(q, pair(-scale, -scale), n), r, q));
+  a = copysignf(v.x, x);
+  b = copysignf(v.y, y);
+}
+
 // 8 channels of a head into the cache; LPH lanes hold the head.  A quantised head's largest magnitude is found as an
 // integer: for the bits of |x| integer order is numeric order, and infinities and NaN lie above all numbers.
 template <int FMT, int LPH>
@@ -147,9 +192,12 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
     if (!live) return;
     unsigned w[2] = {0, 0};
     if (finite) {
+      const float back = __frcp_rn(scale);
+      const bool plain = scale > 1e-30f;         // no step of the quotient underflows; (scale <= 2^121)
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const float a = __fdiv_rn(x[i], scale), b = __fdiv_rn(x[i + 1], scale);
+        float a, b;
+        quotients(x[i], x[i + 1], scale, back, plain, a, b);
         unsigned pair;
         if constexpr (FMT == KVR_CACHE_E4M3) {
           pair = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -169,10 +217,31 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
 // neighbouring lane, a scale is a few shuffles, and a lane's angles serve all of its heads.  `per_token` such groups
 // share a token's heads; kAhead heads are loaded before the first is worked on.
 template <int XT, int FMT, int LPH>
-__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kGroups = kThreads / LPH, kSize = XT == KVR_F32 ? 4 : 2, kAhead = XT == KVR_F32 ? 2 : 4;
   __shared__ TokenAt at[kGroups];
   const int per_token = a.per_token, tokens = kGroups / per_token, first = blockIdx.x * tokens;
+  const int group = threadIdx.x / LPH, d0 = (threadIdx.x % LPH) * 8;
+  const int sub = group % per_token, token = first + group / per_token;
+  // The heads of q, then of k, then of v, kAhead at a time; the next are asked for before these are worked on.  The number of
+  // turns is the same for all lanes: they shuffle.
+  const bool lane_in = token < a.b.n_tokens && d0 < a.c.head_dim;
+  auto rows_of = [&](int part) -> const Rows & { return part == 0 ? a.q : part == 1 ? a.k : a.v; };
+  auto heads_of = [&](int part) { return part == 0 ? a.q_heads : part == 1 ? a.k_heads : a.v_heads; };
+  Raw8<XT> next[kAhead];
+  auto ask = [&](int part, int h0) {
+    const Rows &src = rows_of(part);
+    const int heads = heads_of(part);
+    const char *in = src.data + (long long)token * src.token_stride + (long long)(h0 + sub) * src.head_stride + d0 * kSize;
+    const long long step = (long long)per_token * src.head_stride;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i, in += step) {
+      if (lane_in && h0 + i * per_token + sub < heads) next[i].load(in);
+      else next[i].clear();
+    }
+  };
+  int part = a.q_heads ? 0 : a.k_heads ? 1 : 2, h0 = 0;
+  ask(part, 0);
   if ((int)threadIdx.x < tokens) {
     TokenAt t{-1, -1};
     if (first + (int)threadIdx.x < a.b.n_tokens) {
@@ -188,48 +257,45 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     at[threadIdx.x] = t;
   }
   __syncthreads();
-  const int group = threadIdx.x / LPH, d0 = (threadIdx.x % LPH) * 8;
-  const int sub = group % per_token, token = first + group / per_token;
   const TokenAt t = at[group / per_token];
   const bool lane_live = t.position >= 0 && d0 < a.c.head_dim;
   const Angles<XT> angles(a.rope, lane_live ? t.position : 0, lane_live ? d0 : a.rope.rot);
 
-  // q, then k, turned; kAhead heads at a time.  The trip count is the same for all lanes: they shuffle.
-#pragma unroll 1
-  for (int part = 0; part < 3; ++part) {
-    const Rows &src = part == 0 ? a.q : part == 1 ? a.k : a.v;
-    const int heads = part == 0 ? a.q_heads : part == 1 ? a.k_heads : a.v_heads;
-    const bool live = lane_live && (part == 0 || t.offset >= 0);
-    const char *in = src.data + (long long)token * src.token_stride;
-    char *row = a.c.base + (part == 2 ? a.c.v_offset : 0) + t.offset;
-#pragma unroll 1
-    for (int h0 = 0; h0 < heads; h0 += per_token * kAhead) {
-      float x[kAhead][8];
+  while (part < 3) {
+    const int now = part, at0 = h0;
+    const Rows &src = rows_of(now);
+    const int heads = heads_of(now);
+    const bool live = lane_live && (now == 0 || t.offset >= 0);
+    Raw8<XT> raw[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) raw[i] = next[i];
+    h0 += per_token * kAhead;
+    while (part < 3 && h0 >= heads_of(part)) { ++part; h0 = 0; }
+    if (part < 3) ask(part, h0);
+    float x[kAhead][8];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) raw[i].widen(x[i]);
+    if (a.rope.table && now < 2) {
+      const char *in = src.data + (long long)token * src.token_stride;
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const int head = h0 + i * per_token + sub;
-        if (live && head < heads) load8<XT>(in + (long long)head * src.head_stride + d0 * kSize, x[i]);
-        else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-        }
+        const int head = at0 + i * per_token + sub;
+        angles.template turn<LPH>(x[i], raw[i], in + (long long)head * src.head_stride, live && head < heads ? d0 : a.rope.rot);
       }
-      if (a.rope.table && part < 2) {
+      __syncwarp();                    // q_out may be q: every partner has been read
+    }
+    if (now == 0) {
+      char *to = a.q_out.data + (long long)token * a.q_out.token_stride + (long long)(at0 + sub) * a.q_out.head_stride + d0 * kSize;
+      const long long step = (long long)per_token * a.q_out.head_stride;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int head = h0 + i * per_token + sub;
-          angles.template turn<LPH>(x[i], in + (long long)head * src.head_stride, live && head < heads ? d0 : a.rope.rot);
-        }
-        __syncwarp();                  // q_out may be q: every partner has been read
-      }
+      for (int i = 0; i < kAhead; ++i, to += step)
+        if (live && at0 + i * per_token + sub < heads) store8<XT>(to, x[i]);
+    } else {
+      char *row = a.c.base + (now == 2 ? a.c.v_offset : 0) + t.offset;
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const int head = h0 + i * per_token + sub;
-        if (part == 0) {
-          if (live && head < heads) store8<XT>(a.q_out.data + (long long)token * a.q_out.token_stride + (long long)head * a.q_out.head_stride + d0 * kSize, x[i]);
-        } else {
-          put8<FMT, LPH>(x[i], row, a.c.scale_offset, head, a.c.head_dim, d0, live && head < heads);
-        }
+        const int head = at0 + i * per_token + sub;
+        put8<FMT, LPH>(x[i], row, a.c.scale_offset, head, a.c.head_dim, d0, live && head < heads);
       }
     }
   }
