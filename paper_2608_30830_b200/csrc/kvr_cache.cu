@@ -107,36 +107,43 @@ struct Angles {
       s[i] = pair(x.y * sign, x.w * sign);
     }
   }
-  // d0 >= rot: nothing of the lane's is turned (it still lends its channels to its partner)
-  template <int LPH>
-  __device__ __forceinline__ void turn(float (&x)[8], const Raw8<XT> &raw, const char *src, int d0) const {
-    const int half = rp.rot >> 1;
-    if ((rp.rot & 15) == 0) {
-      if (rp.style == KVR_ROPE_HALF) {
-        const int partner = (d0 < half ? d0 + half : d0 - half) >> 3;
+  // rot % 16 == 0: N heads at once, turned or (turned: false) only lending their channels to their partners
+  template <int LPH, int N>
+  __device__ __forceinline__ void turn_lanes(float (&x)[N][8], const Raw8<XT> (&raw)[N], int d0, bool turned) const {
+    turned = turned && d0 < rp.rot;
+    if (rp.style == KVR_ROPE_HALF) {
+      const int half = rp.rot >> 1, partner = (d0 < half ? d0 + half : d0 - half) >> 3;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
         Raw8<XT> theirs;               // as they were loaded: half the shuffles for 16-bit types
 #pragma unroll
-        for (int i = 0; i < Raw8<XT>::kWords; ++i) theirs.w[i] = __shfl_sync(0xffffffffu, raw.w[i], partner, LPH);
+        for (int i = 0; i < Raw8<XT>::kWords; ++i) theirs.w[i] = __shfl_sync(0xffffffffu, raw[k].w[i], partner, LPH);
+        if (!turned) continue;
         float y[8];
         theirs.widen(y);
-        if (d0 >= rp.rot) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 r = unpair(add2(mul2(pair(x[2 * i], x[2 * i + 1]), c[i]), mul2(pair(y[2 * i], y[2 * i + 1]), s[i])));
-          x[2 * i] = r.x; x[2 * i + 1] = r.y;
-        }
-      } else if (d0 < rp.rot) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float u = x[2 * i], v = x[2 * i + 1];
-          const float2 cs = unpair(c[i >> 1]), sn = unpair(s[i >> 1]);
-          const float ci = i & 1 ? cs.y : cs.x, si = i & 1 ? sn.y : sn.x;
-          x[2 * i] = __fsub_rn(__fmul_rn(u, ci), __fmul_rn(v, si));
-          x[2 * i + 1] = __fadd_rn(__fmul_rn(u, si), __fmul_rn(v, ci));
+          const float2 r = unpair(add2(mul2(pair(x[k][2 * i], x[k][2 * i + 1]), c[i]), mul2(pair(y[2 * i], y[2 * i + 1]), s[i])));
+          x[k][2 * i] = r.x; x[k][2 * i + 1] = r.y;
         }
       }
-      return;
+    } else if (turned) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float u = x[k][2 * i], v = x[k][2 * i + 1];
+          const float2 cs = unpair(c[i >> 1]), sn = unpair(s[i >> 1]);
+          const float ci = i & 1 ? cs.y : cs.x, si = i & 1 ? sn.y : sn.x;
+          x[k][2 * i] = __fsub_rn(__fmul_rn(u, ci), __fmul_rn(v, si));
+          x[k][2 * i + 1] = __fadd_rn(__fmul_rn(u, si), __fmul_rn(v, ci));
+        }
+      }
     }
+  }
+  // other rot
+  __device__ __forceinline__ void turn(float (&x)[8], const char *src, int d0) const {
+    const int half = rp.rot >> 1;
     if (d0 >= rp.rot) return;
     float y[8];
 #pragma unroll
@@ -158,21 +165,6 @@ struct Angles {
   }
 };
 
-// x / scale, rounded once: the product with the correctly rounded reciprocal, corrected by its exact remainder (P. Markstein,
-// "Computation of elementary functions on the IBM RISC System/6000", 1990), two numbers to an instruction.  The remainder of
-// -0 is +0, hence the sign.
-__device__ __forceinline__ void quotients(float x, float y, float scale, float back, bool plain, float &a, float &b) {
-  if (!plain) {
-    a = __fdiv_rn(x, scale);
-    b = __fdiv_rn(y, scale);
-    return;
-  }
-  const Pair n = pair(x, y), r = pair(back, back), q = mul2(n, r);
-  const float2 v = unpair(fma2(fma2(q, pair(-scale, -scale), n), r, q));
-  a = copysignf(v.x, x);
-  b = copysignf(v.y, y);
-}
-
 // 8 channels of a head into the cache; LPH lanes hold the head.  A quantised head's largest magnitude is found as an
 // integer: for the bits of |x| integer order is numeric order, and infinities and NaN lie above all numbers.
 template <int FMT, int LPH>
@@ -192,12 +184,26 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
     if (!live) return;
     unsigned w[2] = {0, 0};
     if (finite) {
-      const float back = __frcp_rn(scale);
-      const bool plain = scale > 1e-30f;         // no step of the quotient underflows; (scale <= 2^121)
+      float y[8];
+      if (scale > 1e-30f) {
+        // x / scale, rounded once: the product with the correctly rounded reciprocal, corrected by its exact remainder (P. Markstein,
+        // "Computation of elementary functions on the IBM RISC System/6000", 1990), two numbers to an instruction; no step of it
+        // underflows.  The remainder of -0 is +0, hence the sign.
+        const float back = __frcp_rn(scale);
+        const Pair r = pair(back, back), minus = pair(-scale, -scale);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const Pair n = pair(x[i], x[i + 1]), q = mul2(n, r);
+          const float2 v = unpair(fma2(fma2(q, minus, n), r, q));
+          y[i] = copysignf(v.x, x[i]); y[i + 1] = copysignf(v.y, x[i + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __fdiv_rn(x[i], scale);
+      }
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        float a, b;
-        quotients(x[i], x[i + 1], scale, back, plain, a, b);
+        const float a = y[i], b = y[i + 1];
         unsigned pair;
         if constexpr (FMT == KVR_CACHE_E4M3) {
           pair = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -276,11 +282,15 @@ __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_consta
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) raw[i].widen(x[i]);
     if (a.rope.table && now < 2) {
-      const char *in = src.data + (long long)token * src.token_stride;
+      if ((a.rope.rot & 15) == 0) {
+        angles.template turn_lanes<LPH, kAhead>(x, raw, d0, lane_live);
+      } else {
+        const char *in = src.data + (long long)token * src.token_stride;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int head = at0 + i * per_token + sub;
-        angles.template turn<LPH>(x[i], raw[i], in + (long long)head * src.head_stride, live && head < heads ? d0 : a.rope.rot);
+        for (int i = 0; i < kAhead; ++i) {
+          const int head = at0 + i * per_token + sub;
+          if (live && head < heads) angles.turn(x[i], in + (long long)head * src.head_stride, d0);
+        }
       }
       __syncwarp();                    // q_out may be q: every partner has been read
     }
