@@ -104,7 +104,8 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   } else {
     tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
     a.row_tile = tiles * 8;
-    a.unit = FastDiv(slices < 4 ? (64 + 16 * slices - 1) / (16 * slices) * 16 * slices : 16 * slices);       // 64 or more: fewer pieces
+    const int turn = 16 * slices * chunks_at_once(spec->format, tiles);      // keys that the warps of a head take at a time
+    a.unit = FastDiv((64 + turn - 1) / turn * turn);             // 64 or more: fewer pieces
   }
   while ((1 << a.row_shift) < a.row_tile) ++a.row_shift;
   // units are numbered in 32 bits; a bound that the lengths on the device keep, whatever they are

@@ -33,10 +33,10 @@ __device__ __forceinline__ unsigned transpose8(unsigned v) {
 template <bool BF16>
 __device__ __forceinline__ void product(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
   if constexpr (BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <int FMT, int DP>
@@ -62,6 +62,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
   using S = Shape<FMT, DP>;
   constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
   constexpr int kStages = S::kStages, kRow = S::kRow, kChunks = kRow / 16, kTiles = DP / 16;
+  // Chunks of 16 keys that a turn takes: two where registers allow it, so that one's chain of dependent steps runs beside the other's
+  // and the maximum is looked for once.
+  constexpr int kAtOnce = chunks_at_once(FMT, NT);
+  static_assert(kStages >= 2 * kAtOnce, "");
   constexpr float kLazy = 4.f;         // a row's maximum moves only when a score passes it by 2^4: fewer rescales,
                                        // probabilities up to 16 (room in f16, see the scale of V below)
   extern __shared__ __align__(128) unsigned char smem[];
@@ -84,7 +88,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
   // chunks of a piece that hold keys: c = begin * unit_chunks ..., of which this warp's keys start at (c * slices + slice) * 16
   auto chunk_end = [&](const Piece &p) {
     const int have = (p.len.keys - slice * 16 + 16 * slices - 1) / (16 * slices);
-    return min(p.end * unit_chunks, max(have, 0));
+    return min(p.end * unit_chunks, (max(have, 0) + kAtOnce - 1) / kAtOnce * kAtOnce);
   };
 
   // ---- loads: a second walk that runs ahead
@@ -145,8 +149,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
     copy_commit();
   };
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) load_chunk(s);
-  int stage = 0, load_stage = kStages - 1;
+  for (int s = 0; s < kStages - kAtOnce; ++s) load_chunk(s);
+  int stage = 0, load_stage = kStages - kAtOnce;
 
   // ---- pieces
   bool again = true;
@@ -214,66 +218,82 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
     int v_exp = -1000;                 // V's scales are multiplied by 2^-v_exp (set by the first chunk)
 
     const int c_end = chunk_end(piece);
-    for (int c = piece.begin * unit_chunks; c < c_end; ++c) {
-      copy_wait<kStages - 2>();
+    for (int c = piece.begin * unit_chunks; c < c_end; c += kAtOnce) {
+      copy_wait<kStages - 2 * kAtOnce>();
       __syncwarp();
-      load_chunk(load_stage);
-      load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
-      unsigned char *st = ring + stage * S::kStageBytes;
-      const unsigned k_at = shared_at(st), v_at = k_at + 16 * kRow;
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-      const int key0 = (c * slices + slice) * 16;
+      unsigned char *st_of[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        load_chunk(load_stage);
+        load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+        st_of[u] = ring + stage * S::kStageBytes;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+      }
       // the lane's keys (rows gid and gid + 8 of S^T)
       const int key_a = kQuant ? (gid >> 1) * 4 + (gid & 1) : gid, key_b = kQuant ? key_a + 2 : gid + 8;
 
-      // S^T = K Q^T
-      float s[NT][4] = {};
+      // S^T = K Q^T; the chunks' products in turn, for a product waits for the one before it
+      float s[kAtOnce][NT][4] = {}, v_scale[kAtOnce][2];
       if constexpr (!kQuant) {
 #pragma unroll
-        for (int k = 0; k < kTiles; ++k) {
-          unsigned f[4];
-          load_matrix4<false>(f, k_at + spread<false, DP>((lane & 7) + ((lane >> 3) & 1) * 8, k * 2 + (lane >> 4)));
+        for (int k = 0; k < kTiles; ++k)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) product<kBf16>(s[n], f, q[n][k][0], q[n][k][1]);
-        }
+          for (int u = 0; u < kAtOnce; ++u) {
+            unsigned f[4];
+            load_matrix4<false>(f, shared_at(st_of[u]) + spread<false, DP>((lane & 7) + ((lane >> 3) & 1) * 8, k * 2 + (lane >> 4)));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) product<kBf16>(s[u][n], f, q[n][k][0], q[n][k][1]);
+          }
       } else {
 #pragma unroll
         for (int w = 0; w < DP / 64; ++w) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(st + spread<true, DP>(key_a, w * 4 + tig));
-          const uint4 y = *reinterpret_cast<const uint4 *>(st + spread<true, DP>(key_b, w * 4 + tig));
-          const unsigned xa[4] = {x.x, x.y, x.z, x.w}, yb[4] = {y.x, y.y, y.z, y.w};
+          uint4 x[kAtOnce], y[kAtOnce];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const unsigned f[4] = {widen<FMT, false>(xa[k]), widen<FMT, false>(yb[k]), widen<FMT, true>(xa[k]), widen<FMT, true>(yb[k])};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) product<false>(s[n], f, q[n][w * 4 + k][0], q[n][w * 4 + k][1]);
+          for (int u = 0; u < kAtOnce; ++u) {
+            x[u] = *reinterpret_cast<const uint4 *>(st_of[u] + spread<true, DP>(key_a, w * 4 + tig));
+            y[u] = *reinterpret_cast<const uint4 *>(st_of[u] + spread<true, DP>(key_b, w * 4 + tig));
           }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+              const unsigned xa = k == 0 ? x[u].x : k == 1 ? x[u].y : k == 2 ? x[u].z : x[u].w, yb = k == 0 ? y[u].x : k == 1 ? y[u].y : k == 2 ? y[u].z : y[u].w;
+              const unsigned f[4] = {widen<FMT, false>(xa), widen<FMT, false>(yb), widen<FMT, true>(xa), widen<FMT, true>(yb)};
+#pragma unroll
+              for (int n = 0; n < NT; ++n) product<false>(s[u][n], f, q[n][w * 4 + k][0], q[n][w * 4 + k][1]);
+            }
         }
       }
-      float k_scale[2] = {1.f, 1.f}, v_scale[2] = {1.f, 1.f};
-      if constexpr (kQuant) {
-        const float *sc = reinterpret_cast<const float *>(st + 32 * kRow);
-        k_scale[0] = sc[key_a]; k_scale[1] = sc[key_b];
-        v_scale[0] = sc[16 + key_a]; v_scale[1] = sc[16 + key_b];
-      }
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int u = 0; u < kAtOnce; ++u) {
+        unsigned char *st = st_of[u];
+        const int key0 = ((c + u) * slices + slice) * 16;
+        float k_scale[2] = {1.f, 1.f};
+        v_scale[u][0] = v_scale[u][1] = 1.f;
+        if constexpr (kQuant) {
+          const float *sc = reinterpret_cast<const float *>(st + 32 * kRow);
+          k_scale[0] = sc[key_a]; k_scale[1] = sc[key_b];
+          v_scale[u][0] = sc[16 + key_a]; v_scale[u][1] = sc[16 + key_b];
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] *= kQuant ? q_scale[n][i & 1] * k_scale[i >> 1] : q_scale[n][i & 1];
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[u][n][i] *= kQuant ? q_scale[n][i & 1] * k_scale[i >> 1] : q_scale[n][i & 1];
 
-      // what a row does not see
-      if (key0 + 16 > len.context) {
+        // what a row does not see
+        if (key0 + 16 > len.context) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int j = key0 + (i ? key_b : key_a) - len.context;        // among the new tokens
+          for (int i = 0; i < 2; ++i) {
+            const int j = key0 + (i ? key_b : key_a) - len.context;      // among the new tokens
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int row = n * 8 + tig * 2 + e;
-              const bool seen = j < 0 || (j < len.fresh && row < rows && sees(a, len.first, (int)a.group.div(piece.row0 + row), j));
-              if (!seen) s[n][i * 2 + e] = -INFINITY;
-            }
+              for (int e = 0; e < 2; ++e) {
+                const int row = n * 8 + tig * 2 + e;
+                const bool seen = j < 0 || (j < len.fresh && row < rows && sees(a, len.first, (int)a.group.div(piece.row0 + row), j));
+                if (!seen) s[u][n][i * 2 + e] = -INFINITY;
+              }
+          }
         }
       }
 
@@ -284,7 +304,8 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float m = fmaxf(s[n][e], s[n][2 + e]);
+          float m = fmaxf(s[0][n][e], s[0][n][2 + e]);
+          if constexpr (kAtOnce == 2) m = fmaxf(m, fmaxf(s[kAtOnce - 1][n][e], s[kAtOnce - 1][n][2 + e]));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -293,9 +314,10 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         }
       int shift = 0;                   // of V's scale, in powers of two
       if constexpr (kQuant) {
-        // p times V's scale has to fit f16: the largest scale of a chunk is brought to 2^7 when it first appears and
+        // p times V's scale has to fit f16: the largest scale is brought to 2^7 when it first appears and
         // again when one passes 2^11, so products stay below 2^15, and one key of 2^-21 times the largest is still normal
-        float big = fmaxf(v_scale[0], v_scale[1]);
+        float big = fmaxf(v_scale[0][0], v_scale[0][1]);
+        if constexpr (kAtOnce == 2) big = fmaxf(big, fmaxf(v_scale[kAtOnce - 1][0], v_scale[kAtOnce - 1][1]));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 4));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 8));
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 16));
@@ -324,106 +346,112 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
           }
       }
       // P^T, as the right operand of the second product
-      unsigned p[NT][2];
       const float v_unit = kQuant && v_exp != -1000 ? power2(-v_exp) : 1.f;
-      // channels of 16-bit V that are not finite must not reach rows that do not see them (0 * infinity): see below
-      float pf[NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float m = top[n][i & 1];
-          const float x = s[n][i] == -INFINITY ? 0.f : exp2_fast(s[n][i] - m);
-          sum[n][i & 1] += x;
-          pf[n][i] = x;
-        }
-      if constexpr (kQuant) {
+      for (int u = 0; u < kAtOnce; ++u) {
+        unsigned char *st = st_of[u];
+        const unsigned v_at = shared_at(st) + 16 * kRow;
+        const int key0 = ((c + u) * slices + slice) * 16;
+        unsigned p[NT][2];
+        // channels of 16-bit V that are not finite must not reach rows that do not see them (0 * infinity): see below
+        float pf[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pf[n][i] = s[n][i] == -INFINITY ? 0.f : pf[n][i] * (v_scale[i >> 1] * v_unit);
-      } else if (key0 + 16 > len.context && (len.fresh > 1 || a.mask)) {
-        // lanes 2k and 2k + 1 look through key k's row of V
-        bool odd = false;
+          for (int i = 0; i < 4; ++i) {
+            const float m = top[n][i & 1];
+            const float x = s[u][n][i] == -INFINITY ? 0.f : exp2_fast(s[u][n][i] - m);
+            sum[n][i & 1] += x;
+            pf[n][i] = x;
+          }
+        if constexpr (kQuant) {
 #pragma unroll
-        for (int i = 0; i < kChunks / 2; ++i) {
-          const uint4 x = *reinterpret_cast<const uint4 *>(st + 16 * kRow + spread<false, DP>(lane >> 1, (lane & 1) * (kChunks / 2) + i));
-          const unsigned w[4] = {x.x, x.y, x.z, x.w};
-          constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) odd = odd || (w[j] & kExp) == kExp || (w[j] >> 16 & kExp) == kExp;
-        }
-        unsigned keys = __ballot_sync(0xffffffffu, odd);
-        keys |= keys >> 1;
-        keys &= 0x55555555u;           // bit 2k: key k
-        while (keys) {
-          const int key = (__ffs(keys) - 1) >> 1;
-          keys &= keys - 1;
-          // added row by row, only where the row sees the key; then the key leaves the product
+            for (int i = 0; i < 4; ++i) pf[n][i] = s[u][n][i] == -INFINITY ? 0.f : pf[n][i] * (v_scale[u][i >> 1] * v_unit);
+        } else if (key0 + 16 > len.context && (len.fresh > 1 || a.mask)) {
+          // lanes 2k and 2k + 1 look through key k's row of V
+          bool odd = false;
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float w[2];
+          for (int i = 0; i < kChunks / 2; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(st + 16 * kRow + spread<false, DP>(lane >> 1, (lane & 1) * (kChunks / 2) + i));
+            const unsigned w[4] = {x.x, x.y, x.z, x.w};
+            constexpr unsigned kExp = kBf16 ? 0x7f80u : 0x7c00u;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              w[e] = __shfl_sync(0xffffffffu, key < 8 ? pf[n][e] : pf[n][2 + e], (key & 7) * 4 + tig);
-              if (gid == (key & 7)) { if (key < 8) pf[n][e] = 0.f; else pf[n][2 + e] = 0.f; }
-            }
+            for (int j = 0; j < 4; ++j) odd = odd || (w[j] & kExp) == kExp || (w[j] >> 16 & kExp) == kExp;
+          }
+          unsigned keys = __ballot_sync(0xffffffffu, odd);
+          keys |= keys >> 1;
+          keys &= 0x55555555u;           // bit 2k: key k
+          while (keys) {
+            const int key = (__ffs(keys) - 1) >> 1;
+            keys &= keys - 1;
+            // added row by row, only where the row sees the key; then the key leaves the product
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
+            for (int n = 0; n < NT; ++n) {
+              float w[2];
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int d = t * 16 + h * 8 + gid;
-                const unsigned char *at = st + 16 * kRow + spread<false, DP>(key, d >> 3) + (d & 7) * 2;
-                const float v = load1<kBf16 ? KVR_BF16 : KVR_F16>(reinterpret_cast<const char *>(at));
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                  if (w[e] > 0.f) o[t][n][h * 2 + e] += w[e] * v;
+              for (int e = 0; e < 2; ++e) {
+                w[e] = __shfl_sync(0xffffffffu, key < 8 ? pf[n][e] : pf[n][2 + e], (key & 7) * 4 + tig);
+                if (gid == (key & 7)) { if (key < 8) pf[n][e] = 0.f; else pf[n][2 + e] = 0.f; }
               }
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const int d = t * 16 + h * 8 + gid;
+                  const unsigned char *at = st + 16 * kRow + spread<false, DP>(key, d >> 3) + (d & 7) * 2;
+                  const float v = load1<kBf16 ? KVR_BF16 : KVR_F16>(reinterpret_cast<const char *>(at));
+#pragma unroll
+                  for (int e = 0; e < 2; ++e)
+                    if (w[e] > 0.f) o[t][n][h * 2 + e] += w[e] * v;
+                }
+            }
+            __syncwarp();
+            for (int i = lane; i < kChunks; i += 32) *reinterpret_cast<uint4 *>(st + 16 * kRow + spread<false, DP>(key, i)) = make_uint4(0, 0, 0, 0);
           }
           __syncwarp();
-          for (int i = lane; i < kChunks; i += 32) *reinterpret_cast<uint4 *>(st + 16 * kRow + spread<false, DP>(key, i)) = make_uint4(0, 0, 0, 0);
         }
-        __syncwarp();
-      }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        p[n][0] = transpose8(kBf16 ? pack_bf16(pf[n][0], pf[n][1]) : pack_f16(pf[n][0], pf[n][1]));
-        p[n][1] = transpose8(kBf16 ? pack_bf16(pf[n][2], pf[n][3]) : pack_f16(pf[n][2], pf[n][3]));
-      }
-      // O^T += V^T P^T
-      if constexpr (!kQuant) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          unsigned f[4];
-          load_matrix4<true>(f, v_at + spread<false, DP>((lane & 7) + (lane >> 4) * 8, t * 2 + ((lane >> 3) & 1)));
-#pragma unroll
-          for (int n = 0; n < NT; ++n) product<kBf16>(o[t][n], f, p[n][0], p[n][1]);
+        for (int n = 0; n < NT; ++n) {
+          p[n][0] = transpose8(kBf16 ? pack_bf16(pf[n][0], pf[n][1]) : pack_f16(pf[n][0], pf[n][1]));
+          p[n][1] = transpose8(kBf16 ? pack_bf16(pf[n][2], pf[n][3]) : pack_f16(pf[n][2], pf[n][3]));
         }
-      } else {
-        // the lane's keys are 4 * tig + 0..3, its channels gid * DP / 8 + 0 .. DP / 8 - 1
-        const unsigned char *v_tile = st + 16 * kRow;
-        constexpr int kWords = DP / 32;                                  // 4 channels each
-        unsigned w[4][kWords];
+        // O^T += V^T P^T
+        if constexpr (!kQuant) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (DP == 64) {
-            const uint2 x = *reinterpret_cast<const uint2 *>(v_tile + spread<true, DP>(tig * 4 + j, gid >> 1) + (gid & 1) * 8);
-            w[j][0] = x.x; w[j][1] = x.y;
-          } else {
+          for (int t = 0; t < kTiles; ++t) {
+            unsigned f[4];
+            load_matrix4<true>(f, v_at + spread<false, DP>((lane & 7) + (lane >> 4) * 8, t * 2 + ((lane >> 3) & 1)));
 #pragma unroll
-            for (int h = 0; h < DP / 128; ++h) {
-              const uint4 x = *reinterpret_cast<const uint4 *>(v_tile + spread<true, DP>(tig * 4 + j, gid * (DP / 128) + h));
-              w[j][h * 4] = x.x; w[j][h * 4 + 1] = x.y; w[j][h * 4 + 2] = x.z; w[j][h * 4 + 3] = x.w;
+            for (int n = 0; n < NT; ++n) product<kBf16>(o[t][n], f, p[n][0], p[n][1]);
+          }
+        } else {
+          // the lane's keys are 4 * tig + 0..3, its channels gid * DP / 8 + 0 .. DP / 8 - 1
+          const unsigned char *v_tile = st + 16 * kRow;
+          constexpr int kWords = DP / 32;                                  // 4 channels each
+          unsigned w[4][kWords];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (DP == 64) {
+              const uint2 x = *reinterpret_cast<const uint2 *>(v_tile + spread<true, DP>(tig * 4 + j, gid >> 1) + (gid & 1) * 8);
+              w[j][0] = x.x; w[j][1] = x.y;
+            } else {
+#pragma unroll
+              for (int h = 0; h < DP / 128; ++h) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(v_tile + spread<true, DP>(tig * 4 + j, gid * (DP / 128) + h));
+                w[j][h * 4] = x.x; w[j][h * 4 + 1] = x.y; w[j][h * 4 + 2] = x.z; w[j][h * 4 + 3] = x.w;
+              }
             }
           }
-        }
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          const int x = t >> 1;
-          const unsigned k01 = __byte_perm(w[0][x], w[1][x], t & 1 ? 0x7362 : 0x5140), k23 = __byte_perm(w[2][x], w[3][x], t & 1 ? 0x7362 : 0x5140);
-          const unsigned f[4] = {widen<FMT, false>(k01), widen<FMT, true>(k01), widen<FMT, false>(k23), widen<FMT, true>(k23)};
+          for (int t = 0; t < kTiles; ++t) {
+            const int x = t >> 1;
+            const unsigned k01 = __byte_perm(w[0][x], w[1][x], t & 1 ? 0x7362 : 0x5140), k23 = __byte_perm(w[2][x], w[3][x], t & 1 ? 0x7362 : 0x5140);
+            const unsigned f[4] = {widen<FMT, false>(k01), widen<FMT, true>(k01), widen<FMT, false>(k23), widen<FMT, true>(k23)};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) product<false>(o[t][n], f, p[n][0], p[n][1]);
+            for (int n = 0; n < NT; ++n) product<false>(o[t][n], f, p[n][0], p[n][1]);
+          }
         }
       }
     }
