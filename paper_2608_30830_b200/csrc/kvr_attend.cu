@@ -99,6 +99,10 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
     a.unit = FastDiv(128);
+    // A segment begun inside a CTA's share costs it a second Q, the wait for the first products and another epilogue: 6 units' worth.
+    // (Trees of 64 tokens over 8 x 16k tokens, us: 186 without, 179 at 3, 174 at 6, 175 at 9, 180 at 12, 186 at 16; trees of 13
+    // over an int8 cache: 134, 130, 126, 127, 131, 135.)  The row kernel's pieces begin while the last one's keys still stream.
+    a.opening = 6;
     a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
     if (a.box_rows && !layer_map(spec, a.c, padded, a.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
   } else {
@@ -109,7 +113,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   }
   while ((1 << a.row_shift) < a.row_tile) ++a.row_shift;
   // units are numbered in 32 bits; a bound that the lengths on the device keep, whatever they are
-  const double most = (double)batch->n_req * (((int64_t)batch->max_new * group + a.row_tile - 1) / a.row_tile) * a.head_groups * (batch->max_tokens / a.unit.d + 1.);
+  const double most = (double)batch->n_req * (((int64_t)batch->max_new * group + a.row_tile - 1) / a.row_tile) * a.head_groups * (batch->max_tokens / a.unit.d + 1. + a.opening);
   if (most >= INT32_MAX) return fail_cache(KVR_ERR_INVALID_ARG, "n_req, max_new and max_tokens are too large for one call");
   a.ctas = sms;
   a.handed_in = static_cast<int *>(workspace);

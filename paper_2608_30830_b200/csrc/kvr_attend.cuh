@@ -27,6 +27,7 @@ struct AttendArgs {
   int q_heads;
   int head_groups, group_heads;      // KV heads are taken group_heads at a time
   int row_tile, row_shift;   // query rows of a segment, 2^row_shift
+  int opening;               // what a segment's start weighs, in units: a CTA that begins one gets fewer keys
   int box_rows;              // tokens of a TMA box (tile kernel): 8 or 16, 0: the block size does not allow one
   int ctas;                  // the grid of the main kernel
   int *handed_in;            // [2][ctas][2]: pieces of a group, groups of a segment; zero between calls
@@ -83,7 +84,7 @@ __device__ __forceinline__ bool find_share(const AttendArgs &a, unsigned *scratc
     units = 0;
     if (r < a.b.n_req) {
       mine = attend_lengths(a, r);
-      units = (unsigned)mine.units * mine.segments;
+      units = mine.units ? (unsigned)(mine.units + a.opening) * mine.segments : 0;
       int first, context, fresh;
       if (blockIdx.x == 0 && !request_lengths(a.b, a.bs.d, r, first, context, fresh)) report(a.b.status, KVR_DEV_BAD_LENGTH);
     }

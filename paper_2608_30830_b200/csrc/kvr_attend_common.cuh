@@ -47,22 +47,25 @@ __device__ __forceinline__ unsigned widen(unsigned w) {
 
 // A CTA's walk over the pieces of segments in its run of units.
 struct Piece {
-  unsigned unit;             // first unit of the piece
+  unsigned unit, next;       // the CTA's share of the segment, its opening included: units unit .. next - 1
   unsigned base;             // first unit of its request
   int r, head_group, row0;   // request, group of KV heads, first query row
   int begin, end;            // units of the segment
   Lengths len;
 };
-__device__ __forceinline__ void open_piece(const AttendArgs &a, Piece &p, unsigned last) {
+// The piece that starts at p.unit; false where the share ends within the segment's opening.
+__device__ __forceinline__ bool open_piece(const AttendArgs &a, Piece &p, unsigned last) {
   // requests without units are passed over (the bound on r cannot be met while p.unit is below the call's units)
-  while (p.unit - p.base >= (unsigned)p.len.units * p.len.segments) {
+  while (p.len.units == 0 || p.unit - p.base >= (unsigned)(p.len.units + a.opening) * p.len.segments) {
     p.base = p.unit;
-    if (++p.r >= a.b.n_req) { p.r = a.b.n_req - 1; p.len = Lengths{0, 0, 0, 0, 1, 1}; break; }
+    if (++p.r >= a.b.n_req) { p.r = a.b.n_req - 1; return false; }
     p.len = attend_lengths(a, p.r);
   }
-  const int offset = (int)((p.unit - p.base) / p.len.units);
-  p.begin = (int)((p.unit - p.base) - offset * p.len.units);
-  p.end = (int)min((unsigned)p.len.units, p.begin + (last - p.unit));
+  const int span = p.len.units + a.opening, offset = (int)((p.unit - p.base) / span), from = (int)((p.unit - p.base) - offset * span);
+  const int to = (int)min((unsigned)span, from + (last - p.unit));
+  p.next = p.unit + (to - from);
+  p.begin = max(from - a.opening, 0);
+  p.end = to - a.opening;
   p.head_group = 0;
   p.row0 = offset << a.row_shift;
   if (a.head_groups > 1) {
@@ -70,12 +73,11 @@ __device__ __forceinline__ void open_piece(const AttendArgs &a, Piece &p, unsign
     p.head_group = offset / tiles;
     p.row0 = (offset - p.head_group * tiles) << a.row_shift;
   }
+  return p.end > 0;
 }
 __device__ __forceinline__ bool next_piece(const AttendArgs &a, Piece &p, unsigned last) {
-  p.unit += p.end - p.begin;
-  if (p.unit >= last) return false;
-  open_piece(a, p, last);
-  return true;
+  p.unit = p.next;
+  return p.unit < last && open_piece(a, p, last);
 }
 
 struct Cut {
@@ -185,11 +187,11 @@ __device__ __noinline__ void join_pieces(const AttendArgs &a, const Piece &p, co
 // the n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.
 template <class Sync, class Join>
 __device__ __forceinline__ bool hand_in(const AttendArgs &a, const Piece &p, const Shares &sh, Sync sync, volatile int *last, int warp, int lane, Join join) {
-  const unsigned begin = p.unit - p.begin;
+  const unsigned span = p.len.units + a.opening, begin = p.unit - (p.unit - p.base) % span;
   Cut cut;
-  cut.c0 = sh.cta_of(begin);
-  cut.c1 = sh.cta_of(begin + p.len.units - 1);
-  cut.which0 = sh.first(cut.c0) == begin ? 0 : 1;
+  cut.c0 = sh.cta_of(begin + a.opening);       // the first with keys
+  cut.c1 = sh.cta_of(begin + span - 1);
+  cut.which0 = sh.first(cut.c0) >= begin ? 0 : 1;
   const int all = cut.c1 - cut.c0 + 1, groups = (all + kJoinAtOnce - 1) / kJoinAtOnce;
   const int group = ((int)blockIdx.x - cut.c0) / kJoinAtOnce, leader = cut.c0 + group * kJoinAtOnce, n = min(kJoinAtOnce, cut.c1 - leader + 1);
   auto come_in = [&](int *counter, int of) {

@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
   if (!find_share(a, scratch, shares, piece.r, piece.base, piece.len)) return;
   const unsigned first = shares.first(blockIdx.x), last = shares.first(blockIdx.x + 1);
   piece.unit = first;
-  open_piece(a, piece, last);
+  if (!open_piece(a, piece, last)) return;     // an opening alone
 
   const int unit_chunks = (int)a.unit.d / (16 * slices);     // of one warp
   unsigned char *ring = smem + warp * (kStages * S::kStageBytes);

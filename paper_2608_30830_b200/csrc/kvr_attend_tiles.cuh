@@ -290,7 +290,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   if (!find_share(a, scratch, shares, piece.r, piece.base, piece.len)) return;
   const unsigned first = shares.first(blockIdx.x), last = shares.first(blockIdx.x + 1);
   piece.unit = first;
-  open_piece(a, piece, last);
+  if (!open_piece(a, piece, last)) return;     // an opening alone
   const int unit_tiles = (int)a.unit.d / kTileKeys;
   auto first_tile = [&](const Piece &p) { return p.begin * unit_tiles; };
   auto last_tile = [&](const Piece &p) { return min(p.end * unit_tiles, (p.len.keys + kTileKeys - 1) / kTileKeys); };
