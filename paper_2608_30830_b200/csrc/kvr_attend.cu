@@ -100,7 +100,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     a.row_tile = rows <= 128 ? 128 : 256;
     a.unit = FastDiv(128);
     // A segment begun inside a CTA's share costs it a second Q, the wait for the first products and another epilogue: 6 units' worth.
-    // (Trees of 64 tokens over 8 x 16k tokens, us: 186 without, 179 at 3, 174 at 6, 175 at 9, 180 at 12, 186 at 16; trees of 13
+    // (Trees of 64 tokens, 16 requests of 8k, us: 186 without, 179 at 3, 174 at 6, 175 at 9, 180 at 12, 186 at 16; trees of 13
     // over an int8 cache: 134, 130, 126, 127, 131, 135.)  The row kernel's pieces begin while the last one's keys still stream.
     a.opening = 6;
     a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
