@@ -87,14 +87,13 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   a.q_heads = q->heads;
   const int padded = spec->head_dim <= 64 ? 64 : spec->head_dim <= 128 ? 128 : 256;
   const int warps = rows_warps(padded);
-  a.head_groups = (spec->kv_heads + warps - 1) / warps;
-  a.group_heads = (spec->kv_heads + a.head_groups - 1) / a.head_groups;
-  const int slices = warps / a.group_heads;
   const int64_t rows = (int64_t)batch->max_new * group;
-  int tiles = 0;
+  int tiles = 0, slices = 0;
   CUtensorMap map{};
-  if (rows > 32 && padded <= 128) {
-    // more rows than the row kernel keeps in registers
+  if (rows > 16 && padded <= 128) {
+    // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
+    // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
+    // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels do not fit tensor memory beside their scores.
     a.head_groups = spec->kv_heads;
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
@@ -103,13 +102,28 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     // (Trees of 64 tokens, 16 requests of 8k, us: 186 without, 179 at 3, 174 at 6, 175 at 9, 180 at 12, 186 at 16; trees of 13
     // over an int8 cache: 134, 130, 126, 127, 131, 135.)  The row kernel's pieces begin while the last one's keys still stream.
     a.opening = 6;
+    // (trees of 64 tokens, blocks of 16, us: boxes of 16 tokens 176, of 8 177, copies by the lanes 217; int8, trees of 13: 125, 129, 133)
     a.box_rows = spec->block_size % 16 == 0 ? 16 : spec->block_size % 8 == 0 ? 8 : 0;
     if (a.box_rows && !layer_map(spec, a.c, padded, a.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
   } else {
-    tiles = rows <= 8 ? 1 : rows <= 16 || padded == 256 ? 2 : 4;
+    tiles = rows <= 8 ? 1 : 2;
     a.row_tile = tiles * 8;
+    a.head_groups = (spec->kv_heads + warps - 1) / warps;
+    a.group_heads = (spec->kv_heads + a.head_groups - 1) / a.head_groups;
+    // Few requests: fewer heads a CTA, its warps then share a head's keys, until no segment is cut into many more than 8 pieces, for
+    // a segment's pieces are joined by one CTA.  (us, 8 rows, 16-bit / int8, all heads in a CTA against this: 1 request of 4k 39 / 44,
+    // 24 / 20; 2 of 16k 67 / 66, 39 / 33; 8 of 16k 111 / 100, 97 / 85; 4 pieces: 96 / 98, 16 pieces: 95 / 85.)  Not where one tile of
+    // rows streams a long 8-bit cache, whose narrow rows and scales are then read in pieces too small: by the caller's bounds, from 512 MB
+    // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316).
+    const int64_t stream = 2ll * batch->n_req * batch->max_tokens * a.c.row_bytes;
+    const bool whole = quantised(spec->format) && tiles == 1 && stream >= 512ll << 20;
+    while (!whole && a.group_heads > 1 && (int64_t)batch->n_req * a.head_groups * 8 < sms) {
+      a.group_heads = (a.group_heads + 1) / 2;
+      a.head_groups = (spec->kv_heads + a.group_heads - 1) / a.group_heads;
+    }
+    slices = warps / a.group_heads;
     const int turn = 16 * slices * chunks_at_once(spec->format, tiles);      // keys that the warps of a head take at a time
-    a.unit = FastDiv((64 + turn - 1) / turn * turn);             // 64 or more: fewer pieces
+    a.unit = FastDiv((64 + turn - 1) / turn * turn);             // 64 or more: fewer pieces; one request of 333 keys 19 us, with 16 keys 25, with 256 28
   }
   while ((1 << a.row_shift) < a.row_tile) ++a.row_shift;
   // units are numbered in 32 bits; a bound that the lengths on the device keep, whatever they are

@@ -583,18 +583,9 @@ cudaError_t launch_rows(const AttendArgs &a, int slices, cudaStream_t s) {
 
 template <int FMT>
 cudaError_t launch_rows(const AttendArgs &a, int tiles, int slices, cudaStream_t s) {
-  if (a.c.head_dim <= 64) {
-    if (tiles == 1) return launch_rows<FMT, 64, 1>(a, slices, s);
-    if (tiles == 2) return launch_rows<FMT, 64, 2>(a, slices, s);
-    return launch_rows<FMT, 64, 4>(a, slices, s);
-  }
-  if (a.c.head_dim <= 128) {
-    if (tiles == 1) return launch_rows<FMT, 128, 1>(a, slices, s);
-    if (tiles == 2) return launch_rows<FMT, 128, 2>(a, slices, s);
-    return launch_rows<FMT, 128, 4>(a, slices, s);
-  }
-  if (tiles == 1) return launch_rows<FMT, 256, 1>(a, slices, s);
-  return launch_rows<FMT, 256, 2>(a, slices, s);
+  if (a.c.head_dim <= 64) return tiles == 1 ? launch_rows<FMT, 64, 1>(a, slices, s) : launch_rows<FMT, 64, 2>(a, slices, s);
+  if (a.c.head_dim <= 128) return tiles == 1 ? launch_rows<FMT, 128, 1>(a, slices, s) : launch_rows<FMT, 128, 2>(a, slices, s);
+  return tiles == 1 ? launch_rows<FMT, 256, 1>(a, slices, s) : launch_rows<FMT, 256, 2>(a, slices, s);
 }
 
 }  // namespace
