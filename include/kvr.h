@@ -466,7 +466,9 @@ kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, i
  * A row that attends to nothing gives out 0 and lse -infinity; what a row does not attend to has no influence on it,
  * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
  * the cache's type.  Scores, sums and accumulators are fp32; probabilities are rounded to the 16-bit type of the product with V.
- * At most 2^30 tokens in one request.  workspace: DEVICE, kvr_attend_workspace(spec) bytes,
+ * At most 2^30 tokens in one request, and n_req, max_new and max_tokens such that tiles of query rows times spans of 64 keys stay below
+ * 2^31 (KVR_ERR_INVALID_ARG).  max_new chooses the kernel and max_tokens how heads are shared out, so bounds near the truth are
+ * faster, never more right.  workspace: DEVICE, kvr_attend_workspace(spec) bytes,
  * 256-byte aligned, zeroed once before its first use (its first 4096 bytes are counters that each call leaves at zero; the rest is
  * of no interest).  Calls that may overlap need their own; after KVR_DEV_GAVE_UP zero it again.
  */

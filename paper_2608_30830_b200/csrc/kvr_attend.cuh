@@ -2,7 +2,8 @@
 //
 // Work is cut along the keys.  A segment is one request, one group of KV heads and one tile of its query rows (row =
 // new token x query heads of one KV head + query head); a unit is a fixed number of keys of a segment.  Segments follow each
-// other request by request, and the units of all of them are dealt out in equal runs, one to each CTA of a grid that
+// other request by request, and the units of all of them are dealt out in equal runs (a segment's start may weigh some units of
+// its own), one to each CTA of a grid that
 // fills the GPU once: ragged requests keep all SMs busy to the end, and the cut needs nothing from the host but the
 // grid's size.  A CTA that holds a whole segment writes its result; the pieces of a cut segment go to the workspace as
 // (maximum, sum, accumulator), and the CTA that hands in the last one joins them.  More than 16 pieces are joined by groups of 16

