@@ -123,8 +123,9 @@ struct Angles {
         theirs.widen(y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 r = unpair(add2(mul2(pair(x[k][2 * i], x[k][2 * i + 1]), c[i]), mul2(pair(y[2 * i], y[2 * i + 1]), s[i])));
-          x[k][2 * i] = r.x; x[k][2 * i + 1] = r.y;
+          // sums one by one: of products by add.f32x2, or by fma.f32x2 with 1, one was not rounded
+          const float2 u = unpair(mul2(pair(x[k][2 * i], x[k][2 * i + 1]), c[i])), v = unpair(mul2(pair(y[2 * i], y[2 * i + 1]), s[i]));
+          x[k][2 * i] = __fadd_rn(u.x, v.x); x[k][2 * i + 1] = __fadd_rn(u.y, v.y);
         }
       }
     } else if (turned) {
