@@ -45,6 +45,9 @@ __device__ __forceinline__ unsigned widen(unsigned w) {
   }
 }
 
+// 0x80 in the bytes of w that are NaN as e4m3 (0x7f, 0xff): a sum of 7 bits and one does not carry out of its byte
+__device__ __forceinline__ unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // A CTA's walk over the pieces of segments in its run of units.
 struct Piece {
   unsigned unit, next;       // the CTA's share of the segment, its opening included: units unit .. next - 1

@@ -221,6 +221,9 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
 #pragma unroll
     for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY, sum[n][0] = sum[n][1] = 0.f;
     int v_exp = -1000;                 // V's scales are multiplied by 2^-v_exp (set by the first chunk)
+    bool odd = false;                  // this lane has found a code of V that is NaN
+    // from this turn on chunks reach past the context, where some rows may not see all keys
+    const int look_from = len.fresh > 1 || a.mask ? (len.context - slice * 16 + 16 * slices - 1) / (16 * slices) - kAtOnce : 1 << 30;
 
     const int c_end = chunk_end(piece);
     for (int c = piece.begin * unit_chunks; c < c_end; c += kAtOnce) {
@@ -233,6 +236,24 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
         st_of[u] = ring + stage * S::kStageBytes;
         stage = stage + 1 == kStages ? 0 : stage + 1;
+      }
+      if constexpr (FMT == KVR_CACHE_E4M3) {
+        // Codes of V that are NaN must not meet the zero probabilities of rows that do not see their key: set to zero here, and
+        // to NaN the sums of the rows that do see it, at the piece's end (append stores no such code).  Done as for 16 bits below, in
+        // the loop and channel by channel, the registers it takes cost long caches 6 % (435 against 463 us); so 1 %.
+        if (c >= look_from) {
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+            for (int i = max(len.context - ((c + u) * slices + slice) * 16, 0) * kChunks + lane; i < 16 * kChunks; i += 32) {
+              unsigned *w = reinterpret_cast<unsigned *>(st_of[u] + 16 * kRow + i * 16);        // a key's columns lie side by side
+              const uint4 x = *reinterpret_cast<const uint4 *>(w);
+              if (!(nan_codes(x.x) | nan_codes(x.y) | nan_codes(x.z) | nan_codes(x.w))) continue;
+              odd = true;
+#pragma unroll 1
+              for (int k = 0; k < 4; ++k) w[k] &= ~(nan_codes(w[k]) / 0x80u * 0xffu);
+            }
+          __syncwarp();
+        }
       }
       // the lane's keys (rows gid and gid + 8 of S^T)
       const int key_a = kQuant ? (gid >> 1) * 4 + (gid & 1) : gid, key_b = kQuant ? key_a + 2 : gid + 8;
@@ -478,6 +499,35 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[t][n][i] *= unit;
+    }
+    if (FMT == KVR_CACHE_E4M3 && __any_sync(0xffffffffu, odd)) {
+      // the new tokens among this warp's keys again, as they lie in the cache: a bit for each of the lane's channels
+      unsigned nan[NT][2] = {};
+#pragma unroll 1
+      for (int c = piece.begin * unit_chunks; c < c_end; ++c)
+#pragma unroll 1
+        for (int j = max((c * slices + slice) * 16, len.context); j < min((c * slices + slice) * 16 + 16, len.keys); ++j) {
+          const long long off = token_offset(a.b, a.c, a.bs, piece.r, j);
+          const char *v = a.c.base + a.c.v_offset + (long long)head * a.c.head_dim + off;
+          unsigned bits = 0;
+#pragma unroll 1
+          for (int d = gid * (DP / 8); d < min((gid + 1) * (DP / 8), a.c.head_dim) && off >= 0 && live; ++d)
+            bits |= (unsigned)((v[d] & 0x7f) == 0x7f) << (d - gid * (DP / 8));
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int row = n * 8 + tig * 2 + e;
+              if (row < rows && sees(a, len.first, (int)a.group.div(piece.row0 + row), j - len.context)) nan[n][e] |= bits;
+            }
+        }
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (nan[n][i & 1] >> (t * 2 + (i >> 1)) & 1) o[t][n][i] = NAN;
     }
     if (slices > 1) {
       // slices of a head are joined through shared memory, one n-tile at a time, in slice order

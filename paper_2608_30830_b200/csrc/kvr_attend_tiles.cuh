@@ -269,6 +269,41 @@ __device__ __noinline__ void join_rows(const AttendArgs &a, const Piece &p, cons
   }
 }
 
+// Codes that are NaN set to zero in KEYS rows of DP codes, by a warp; were there any?  Out of line: the callers'
+// loops need the registers.
+template <int DP, int KEYS>
+__device__ __noinline__ bool clear_nan(unsigned char *rows, int lane) {
+  unsigned found = 0;
+#pragma unroll 8
+  for (int i = lane; i < KEYS * DP / 16; i += 32) {
+    const uint4 x = *reinterpret_cast<const uint4 *>(rows + i * 16);
+    found |= nan_codes(x.x) | nan_codes(x.y) | nan_codes(x.z) | nan_codes(x.w);
+  }
+  if (!__any_sync(0xffffffffu, found != 0)) return false;
+#pragma unroll 1
+  for (int i = lane; i < KEYS * DP / 4; i += 32) {
+    unsigned *w = reinterpret_cast<unsigned *>(rows) + i;
+    *w &= ~(nan_codes(*w) / 0x80u * 0xffu);
+  }
+  __syncwarp();
+  return true;
+}
+
+// Channels d .. d + 31 of V (bits) in which a key among key0 .. key0 + n - 1 that this thread's row sees is NaN, of an e4m3 cache.  (Of
+// the tiles that the loaders look through: those that reach past the context.)
+__device__ __noinline__ unsigned nan_channels(const AttendArgs &a, const Lengths &len, int r, int head, int key0, int n, bool have, int t_row, int d) {
+  unsigned bits = 0;
+#pragma unroll 1
+  for (int j = max(key0, len.context / kTileKeys * kTileKeys); j < min(key0 + n, len.keys); ++j) {
+    const long long off = token_offset(a.b, a.c, a.bs, r, j);
+    if (off < 0 || !have || (j >= len.context && !sees(a, len.first, t_row, j - len.context))) continue;
+    const char *v = a.c.base + a.c.v_offset + off + (long long)head * a.c.head_dim;
+#pragma unroll 1
+    for (int i = 0; i < min(32, a.c.head_dim - d); ++i) bits |= (unsigned)((v[d + i] & 0x7f) == 0x7f) << i;
+  }
+  return bits;
+}
+
 template <int FMT, int DP, bool TWO>
 __global__ void __launch_bounds__(TileShape<FMT, DP, TWO>::kThreads, 1)
 attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
@@ -282,6 +317,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ unsigned tm_slot;
   __shared__ int gave_up_word, last_in;
   __shared__ unsigned long long odd_keys[5][2];  // by ring slot: keys of a V tile with elements that are not finite
+  __shared__ volatile int odd_codes;             // a loader has met codes of V that are NaN among a request's new tokens
   __shared__ float2 join_ml[2][128];
   __shared__ int box_ids[S::kLoaders][64];                 // by loader: block ids of the boxes around its step
   volatile int *gave_up = &gave_up_word;
@@ -303,6 +339,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 
   if (threadIdx.x == 0) {
     gave_up_word = 0;
+    odd_codes = 0;
     for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), S::kPerStep); bar_init(shared_at(&bars.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) { bar_init(shared_at(&bars.s_full[w]), 1); bar_init(shared_at(&bars.p_full[w]), 4); bar_init(shared_at(&bars.pv_done[w]), 1); }
     bar_init(shared_at(&bars.q_full), 8);
@@ -487,6 +524,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         const int c0 = (chunk & 3) * 2, swap = ((chunk >> 2) ^ sub) & 1;
         const unsigned char *src = stage + sub * DP + chunk * 16;
         unsigned char *row = ring + slot * S::kBuffer + (chunk >> 2) * (kTileKeys * 128) + (span0 + sub) * 128;
+        if (FMT == KVR_CACHE_E4M3 && v && (tile + 1) * kTileKeys > at.p.len.context && (at.p.len.fresh > 1 || a.mask)) {
+          // Codes of V that are NaN must not meet the zero probabilities of rows that do not see their key: set to zero, and the
+          // softmax threads are told that there were some (append stores none).
+          if (clear_nan<DP, S::kSpan>(stage, lane)) odd_codes = 1;
+        }
 #pragma unroll 4
         for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
           const int key = i * kAtOnce + sub;             // kAtOnce is even: the key's parity is sub's
@@ -865,6 +907,14 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           if (other != 0.f) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] += ex[((1 - w) * 32 + i) * 128 + tid] * other;
+          }
+        }
+        if constexpr (FMT == KVR_CACHE_E4M3) {
+          if (__builtin_expect(odd_codes, 0)) {  // set before the products that are waited for above
+            const Lengths copy = len;    // what the call is shown lies in memory
+            const unsigned nan = nan_channels(a, copy, piece.r, head, t0 * kTileKeys, n * kTileKeys, have, t_row, d_own + c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) if (nan >> i & 1) o[i] = NAN;
           }
         }
 #pragma unroll
