@@ -466,6 +466,8 @@ kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, i
  * A row that attends to nothing gives out 0 and lse -infinity; what a row does not attend to has no influence on it,
  * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
  * the cache's type.  Scores, sums and accumulators are fp32; probabilities are rounded to the 16-bit type of the product with V.
+ * For 8-bit caches probability times V's scale is rounded to f16 (11 bits, or 2^-32 of the largest scale among the keys that the
+ * row sees, whichever is more).
  * At most 2^30 tokens in one request, and n_req, max_new and max_tokens such that tiles of query rows times spans of 64 keys stay below
  * 2^31 (KVR_ERR_INVALID_ARG).  max_new chooses the kernel and max_tokens how heads are shared out, so bounds near the truth are
  * faster, never more right.  workspace: DEVICE, kvr_attend_workspace(spec) bytes,

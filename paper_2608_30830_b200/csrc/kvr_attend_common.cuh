@@ -24,8 +24,15 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// 2^e exactly; 0 below the normal numbers
-__device__ __forceinline__ float power2(int e) { return e < -126 ? 0.f : __uint_as_float((unsigned)(e + 127) << 23); }
+// The unit of V's scales in a row's sums (8-bit caches): a power of two that scales are multiplied by, between 2^-126 and 2^126.  A
+// probability (up to 2^4) times a scale has to fit f16: when a scale that the row sees passes 2^11 units, the unit is set so that
+// it lies at 2^7 to 2^8 (2^126 at most, which is where rows begin).  Products stay below 2^15, and what a key adds is rounded to
+// 11 bits, or to 2^-32 of the largest scale that the row sees, whichever is more.  Scales that the row does not see have no part in
+// it: past the context rows have units of their own.  (One that it sees and that is not finite decides the row's result anyway.)
+constexpr float kUnitLimit = 2048.f;
+__device__ __forceinline__ float unit_first(bool row) { return __uint_as_float((row ? 253u : 1u) << 23); }   // no row: never passed
+__device__ __forceinline__ float unit_of(float scale) { return __uint_as_float(min(253u, 261u - (__float_as_uint(scale) >> 23)) << 23); }   // 2^(7 - e)
+__device__ __forceinline__ float unit_back(float unit) { return __uint_as_float((254u << 23) - __float_as_uint(unit)); }       // 1 / unit
 
 // two 8-bit codes (bytes 0 and 1, or 2 and 3, of w) as f16
 template <int FMT, bool HIGH>

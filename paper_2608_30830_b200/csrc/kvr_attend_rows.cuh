@@ -220,7 +220,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
     float top[NT][2], sum[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY, sum[n][0] = sum[n][1] = 0.f;
-    int v_exp = -1000;                 // V's scales are multiplied by 2^-v_exp (set by the first chunk)
+    float unit[NT][2];                 // of V's scales, by row
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) unit[n][e] = unit_first(n * 8 + tig * 2 + e < rows);
     bool odd = false;                  // this lane has found a code of V that is NaN
     // from this turn on chunks reach past the context, where some rows may not see all keys
     const int look_from = len.fresh > 1 || a.mask ? (len.context - slice * 16 + 16 * slices - 1) / (16 * slices) - kAtOnce : 1 << 30;
@@ -338,24 +342,42 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
           best[n][e] = m;
           moved = moved || m > top[n][e] + kLazy;                        // from -infinity: any score moves it
         }
-      int shift = 0;                   // of V's scale, in powers of two
       if constexpr (kQuant) {
-        // p times V's scale has to fit f16: the largest scale is brought to 2^7 when it first appears and
-        // again when one passes 2^11, so products stay below 2^15, and one key of 2^-21 times the largest is still normal
         float big = fmaxf(v_scale[0][0], v_scale[0][1]);
         if constexpr (kAtOnce == 2) big = fmaxf(big, fmaxf(v_scale[kAtOnce - 1][0], v_scale[kAtOnce - 1][1]));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 4));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 8));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 16));
-        const int e = (int)(__float_as_uint(big) >> 23) - 127;           // big >= 0; NaN scales are not the largest
-        if (big > 0.f && big < INFINITY && e - v_exp >= 11) {
-          const int next = max(e - 7, -126);
-          shift = v_exp == -1000 ? 0 : next - v_exp;
-          v_exp = next;
+        bool far = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) far = far || big * unit[n][e] >= kUnitLimit;
+        if (__any_sync(0xffffffffu, far)) {
+          // the largest that each row sees
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float own = 0.f;
+#pragma unroll
+              for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                  if (s[u][n][i * 2 + e] != -INFINITY) own = fmaxf(own, v_scale[u][i]);
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 4));
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 8));
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 16));
+              if (own * unit[n][e] >= kUnitLimit) {
+                const float less = unit_of(own) * unit_back(unit[n][e]);
+                unit[n][e] = unit_of(own);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                  o[t][n][e] *= less;
+                  o[t][n][2 + e] *= less;
+                }
+              }
+            }
         }
       }
-      if (__any_sync(0xffffffffu, moved) || (kQuant && shift != 0)) {
-        const float less = kQuant ? power2(-shift) : 1.f;
+      if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -366,13 +388,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
             sum[n][e] *= f;
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-              o[t][n][e] *= f * less;
-              o[t][n][2 + e] *= f * less;
+              o[t][n][e] *= f;
+              o[t][n][2 + e] *= f;
             }
           }
       }
       // P^T, as the right operand of the second product
-      const float v_unit = kQuant && v_exp != -1000 ? power2(-v_exp) : 1.f;
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         unsigned char *st = st_of[u];
@@ -394,7 +415,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pf[n][i] = s[u][n][i] == -INFINITY ? 0.f : pf[n][i] * (v_scale[u][i >> 1] * v_unit);
+            for (int i = 0; i < 4; ++i) pf[n][i] = s[u][n][i] == -INFINITY ? 0.f : pf[n][i] * (v_scale[u][i >> 1] * unit[n][i & 1]);
         } else if (key0 + 16 > len.context && (len.fresh > 1 || a.mask)) {
           // lanes 2k and 2k + 1 look through key k's row of V
           bool odd = false;
@@ -492,13 +513,12 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 16);
       }
     if constexpr (kQuant) {
-      const float unit = v_exp == -1000 ? 1.f : power2(v_exp);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[t][n][i] *= unit;
+          for (int i = 0; i < 4; ++i) o[t][n][i] *= unit_back(unit[n][i & 1]);
     }
     if (FMT == KVR_CACHE_E4M3 && __any_sync(0xffffffffu, odd)) {
       // the new tokens among this warp's keys again, as they lie in the cache: a bit for each of the lane's channels

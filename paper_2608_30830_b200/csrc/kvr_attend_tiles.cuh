@@ -195,6 +195,25 @@ __device__ __forceinline__ unsigned long long visible(const AttendArgs &a, const
   return vis;
 }
 
+// The largest of a tile's 128 scales among the keys that this thread's row sees.  Out of line, as it is seldom asked for.
+__device__ __noinline__ float largest_seen(const AttendArgs &a, const Lengths &len, int key0, bool have, int t_row, const float *scales) {
+  float big = 0.f;
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    const unsigned long long vis = visible(a, len, key0 + h * 64, have, t_row);
+    if (vis == 0) continue;
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
+      const float4 x = *reinterpret_cast<const float4 *>(scales + h * 64 + i);
+      if (vis >> i & 1) big = fmaxf(big, x.x);
+      if (vis >> (i + 1) & 1) big = fmaxf(big, x.y);
+      if (vis >> (i + 2) & 1) big = fmaxf(big, x.z);
+      if (vis >> (i + 3) & 1) big = fmaxf(big, x.w);
+    }
+  }
+  return big;
+}
+
 // The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  256 threads.
 // First, a thread a row, what each piece counts for (weights[piece][row]); then the sums, a thread four rows and 8 channels at a
 // time: pieces lie channel by channel, and 16 loads of 16 bytes are under way for each thread (a row a thread, 4 bytes at a time, took
@@ -686,7 +705,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         if (lane == 0) bar_arrive(shared_at(&bars.q_full));
       }
       float top = -INFINITY, sum = 0.f;  // top: of scaled scores
-      int v_exp = -1000, mine = 0;       // mine: jobs of this warpgroup in this piece
+      float v_unit = unit_first(have);   // of V's scales
+      int mine = 0;                      // jobs of this warpgroup in this piece
 #pragma unroll 1
       for (int t = TWO ? 0 : w; t < n; t += TWO ? 1 : 2) {
         const int key0 = (t0 + t) * kTileKeys, tile = tiles_before + t;
@@ -716,20 +736,23 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             }
           }
         };
-        float v_unit = 1.f, f_unit = 1.f;        // V's scales' unit, and what its change does to O
+        float f_unit = 1.f;                      // what a change of V's unit does to O
         if constexpr (kQuant) {
-          // the row kernel's rule for V's scales
           const float *vs = ks + 128;
           float big = fmaxf(fmaxf(vs[lane], vs[lane + 32]), fmaxf(vs[lane + 64], vs[lane + 96]));
 #pragma unroll
           for (int d = 16; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
-          const int e = (int)(__float_as_uint(big) >> 23) - 127;
-          if (big > 0.f && big < INFINITY && e - v_exp >= 11) {
-            const int next = max(e - 7, -126);
-            if (v_exp != -1000) f_unit = power2(v_exp - next);
-            v_exp = next;
+          if (__any_sync(0xffffffffu, big * v_unit >= kUnitLimit)) {
+            if (edge) {
+              const Lengths copy = len;          // what the call is shown lies in memory
+              big = largest_seen(a, copy, key0, have, t_row, vs);
+            }
+            if (big * v_unit >= kUnitLimit) {
+              f_unit = unit_of(big) * unit_back(v_unit);
+              v_unit = unit_of(big);
+            }
+            __syncwarp();
           }
-          if (v_exp != -1000) v_unit = power2(-v_exp);
         }
         const Pair scale2 = pair(scale, scale), unit2 = pair(v_unit, v_unit);
 #pragma unroll 1
@@ -865,7 +888,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       tc_after();
       tiles_before += n;
       steps_before += 2 * n;
-      const float unit = kQuant && v_exp != -1000 ? power2(v_exp) : 1.f;
+      const float unit = kQuant ? unit_back(v_unit) : 1.f;
       // The row's sums, to the output or to the workspace.  Not TWO: the warpgroups have sums of the same rows.  Each takes half of
       // the channels, 32 at a time, and gives the other's half away.
       constexpr int kOwn = TWO ? DP : DP / 2;

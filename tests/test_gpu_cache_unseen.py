@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2608_30830_b200 import kvr
 from test_gpu_cache import KIND, U, Setup, assert_within, attend64, rand
 
 pytestmark = pytest.mark.gpu
@@ -100,3 +101,56 @@ def test_a_single_nan_code_reaches_its_channel_in_rows_that_see_it(code, heads, 
     top = max(float(x.abs().max()) for x in v64)
     bound = (U["f16"] + U["bf16"] + 2.0 ** -13) * mag + 2.0 ** -24 * top * math.sqrt(CONTEXT[-1] + new)
     assert_within(torch.where(want, 0, out), torch.where(want, 0, ref), bound)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("size", [1e12, 1e30, -math.inf])
+@pytest.mark.parametrize("heads,group,dim,bs,new", SHAPES)
+def test_the_scale_of_a_token_that_a_row_does_not_see(fmt, size, heads, group, dim, bs, new):
+    """V of one branch is far larger than all other: the other branch is as if it were not there, its own rows are right."""
+    t = Trees(fmt, "bf16", heads, group, dim, bs, new, seed=new + dim + 2)
+    s = t.s
+    clean = t.attend()
+    if math.isfinite(size):
+        one = kvr.Batch(torch.arange(len(CONTEXT) + 1, dtype=torch.int32, device="cuda"), s.arrays[1] + t.odd, s.arrays[2], 1,
+                        CONTEXT[-1] + new, s.status)
+        s.cache.append(s.pool, 0, one, v=rand(s, len(CONTEXT), heads, dim, dtype=torch.float32) * size)
+    else:                                                    # bytes that append does not write: a scale of infinity
+        v, slots = t.odd_rows(1)
+        if fmt == "bf16":
+            v[slots] = torch.full((heads * dim,), size, dtype=torch.bfloat16, device="cuda").view(torch.uint8)
+        else:
+            v[slots, heads * dim:heads * dim + 4 * heads] = torch.full((heads,), -size, device="cuda").view(torch.uint8)
+    out, lse = t.attend()
+    t.same_but_for_those_that_see_it(clean, (out, lse))
+    assert torch.equal(lse, clean[1])
+    if not math.isfinite(size):
+        assert not torch.isfinite(out[t.hit]).any()
+        return
+    kv = [[s.decode(0, i)[0][s.slots(r, 0, c + new)] for r, c in enumerate(CONTEXT)] for i in (0, 1)]
+    want, _, mag = attend64(s, t.q, *kv, 1 / math.sqrt(dim), t.seen)
+    u_p = U["bf16"] if fmt == "bf16" else U["f16"]
+    # what a key adds is f16 against the largest |v| that the row sees
+    top = torch.where(t.hit, max(float(x.abs().max()) for x in kv[1]), max(float(x[:c].abs().max()) if c else 0.0 for x, c in zip(kv[1], CONTEXT)))
+    tiny = 0 if fmt == "bf16" else 2.0 ** -24 * math.sqrt(CONTEXT[-1] + new) * top[:, None, None]
+    assert_within(out, want, (u_p + U["bf16"] + 2.0 ** -13) * mag + tiny + 2.0 ** -100)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("heads,group,dim,bs,new", SHAPES)
+def test_an_infinite_scale_beside_one_that_grows(fmt, heads, group, dim, bs, new):
+    """An unseen scale of infinity must not keep the unit of a row from following a scale that the row does see."""
+    t = Trees(fmt, "bf16", heads, group, dim, bs, new, seed=new + dim + 3)
+    s = t.s
+    one = kvr.Batch(torch.arange(len(CONTEXT) + 1, dtype=torch.int32, device="cuda"), s.arrays[1], s.arrays[2], 1, CONTEXT[-1] + new, s.status)
+    s.cache.append(s.pool, 0, one, v=rand(s, len(CONTEXT), heads, dim, dtype=torch.float32) * 2.0 ** 24)      # token 0, which all see but `odd`
+    clean = t.attend()
+    v, slots = t.odd_rows(1)
+    kv = [[s.decode(0, i)[0][s.slots(r, 0, c + new)] for r, c in enumerate(CONTEXT)] for i in (0, 1)]
+    v[slots, heads * dim:heads * dim + 4 * heads] = torch.full((heads,), math.inf, device="cuda").view(torch.uint8)
+    out, lse = t.attend()
+    t.same_but_for_those_that_see_it(clean, (out, lse))
+    want, _, mag = attend64(s, t.q, *kv, 1 / math.sqrt(dim), t.seen)
+    top = max(float(x.abs().max()) for x in kv[1])
+    bound = (U["f16"] + U["bf16"] + 2.0 ** -13) * mag + 2.0 ** -24 * top * math.sqrt(CONTEXT[-1] + new)
+    assert_within(out[~t.hit], want[~t.hit], bound[~t.hit])
