@@ -645,6 +645,12 @@ kvr_status kvr_test_plan(const kvr_geometry *g, const int64_t *n_tokens, int32_t
                          uint64_t resume_single_bytes, int64_t *chunks, int64_t *copies, int64_t *segs, int64_t cap, int64_t *counts);
 
 /*
+ * How attention's kernels are made ready once on every device, for tests (pure host code).  For i < n an action that would
+ * return results[i] is asked for on devices[i]; returned[i] is what the caller gets.  Returns how many actions were run.
+ */
+int32_t kvr_test_once(const int32_t *devices, const int32_t *results, int32_t n, int32_t *returned);
+
+/*
  * Placement of the library's own arena (no counterpart in the paper).  Host DRAM is shared between the GPUs of a
  * node; each pool's arena is faulted in by threads bound to the CPUs of the NUMA node its GPU hangs off, so the
  * pages land next to that GPU's link.  kvr_pool_numa_node: the node used (-1: unknown, single-node host, caller's

@@ -11,7 +11,7 @@ SO = os.path.join(PKG, "libkvr.so")
 SOURCES = ["kvr_kernels.cu", "kvr_engine.cu", "kvr_lib.cu", "kvr_noalloc.cu", "kvr_policy.cpp", "kvr_controller.cpp", "kvr_numa.cpp",
            "kvr_cache.cu", "kvr_attend.cu", "kvr_attend_bf16.cu", "kvr_attend_f16.cu", "kvr_attend_e4m3.cu", "kvr_attend_int8.cu"]
 DEPS = SOURCES + ["kvr_kernels.cuh", "kvr_cache.cuh", "kvr_attend.cuh", "kvr_attend_common.cuh",
-                  "kvr_attend_rows.cuh", "kvr_attend_tiles.cuh", "kvr_meta.hpp", "kvr_numa.hpp", "kvr_pool.hpp", os.path.join("..", "..", "include", "kvr.h")]
+                  "kvr_attend_rows.cuh", "kvr_attend_tiles.cuh", "kvr_meta.hpp", "kvr_numa.hpp", "kvr_once.hpp", "kvr_pool.hpp", os.path.join("..", "..", "include", "kvr.h")]
 
 
 def stale():

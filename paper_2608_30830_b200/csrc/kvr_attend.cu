@@ -3,6 +3,8 @@
 
 #include <cmath>
 
+#include "kvr_once.hpp"
+
 namespace kvr {
 namespace {
 
@@ -142,4 +144,11 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     default: e = launch_attend_int8(a, tiles, slices, map, s);
   }
   return e == cudaSuccess ? KVR_OK : fail_cache(KVR_ERR_CUDA, cudaGetErrorString(e));
+}
+
+extern "C" int32_t kvr_test_once(const int32_t *devices, const int32_t *results, int32_t n, int32_t *returned) {
+  OncePerDevice once;
+  int32_t runs = 0;
+  for (int32_t i = 0; i < n; ++i) returned[i] = once(devices[i], [&] { ++runs; return results[i]; });
+  return runs;
 }

@@ -1,9 +1,20 @@
 // Device helpers of both attention kernels: asynchronous copies, conversions, and the walk over a CTA's pieces.
 #pragma once
 #include "kvr_attend.cuh"
+#include "kvr_once.hpp"
 
 namespace kvr {
 namespace {
+
+// Lets `kernel` have `bytes` of dynamic shared memory on the current device.
+template <class Kernel>
+cudaError_t allow_shared(OncePerDevice &once, Kernel kernel, int bytes) {
+  int device = -1;
+  if (const cudaError_t e = cudaGetDevice(&device)) return e;
+  const cudaError_t e = once(device, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+  if (e != cudaSuccess) cudaGetLastError();      // reported by this call, not by the next one's launch
+  return e;
+}
 
 __device__ __forceinline__ unsigned shared_at(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(unsigned dst, const void *src, bool valid) {

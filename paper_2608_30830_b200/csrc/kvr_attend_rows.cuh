@@ -650,8 +650,8 @@ cudaError_t launch_rows(const AttendArgs &a, int slices, cudaStream_t s) {
   const int warps = a.group_heads * slices;
   const int merge = slices > 1 ? (slices - 1) * a.group_heads * (DP * 8 + 16) * 4 : 0;
   const int bytes = warps * S::kStages * S::kStageBytes + merge;
-  static const cudaError_t set = cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 512);
-  if (set != cudaSuccess) return set;
+  static OncePerDevice once;
+  if (const cudaError_t e = allow_shared(once, attend_rows_kernel<FMT, DP, NT>, 227 * 1024 - 512)) return e;
   attend_rows_kernel<FMT, DP, NT><<<a.ctas, warps * 32, bytes, s>>>(a, slices);
   return cudaGetLastError();
 }

@@ -989,10 +989,8 @@ template <int FMT, int DP, bool TWO>
 cudaError_t launch_tiles(const AttendArgs &a, const CUtensorMap &map, cudaStream_t s) {
   using S = TileShape<FMT, DP, TWO>;
   const auto kernel = attend_tiles_kernel<FMT, DP, TWO>;
-  static const cudaError_t set = [&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-  }();
-  if (set != cudaSuccess) return set;
+  static OncePerDevice once;
+  if (const cudaError_t e = allow_shared(once, kernel, S::kBytes)) return e;
   kernel<<<a.ctas, S::kThreads, S::kBytes, s>>>(a, map);
   return cudaGetLastError();
 }

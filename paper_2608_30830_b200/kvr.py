@@ -114,7 +114,7 @@ EXPORTS = [
     "kvr_controller_create", "kvr_controller_destroy", "kvr_controller_calibrate", "kvr_controller_suspend",
     "kvr_controller_advance", "kvr_controller_resume", "kvr_controller_get_stats",
     "kvr_cache_geometry", "kvr_rope_frequencies", "kvr_rope_table", "kvr_cache_append", "kvr_cache_read",
-    "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep",
+    "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep", "kvr_test_once",
 ]
 
 _lib = None
@@ -247,6 +247,8 @@ def lib():
     L.kvr_cache_attend.argtypes = [spec, vp, i32, batch, rows, rows, vp, vp, i32, C.c_float, vp, u64, vp]
     L.kvr_cache_keep.restype = i32
     L.kvr_cache_keep.argtypes = [spec, vp, batch, vp, i32, vp, vp]
+    L.kvr_test_once.restype = i32
+    L.kvr_test_once.argtypes = [pi32, pi32, i32, pi32]
     _lib = L
     return L
 
@@ -364,6 +366,17 @@ def test_plan(geom, n_tokens, slot_bytes, slots, launch_slots, ring_next=0, resu
 
 
 test_plan.__test__ = False      # a library call, not a pytest test
+
+
+def test_once(devices, results):
+    """kvr_test_once: (what each call returns, how many actions were run)."""
+    d, r = (np.ascontiguousarray(x, dtype=np.int32) for x in (devices, results))
+    p32, returned = lambda a: a.ctypes.data_as(C.POINTER(C.c_int32)), np.zeros(len(d), dtype=np.int32)   # noqa: E731
+    runs = lib().kvr_test_once(p32(d), p32(r), min(len(d), len(r)), p32(returned))
+    return returned.tolist(), runs
+
+
+test_once.__test__ = False
 
 
 def numa_lookup(sysfs_root, pci_bus_id, cap=4096):
