@@ -679,8 +679,10 @@ def rope_frequencies(rot_dim, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0
 def rope_table(out, first=0, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0, high=4.0, original=0, stream=None):
     """kvr_rope_table into a float32 CUDA tensor [positions, rot_dim / 2, 2]."""
     sc = RopeScaling(base, factor, low, high, original, kind)
-    dev = _device()
-    _check(lib().kvr_rope_table(C.byref(sc), 2 * out.shape[1], first, out.shape[0], _array(out, "out", _torch.float32, 3, dev),
+    dev, shape = _device(), out.shape
+    if len(shape) != 3 or shape[2] != 2:
+        raise ValueError("out must be [positions, rot_dim / 2, 2]")
+    _check(lib().kvr_rope_table(C.byref(sc), 2 * shape[1], first, shape[0], _array(out, "out", _torch.float32, 3, dev),
                                 _stream(stream, dev)))
 
 

@@ -1,0 +1,56 @@
+"""What the binding of the cache operators refuses, and what it hands to the library, without a GPU.
+
+Host tensors stand in for device tensors (their device ordinal is -1), and a recorder stands in for the library, so that
+nothing is launched whatever is let pass.
+"""
+import pytest
+import torch
+
+from paper_2608_30830_b200 import kvr
+
+
+class Recorder:
+    """Takes the place of the loaded library: keeps a copy of each call's kvr_batch and returns KVR_OK."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def entry(*args):
+            self.calls.append((name, [a._obj for a in args if hasattr(a, "_obj")], args))
+            return kvr.OK
+        return entry
+
+    def batch(self):
+        return next(x for x in self.calls[-1][1] if isinstance(x, kvr.BatchStruct))
+
+
+@pytest.fixture
+def library(monkeypatch):
+    kvr.lib()
+    kvr._use_torch()
+    monkeypatch.setattr(kvr, "_device", lambda: -1)
+    cache = kvr.Cache(1, 2, 64, 16, 8)                        # made by the library itself
+    recorder = Recorder()
+    monkeypatch.setattr(kvr, "_lib", recorder)
+    recorder.cache = cache
+    recorder.pool = torch.zeros(cache.pool_bytes, dtype=torch.uint8)
+    return recorder
+
+
+def i32(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def bf(*shape):
+    return torch.zeros(*shape, dtype=torch.bfloat16)
+
+
+def test_a_rotary_table_is_written_only_into_its_own_shape(library):
+    kvr.rope_table(torch.zeros(10, 32, 2), stream=0)
+    assert library.calls[-1][0] == "kvr_rope_table" and library.calls[-1][2][1:4] == (64, 0, 10)
+    made = len(library.calls)
+    for shape in [(10, 32, 1), (10, 32, 0), (10, 32, 3), (10, 64), (10, 32, 2, 1)]:
+        with pytest.raises(ValueError):
+            kvr.rope_table(torch.zeros(shape), stream=0)
+    assert len(library.calls) == made
