@@ -708,15 +708,22 @@ class Batch:
             raise ValueError("token_start has n_req + 1 entries, context n_req, tables n_req rows")
         if tables.dtype is not i32 or tables.get_device() != dev or (shape[1] > 1 and stride[1] != 1) or (n > 1 and stride[0] < shape[1]):
             raise ValueError("tables must be of int32 on the current CUDA device, with dense rows that do not overlap")
-        # a row's entries are counted by the stride: with one request, or rows cut from wider ones, by the shape alone
+        # The library counts a row's entries by the stride (one request: by the shape).  Rows cut from wider ones have fewer: their width
+        # bounds the tokens of a request.
+        self.width = shape[1] if n > 1 and shape[1] < stride[0] else 0
         self.struct = BatchStruct(n, 0, max_new, max_tokens, stride[0] if n > 1 else shape[1],
                                   _array(token_start, "token_start", i32, 1, dev), _array(context, "context", i32, 1, dev),
                                   tables.data_ptr(), None if status is None else _array(status, "status", i32, 1, dev))
         self.arrays = (token_start, context, tables, status)          # kept alive
         self._ref = _ref(self.struct)
 
-    def of(self, n_tokens):
+    def of(self, n_tokens, block_size):
+        """The struct for a call over rows of n_tokens tokens."""
         self.struct.n_tokens = n_tokens
+        if self.width and self.width * block_size < self.struct.max_tokens:
+            b = BatchStruct.from_buffer_copy(self.struct)
+            b.max_tokens = self.width * block_size
+            return _ref(b)
         return self._ref
 
 
@@ -756,7 +763,7 @@ class Cache:
         n = (q if q is not None else k if k is not None else v).shape[0]
         if positions is not None and positions.shape[0] != n:
             raise ValueError("positions must have %d entries" % n)
-        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(q, n, "q", dev),
+        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
                                    self._rows(k, n, "k", dev), self._rows(v, n, "v", dev), self._rows(q_out, n, "q_out", dev),
                                    None if rope is None else _ref(rope.struct),
                                    None if positions is None else _array(positions, "positions", _torch.int32, 1, dev), _stream(stream, dev))
@@ -767,7 +774,7 @@ class Cache:
         """kvr_cache_read: the tokens [context, context + new) of each request into k and v."""
         dev = _device()
         n = (k if k is not None else v).shape[0]
-        st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(k, n, "k", dev),
+        st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(k, n, "k", dev),
                                  self._rows(v, n, "v", dev), _stream(stream, dev))
         if st:
             _check(st)
@@ -787,7 +794,7 @@ class Cache:
             raise ValueError("mask must be [tokens, words]")
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
-        st = _lib.kvr_cache_attend(self._spec, self._pool(pool, dev), layer, batch.of(n), self._rows(q, n, "q", dev),
+        st = _lib.kvr_cache_attend(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
                                    self._rows(out, n, "out", dev), None if lse is None else _array(lse, "lse", _torch.float32, 2, dev),
                                    None if mask is None else _array(mask, "mask", _torch.int64, 2, dev),
                                    0 if mask is None else mask.shape[1], self._scale if scale is None else scale,
@@ -801,7 +808,7 @@ class Cache:
         dev, b = _device(), batch.struct
         if index.shape[0] != b.n_req or count.shape[0] != b.n_req:
             raise ValueError("index and count must have a row for each request")
-        st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(min(b.n_req * b.max_new, 2**31 - 1)),
+        st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(min(b.n_req * b.max_new, 2**31 - 1), self.spec.block_size),
                                  _array(index, "index", _torch.int32, 2, dev), index.shape[1],
                                  _array(count, "count", _torch.int32, 1, dev), _stream(stream, dev))
         if st:

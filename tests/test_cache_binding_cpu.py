@@ -54,3 +54,24 @@ def test_a_rotary_table_is_written_only_into_its_own_shape(library):
         with pytest.raises(ValueError):
             kvr.rope_table(torch.zeros(shape), stream=0)
     assert len(library.calls) == made
+
+
+@pytest.mark.parametrize("width,bound", [(3, 48), (8, 100)])
+def test_tables_cut_from_wider_ones_end_with_their_rows(library, width, bound):
+    """Rows are `stride` entries apart, but only `width` of them are the table's: no request may reach into what follows (which
+    for the last row lies beyond the memory)."""
+    wide = i32(2, 8)
+    b = kvr.Batch(i32(3), i32(2), wide[:, 8 - width:], 4, 100)
+    assert b.struct.table_stride == 8
+    c, pool = library.cache, library.pool
+    c.append(pool, 0, b, k=bf(2, 2, 64), stream=0)
+    assert library.batch().max_tokens == bound
+    c.read(pool, 0, b, k=bf(2, 2, 64), stream=0)
+    assert library.batch().max_tokens == bound
+    c.attend(pool, 0, b, bf(2, 4, 64), bf(2, 4, 64), i32(4), stream=0)
+    assert library.batch().max_tokens == bound
+    c.keep(pool, b, i32(2, 1), i32(2), stream=0)
+    assert library.batch().max_tokens == bound
+    b.struct.max_tokens = 20                                  # a bound that is lower stays
+    c.read(pool, 0, b, k=bf(2, 2, 64), stream=0)
+    assert library.batch().max_tokens == 20
