@@ -715,16 +715,14 @@ class Batch:
                                   _array(token_start, "token_start", i32, 1, dev), _array(context, "context", i32, 1, dev),
                                   tables.data_ptr(), None if status is None else _array(status, "status", i32, 1, dev))
         self.arrays = (token_start, context, tables, status)          # kept alive
-        self._ref = _ref(self.struct)
 
     def of(self, n_tokens, block_size):
-        """The struct for a call over rows of n_tokens tokens."""
-        self.struct.n_tokens = n_tokens
-        if self.width and self.width * block_size < self.struct.max_tokens:
-            b = BatchStruct.from_buffer_copy(self.struct)
+        """A struct of its own for a call over rows of n_tokens tokens: calls of several threads do not meet in it."""
+        b = BatchStruct.from_buffer_copy(self.struct)
+        b.n_tokens = n_tokens
+        if self.width and self.width * block_size < b.max_tokens:
             b.max_tokens = self.width * block_size
-            return _ref(b)
-        return self._ref
+        return _ref(b)
 
 
 class Cache:

@@ -75,3 +75,15 @@ def test_tables_cut_from_wider_ones_end_with_their_rows(library, width, bound):
     b.struct.max_tokens = 20                                  # a bound that is lower stays
     c.read(pool, 0, b, k=bf(2, 2, 64), stream=0)
     assert library.batch().max_tokens == 20
+
+
+def test_calls_over_one_batch_do_not_share_their_struct(library):
+    """A call of another thread may come while the library still reads this one's (it is called without the interpreter's lock)."""
+    b = kvr.Batch(i32(3), i32(2), i32(2, 8), 4, 100)
+    c, pool = library.cache, library.pool
+    c.append(pool, 0, b, k=bf(5, 2, 64), stream=0)
+    first = library.batch()
+    c.keep(pool, b, i32(2, 1), i32(2), stream=0)
+    c.read(pool, 0, b, k=bf(7, 2, 64), stream=0)
+    assert first.n_tokens == 5 and library.batch().n_tokens == 7 and library.batch() is not first
+    assert b.struct.n_tokens == 0
