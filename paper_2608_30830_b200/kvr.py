@@ -806,7 +806,8 @@ class Cache:
         dev, b = _device(), batch.struct
         if index.shape[0] != b.n_req or count.shape[0] != b.n_req:
             raise ValueError("index and count must have a row for each request")
-        st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(min(b.n_req * b.max_new, 2**31 - 1), self.spec.block_size),
+        n = 2**31 - 1 if b.n_req and b.max_new else 0          # no tensor here has a row for each token
+        st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(n, self.spec.block_size),
                                  _array(index, "index", _torch.int32, 2, dev), index.shape[1],
                                  _array(count, "count", _torch.int32, 1, dev), _stream(stream, dev))
         if st:

@@ -87,3 +87,13 @@ def test_calls_over_one_batch_do_not_share_their_struct(library):
     c.read(pool, 0, b, k=bf(7, 2, 64), stream=0)
     assert first.n_tokens == 5 and library.batch().n_tokens == 7 and library.batch() is not first
     assert b.struct.n_tokens == 0
+
+
+def test_keep_does_not_guess_where_the_rows_end(library):
+    """token_start need not begin at 0: a part of a step's requests has its rows further on."""
+    c, pool = library.cache, library.pool
+    b = kvr.Batch(torch.tensor([100, 104, 108], dtype=torch.int32), i32(2), i32(2, 8), 4, 100)
+    c.keep(pool, b, i32(2, 1), i32(2), stream=0)
+    assert library.batch().n_tokens >= 108
+    c.keep(pool, kvr.Batch(i32(1), i32(0), i32(0, 8), 4, 100), i32(0, 1), i32(0), stream=0)
+    assert library.batch().n_tokens == 0                      # no requests: no tokens either
