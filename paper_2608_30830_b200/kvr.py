@@ -757,8 +757,10 @@ class Cache:
 
     def append(self, pool, layer, batch, q=None, k=None, v=None, q_out=None, rope=None, positions=None, stream=None):
         """kvr_cache_append: write k (turned) and v of the step's tokens into the cache, q turned to q_out."""
-        dev = _device()
-        n = (q if q is not None else k if k is not None else v).shape[0]
+        dev, x = _device(), q if q is not None else k if k is not None else v
+        if x is None:
+            raise ValueError("one of q, k and v is needed")
+        n = x.shape[0]
         if positions is not None and positions.shape[0] != n:
             raise ValueError("positions must have %d entries" % n)
         st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
@@ -770,8 +772,10 @@ class Cache:
 
     def read(self, pool, layer, batch, k=None, v=None, stream=None):
         """kvr_cache_read: the tokens [context, context + new) of each request into k and v."""
-        dev = _device()
-        n = (k if k is not None else v).shape[0]
+        dev, x = _device(), k if k is not None else v
+        if x is None:
+            raise ValueError("k or v is needed")
+        n = x.shape[0]
         st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(k, n, "k", dev),
                                  self._rows(v, n, "v", dev), _stream(stream, dev))
         if st:

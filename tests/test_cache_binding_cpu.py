@@ -97,3 +97,12 @@ def test_keep_does_not_guess_where_the_rows_end(library):
     assert library.batch().n_tokens >= 108
     c.keep(pool, kvr.Batch(i32(1), i32(0), i32(0, 8), 4, 100), i32(0, 1), i32(0), stream=0)
     assert library.batch().n_tokens == 0                      # no requests: no tokens either
+
+
+def test_calls_without_any_tensor_are_refused_as_the_library_refuses_them(library):
+    b = kvr.Batch(i32(3), i32(2), i32(2, 8), 4, 100)
+    for call in (lambda: library.cache.append(library.pool, 0, b, stream=0), lambda: library.cache.read(library.pool, 0, b, stream=0),
+                 lambda: library.cache.append(library.pool, 0, b, q_out=bf(2, 2, 64), stream=0)):
+        with pytest.raises(ValueError):
+            call()
+    assert not library.calls
