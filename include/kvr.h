@@ -651,6 +651,12 @@ kvr_status kvr_test_plan(const kvr_geometry *g, const int64_t *n_tokens, int32_t
 int32_t kvr_test_once(const int32_t *devices, const int32_t *results, int32_t n, int32_t *returned);
 
 /*
+ * How often attention's waits ask before they give up (KVR_DEV_GAVE_UP), for tests; 0: all give up at the first barrier that is
+ * not complete.  Holds for the calls of the whole process from now on; returns what held before.
+ */
+uint32_t kvr_test_attend_polls(uint32_t polls);
+
+/*
  * Placement of the library's own arena (no counterpart in the paper).  Host DRAM is shared between the GPUs of a
  * node; each pool's arena is faulted in by threads bound to the CPUs of the NUMA node its GPU hangs off, so the
  * pages land next to that GPU's link.  kvr_pool_numa_node: the node used (-1: unknown, single-node host, caller's

@@ -1,12 +1,15 @@
 // kvr_cache_attend: argument checks and the choice of kernel.
 #include "kvr_attend.cuh"
 
+#include <atomic>
 #include <cmath>
 
 #include "kvr_once.hpp"
 
 namespace kvr {
 namespace {
+
+std::atomic<unsigned> g_polls{kPolls};
 
 int sm_count() {
   static int counts[64];
@@ -132,6 +135,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   const double most = (double)batch->n_req * (((int64_t)batch->max_new * group + a.row_tile - 1) / a.row_tile) * a.head_groups * (batch->max_tokens / a.unit.d + 1. + a.opening);
   if (most >= INT32_MAX) return fail_cache(KVR_ERR_INVALID_ARG, "n_req, max_new and max_tokens are too large for one call");
   a.ctas = sms;
+  a.polls = g_polls.load(std::memory_order_relaxed);
   a.handed_in = static_cast<int *>(workspace);
   a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + kCounterBytes);
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace) + kCounterBytes + (size_t)kMaxSms * 2 * kPartRows * 8);
@@ -152,3 +156,5 @@ extern "C" int32_t kvr_test_once(const int32_t *devices, const int32_t *results,
   for (int32_t i = 0; i < n; ++i) returned[i] = once(devices[i], [&] { ++runs; return results[i]; });
   return runs;
 }
+
+extern "C" uint32_t kvr_test_attend_polls(uint32_t polls) { return g_polls.exchange(polls); }

@@ -31,6 +31,7 @@ struct AttendArgs {
   int opening;               // what a segment's start weighs, in units: a CTA that begins one gets fewer keys
   int box_rows;              // tokens of a TMA box (tile kernel): 8 or 16, 0: the block size does not allow one
   int ctas;                  // the grid of the main kernel
+  unsigned polls;            // of a barrier, before a wait of the tile kernel gives up; 0: all do at once (tests)
   int *handed_in;            // [2][ctas][2]: pieces of a group, groups of a segment; zero between calls
   float *part_o;             // [ctas][2][group_heads][row_tile][head_dim]; of the tile kernel [ctas][2][head_dim][row_tile]
   float2 *part_ml;           // [ctas][2][group_heads][row_tile]: maximum (log2), sum
@@ -41,6 +42,7 @@ constexpr int kPartRows = 256;
 constexpr int kMaxSms = 160;
 constexpr int kCounterBytes = 4096;
 constexpr int kJoinAtOnce = 16;
+constexpr unsigned kPolls = 1u << 18;
 static_assert(kMaxSms * 4 * 4 <= kCounterBytes, "");
 
 #ifdef __CUDACC__

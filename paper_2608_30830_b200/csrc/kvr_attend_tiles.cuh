@@ -37,7 +37,6 @@ namespace {
 
 constexpr int kTileKeys = 128;
 constexpr int kSoftmax = 256;
-constexpr unsigned kTileSpin = 1u << 18;
 
 // ---- barriers, fences, tensor memory
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -48,13 +47,15 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// A warp's wait, by all of its lanes (95 clocks on a barrier that is complete; one lane's loop with the others waiting for it
-// takes 170).  One that runs out, here or in another role, sets the flag and goes on like one that did not, on whatever is there: all
-// addresses stay in bounds, later waits give up at once, and the roles look at the flag once a step.
-__device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *gave_up) {
+// A warp's wait.  All lanes ask and meet again behind it: what follows are instructions of the whole warp (tcgen05.ld, .mma, .commit) with
+// operands in uniform registers, and a loop that one lane ran while the others waited ahead of them led to wild addresses (it
+// was also slower, 170 clocks on a barrier that is complete against 95).  A wait that runs out (after `polls`), here or in another role,
+// sets the flag and goes on like one that did not, on whatever is there: all addresses stay in bounds, later waits give up at
+// once, and the roles look at the flag once a step.
+__device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned polls) {
   unsigned spin = 0;
   while (!bar_try(bar, parity)) {
-    if (++spin == kTileSpin) *gave_up = 1;
+    if (++spin == polls) *gave_up = 1;
     if ((spin & 15) == 0 && *gave_up) break;
   }
   __syncwarp();
@@ -357,7 +358,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   auto last_tile = [&](const Piece &p) { return min(p.end * unit_tiles, (p.len.keys + kTileKeys - 1) / kTileKeys); };
 
   if (threadIdx.x == 0) {
-    gave_up_word = 0;
+    gave_up_word = a.polls == 0;
     odd_codes = 0;
     for (int i = 0; i < S::kRing; ++i) { bar_init(shared_at(&bars.full[i]), S::kPerStep); bar_init(shared_at(&bars.empty[i]), 1); }
     for (int w = 0; w < 2; ++w) { bar_init(shared_at(&bars.s_full[w]), 1); bar_init(shared_at(&bars.p_full[w]), 4); bar_init(shared_at(&bars.pv_done[w]), 1); }
@@ -454,7 +455,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     };
     bool ok = true;
     auto slot_free = [&](int step) {     // has the buffer's previous tenant been used up?
-      if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up);
+      if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up, a.polls);
       return __any_sync(0xffffffffu, *gave_up != 0) == 0;
     };
     auto mine = [&]() { while (at.more && at.step % S::kSteps != group) at.advance(a, unit_tiles, last); };
@@ -532,7 +533,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         ok = slot_free(at.step);
         copy_wait<0>();
         if (boxes) {
-          bar_wait(shared_at(&bars.raw_full[me]), phase, gave_up);
+          bar_wait(shared_at(&bars.raw_full[me]), phase, gave_up, a.polls);
           ok = __any_sync(0xffffffffu, *gave_up != 0) == 0 && ok;
           phase ^= 1;
         }
@@ -586,7 +587,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     int used[2] = {0, 0}, pieces = 0, slot = 0, round = 0;     // jobs whose product with V is issued; the step's place in the ring
     bool again = true;
     auto take = [&]() {                        // the next step's buffer, when it is full
-      bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up);
+      bar_wait(shared_at(&bars.full[slot]), round & 1, gave_up, a.polls);
       const int s = slot;
       if (++slot == S::kRing) { slot = 0; ++round; }
       return s;
@@ -600,7 +601,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     };
     while (again) {
       const int n = last_tile(piece) - first_tile(piece), head_start = min(kAhead, n);
-      bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up);
+      bar_wait(shared_at(&bars.q_full), pieces & 1, gave_up, a.polls);
       ++pieces;
       for (int t = 0; t < head_start; ++t) {
         const int k_slot = take();
@@ -617,7 +618,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 #pragma unroll 1
         for (int i = 0; i < (TWO ? 2 : 1); ++i) {
           const int w = TWO ? i : t & 1;
-          bar_wait(shared_at(&bars.p_full[w]), (w ? used[1] : used[0]) & 1, gave_up);
+          bar_wait(shared_at(&bars.p_full[w]), (w ? used[1] : used[0]) & 1, gave_up, a.polls);
           tc_after();
 #pragma unroll
           for (int s = 0; s < kTileKeys / 16; ++s)
@@ -635,7 +636,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     }
     // all products have ended before tensor memory is given back
     tc_commit(shared_at(&bars.drained), leader);
-    bar_wait(shared_at(&bars.drained), 0, gave_up);
+    bar_wait(shared_at(&bars.drained), 0, gave_up, a.polls);
   } else if (warp < 8) {
     // ---- softmax: warpgroup w, thread = row
     const int w = warp >> 2, tid = threadIdx.x & 127;
@@ -643,7 +644,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     int jobs = 0, joins = 0, tiles_before = 0, steps_before = 0;
     bool ok = true, again = true;
     // A wait that runs out goes on like one that did not, on whatever is there; the flag is looked at once a tile.
-    auto wait = [&](unsigned long long *bar, unsigned parity) { bar_wait(shared_at(bar), parity, gave_up); };
+    auto wait = [&](unsigned long long *bar, unsigned parity) { bar_wait(shared_at(bar), parity, gave_up, a.polls); };
     // The product of job j with V.  That of job j - 1 has ended when the scores of job j are there, which were issued behind it.
     auto wait_product = [&](int j) { wait(&bars.pv_done[w], j & 1); };
     auto join = [&]() {

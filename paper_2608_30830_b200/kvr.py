@@ -114,7 +114,7 @@ EXPORTS = [
     "kvr_controller_create", "kvr_controller_destroy", "kvr_controller_calibrate", "kvr_controller_suspend",
     "kvr_controller_advance", "kvr_controller_resume", "kvr_controller_get_stats",
     "kvr_cache_geometry", "kvr_rope_frequencies", "kvr_rope_table", "kvr_cache_append", "kvr_cache_read",
-    "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep", "kvr_test_once",
+    "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep", "kvr_test_once", "kvr_test_attend_polls",
 ]
 
 _lib = None
@@ -247,6 +247,8 @@ def lib():
     L.kvr_cache_attend.argtypes = [spec, vp, i32, batch, rows, rows, vp, vp, i32, C.c_float, vp, u64, vp]
     L.kvr_cache_keep.restype = i32
     L.kvr_cache_keep.argtypes = [spec, vp, batch, vp, i32, vp, vp]
+    L.kvr_test_attend_polls.restype = u32
+    L.kvr_test_attend_polls.argtypes = [u32]
     L.kvr_test_once.restype = i32
     L.kvr_test_once.argtypes = [pi32, pi32, i32, pi32]
     _lib = L
