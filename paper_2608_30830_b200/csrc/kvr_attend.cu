@@ -98,7 +98,11 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   if (rows > 16 && padded <= 128) {
     // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
     // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
-    // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels do not fit tensor memory beside their scores.
+    // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels stay with the row kernel: two jobs' sums and scores
+    // would take 768 of tensor memory's 512 columns.  One job of 128 rows would fit (384), but is not built: such rows read the cache once
+    // for every 16 of them (8 requests of 4k, 256 channels, trees of 16 tokens 282 us, of 64 1,039, against 42 and 44 for one reading).
+    // One kernel for the whole call, by its longest request: a chunk of 512 tokens beside 31 single tokens over 4k each takes 188 us, as two
+    // calls 77 + 90 (e4m3 331, 113 + 70).
     a.head_groups = spec->kv_heads;
     a.group_heads = 1;
     a.row_tile = rows <= 128 ? 128 : 256;
@@ -128,7 +132,10 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     }
     slices = warps / a.group_heads;
     const int turn = 16 * slices * chunks_at_once(spec->format, tiles);      // keys that the warps of a head take at a time
-    a.unit = FastDiv((64 + turn - 1) / turn * turn);             // 64 or more: fewer pieces; one request of 333 keys 19 us, with 16 keys 25, with 256 28
+    a.unit = FastDiv((64 + turn - 1) / turn * turn);
+    // 64 or more: fewer pieces.  (us, units of 16 / 64 / 128 / 256 / 512 keys, one token, bf16: 32 requests of 333 tokens 21.4 / 18.5 / 18.8 /
+    // 25.3 / 23.6, 16 of them 25.9 / 15.6 / 15.7 / 18.6 / 15.8.  Of few requests a turn is 128 keys anyway: one of 333 13.8 / 13.5 /
+    // 13.7 / 14.4 / 9.5, of 1,000 15.1 / 15.1 / 15.1 / 15.1 / 16.0.)
   }
   while ((1 << a.row_shift) < a.row_tile) ++a.row_shift;
   // units are numbered in 32 bits; a bound that the lengths on the device keep, whatever they are

@@ -141,13 +141,13 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int 
 }
 #endif
 
-// warps of a CTA of the row kernel: KV heads of a group x slices of the keys
 // chunks of 16 keys that a warp of the row kernel takes at a time (tiles: of 8 rows); a unit holds a multiple of them
 __host__ __device__ constexpr int chunks_at_once(int format, int tiles) { return quantised(format) && tiles == 1 ? 2 : 1; }
+// warps of a CTA of the row kernel: KV heads of a group x slices of the keys
 __host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim == 256 ? 4 : 8; }
 
 // By cache format, one translation unit each (kvr_attend_<format>.cu).  tiles: of the row kernel, query rows of a segment / 8,
-// 1, 2 or 4 (at most 2 above 128 channels); 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment, with its map of
+// 1 or 2; 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment, with its map of
 // the layer's K and V planes.
 cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
 cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);

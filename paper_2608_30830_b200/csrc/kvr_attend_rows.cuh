@@ -11,12 +11,18 @@
 //
 // 8-bit codes become f16 in registers, exactly; k and m indices of the products are assigned to channels so that a
 // lane's fragments are contiguous bytes (16 channels of a key).  A query row is scaled by a power of two into [1, 2)
-// first (exact), so f16 holds all of a bf16 row; K's scale multiplies the score, V's scale the probability.
+// first (exact) and rounded to f16: elements down to 2^-14 of the row's largest keep 11 bits, which is all of a bf16 element, smaller
+// ones an error of 2^-25 of the largest.  (f16 and not bf16, which codes would fit as well: e4m3 is widened to f16 by one instruction,
+// and probabilities keep 11 bits.  tf32 would halve the rate.)  K's scale multiplies the score, V's scale the probability.
+//
+// Probabilities are rounded to the type of V's operand, bf16 or f16, for a product has both of one type.  Against 64 bits outputs of a bf16 cache are then
+// off by 0.0022 (relative, root of the mean square; 32 requests of 8k) where rounding the output alone gives 0.0017; p in two parts would
+// mean the second product twice.
 //
 // Measured, 8 KV heads of 128.  32 requests, median 8k tokens, one token of 4 query heads, bf16: 1.27 GB in 198 us, 6.4 TB/s (DRAM
-// traffic is the algorithm's to 0.1 %): bound by memory.  8 requests of 128k, e4m3: 2.21 GB in 433 us, 5.1 TB/s: half the bytes
-// a key, but each element is widened by the ALU, and two warps a scheduler issue in 46 % of the cycles.  One request
-// of 333 tokens: 13.5 us, the chain of table, K, softmax, V and join.
+// traffic is the algorithm's to 0.1 %): bound by memory.  8 requests of 128k, e4m3: 2.21 GB in 439 to 450 us, 5.0 TB/s: half the
+// bytes a key, but each element is widened by the ALU, and two warps a scheduler issue in 46 % of the cycles (ALU 47 %): neither is
+// full, each warp waits on its own chain.  One request of 333 tokens: 13.5 us, the chain of table, K, softmax, V and join.
 #pragma once
 #include "kvr_attend_common.cuh"
 

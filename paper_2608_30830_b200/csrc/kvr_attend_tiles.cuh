@@ -21,13 +21,18 @@
 // widens them to f16 into the ring, exactly (three pairs of such warps, against three).  Scales multiply scores and probabilities as in
 // the row kernel.
 //
-// Measured, 8 KV heads of 128, 256 rows (TWO), 16 requests of 8k, bf16: 171 us for 581 MB and 144 GFLOP (3.4 TB/s, 840 TFLOP/s; either alone
-// would take 89 us).  A tile of 128 keys takes 2.0 us, in which a warpgroup is busy for 1.3 with its exponentials and waits 0.7
+// Measured, 8 KV heads of 128, 256 rows (TWO), 16 requests of 8k, bf16: 169 to 191 us by the GPU and its clock, for 581 MB and 144 GFLOP
+// (3.4 to 3.0 TB/s, 850 to 755 TFLOP/s; either alone would take 89 us); over an e4m3 cache 303.  In the fast case a tile of 128 keys takes 2.0 us, in which a warpgroup is busy for 1.3 with its exponentials and waits 0.7
 // for its products, whose scores cannot be asked for before the probabilities in the same place are used up.  Around the stream:
 // 7 us until Q is in and the first scores are there, 5 for each epilogue, 12 to 15 for a join.  104 rows of an int8 cache, 2 KV heads, 32
-// requests of 8k: 121 us for 152 MB: 2.5 us a tile, of which a widening warp takes 1.4 for its half of K or V.
+// requests of 8k: 121 to 124 us for 152 MB: 2.5 us a tile, of which a widening warp takes 1.4 for its half of K or V.
 //
-// Every wait is bounded.  One that runs out sets a flag which all roles see, and the kernel ends in the ordinary way (copies
+// Prompts and chunks run here too, but nothing is made for them: each tile of rows streams all keys, those behind its last row
+// included, and past the context every tile is masked and (16 bits) its V looked through.  One prompt of 8k, 32 query heads: 1.8 ms
+// (bf16), 2.3 ms (e4m3), against 0.34 ms for the causal half of the products; 2k over a context of 32k: 1.1 to 1.3 and 1.9 against 0.69.
+//
+// Every wait on a barrier is bounded (the allocation of tensor memory is not: it waits until other kernels on the SM have given theirs
+// back).  One that runs out sets a flag which all roles see, and the kernel ends in the ordinary way (copies
 // drained, products drained, tensor memory freed) with the status word set.
 #pragma once
 #include "kvr_attend_common.cuh"

@@ -2,7 +2,8 @@
 // table), read (the way back), keep (accepted rows of drafted tokens), and the rotary tables.
 //
 // A token's rows are read once and written once, with a few operations an element in between: large calls are bound by memory (read,
-// keep) or by memory and issue alike (append), small ones by the launch and three or four dependent loads.
+// keep, append to a 16-bit cache) or, short of it, by what 16 warps an SM can have under way (append to an 8-bit one), small ones by the
+// launch and three or four dependent loads.
 #include "kvr_cache.cuh"
 
 #include <cmath>
@@ -188,8 +189,9 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
       float y[8];
       if (scale > 1e-30f) {
         // x / scale, rounded once: the product with the correctly rounded reciprocal, corrected by its exact remainder (P. Markstein,
-        // "Computation of elementary functions on the IBM RISC System/6000", 1990), two numbers to an instruction; no step of it
-        // underflows.  The remainder of -0 is +0, hence the sign.
+        // "Computation of elementary functions on the IBM RISC System/6000", 1990), two numbers to an instruction.  (At
+        // scales near 2^-100 the remainder of elements below an eighth of the scale is subnormal: what it loses is 2^-50 in the quotient, whose
+        // last bit is 2^-33 where codes are not 0 any more.)  The remainder of -0 is +0, hence the sign.
         const float back = __frcp_rn(scale);
         const Pair r = pair(back, back), minus = pair(-scale, -scale);
 #pragma unroll
@@ -224,8 +226,9 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
 // neighbouring lane, a scale is a few shuffles, and a lane's angles serve all of its heads.  `per_token` such groups
 // share a token's heads; kAhead heads are loaded before the first is worked on.
 //
-// 32k tokens of 32 query and 8 KV heads of 128 into an e4m3 cache: 734 MB in 159 us, 4.6 TB/s.  Two CTAs an SM (128 registers) issue in
-// half of the cycles; bytes alone would take 112 us.  Fewer heads ahead for more CTAs: 170 us (three), 179 us (four).  A step of 32
+// 32k tokens of 32 query and 8 KV heads of 128 into an e4m3 cache: 734 MB in 156 to 160 us, 4.7 TB/s (int8 165).  Two CTAs an SM (128
+// registers) issue in half of the cycles and DRAM is busy for 54 %: neither is full, the warps wait on their loads; bytes alone would
+// take 112 us.  Into a bf16 cache 797 MB in 140 us, 5.7 TB/s.  Fewer heads ahead for more CTAs: 170 us (three), 179 us (four).  A step of 32
 // tokens takes 5.5 us replayed in a graph (dependent loads: token_start, block table, angles); a call from Python more than that.
 template <int XT, int FMT, int LPH>
 __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_constant__ AppendArgs a) {
