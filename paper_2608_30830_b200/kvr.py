@@ -646,6 +646,13 @@ def _device():
     return (_torch or _use_torch()).cuda.current_device()
 
 
+def _int32(x, what):
+    """x, if the library's 32 bits hold it (ctypes would drop the rest)."""
+    if not -2**31 <= x < 2**31:
+        raise ValueError("%s does not fit 32 bits" % what)
+    return x
+
+
 def _array(t, what, dtype, dims, device):
     """Device pointer of a dense array."""
     if t.dtype is not dtype or t.dim() != dims or not t.is_contiguous() or t.get_device() != device:
@@ -684,8 +691,8 @@ def rope_table(out, first=0, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0,
     dev, shape = _device(), out.shape
     if len(shape) != 3 or shape[2] != 2:
         raise ValueError("out must be [positions, rot_dim / 2, 2]")
-    _check(lib().kvr_rope_table(C.byref(sc), 2 * shape[1], first, shape[0], _array(out, "out", _torch.float32, 3, dev),
-                                _stream(stream, dev)))
+    _check(lib().kvr_rope_table(C.byref(sc), _int32(2 * shape[1], "rot_dim"), _int32(first, "first"), _int32(shape[0], "positions"),
+                                _array(out, "out", _torch.float32, 3, dev), _stream(stream, dev)))
 
 
 class Rope:
@@ -713,7 +720,8 @@ class Batch:
         # The library counts a row's entries by the stride (one request: by the shape).  Rows cut from wider ones have fewer: their width
         # bounds the tokens of a request.
         self.width = shape[1] if n > 1 and shape[1] < stride[0] else 0
-        self.struct = BatchStruct(n, 0, max_new, max_tokens, stride[0] if n > 1 else shape[1],
+        self.struct = BatchStruct(_int32(n, "n_req"), 0, _int32(max_new, "max_new"), _int32(max_tokens, "max_tokens"),
+                                  _int32(stride[0] if n > 1 else shape[1], "the tables' stride"),
                                   _array(token_start, "token_start", i32, 1, dev), _array(context, "context", i32, 1, dev),
                                   tables.data_ptr(), None if status is None else _array(status, "status", i32, 1, dev))
         self.arrays = (token_start, context, tables, status)          # kept alive
@@ -732,6 +740,8 @@ class Cache:
     each call.  Errors raise KvrError, malformed tensors ValueError."""
 
     def __init__(self, layers, kv_heads, head_dim, block_size, num_blocks, fmt="bf16", layout=LAYER_MAJOR):
+        for x, what in ((layers, "layers"), (kv_heads, "kv_heads"), (head_dim, "head_dim"), (block_size, "block_size"), (num_blocks, "num_blocks")):
+            _int32(x, what)
         self.spec = CacheSpec(layers, kv_heads, head_dim, block_size, num_blocks, _FORMATS.get(fmt, fmt), layout)
         g = Geometry()
         _check(lib().kvr_cache_geometry(C.byref(self.spec), C.byref(g)))
@@ -765,7 +775,7 @@ class Cache:
         n = x.shape[0]
         if positions is not None and positions.shape[0] != n:
             raise ValueError("positions must have %d entries" % n)
-        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
+        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), _int32(layer, "layer"), batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
                                    self._rows(k, n, "k", dev), self._rows(v, n, "v", dev), self._rows(q_out, n, "q_out", dev),
                                    None if rope is None else _ref(rope.struct),
                                    None if positions is None else _array(positions, "positions", _torch.int32, 1, dev), _stream(stream, dev))
@@ -778,7 +788,7 @@ class Cache:
         if x is None:
             raise ValueError("k or v is needed")
         n = x.shape[0]
-        st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(k, n, "k", dev),
+        st = _lib.kvr_cache_read(self._spec, self._pool(pool, dev), _int32(layer, "layer"), batch.of(n, self.spec.block_size), self._rows(k, n, "k", dev),
                                  self._rows(v, n, "v", dev), _stream(stream, dev))
         if st:
             _check(st)
@@ -798,7 +808,7 @@ class Cache:
             raise ValueError("mask must be [tokens, words]")
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
-        st = _lib.kvr_cache_attend(self._spec, self._pool(pool, dev), layer, batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
+        st = _lib.kvr_cache_attend(self._spec, self._pool(pool, dev), _int32(layer, "layer"), batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
                                    self._rows(out, n, "out", dev), None if lse is None else _array(lse, "lse", _torch.float32, 2, dev),
                                    None if mask is None else _array(mask, "mask", _torch.int64, 2, dev),
                                    0 if mask is None else mask.shape[1], self._scale if scale is None else scale,

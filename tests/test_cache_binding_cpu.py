@@ -106,3 +106,26 @@ def test_calls_without_any_tensor_are_refused_as_the_library_refuses_them(librar
         with pytest.raises(ValueError):
             call()
     assert not library.calls
+
+
+def test_numbers_beyond_32_bits_are_refused_and_not_wrapped(library, monkeypatch):
+    """A bound of 2^62 for "none" must not become 0, which leaves every request out."""
+    b = kvr.Batch(i32(3), i32(2), i32(2, 8), 2**31 - 1, 2**31 - 1)
+    assert (b.struct.max_new, b.struct.max_tokens) == (2**31 - 1, 2**31 - 1)
+    for max_new, max_tokens in [(4, 1 << 62), (4, 2**32 + 100), (4, 2**31), (1 << 40, 100), (4, -2**31 - 1)]:
+        with pytest.raises(ValueError):
+            kvr.Batch(i32(3), i32(2), i32(2, 8), max_new, max_tokens)
+    with pytest.raises(ValueError):
+        kvr.rope_table(torch.zeros(10, 32, 2), first=2**32, stream=0)
+    for layer in (2**32, -2**32):
+        with pytest.raises(ValueError):
+            library.cache.read(library.pool, layer, b, k=bf(2, 2, 64), stream=0)
+        with pytest.raises(ValueError):
+            library.cache.append(library.pool, layer, b, k=bf(2, 2, 64), stream=0)
+        with pytest.raises(ValueError):
+            library.cache.attend(library.pool, layer, b, bf(2, 4, 64), bf(2, 4, 64), i32(4), stream=0)
+    assert not library.calls
+    monkeypatch.undo()                                        # the library itself: a cache of 2^32 + 8 blocks is not one of 8
+    for wide in (dict(num_blocks=2**32 + 8), dict(layers=2**32 + 1), dict(block_size=2**40 + 16)):
+        with pytest.raises(ValueError):
+            kvr.Cache(**{**dict(layers=1, kv_heads=2, head_dim=64, block_size=16, num_blocks=8), **wide})
