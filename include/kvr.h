@@ -350,14 +350,23 @@ kvr_status kvr_gather_noalloc(const void *device_pool, const kvr_geometry *g, in
  *   INT8 : scale = max(largest |x| * (1/127), 2^-126), code = x / scale rounded to the nearest integer (ties to even)
  * (all in fp32; the constant is rounded to fp32, and a code that this would push past 448 or 127 stays there).
  * A head with an element that is not finite gets scale NaN: all of it reads back as NaN.
+ *
+ * Or 4-bit codes (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), for a request that is 3.2 times smaller than in 16 bits (128
+ * channels).  A token's row is then [kv_heads] records: head_dim / 2 bytes of codes (channel 2i in the low half of byte i), the head's
+ * scale (fp32), a scale for each 16 channels (e4m3), zeros up to a multiple of 16 bytes.  head_dim is a multiple of 32.
+ *   E2M1 : scale = max(largest |x| * (1/2688), 2^-100);   of a group g = its largest |x| * ((1/scale) * (1/6)) rounded to the nearest e4m3
+ *          (at most 448);   code = x * (1 / (g * scale)) rounded to the nearest e2m1 (at most 6), 0 in a group with g = 0
+ * (in fp32, each quotient and product rounded on its own, constants too; roundings to codes and to e4m3 are ties to even).  An element reads back
+ * as code * g * scale.  A head with an element that is not finite gets scale NaN, g and codes 0.  The sign of a g is not read, and a byte 0x7f, which append
+ * does not write, counts as 480.
  */
 enum { KVR_BF16 = 0, KVR_F16 = 1, KVR_F32 = 2 };                                             /* kvr_rows.type */
-enum { KVR_CACHE_BF16 = 0, KVR_CACHE_F16 = 1, KVR_CACHE_E4M3 = 2, KVR_CACHE_INT8 = 3 };     /* kvr_cache_spec.format */
+enum { KVR_CACHE_BF16 = 0, KVR_CACHE_F16 = 1, KVR_CACHE_E4M3 = 2, KVR_CACHE_INT8 = 3, KVR_CACHE_E2M1 = 4 };  /* kvr_cache_spec.format */
 enum { KVR_ROPE_HALF = 0, KVR_ROPE_INTERLEAVED = 1 };                                       /* kvr_rope.style */
 
 typedef struct {
   int32_t layers, kv_heads;
-  int32_t head_dim;          /* multiple of 16, at most 256 */
+  int32_t head_dim;          /* multiple of 16 (E2M1: of 32), at most 256 */
   int32_t block_size, num_blocks;
   int32_t format;            /* KVR_CACHE_* */
   int32_t layout;            /* KVR_LAYER_MAJOR or KVR_BLOCK_MAJOR */
@@ -451,6 +460,20 @@ kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_pool, int32
                             const kvr_rope *rope, const int32_t *positions, void *stream);
 
 /*
+ * The same with positions of several axes (time, height and width of a picture's or a video's tokens): pair p of a head is turned by
+ * table[positions[token * axes + of_pair[p]]][p].  positions: DEVICE int32 [n_tokens][axes], every one inside the table (a token with one
+ * outside is left out: KVR_DEV_BAD_POSITION).  of_pair holds rot_dim / 2 entries below `axes`: runs of pairs for each axis, axes in
+ * turn, or anything else.  rope is needed.
+ */
+typedef struct {
+  int32_t axes;              /* 1 to 4 */
+  uint8_t of_pair[128];
+} kvr_rope_axes;
+kvr_status kvr_cache_append_axes(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch,
+                                 const kvr_rows *q, const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out,
+                                 const kvr_rope *rope, const kvr_rope_axes *axes, const int32_t *positions, void *stream);
+
+/*
  * Read tokens back: row token_start[r] + i of k and v (either may be NULL; any type) becomes logical token context[r] + i
  * of request r, code times scale in fp32, rounded once.  With context 0 and token_start the lengths' sums these are whole requests.
  */
@@ -490,6 +513,39 @@ kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *device_pool,
  */
 kvr_status kvr_cache_keep(const kvr_cache_spec *spec, void *device_pool, const kvr_batch *batch, const int32_t *index,
                           int32_t index_stride, const int32_t *count, void *stream);
+
+/*
+ * Copy blocks, in all layers, K and V: for i < n_pairs the first rows[i] tokens (rows NULL: all) of block pairs[2i] to block
+ * pairs[2i + 1].  pairs, rows: DEVICE int32, read on the device only.  A pair whose source is -1 is passed over, so that a captured graph may
+ * copy fewer than n_pairs.  A pair with an id outside [0, num_blocks) (KVR_DEV_BAD_BLOCK) or with rows outside [0, block_size]
+ * (KVR_DEV_BAD_LENGTH) is left out; status as in kvr_batch.  One block may be the source of many pairs.  The pairs are copied in no order: a
+ * block that is the destination of two pairs, or destination of one and source of another, leaves a mixture (of those blocks' bytes) behind.
+ */
+kvr_status kvr_cache_copy(const kvr_cache_spec *spec, void *device_pool, const int32_t *pairs, const int32_t *rows, int32_t n_pairs,
+                          int32_t *status, void *stream);
+
+/*
+ * Requests that share, grow and shrink, and a pool without holes.  Where these copy rows they enqueue the copies on `stream` (a cudaStream_t
+ * of the pool's device, the one that the caller's kernels write the blocks from; NULL: the default stream), and later moves of this pool are ordered
+ * behind them.  The stream must not be under capture (KVR_ERR_INVALID_ARG).  With KVR_METADATA_ONLY they keep the books alone.
+ *
+ * kvr_request_fork: request new_id begins as the first n_tokens tokens of donor_id (ACTIVE or RETAINED): full blocks are shared, as in
+ * kvr_request_admit_sharing, and the rows of a last block that is not full are copied into a block of its own, so either may go on writing.
+ * A donor whose resume is in flight is waited for.  out_blocks as in kvr_request_admit.
+ *
+ * kvr_request_resize: an ACTIVE request gets n_tokens tokens.  More: blocks from the head of the free queue are added.  Fewer (drafted tokens that
+ * were not accepted): blocks behind the last are let go, in logical order; a last block that is then partly the request's, and that others refer
+ * to, is replaced by a copy of its own.  A resume in flight is waited for.  out_blocks receives the whole table.
+ *   both: KVR_HBM_FULL (nothing changes), KVR_ERR_UNKNOWN_REQUEST, KVR_ERR_BAD_STATE, KVR_ERR_INVALID_ARG
+ *
+ * kvr_pool_compact: while a block that somebody refers to lies above a free one, the highest such block moves to the lowest free one, at most
+ * max_moves times; every table that names it follows, the prefixes of requests on the host too, and it joins the free tail.  moves (HOST, 2 *
+ * max_moves entries, may be NULL) receives (from, to) of each in order, *n_moves their number: tables that the caller keeps are his to rewrite.
+ * Waits for all moves in flight.  Until the copies are through, the caller's kernels have to be on `stream`, or behind it.
+ */
+kvr_status kvr_request_fork(kvr_pool *pool, uint64_t new_id, uint64_t donor_id, int64_t n_tokens, int32_t *out_blocks, int32_t cap, void *stream);
+kvr_status kvr_request_resize(kvr_pool *pool, uint64_t req, int64_t n_tokens, int32_t *out_blocks, int32_t cap, void *stream);
+kvr_status kvr_pool_compact(kvr_pool *pool, int32_t max_moves, int32_t *moves, int32_t *n_moves, void *stream);
 
 /*
  * Observe one request.  Any out pointer may be NULL.  blocks (cap entries) is

@@ -67,6 +67,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     return fail_cache(KVR_ERR_INVALID_ARG, "q and out must have one 16-bit type and the same heads");
   if ((spec->format == KVR_CACHE_BF16 && q->type != KVR_BF16) || (spec->format == KVR_CACHE_F16 && q->type != KVR_F16))
     return fail_cache(KVR_ERR_INVALID_ARG, "q must have the type of a 16-bit cache");
+  if (four_bit(spec->format)) return fail_cache(KVR_ERR_INVALID_ARG, "attention over 4-bit caches is not there yet");
   if (q->heads % spec->kv_heads) return fail_cache(KVR_ERR_INVALID_ARG, "q's heads must be a multiple of kv_heads");
   const int group = q->heads / spec->kv_heads;
   if ((int64_t)batch->max_new * group > (1 << 28)) return fail_cache(KVR_ERR_INVALID_ARG, "too many new tokens in one request");

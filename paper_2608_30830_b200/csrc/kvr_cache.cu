@@ -18,11 +18,14 @@ void set_last_error(const char *msg);
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMaxAxes = 4;
 
 struct RopeView {
   const float *table;
   int positions, rot, style;
   float sign;                // of the sine: -1 turns back
+  int axes;                  // positions of a token
+  uint16_t axis_of[16];      // the axes of pairs 8 i .. 8 i + 7, two bits each
 };
 
 struct AppendArgs {
@@ -82,24 +85,44 @@ struct Raw8 {
   }
 };
 
-// The angles of 8 channels d0 .. d0 + 7 at one position, and the turn by them.  Products and sums are rounded one by
+// The angles of 8 channels d0 .. d0 + 7 at one position (AXES: at the positions of their pairs' axes), and the turn by them.  Products and sums are rounded one by
 // one, so the result does not depend on what a compiler contracts.
 //   rot % 16 == 0, halves: partners are whole lanes; 8 (cos, sin)
 //   rot % 16 == 0, interleaved: partners are the lane's own; 4 (cos, sin)
 //   other rot: partners are read again, angles where they are used
-template <int XT>
+template <int XT, bool AXES>
 struct Angles {
   const RopeView &rp;
-  const float *row;          // (cos, sin) of this position
+  const float *row;          // (cos, sin) of this position; AXES: of position 0
+  const int *where;          // AXES: the token's positions
   Pair c[4], s[4];           // halves: the sine's sign is the channel's side
-  __device__ __forceinline__ Angles(const RopeView &rope, int position, int d0) : rp(rope), row(nullptr) {
+  __device__ __forceinline__ Angles(const RopeView &rope, const int *position, int d0) : rp(rope), row(nullptr), where(position) {
     if (!rp.table) return;
-    row = rp.table + (long long)position * rp.rot;
+    row = rp.table + (AXES ? 0ll : (long long)*position * rp.rot);
     const bool low = d0 < (rp.rot >> 1);
     if ((rp.rot & 15) || d0 >= rp.rot) return;
     const bool halves = rp.style == KVR_ROPE_HALF;
-    const float4 *t = reinterpret_cast<const float4 *>(row + (!halves ? d0 : 2 * (low ? d0 : d0 - (rp.rot >> 1))));
+    const int pair0 = !halves ? d0 >> 1 : low ? d0 : d0 - (rp.rot >> 1);       // the lane's first pair, a multiple of 4 or 8
     const float sign = halves && low ? -rp.sign : rp.sign;
+    const float *from = row + 2 * pair0;
+    if constexpr (AXES) {
+      const unsigned axes = rp.axis_of[pair0 >> 3] >> (pair0 & 7) * 2 & (halves ? 0xffffu : 0xffu), one = axes & 3;
+      if (axes != one * (halves ? 0x5555u : 0x55u)) {        // pair by pair; else the lane's pairs lie side by side
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i >= 2 && !halves) break;
+          float2 x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            x[e] = __ldg(reinterpret_cast<const float2 *>(from + (long long)where[axes >> (4 * i + 2 * e) & 3] * rp.rot) + 2 * i + e);
+          c[i] = pair(x[0].x, x[1].x);
+          s[i] = pair(x[0].y * sign, x[1].y * sign);
+        }
+        return;
+      }
+      from += (long long)where[one] * rp.rot;
+    }
+    const float4 *t = reinterpret_cast<const float4 *>(from);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i >= 2 && !halves) break;
@@ -160,7 +183,9 @@ struct Angles {
       if (d >= rp.rot) continue;
       const bool first = rp.style == KVR_ROPE_INTERLEAVED ? (d & 1) == 0 : d < half;
       const int p = rp.style == KVR_ROPE_INTERLEAVED ? d >> 1 : first ? d : d - half;
-      const float2 t = __ldg(reinterpret_cast<const float2 *>(row) + p);
+      const float *from = row;
+      if constexpr (AXES) from += (long long)where[rp.axis_of[p >> 3] >> (p & 7) * 2 & 3] * rp.rot;
+      const float2 t = __ldg(reinterpret_cast<const float2 *>(from) + p);
       const float sn = t.y * rp.sign;
       x[i] = first ? __fsub_rn(__fmul_rn(x[i], t.x), __fmul_rn(y[i], sn)) : __fadd_rn(__fmul_rn(y[i], sn), __fmul_rn(x[i], t.x));
     }
@@ -173,6 +198,37 @@ template <int FMT, int LPH>
 __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_offset, int head, int head_dim, int d0, bool live) {
   if constexpr (!quantised(FMT)) {
     if (live) store8<FMT == KVR_CACHE_BF16 ? KVR_BF16 : KVR_F16>(row + ((long long)head * head_dim + d0) * 2, x);
+  } else if constexpr (four_bit(FMT)) {
+    // Two lanes hold a group.  Reciprocals and products are rounded one by one, as the header has them.
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    if (!live) top = 0;
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1, LPH));
+    unsigned most = top;
+#pragma unroll
+    for (int m = 2; m < LPH; m <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, m, LPH));
+    const bool finite = most < 0x7f800000u;
+    const float scale = finite ? fmaxf(__fmul_rn(__uint_as_float(most), 1.f / 2688.f), 7.8886091e-31f) : __uint_as_float(0x7fc00000u);
+    const float largest = __fmul_rn(__uint_as_float(top), __fmul_rn(__frcp_rn(scale), 1.f / 6.f));
+    const unsigned byte = finite ? __nv_cvt_float_to_fp8(largest, __NV_SATFINITE, __NV_E4M3) : 0u;
+    const float step = __fmul_rn(__half2float(__ushort_as_half((unsigned short)group_scale(byte))) * kGroupUnit, scale);
+    const float back = byte ? __frcp_rn(step) : 0.f;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(x[i], back);
+    const unsigned codes = finite ? narrow_e2m1(y) : 0u;
+    // the scales, 8 lanes' (4 groups') to a word, then a word to a lane: the head's scale, the groups', zeros
+    const int lane = d0 >> 3;
+    unsigned word = lane & 1 ? 0u : byte << ((lane & 6) * 4);
+    word |= __shfl_xor_sync(0xffffffffu, word, 2, LPH);
+    word |= __shfl_xor_sync(0xffffffffu, word, 4, LPH);
+    const unsigned groups = __shfl_sync(0xffffffffu, word, (lane - 1) * 8, LPH);
+    if (!live) return;
+    char *record = row + (long long)head * record_bytes(head_dim);
+    *reinterpret_cast<unsigned *>(record + (d0 >> 1)) = codes;
+    if (lane * 4 < record_bytes(head_dim) - head_dim / 2)
+      *reinterpret_cast<unsigned *>(record + head_dim / 2 + lane * 4) = lane == 0 ? __float_as_uint(scale) : lane <= LPH / 8 ? groups : 0u;
   } else {
     unsigned top = 0;
 #pragma unroll
@@ -230,10 +286,11 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
 // registers) issue in half of the cycles and DRAM is busy for 54 %: neither is full, the warps wait on their loads; bytes alone would
 // take 112 us.  Into a bf16 cache 797 MB in 140 us, 5.7 TB/s.  Fewer heads ahead for more CTAs: 170 us (three), 179 us (four).  A step of 32
 // tokens takes 5.5 us replayed in a graph (dependent loads: token_start, block table, angles); a call from Python more than that.
-template <int XT, int FMT, int LPH>
+template <int XT, int FMT, int LPH, bool AXES>
 __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kGroups = kThreads / LPH, kSize = XT == KVR_F32 ? 4 : 2, kAhead = XT == KVR_F32 ? 2 : 4;
   __shared__ TokenAt at[kGroups];
+  __shared__ int places[AXES ? kGroups : 1][kMaxAxes];
   const int per_token = a.per_token, tokens = kGroups / per_token, first = blockIdx.x * tokens;
   const int group = threadIdx.x / LPH, d0 = (threadIdx.x % LPH) * 8;
   const int sub = group % per_token, token = first + group / per_token;
@@ -261,8 +318,19 @@ __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_consta
     if (first + (int)threadIdx.x < a.b.n_tokens) {
       t = locate_token(a.b, a.c, a.bs, first + threadIdx.x);
       if (t.position >= 0 && a.rope.table) {
-        if (a.positions) t.position = __ldg(a.positions + first + threadIdx.x);
-        if ((unsigned)t.position >= (unsigned)a.rope.positions) {
+        bool known = true;
+        if constexpr (AXES) {
+#pragma unroll
+          for (int x = 0; x < kMaxAxes; ++x) {
+            const int place = x < a.rope.axes ? __ldg(a.positions + (long long)(first + threadIdx.x) * a.rope.axes + x) : 0;
+            known = known && (unsigned)place < (unsigned)a.rope.positions;
+            places[threadIdx.x][x] = place;
+          }
+        } else {
+          if (a.positions) t.position = __ldg(a.positions + first + threadIdx.x);
+          known = (unsigned)t.position < (unsigned)a.rope.positions;
+        }
+        if (!known) {
           report(a.b.status, KVR_DEV_BAD_POSITION);
           t.position = -1;
         }
@@ -273,7 +341,8 @@ __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_consta
   __syncthreads();
   const TokenAt t = at[group / per_token];
   const bool lane_live = t.position >= 0 && d0 < a.c.head_dim;
-  const Angles<XT> angles(a.rope, lane_live ? t.position : 0, lane_live ? d0 : a.rope.rot);
+  const int zero = 0;
+  const Angles<XT, AXES> angles(a.rope, AXES ? places[AXES ? group / per_token : 0] : lane_live ? &t.position : &zero, lane_live ? d0 : a.rope.rot);
 
   while (part < 3) {
     const int now = part, at0 = h0;
@@ -354,6 +423,11 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
       const char *row = a.c.base + (is_v ? a.c.v_offset : 0) + offset;
       if constexpr (!quantised(FMT)) {
         raw[i] = *reinterpret_cast<const uint4 *>(row + ((long long)head * a.c.head_dim + d0) * 2);
+      } else if constexpr (four_bit(FMT)) {
+        const char *record = row + (long long)head * a.c.head_bytes;
+        raw[i].x = *reinterpret_cast<const unsigned *>(record + (d0 >> 1));
+        raw[i].y = *reinterpret_cast<const unsigned char *>(record + a.c.scale_offset + 4 + (d0 >> 4));
+        scale[i] = *reinterpret_cast<const float *>(record + a.c.scale_offset);
       } else {
         const uint2 w = *reinterpret_cast<const uint2 *>(row + (long long)head * a.c.head_dim + d0);
         raw[i].x = w.x; raw[i].y = w.y;
@@ -369,6 +443,12 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
       float x[8];
       if constexpr (!quantised(FMT)) {
         widen8<FMT == KVR_CACHE_BF16 ? KVR_BF16 : KVR_F16>(raw[i], x);
+      } else if constexpr (four_bit(FMT)) {
+        const float group = __half2float(__ushort_as_half((unsigned short)group_scale(raw[i].y))) * kGroupUnit;
+        const unsigned w[4] = {widen_e2m1<0>(raw[i].x), widen_e2m1<1>(raw[i].x), widen_e2m1<2>(raw[i].x), widen_e2m1<3>(raw[i].x)};
+        widen8<KVR_F16>(make_uint4(w[0], w[1], w[2], w[3]), x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * group * scale[i];        // code times group is exact
       } else {
         const unsigned u[2] = {raw[i].x, raw[i].y};
 #pragma unroll
@@ -488,11 +568,16 @@ int groups_per_token(int n_tokens, int heads, int groups) {
   return g;
 }
 
+template <int XT, int FMT, bool AXES>
+void launch_append(const AppendArgs &a, int lanes, int grid, cudaStream_t s) {
+  if (lanes == 8) append_kernel<XT, FMT, 8, AXES><<<grid, kThreads, 0, s>>>(a);
+  else if (lanes == 16) append_kernel<XT, FMT, 16, AXES><<<grid, kThreads, 0, s>>>(a);
+  else append_kernel<XT, FMT, 32, AXES><<<grid, kThreads, 0, s>>>(a);
+}
 template <int XT, int FMT>
 void launch_append(const AppendArgs &a, int lanes, int grid, cudaStream_t s) {
-  if (lanes == 8) append_kernel<XT, FMT, 8><<<grid, kThreads, 0, s>>>(a);
-  else if (lanes == 16) append_kernel<XT, FMT, 16><<<grid, kThreads, 0, s>>>(a);
-  else append_kernel<XT, FMT, 32><<<grid, kThreads, 0, s>>>(a);
+  if (a.rope.axes > 1) launch_append<XT, FMT, true>(a, lanes, grid, s);
+  else launch_append<XT, FMT, false>(a, lanes, grid, s);
 }
 template <int XT>
 void launch_append(const AppendArgs &a, int format, int lanes, int grid, cudaStream_t s) {
@@ -500,6 +585,7 @@ void launch_append(const AppendArgs &a, int format, int lanes, int grid, cudaStr
     case KVR_CACHE_BF16: return launch_append<XT, KVR_CACHE_BF16>(a, lanes, grid, s);
     case KVR_CACHE_F16: return launch_append<XT, KVR_CACHE_F16>(a, lanes, grid, s);
     case KVR_CACHE_E4M3: return launch_append<XT, KVR_CACHE_E4M3>(a, lanes, grid, s);
+    case KVR_CACHE_E2M1: return launch_append<XT, KVR_CACHE_E2M1>(a, lanes, grid, s);
     default: return launch_append<XT, KVR_CACHE_INT8>(a, lanes, grid, s);
   }
 }
@@ -516,6 +602,7 @@ void launch_read(const ReadArgs &a, int format, int lanes, int grid, cudaStream_
     case KVR_CACHE_BF16: return launch_read<KVR_CACHE_BF16, OT>(a, lanes, grid, s);
     case KVR_CACHE_F16: return launch_read<KVR_CACHE_F16, OT>(a, lanes, grid, s);
     case KVR_CACHE_E4M3: return launch_read<KVR_CACHE_E4M3, OT>(a, lanes, grid, s);
+    case KVR_CACHE_E2M1: return launch_read<KVR_CACHE_E2M1, OT>(a, lanes, grid, s);
     default: return launch_read<KVR_CACHE_INT8, OT>(a, lanes, grid, s);
   }
 }
@@ -528,6 +615,7 @@ kvr_status launched() {
 }
 
 int64_t row_bytes_of(const kvr_cache_spec *s) {
+  if (four_bit(s->format)) return (int64_t)s->kv_heads * record_bytes(s->head_dim);
   const int64_t elements = (int64_t)s->kv_heads * s->head_dim;
   return quantised(s->format) ? elements + (4ll * s->kv_heads + 15) / 16 * 16 : 2 * elements;
 }
@@ -541,7 +629,8 @@ kvr_status check_spec(const kvr_cache_spec *s) {
   if (s->layers < 1 || s->kv_heads < 1 || s->block_size < 1 || s->num_blocks < 1)
     return fail_cache(KVR_ERR_GEOMETRY, "layers, kv_heads, block_size and num_blocks must be at least 1");
   if (s->head_dim < 16 || s->head_dim > 256 || s->head_dim % 16) return fail_cache(KVR_ERR_GEOMETRY, "head_dim must be a multiple of 16, at most 256");
-  if (s->format < KVR_CACHE_BF16 || s->format > KVR_CACHE_INT8) return fail_cache(KVR_ERR_INVALID_ARG, "unknown cache format");
+  if (s->format < KVR_CACHE_BF16 || s->format > KVR_CACHE_E2M1) return fail_cache(KVR_ERR_INVALID_ARG, "unknown cache format");
+  if (four_bit(s->format) && s->head_dim % 32) return fail_cache(KVR_ERR_GEOMETRY, "head_dim of a 4-bit cache must be a multiple of 32");
   if (s->layout != KVR_LAYER_MAJOR && s->layout != KVR_BLOCK_MAJOR) return fail_cache(KVR_ERR_INVALID_ARG, "unknown layout");
   if (row_bytes_of(s) > (1ll << 30) || row_bytes_of(s) * s->block_size > (1ll << 30)) return fail_cache(KVR_ERR_GEOMETRY, "one tile exceeds 1 GiB");
   return KVR_OK;
@@ -595,7 +684,8 @@ kvr_status layer_view(const kvr_cache_spec *s, const void *pool, int layer, Cach
   out->v_offset = plane;
   out->base = static_cast<char *>(const_cast<void *>(pool)) + 2ll * layer * plane;
   out->row_bytes = (int)row;
-  out->scale_offset = s->kv_heads * s->head_dim;
+  out->scale_offset = four_bit(s->format) ? s->head_dim / 2 : s->kv_heads * s->head_dim;
+  out->head_bytes = four_bit(s->format) ? record_bytes(s->head_dim) : s->head_dim * (quantised(s->format) ? 1 : 2);
   out->block_size = s->block_size;
   out->num_blocks = s->num_blocks;
   out->kv_heads = s->kv_heads;
@@ -678,9 +768,9 @@ extern "C" kvr_status kvr_rope_table(const kvr_rope_scaling *s, int32_t rot_dim,
   return launched();
 }
 
-extern "C" kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch,
-                                       const kvr_rows *q, const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out,
-                                       const kvr_rope *rope, const int32_t *positions, void *stream) {
+static kvr_status append(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch, const kvr_rows *q,
+                         const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out, const kvr_rope *rope, const kvr_rope_axes *axes,
+                         const int32_t *positions, void *stream) {
   AppendArgs a{};
   if (kvr_status st = layer_view(spec, device_pool, layer, &a.c)) return st;
   if (kvr_status st = check_batch(batch)) return st;
@@ -706,7 +796,17 @@ extern "C" kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_
     if (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > spec->head_dim) return fail_cache(KVR_ERR_INVALID_ARG, "rope: rot_dim must be even and at most head_dim");
     if (rope->positions < 1) return fail_cache(KVR_ERR_INVALID_ARG, "rope: an empty table");
     if (rope->style != KVR_ROPE_HALF && rope->style != KVR_ROPE_INTERLEAVED) return fail_cache(KVR_ERR_INVALID_ARG, "rope: unknown style");
-    a.rope = RopeView{rope->table, rope->positions, rope->rot_dim, rope->style, rope->inverse ? -1.f : 1.f};
+    a.rope = RopeView{rope->table, rope->positions, rope->rot_dim, rope->style, rope->inverse ? -1.f : 1.f, 1, {}};
+  }
+  if (axes) {
+    if (!rope) return fail_cache(KVR_ERR_INVALID_ARG, "axes without rope");
+    if (axes->axes < 1 || axes->axes > kMaxAxes) return fail_cache(KVR_ERR_INVALID_ARG, "axes: 1 to 4 of them");
+    if (!positions) return fail_cache(KVR_ERR_INVALID_ARG, "axes: positions are needed");
+    a.rope.axes = axes->axes;
+    for (int p = 0; p < rope->rot_dim / 2; ++p) {
+      if (axes->of_pair[p] >= axes->axes) return fail_cache(KVR_ERR_INVALID_ARG, "axes: a pair's axis is out of range");
+      a.rope.axis_of[p >> 3] |= (uint16_t)(axes->of_pair[p] << (p & 7) * 2);
+    }
   }
   if (positions && ((uintptr_t)positions & 3)) return fail_cache(KVR_ERR_INVALID_ARG, "positions must be 4-byte aligned");
   if (batch->n_tokens == 0) return KVR_OK;
@@ -725,6 +825,19 @@ extern "C" kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_
   else if (type == KVR_F16) launch_append<KVR_F16>(a, spec->format, lanes, grid, s);
   else launch_append<KVR_F32>(a, spec->format, lanes, grid, s);
   return launched();
+}
+
+extern "C" kvr_status kvr_cache_append(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch,
+                                       const kvr_rows *q, const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out,
+                                       const kvr_rope *rope, const int32_t *positions, void *stream) {
+  return append(spec, device_pool, layer, batch, q, k, v, q_out, rope, nullptr, positions, stream);
+}
+
+extern "C" kvr_status kvr_cache_append_axes(const kvr_cache_spec *spec, void *device_pool, int32_t layer, const kvr_batch *batch,
+                                            const kvr_rows *q, const kvr_rows *k, const kvr_rows *v, const kvr_rows *q_out,
+                                            const kvr_rope *rope, const kvr_rope_axes *axes, const int32_t *positions, void *stream) {
+  if (!axes) return fail_cache(KVR_ERR_INVALID_ARG, "axes is NULL");
+  return append(spec, device_pool, layer, batch, q, k, v, q_out, rope, axes, positions, stream);
 }
 
 extern "C" kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, int32_t layer, const kvr_batch *batch,

@@ -24,7 +24,8 @@ struct CacheView {
   char *base;                // K plane of the layer
   long long v_offset;        // from a K plane to its V plane
   long long block_stride;    // from one block to the next within a plane
-  int row_bytes, scale_offset;   // of a token's row; the scales lie behind the codes (quantised formats)
+  int row_bytes, scale_offset;   // of a token's row; the scales lie behind the codes (8-bit: of all heads; 4-bit: of a head)
+  int head_bytes;            // from one head's elements to the next's
   int block_size, num_blocks;
   int kv_heads, head_dim;
 };
@@ -139,6 +140,29 @@ __device__ __forceinline__ unsigned pack_f16(float lo, float hi) {
   return *reinterpret_cast<const unsigned *>(&v);
 }
 
+// Byte BYTE of w, two e2m1 codes, as f16: exact.
+template <int BYTE>
+__device__ __forceinline__ unsigned widen_e2m1(unsigned w) {
+  unsigned r;
+  if constexpr (BYTE == 0) asm("{.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 1) asm("{.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 2) asm("{.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;}" : "=r"(r) : "r"(w));
+  else asm("{.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, d;}" : "=r"(r) : "r"(w));
+  return r;
+}
+// 8 numbers as codes: to the nearest, ties to even, at most 6.
+__device__ __forceinline__ unsigned narrow_e2m1(const float (&y)[8]) {
+  unsigned r;
+  asm("{.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};}"
+      : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return r;
+}
+// The scale of a group of 16 channels by its byte, times 2^-8 (as f16, exact): the fields of an e4m3 number 7 places up lie where f16
+// has them.  The sign is not read, and 0x7f is 480: there is no NaN among these.
+constexpr float kGroupUnit = 256.f;
+__device__ __forceinline__ unsigned group_scale(unsigned byte) { return (byte & 0x7fu) << 7; }
+
 template <int TYPE>
 __device__ __forceinline__ void store8(char *p, const float (&x)[8]) {
   if constexpr (TYPE == KVR_F32) {
@@ -153,7 +177,10 @@ __device__ __forceinline__ void store8(char *p, const float (&x)[8]) {
 }
 #endif  // __CUDACC__
 
-__host__ __device__ constexpr bool quantised(int format) { return format == KVR_CACHE_E4M3 || format == KVR_CACHE_INT8; }
+__host__ __device__ constexpr bool quantised(int format) { return format >= KVR_CACHE_E4M3; }     // codes with scales
+__host__ __device__ constexpr bool four_bit(int format) { return format == KVR_CACHE_E2M1; }
+// A head's record in a 4-bit row: codes, the head's scale, a scale for each 16 channels, zeros up to a multiple of 16 bytes.
+__host__ __device__ constexpr int record_bytes(int head_dim) { return (head_dim / 2 + 4 + head_dim / 16 + 15) / 16 * 16; }
 
 // host side (kvr_cache.cu): argument checks with a message, shared by the entries
 kvr_status fail_cache(kvr_status st, const char *msg);

@@ -1,6 +1,7 @@
 // C ABI of the KV retention mover: argument checks and bookkeeping of every entry point.  Each batch call settles
 // the bookkeeping at once (states, block tables, arena offsets: the same answers a synchronous implementation
 // gives) and hands the byte movement to the transfer engine (kvr_engine.cu), which queues it on the streams.
+#include "kvr_pages.cuh"
 #include "kvr_pool.hpp"
 
 using namespace kvr;
@@ -111,6 +112,41 @@ kvr_status admit_common(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_
   // the caller will write the new blocks from its own stream: let any gather still reading them finish
   if (tag && !p->meta_only) return wait_unlocked(p, lock, tag, true, 60000);
   return KVR_OK;
+}
+
+// A stream that copies may be enqueued on.
+kvr_status check_copy_stream(kvr_pool *p, cudaStream_t s) {
+  if (p->meta_only) return KVR_OK;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (const cudaError_t e = cudaStreamIsCapturing(s, &capture)) {
+    cudaGetLastError();              // reported here, not by the next launch
+    return fail(KVR_ERR_CUDA, "cudaStreamIsCapturing: %s", cudaGetErrorString(e));
+  }
+  return capture == cudaStreamCaptureStatusNone ? KVR_OK : fail(KVR_ERR_INVALID_ARG, "the stream is under capture");
+}
+
+// Enqueues copies of `rows` rows on the caller's stream (behind the gather `tag`, which may still read a destination), and orders the pool's
+// own streams behind what that stream holds by then.  On failure nothing of it is left in the stream.
+kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag) {
+  const PoolView view{p->d_pool, p->plane_stride, p->block_stride, p->planes, p->NB, p->BS, p->row};
+  cudaEvent_t reached = nullptr;
+  try {
+    p->event_pool.reserve(p->event_pool.size() + 1);         // nothing below allocates on the host
+  } catch (const std::bad_alloc &) {
+    return fail(KVR_ERR_NOMEM, "out of host memory");
+  }
+  auto run = [&]() -> kvr_status {
+    if (kvr_status st = get_event(p, &reached)) return st;
+    if (kvr_status st = stream_after(p, s, tag, true)) return st;
+    CUP(p, copy_blocks(view, pairs.data(), (int)pairs.size(), rows, s));
+    CUP(p, cudaEventRecord(reached, s));
+    for (cudaStream_t own : {p->s_gather, p->s_d2h, p->s_h2d, p->s_scatter}) CUP(p, cudaStreamWaitEvent(own, reached, 0));
+    return KVR_OK;
+  };
+  const kvr_status st = run();
+  if (st != KVR_OK) cudaStreamSynchronize(s);
+  put_event(p, reached);
+  return st;
 }
 
 }  // namespace
@@ -313,6 +349,148 @@ kvr_status kvr_request_release(kvr_pool *p, uint64_t id) {
     if (r.state != KVR_EXPIRED) drop_all_blocks(p, r);
     p->reqs.erase(it);
     return KVR_OK;
+  }
+}
+
+kvr_status kvr_request_fork(kvr_pool *p, uint64_t id, uint64_t donor_id, int64_t n_tokens, int32_t *out_blocks, int32_t cap, void *stream) {
+  if (kvr_status s = check_pool(p)) return s;
+  Enter enter(p);
+  if (n_tokens < 0) return fail(KVR_ERR_INVALID_ARG, "n_tokens < 0");
+  if (donor_id == id) return fail(KVR_ERR_INVALID_ARG, "a request cannot be forked from itself");
+  if (kvr_status s = check_copy_stream(p, (cudaStream_t)stream)) return s;
+  for (;;) {
+    auto d = p->reqs.find(donor_id);
+    if (d == p->reqs.end()) return fail(KVR_ERR_UNKNOWN_REQUEST, "unknown donor");
+    if (d->second.state != KVR_ACTIVE && d->second.state != KVR_RETAINED) return fail(KVR_ERR_BAD_STATE, "the donor holds no blocks");
+    if (!d->second.pending_op) break;
+    if (kvr_status s = wait_unlocked(p, enter.lock, d->second.pending_op, false, 60000)) return s;
+  }
+  const Request &donor = p->reqs.find(donor_id)->second;
+  if (n_tokens > donor.n_tokens) return fail(KVR_ERR_INVALID_ARG, "the donor has %lld tokens", (long long)donor.n_tokens);
+  auto it = p->reqs.find(id);
+  const bool existed = it != p->reqs.end();
+  if (existed && it->second.state != KVR_EXPIRED) return fail(KVR_ERR_BAD_STATE, "request exists");
+  const int32_t full = (int32_t)(n_tokens / p->BS), part = (int32_t)(n_tokens % p->BS), nb = full + (part > 0);
+  if (out_blocks && cap < nb) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
+  if (nb - full > p->fq.size()) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
+  try {
+    std::vector<int32_t> table(donor.blocks.begin(), donor.blocks.begin() + nb);
+    std::vector<int2> pairs;
+    uint64_t tag = 0;
+    if (part) {
+      pairs.push_back(make_int2(table[full], 0));
+      if (!existed) p->reqs[id].state = KVR_EXPIRED;         // the node is there before anything is taken
+      tag = p->fq.pop(1, &table[full]);
+      pairs[0].y = table[full];
+      const kvr_status s = p->meta_only ? KVR_OK : enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag);
+      if (s != KVR_OK) {
+        p->fq.unpop(&table[full], 1);
+        if (!existed) p->reqs.erase(id);
+        return s;
+      }
+    }
+    Request &r = p->reqs[id];
+    r = Request();
+    r.state = KVR_ACTIVE; r.n_tokens = n_tokens; r.nb = nb; r.n_shared = full;
+    r.image_bytes = (uint64_t)part * p->bpt;
+    r.blocks.swap(table);
+    for (int32_t i = 0; i < full; ++i) p->fq.add_ref(r.blocks[i]);
+    if (out_blocks && nb) memcpy(out_blocks, r.blocks.data(), (size_t)nb * 4);
+    // safe to write when the call returns, from any stream, but for what this one still copies
+    if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);
+    return KVR_OK;
+  } catch (const std::bad_alloc &) {
+    return fail(KVR_ERR_NOMEM, "out of host memory");
+  }
+}
+
+kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_t *out_blocks, int32_t cap, void *stream) {
+  if (kvr_status s = check_pool(p)) return s;
+  Enter enter(p);
+  if (n_tokens < 0) return fail(KVR_ERR_INVALID_ARG, "n_tokens < 0");
+  const int64_t blocks = (n_tokens + p->BS - 1) / p->BS;
+  if (out_blocks && cap < blocks) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
+  if (kvr_status s = check_copy_stream(p, (cudaStream_t)stream)) return s;
+  for (;;) {
+    auto it = p->reqs.find(id);
+    if (it == p->reqs.end()) return fail(KVR_ERR_UNKNOWN_REQUEST, "unknown request");
+    if (it->second.state != KVR_ACTIVE) return fail(KVR_ERR_BAD_STATE, "request is not active");
+    if (!it->second.pending_op) break;
+    if (kvr_status s = wait_unlocked(p, enter.lock, it->second.pending_op, false, 60000)) return s;
+  }
+  Request &r = p->reqs.find(id)->second;
+  if (blocks - r.nb > p->fq.size()) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
+  const int32_t nb = (int32_t)blocks, part = (int32_t)(n_tokens % p->BS);
+  uint64_t tag = 0;
+  try {
+    if (nb > r.nb) {
+      r.blocks.resize((size_t)nb);
+      tag = p->fq.pop(nb - r.nb, r.blocks.data() + r.nb);
+    } else {
+      // A last block that others refer to must not be written on: its rows go to a block of the free queue, or to one that this call lets go.
+      std::vector<int2> pairs;
+      int32_t own = -1;
+      bool popped = false;
+      if (part && p->fq.refs(r.blocks[nb - 1]) > 1) {
+        pairs.reserve(1);
+        popped = p->fq.size() > 0;
+        if (popped) tag = p->fq.pop(1, &own);
+        else for (int32_t i = nb; i < r.nb && own < 0; ++i) if (p->fq.refs(r.blocks[i]) == 1) own = r.blocks[i];
+        if (own < 0) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
+        pairs.push_back(make_int2(r.blocks[nb - 1], own));
+      }
+      if (!p->meta_only && (nb < r.nb || own >= 0)) {        // blocks change hands: later moves come behind the caller's work on them
+        if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag)) {
+          if (popped) p->fq.unpop(&own, 1);
+          return s;
+        }
+      }
+      if (own >= 0) {
+        if (!popped) p->fq.add_ref(own);                     // stays, while the tail goes
+        p->fq.drop_ref(r.blocks[nb - 1]);
+        r.blocks[nb - 1] = own;
+      }
+      unref(p, r, nb, r.nb);
+      r.blocks.resize((size_t)nb);
+    }
+  } catch (const std::bad_alloc &) {
+    return fail(KVR_ERR_NOMEM, "out of host memory");
+  }
+  r.nb = nb; r.n_tokens = n_tokens;
+  r.n_shared = std::min(r.n_shared, (int32_t)(n_tokens / p->BS));
+  r.image_bytes = (uint64_t)private_tokens(p, r) * p->bpt;
+  if (out_blocks && nb) memcpy(out_blocks, r.blocks.data(), (size_t)nb * 4);
+  if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);       // a gather may still be reading the added blocks
+  return KVR_OK;
+}
+
+kvr_status kvr_pool_compact(kvr_pool *p, int32_t max_moves, int32_t *moves, int32_t *n_moves, void *stream) {
+  if (kvr_status s = check_pool(p)) return s;
+  Enter enter(p);
+  if (n_moves) *n_moves = 0;
+  if (max_moves < 0) return fail(KVR_ERR_INVALID_ARG, "max_moves < 0");
+  if (kvr_status s = check_copy_stream(p, (cudaStream_t)stream)) return s;
+  if (!p->meta_only) { if (kvr_status s = wait_unlocked(p, enter.lock, 0, false, 60000)) return s; }
+  try {
+    std::vector<int2> pairs;
+    for (int32_t lo = 0, hi = p->NB - 1; (int32_t)pairs.size() < max_moves;) {
+      while (lo < hi && !p->fq.is_free(lo)) ++lo;
+      while (lo < hi && p->fq.is_free(hi)) --hi;
+      if (lo >= hi) break;
+      pairs.push_back(make_int2(hi--, lo++));
+    }
+    if (pairs.empty()) return KVR_OK;
+    std::vector<int32_t> now((size_t)p->NB);
+    for (int32_t b = 0; b < p->NB; ++b) now[b] = b;
+    if (!p->meta_only) { if (kvr_status s = enqueue_copies(p, pairs, p->BS, (cudaStream_t)stream, 0)) return s; }
+    for (const int2 &m : pairs) { p->fq.move(m.x, m.y); now[m.x] = m.y; }
+    for (auto &entry : p->reqs)
+      for (int32_t &b : entry.second.blocks) b = now[b];
+    for (size_t i = 0; moves && i < pairs.size(); ++i) { moves[2 * i] = pairs[i].x; moves[2 * i + 1] = pairs[i].y; }
+    if (n_moves) *n_moves = (int32_t)pairs.size();
+    return KVR_OK;
+  } catch (const std::bad_alloc &) {
+    return fail(KVR_ERR_NOMEM, "out of host memory");
   }
 }
 

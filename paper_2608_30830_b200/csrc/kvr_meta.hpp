@@ -85,6 +85,13 @@ class FreeQueue {
     link_tail(b);
     return true;
   }
+  // Block src becomes the free block dst: its references go over, and it joins the tail itself.
+  void move(int32_t src, int32_t dst) {
+    unlink(dst);
+    refs_[dst] = refs_[src];
+    refs_[src] = 0;
+    link_tail(src);
+  }
   void note_reader(const int32_t *ids, int32_t n, uint64_t seq) {
     for (int32_t i = 0; i < n; ++i) if (tag_[ids[i]] < seq) tag_[ids[i]] = seq;
   }

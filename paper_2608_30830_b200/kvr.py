@@ -20,7 +20,7 @@ LAYER_MAJOR, BLOCK_MAJOR = 0, 1
 KERNEL_WARP, KERNEL_BULK = 1, 2
 ALL = 2**64 - 1
 BF16, F16, F32 = 0, 1, 2
-CACHE_BF16, CACHE_F16, CACHE_E4M3, CACHE_INT8 = 0, 1, 2, 3
+CACHE_BF16, CACHE_F16, CACHE_E4M3, CACHE_INT8, CACHE_E2M1 = 0, 1, 2, 3, 4
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_BANDS, SCALE_RAMP = 0, 1, 2, 3, 4
 DEV_GAVE_UP, DEV_BAD_BLOCK, DEV_BAD_LENGTH, DEV_BAD_POSITION, DEV_BAD_INDEX = 1, 3, 4, 5, 6
@@ -98,6 +98,10 @@ class RopeStruct(C.Structure):
     _fields_ = [("table", C.c_void_p)] + [(n, C.c_int32) for n in ("positions", "rot_dim", "style", "inverse")]
 
 
+class RopeAxes(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("of_pair", C.c_uint8 * 128)]
+
+
 class RopeScaling(C.Structure):
     _fields_ = [(n, C.c_double) for n in ("base", "factor", "low", "high")] + [("original", C.c_int32), ("kind", C.c_int32)]
 
@@ -113,7 +117,8 @@ EXPORTS = [
     "kvr_policy_break_evens", "kvr_policy_host_ttl", "kvr_policy_replay", "kvr_policy_select",
     "kvr_controller_create", "kvr_controller_destroy", "kvr_controller_calibrate", "kvr_controller_suspend",
     "kvr_controller_advance", "kvr_controller_resume", "kvr_controller_get_stats",
-    "kvr_cache_geometry", "kvr_rope_frequencies", "kvr_rope_table", "kvr_cache_append", "kvr_cache_read",
+    "kvr_cache_geometry", "kvr_rope_frequencies", "kvr_rope_table", "kvr_cache_append", "kvr_cache_append_axes", "kvr_cache_read",
+    "kvr_cache_copy", "kvr_request_fork", "kvr_request_resize", "kvr_pool_compact",
     "kvr_attend_workspace", "kvr_cache_attend", "kvr_cache_keep", "kvr_test_once", "kvr_test_attend_polls",
 ]
 
@@ -239,6 +244,16 @@ def lib():
     L.kvr_rope_table.argtypes = [C.POINTER(RopeScaling), i32, i32, i32, vp, vp]
     L.kvr_cache_append.restype = i32
     L.kvr_cache_append.argtypes = [spec, vp, i32, batch, rows, rows, rows, rows, C.POINTER(RopeStruct), vp, vp]
+    L.kvr_cache_append_axes.restype = i32
+    L.kvr_cache_append_axes.argtypes = [spec, vp, i32, batch, rows, rows, rows, rows, C.POINTER(RopeStruct), C.POINTER(RopeAxes), vp, vp]
+    L.kvr_cache_copy.restype = i32
+    L.kvr_cache_copy.argtypes = [spec, vp, vp, vp, i32, vp, vp]
+    L.kvr_request_fork.restype = i32
+    L.kvr_request_fork.argtypes = [vp, u64, u64, i64, pi32, i32, vp]
+    L.kvr_request_resize.restype = i32
+    L.kvr_request_resize.argtypes = [vp, u64, i64, pi32, i32, vp]
+    L.kvr_pool_compact.restype = i32
+    L.kvr_pool_compact.argtypes = [vp, i32, pi32, pi32, vp]
     L.kvr_cache_read.restype = i32
     L.kvr_cache_read.argtypes = [spec, vp, i32, batch, rows, rows, vp]
     L.kvr_attend_workspace.restype = u64
@@ -494,6 +509,27 @@ class Pool:
         blocks = np.ascontiguousarray(private_blocks, dtype=np.int32)
         return lib().kvr_request_admit_sharing_into(self._h, rid, n_tokens, donor, n_shared, _i32p(blocks), len(blocks))
 
+    def _resized(self, fn, n_tokens, *args):
+        nb = max(0, -(-n_tokens // self.geom[4]))
+        out = np.zeros(max(nb, 1), dtype=np.int32)
+        st = fn(self._h, *args[:-1], n_tokens, _i32p(out), nb, args[-1])
+        return st, (out[:nb].copy() if st == OK else None)
+
+    def fork(self, rid, donor, n_tokens, stream=None):
+        """kvr_request_fork: (status, block table of the new request).  stream: a cudaStream_t; None is the default stream."""
+        return self._resized(lib().kvr_request_fork, n_tokens, rid, donor, stream)
+
+    def resize(self, rid, n_tokens, stream=None):
+        """kvr_request_resize: (status, the request's whole block table)."""
+        return self._resized(lib().kvr_request_resize, n_tokens, rid, stream)
+
+    def compact(self, max_moves=None, stream=None):
+        """kvr_pool_compact: (status, [[from, to], ...] in order)."""
+        most = self.NB if max_moves is None else max_moves
+        moves, n = np.zeros((max(most, 1), 2), dtype=np.int32), C.c_int32()
+        st = lib().kvr_pool_compact(self._h, most, _i32p(moves), C.byref(n), stream)
+        return st, moves[:n.value].copy()
+
     def sharing(self, rid):
         """(status, shared-prefix block ids the request refers to)."""
         ns = C.c_int32()
@@ -626,7 +662,7 @@ class Pool:
 
 # ---- operators over the cache -------------------------------------------------------
 
-_FORMATS = {"bf16": CACHE_BF16, "f16": CACHE_F16, "e4m3": CACHE_E4M3, "int8": CACHE_INT8}
+_FORMATS = {"bf16": CACHE_BF16, "f16": CACHE_F16, "e4m3": CACHE_E4M3, "int8": CACHE_INT8, "e2m1": CACHE_E2M1}
 _STYLES = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
 _torch = None        # the module, imported by the first call that is given a tensor
 _types = {}          # torch dtype -> kvr_rows.type
@@ -696,14 +732,21 @@ def rope_table(out, first=0, base=10000.0, kind=SCALE_NONE, factor=1.0, low=1.0,
 
 
 class Rope:
-    """kvr_rope over a table of rope_table()."""
+    """kvr_rope over a table of rope_table().  axes: the axis of each of the rot_dim / 2 pairs, for positions of several axes
+    (kvr_rope_axes; append() then takes positions [tokens, number of axes])."""
 
-    def __init__(self, table, rot_dim, style="half", inverse=False):
+    def __init__(self, table, rot_dim, style="half", inverse=False, axes=None):
         dev, shape = _device(), table.shape
         if len(shape) != 3 or 2 * shape[1] != rot_dim or shape[2] != 2:
             raise ValueError("table must be [positions, rot_dim / 2, 2]")
         self.struct = RopeStruct(_array(table, "table", _torch.float32, 3, dev), shape[0], rot_dim, _STYLES[style], inverse)
         self.table = table          # kept alive
+        self.axes = None
+        if axes is not None:
+            if 2 * len(axes) != rot_dim or len(axes) > 128 or min(axes) < 0 or max(axes) > 3:
+                raise ValueError("axes must have rot_dim / 2 entries from 0 to 3")
+            self.axes = RopeAxes(max(axes) + 1, (C.c_uint8 * 128)(*axes))
+            self._axes = _ref(self.axes)
 
 
 class Batch:
@@ -768,17 +811,23 @@ class Cache:
         return _ref(rows(t, self.head_dim, what, device))
 
     def append(self, pool, layer, batch, q=None, k=None, v=None, q_out=None, rope=None, positions=None, stream=None):
-        """kvr_cache_append: write k (turned) and v of the step's tokens into the cache, q turned to q_out."""
+        """kvr_cache_append (kvr_cache_append_axes, if rope has axes): write k (turned) and v of the step's tokens into the cache, q
+        turned to q_out."""
         dev, x = _device(), q if q is not None else k if k is not None else v
         if x is None:
             raise ValueError("one of q, k and v is needed")
-        n = x.shape[0]
+        n, axes = x.shape[0], None if rope is None else rope.axes
         if positions is not None and positions.shape[0] != n:
             raise ValueError("positions must have %d entries" % n)
-        st = _lib.kvr_cache_append(self._spec, self._pool(pool, dev), _int32(layer, "layer"), batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
-                                   self._rows(k, n, "k", dev), self._rows(v, n, "v", dev), self._rows(q_out, n, "q_out", dev),
-                                   None if rope is None else _ref(rope.struct),
-                                   None if positions is None else _array(positions, "positions", _torch.int32, 1, dev), _stream(stream, dev))
+        if axes is not None and (positions is None or positions.dim() != 2 or positions.shape[1] != axes.axes):
+            raise ValueError("positions must be [tokens, %d]" % axes.axes)
+        args = (self._spec, self._pool(pool, dev), _int32(layer, "layer"), batch.of(n, self.spec.block_size), self._rows(q, n, "q", dev),
+                self._rows(k, n, "k", dev), self._rows(v, n, "v", dev), self._rows(q_out, n, "q_out", dev), None if rope is None else _ref(rope.struct))
+        where = None if positions is None else _array(positions, "positions", _torch.int32, 1 if axes is None else 2, dev)
+        if axes is None:
+            st = _lib.kvr_cache_append(*args, where, _stream(stream, dev))
+        else:
+            st = _lib.kvr_cache_append_axes(*args, rope._axes, where, _stream(stream, dev))
         if st:
             _check(st)
 
@@ -826,5 +875,17 @@ class Cache:
         st = _lib.kvr_cache_keep(self._spec, self._pool(pool, dev), batch.of(n, self.spec.block_size),
                                  _array(index, "index", _torch.int32, 2, dev), index.shape[1],
                                  _array(count, "count", _torch.int32, 1, dev), _stream(stream, dev))
+        if st:
+            _check(st)
+
+    def copy(self, pool, pairs, rows=None, status=None, stream=None):
+        """kvr_cache_copy: blocks pairs[:, 0] to blocks pairs[:, 1] (int32 [n, 2]; a source of -1: none), in all layers; rows: how many
+        tokens of each (int32 [n]), None is all.  status: as in Batch."""
+        dev, n = _device(), pairs.shape[0]
+        if pairs.dim() != 2 or pairs.shape[1] != 2 or (rows is not None and rows.shape[0] != n):
+            raise ValueError("pairs must be [n, 2], rows [n]")
+        st = _lib.kvr_cache_copy(self._spec, self._pool(pool, dev), _array(pairs, "pairs", _torch.int32, 2, dev),
+                                 None if rows is None else _array(rows, "rows", _torch.int32, 1, dev), _int32(n, "the number of pairs"),
+                                 None if status is None else _array(status, "status", _torch.int32, 1, dev), _stream(stream, dev))
         if st:
             _check(st)
