@@ -67,7 +67,6 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     return fail_cache(KVR_ERR_INVALID_ARG, "q and out must have one 16-bit type and the same heads");
   if ((spec->format == KVR_CACHE_BF16 && q->type != KVR_BF16) || (spec->format == KVR_CACHE_F16 && q->type != KVR_F16))
     return fail_cache(KVR_ERR_INVALID_ARG, "q must have the type of a 16-bit cache");
-  if (four_bit(spec->format)) return fail_cache(KVR_ERR_INVALID_ARG, "attention over 4-bit caches is not there yet");
   if (q->heads % spec->kv_heads) return fail_cache(KVR_ERR_INVALID_ARG, "q's heads must be a multiple of kv_heads");
   const int group = q->heads / spec->kv_heads;
   if ((int64_t)batch->max_new * group > (1 << 28)) return fail_cache(KVR_ERR_INVALID_ARG, "too many new tokens in one request");
@@ -92,11 +91,11 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   a.scale_log2 = scale * 1.4426950408889634f;
   a.q_heads = q->heads;
   const int padded = spec->head_dim <= 64 ? 64 : spec->head_dim <= 128 ? 128 : 256;
-  const int warps = rows_warps(padded);
+  const int warps = rows_warps(spec->format, padded);
   const int64_t rows = (int64_t)batch->max_new * group;
   int tiles = 0, slices = 0;
   CUtensorMap map{};
-  if (rows > 16 && padded <= 128) {
+  if (rows > 16 && padded <= 128 && !four_bit(spec->format)) {
     // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
     // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
     // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels stay with the row kernel: two jobs' sums and scores
@@ -152,6 +151,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   switch (spec->format) {
     case KVR_CACHE_BF16: e = launch_attend_bf16(a, tiles, slices, map, s); break;
     case KVR_CACHE_F16: e = launch_attend_f16(a, tiles, slices, map, s); break;
+    case KVR_CACHE_E2M1: e = launch_attend_e2m1(a, tiles, slices, map, s); break;
     case KVR_CACHE_E4M3: e = launch_attend_e4m3(a, tiles, slices, map, s); break;
     default: e = launch_attend_int8(a, tiles, slices, map, s);
   }

@@ -743,9 +743,12 @@ class Rope:
         self.table = table          # kept alive
         self.axes = None
         if axes is not None:
-            if 2 * len(axes) != rot_dim or len(axes) > 128 or min(axes) < 0 or max(axes) > 3:
+            axes = bytes(axes)       # refuses what is not in [0, 255]
+            if 2 * len(axes) != rot_dim or len(axes) > 128 or max(axes) > 3:
                 raise ValueError("axes must have rot_dim / 2 entries from 0 to 3")
-            self.axes = RopeAxes(max(axes) + 1, (C.c_uint8 * 128)(*axes))
+            self.axes = RopeAxes()
+            self.axes.axes = max(axes) + 1
+            C.memmove(self.axes.of_pair, axes, len(axes))
             self._axes = _ref(self.axes)
 
 

@@ -211,7 +211,7 @@ def test_refusals():
         assert p.admit(1, 5)[0] == kvr.OK
         assert p.fork(2, 1, -1)[0] == p.fork(1, 1, 3)[0] == p.fork(2, 1, 6)[0] == kvr.ERR_INVALID_ARG and kvr.last_error()
         assert p.fork(2, 7, 1)[0] == p.resize(7, 1)[0] == kvr.ERR_UNKNOWN_REQUEST
-        assert p.resize(1, -1)[0] == kvr.ERR_INVALID_ARG and p.resize(1, 17)[0] == kvr.HBM_FULL and p.resize(1, 1 << 60)[0] == kvr.HBM_FULL
+        assert p.resize(1, -1)[0] == kvr.ERR_INVALID_ARG and p.resize(1, 17)[0] == kvr.HBM_FULL and L.kvr_request_resize(p._h, 1, 1 << 60, None, 0, None) == kvr.HBM_FULL
         assert p.fork(2, 1, 5)[0] == kvr.OK and p.fork(2, 1, 5)[0] == kvr.ERR_BAD_STATE
         out = np.zeros(1, dtype=np.int32)
         assert L.kvr_request_fork(p._h, 3, 1, 5, kvr._i32p(out), 1, None) == L.kvr_request_resize(p._h, 1, 5, kvr._i32p(out), 1, None) == kvr.ERR_INVALID_ARG

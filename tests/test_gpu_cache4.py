@@ -304,3 +304,248 @@ def test_copies_beyond_4_gib():
     for b in (3, 149_999):
         assert torch.equal(tiles[:, b], tiles[:, 149_998])
     assert not tiles[:, 4].any() and not tiles[:, 149_997].any()
+
+
+# ---- attend ------------------------------------------------------------------------
+
+DIMS = [(8, 4, 128, 16), (2, 8, 128, 16), (1, 1, 64, 8), (3, 5, 96, 5), (4, 2, 256, 16), (12, 1, 64, 16), (5, 3, 32, 7), (8, 7, 64, 32), (1, 16, 192, 1), (17, 1, 128, 16),
+        (2, 3, 224, 16), (1, 4, 160, 24)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,group,dim,bs", DIMS)
+def test_attend_single_tokens(dtype, heads, group, dim, bs):
+    """One new token a request, contexts from none to thousands of tokens."""
+    s = Setup("e2m1", heads, dim, bs, [0, 1, 14, 15, 16, 17, 63, 64, 255, 700, 3001], [1] * 11, seed=heads * dim)
+    base.check_attend(s, heads * group, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,group,dim,bs", DIMS)
+def test_attend_trees_with_empty_rows(dtype, heads, group, dim, bs):
+    """Trees of up to 70 tokens (two mask words); rows that see nothing at all where there is no context."""
+    s = Setup("e2m1", heads, dim, bs, [0, 0, 100, 511, 1000, 33, 0], [1, 7, 13, 64, 70, 0, 70], seed=heads * dim + 1, layout=heads % 2)
+    mask, seen = base.tree(s, np.random.default_rng(dim), empty=0.15)
+    out, lse, _ = base.check_attend(s, heads * group, dtype, mask, seen, strided=True)
+    empty = torch.cat([~m.any(1) for m in seen])
+    assert empty.any() and (out[empty] == 0).all() and (lse[empty] == -math.inf).all()
+
+
+def test_attend_causal_chunks():
+    s = Setup("e2m1", 2, 128, 16, [0, 300, 5], [200, 129, 1], seed=3)
+    base.check_attend(s, 8, "bf16")
+
+
+@pytest.mark.parametrize("new", [2, 3, 4, 5, 8, 9, 15, 16, 17, 31, 32, 33, 48, 63, 64, 65])
+def test_attend_every_tile_of_rows(new):
+    s = Setup("e2m1", 2, 128, 16, [129, 40], [new, max(1, new // 2)], seed=new)
+    mask, seen = base.tree(s, np.random.default_rng(new))
+    base.check_attend(s, 8, "bf16", mask, seen)
+
+
+@pytest.mark.parametrize("group", [1, 8])
+@pytest.mark.parametrize("bs", [16, 5])
+def test_attend_ignores_what_a_row_does_not_see(group, bs):
+    """Some drafted tokens are NaN as append writes it (the head's scale), others hold the largest codes and scales there are, their groups' bytes
+    too; rows that do not see them give the formula over what they see, rows that see a NaN give NaN."""
+    s = Setup("e2m1", 2, 64, bs, [0, 50, 200], [9, 20, 33], seed=11)
+    mask, seen = base.tree(s, np.random.default_rng(4))
+    s.fill()
+    for r, (c, t) in enumerate(zip(s.context, s.new)):
+        one = kvr.Batch(torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.tensor([c + 1], dtype=torch.int32, device="cuda"),
+                        s.arrays[2][r:r + 1].contiguous(), 1, c + t, s.status)
+        x = torch.ones(1, 2, 64, device="cuda", dtype=torch.float32)
+        x[0, 1, 5] = math.nan
+        s.cache.append(s.pool, 0, one, k=x, v=x)
+        s.plane(0, 1)[s.slot(r, c + 3)] = 0x7f                                       # any bytes: groups' scales of 480, a scale of 3e38
+    finite = [torch.ones(t, dtype=torch.bool, device="cuda") for t in s.new]
+    vals = [s.decode(0, i)[0] for i in (0, 1)]
+    kv = [[x[s.slots(r, 0, c + t)] for r, (c, t) in enumerate(zip(s.context, s.new))] for x in vals]
+    q = rand(s, s.tokens, 2 * group, 64)
+    out, ws = torch.zeros_like(q), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    s.cache.attend(s.pool, 0, s.batch, q, out, ws, mask=mask)
+    s.ok()
+    at = 0
+    for r, (c, t) in enumerate(zip(s.context, s.new)):
+        clean = ~(seen[r][:, c + 1] | seen[r][:, c + 3])
+        assert clean.any() and finite[r].all()
+        for i in torch.nonzero(clean)[:, 0].tolist():
+            keys = torch.nonzero(seen[r][i])[:, 0]
+            for h in range(2 * group):
+                kk, vv = kv[0][r][keys, h // group], kv[1][r][keys, h // group]
+                p = torch.softmax(kk @ q[at + i, h].double() / 8.0, 0)
+                assert_within(out[at + i, h], p @ vv, (U["f16"] + U["bf16"] + 2.0 ** -13) * (p @ vv.abs()) + 2.0 ** -12)
+        hit = seen[r][:, c + 1]
+        assert hit.any() and torch.isnan(out[at:at + t][hit][:, group:]).all()
+        assert torch.isfinite(out[at:at + t][hit & ~seen[r][:, c + 3]][:, :group]).all()         # the other head of that token is finite
+        at += t
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attend_large_and_unlike_values(new):
+    """Scores far apart (the running maximum moves late and far), values of V across many magnitudes."""
+    s = Setup("e2m1", 2, 128, 16, [900, 64], [new, new], seed=21, poison=False)
+    s.fill()
+    lens = [c + t for c, t in zip(s.context, s.new)]
+    starts = torch.tensor([0, lens[0], sum(lens)], dtype=torch.int32, device="cuda")
+    whole = kvr.Batch(starts, torch.zeros_like(s.arrays[1]), s.arrays[2], max(lens), max(lens), s.status)
+    n = sum(lens)
+    kk = rand(s, n, 2, 128, dtype=torch.float32) * torch.linspace(0.1, 3.0, n, device="cuda")[:, None, None]
+    vv = rand(s, n, 2, 128, dtype=torch.float32) * torch.exp2(torch.randint(-6, 7, (n, 2, 1), device="cuda", generator=s.gen).float())
+    s.cache.append(s.pool, 0, whole, k=kk, v=vv)
+    vals = [s.decode(0, i)[0] for i in (0, 1)]
+    base.check_attend(s, 8, "bf16", scale=0.5, kv=[[x[s.slots(r, 0, m)] for r, m in enumerate(lens)] for x in vals])
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("size", [1e-24, 1e-6, 1e6, 1e30])
+def test_attend_small_and_large_values_of_v(size, new):
+    s = Setup("e2m1", 2, 64, 16, [200], [new], seed=22)
+    n = 200 + new
+    whole = kvr.Batch(torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.zeros_like(s.arrays[1]), s.arrays[2], n, n, s.status)
+    k, v = rand(s, n, 2, 64, dtype=torch.float32), rand(s, n, 2, 64, dtype=torch.float32)
+    s.cache.append(s.pool, 0, whole, k=k, v=v * size)
+    kv = [[s.decode(0, i)[0][s.slots(0, 0, n)]] for i in (0, 1)]
+    q, ws = rand(s, new, 4, 64), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(new, 4, 64, dtype=torch.bfloat16, device="cuda")
+    s.cache.attend(s.pool, 0, s.batch, q, out, ws)
+    s.ok()
+    want, _, mag = base.attend64(s, q, *kv, 1 / 8.0, base.causal(s))
+    assert_within(out, want, (U["f16"] + U["bf16"] + 2.0 ** -13) * mag + 2.0 ** -24 * 8 * size * 16)
+
+
+@pytest.mark.parametrize("new,heads", [(1, 8), (33, 8), (1, 1), (3, 2)])
+def test_attend_many_requests_and_many_pieces(new, heads):
+    rng = np.random.default_rng(1)
+    n = 600 if new == 1 else 40
+    s = Setup("e2m1", heads, 64, 16, [int(x) for x in rng.integers(0, 40, n)], [new] * n, seed=31)
+    base.check_attend(s, heads * 2, "bf16")
+    s = Setup("e2m1", heads, 64, 16, [20000], [new], seed=32)
+    base.check_attend(s, heads * 2, "bf16")
+    if new > 1:
+        s = Setup("e2m1", heads, 64, 16, [3, 5, 20000, 0], [0, new, new, 0], seed=33)
+        mask, seen = base.tree(s, rng)
+        base.check_attend(s, heads * 2, "bf16", mask, seen)
+
+
+def test_attend_offsets_beyond_32_bits():
+    """Blocks behind the first 4 GiB of a plane, from both ends of the pool."""
+    heads, dim, bs = 8, 128, 16
+    for new in (1, 20):
+        s = Setup("e2m1", heads, dim, bs, [100, 30], [new, 1], layers=1, spare=(5 << 30) // (640 * bs), seed=41, poison=False)
+        width = s.host_tables.shape[1]
+        s.host_tables[:] = (s.nb - 1 - np.arange(2 * width).reshape(2, width)).astype(np.int32)
+        s.arrays[2].copy_(torch.from_numpy(s.host_tables))
+        n = 131 + new
+        k, v = (rand(s, n, heads, dim) for _ in range(2))
+        lens = [100 + new, 31]
+        whole = kvr.Batch(torch.tensor([0, lens[0], n], dtype=torch.int32, device="cuda"), torch.zeros_like(s.arrays[1]), s.arrays[2], 120, 120, s.status)
+        s.cache.append(s.pool, 0, whole, k=k, v=v)
+        got = [torch.zeros(n, heads, dim, device="cuda") for _ in range(2)]
+        s.cache.read(s.pool, 0, whole, k=got[0], v=got[1])
+        assert got[0].abs().max() > 0.5
+        base.check_attend(s, 32, "bf16", kv=[[x[:lens[0]].double(), x[lens[0]:].double()] for x in got])
+
+
+def test_attend_leaves_out_what_does_not_fit():
+    for new in (2, 20):
+        s = Setup("e2m1", 2, 64, 16, [20, 20, 20], [new] * 3, seed=51)
+        s.fill()
+        q, ws = rand(s, 3 * new, 4, 64), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+        for what in ("block", "tokens"):
+            starts, context, tables = (x.clone() for x in s.arrays)
+            if what == "block":
+                tables[1, 1] = s.nb
+            else:
+                context[1] = 21
+            out = torch.full_like(q, 3.0)
+            s.status.zero_()
+            s.cache.attend(s.pool, 0, kvr.Batch(starts, context, tables, new, 20 + new, s.status), q, out, ws)
+            torch.cuda.synchronize()
+            assert int(s.status) == (kvr.DEV_BAD_BLOCK if what == "block" else kvr.DEV_BAD_LENGTH)
+            assert (out[:new] != 3).any() and (out[2 * new:] != 3).any() and (what == "block" or (out[new:2 * new] == 3).all())
+
+
+# ---- together ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("new", [6, 40])
+def test_a_step_on_another_stream_and_in_a_graph(new):
+    """append (several axes) -> attend -> keep -> copy captured once and replayed with other lengths in the same arrays."""
+    s = Setup("e2m1", 2, 64, 16, [100, 64], [new, new], layers=1, seed=71)
+    s.fill()
+    mask, _ = base.tree(s, np.random.default_rng(3))
+    n = 2 * new
+    q, kn, vn = rand(s, n, 8, 64), rand(s, n, 2, 64), rand(s, n, 2, 64)
+    out, ws = torch.zeros_like(q), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    index, count = torch.tensor([[0, 2], [1, 5]], dtype=torch.int32, device="cuda"), torch.tensor([2, 2], dtype=torch.int32, device="cuda")
+    where = torch.randint(0, 200, (n, 3), device="cuda", dtype=torch.int32)
+    rope = kvr.Rope(table_of(64, 200), 64, axes=[0] * 8 + [1] * 12 + [2] * 12)
+    b = kvr.Batch(*s.arrays, new, 100 + new, s.status)
+    free = [x for x in range(s.nb) if x not in set(s.host_tables[:, :-(-(100 + new) // 16)].ravel().tolist())][:1]
+    pairs = torch.tensor([[int(s.host_tables[0, 0]), free[0]]], dtype=torch.int32, device="cuda")
+
+    def step():
+        s.cache.append(s.pool, 0, b, q=q, k=kn, v=vn, q_out=q, rope=rope, positions=where)
+        s.cache.attend(s.pool, 0, b, q, out, ws, mask=mask)
+        s.cache.keep(s.pool, b, index, count)
+        s.cache.copy(s.pool, pairs, status=s.status)
+
+    start_pool, start_q, side = s.pool.clone(), q.clone(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    first, pool_after = out.clone(), s.pool.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for lengths in ([100, 64], [41, 50]):
+        s.pool.copy_(start_pool)
+        q.copy_(start_q)
+        s.arrays[1].copy_(torch.tensor(lengths, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        if lengths == [100, 64]:
+            assert torch.equal(out, first) and torch.equal(s.pool, pool_after)
+        else:
+            replayed = out.clone()
+            s.pool.copy_(start_pool)
+            q.copy_(start_q)
+            step()
+            torch.cuda.synchronize()
+            assert torch.equal(out, replayed) and not torch.equal(out, first)
+    assert int(s.status) == 0
+
+
+def test_a_4_bit_request_is_forked_suspended_compacted_and_answers_the_same():
+    """The pool's movers and copies carry codes and scales: the answer after a fork, a suspend, a resume into other blocks and a compaction is the
+    same, bit for bit, and the host holds 80 bytes a head."""
+    c = kvr.Cache(2, 4, 128, 16, 200, "e2m1")
+    pool = torch.zeros(c.pool_bytes, dtype=torch.uint8, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    n, new = 500, 5
+    with kvr.Pool(*c.geometry, 200, 64 << 20, initial_free_order=np.random.default_rng(1).permutation(200).astype(np.int32), device_pool=pool.data_ptr()) as p:
+        st, blocks = p.admit(1, n)
+        assert st == kvr.OK
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")       # noqa: E731
+        k, v, q = (torch.randn(n, h, 128, device="cuda", generator=gen).bfloat16() for h in (4, 4, 8))
+        for layer in range(2):
+            c.append(pool, layer, kvr.Batch(i32([0, n]), i32([0]), i32(blocks)[None], n, n), k=k, v=v)
+        ws = torch.zeros(c.workspace_bytes(), dtype=torch.uint8, device="cuda")
+
+        def answer(rid):
+            out = torch.zeros(2, new, 8, 128, dtype=torch.bfloat16, device="cuda")
+            for layer in range(2):
+                c.attend(pool, layer, kvr.Batch(i32([0, new]), i32([n - new]), i32(p.info(rid)[1]["blocks"])[None], new, n), q[:new], out[layer], ws)
+            torch.cuda.synchronize()
+            return out
+
+        first = answer(1)
+        assert p.fork(2, 1, n)[0] == kvr.OK and torch.equal(answer(2), first)
+        assert p.suspend_to_host([1], kvr.SYNC)[0] == kvr.OK
+        assert p.stats()["bytes_suspended"] == n * 2 * 2 * 4 * 80
+        assert torch.equal(answer(2), first)
+        assert p.resume_from_host([1], kvr.SYNC)[0] == kvr.OK and torch.equal(answer(1), first)
+        assert p.info(1)[1]["blocks"].tolist() != blocks.tolist()
+        assert len(p.compact()[1]) > 0 and torch.equal(answer(1), first) and torch.equal(answer(2), first)
