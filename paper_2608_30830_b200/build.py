@@ -12,7 +12,7 @@ SOURCES = ["kvr_kernels.cu", "kvr_engine.cu", "kvr_lib.cu", "kvr_noalloc.cu", "k
            "kvr_cache.cu", "kvr_pages.cu", "kvr_attend.cu", "kvr_attend_bf16.cu", "kvr_attend_f16.cu", "kvr_attend_e4m3.cu", "kvr_attend_int8.cu",
            "kvr_attend_e2m1.cu"]
 DEPS = SOURCES + ["kvr_kernels.cuh", "kvr_cache.cuh", "kvr_pages.cuh", "kvr_attend.cuh", "kvr_attend_common.cuh",
-                  "kvr_attend_rows.cuh", "kvr_attend_tiles.cuh", "kvr_meta.hpp", "kvr_numa.hpp", "kvr_once.hpp", "kvr_pool.hpp", os.path.join("..", "..", "include", "kvr.h")]
+                  "kvr_attend_rows.cuh", "kvr_attend_rows4.cuh", "kvr_attend_tiles.cuh", "kvr_meta.hpp", "kvr_numa.hpp", "kvr_once.hpp", "kvr_pool.hpp", os.path.join("..", "..", "include", "kvr.h")]
 
 
 def stale():

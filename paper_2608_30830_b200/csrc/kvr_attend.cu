@@ -3,6 +3,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 
 #include "kvr_once.hpp"
 
@@ -23,17 +24,34 @@ int sm_count() {
   return counts[dev];
 }
 
-// The layer's planes as [plane][block][token][head][channel]: boxes are `box_rows` tokens of one head, 128 bytes wide (128-byte
-// swizzle, the products' operand layout) or a whole 8-bit head; channels beyond head_dim read as zero.
-bool layer_map(const kvr_cache_spec *s, const CacheView &c, int padded, int box_rows, CUtensorMap *map) {
-  typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+typedef CUresult (*Encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                           const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
   static const Encode encode = [] {
     void *f = nullptr;
     cudaDriverEntryPointQueryResult found;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
     return reinterpret_cast<Encode>(f);
   }();
+  return encode;
+}
+
+// A 4-bit layer's planes as [plane][block][token][8 bytes of a row]: boxes are `box_rows` tokens of a group of heads, `width` bytes each; bytes beyond
+// the row read as zero.
+bool record_map(const kvr_cache_spec *s, const CacheView &c, int width, int box_rows, CUtensorMap *map) {
+  const Encode encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.row_bytes / 8, (cuuint64_t)s->block_size, (cuuint64_t)s->num_blocks, 2};
+  const cuuint64_t strides[3] = {(cuuint64_t)c.row_bytes, (cuuint64_t)c.block_stride, (cuuint64_t)c.v_offset};
+  const cuuint32_t box[4] = {(cuuint32_t)width / 8, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 4, c.base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The layer's planes as [plane][block][token][head][channel]: boxes are `box_rows` tokens of one head, 128 bytes wide (128-byte
+// swizzle, the products' operand layout) or a whole 8-bit head; channels beyond head_dim read as zero.
+bool layer_map(const kvr_cache_spec *s, const CacheView &c, int padded, int box_rows, CUtensorMap *map) {
+  const Encode encode = encoder();
   if (!encode) return false;
   const bool quant = quantised(s->format);
   const cuuint64_t element = quant ? 1 : 2;
@@ -91,11 +109,13 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   a.scale_log2 = scale * 1.4426950408889634f;
   a.q_heads = q->heads;
   const int padded = spec->head_dim <= 64 ? 64 : spec->head_dim <= 128 ? 128 : 256;
-  const int warps = rows_warps(spec->format, padded);
+  const bool four = four_bit(spec->format);
+  const int warps = four ? rows4_warps(padded) : rows_warps(padded);
   const int64_t rows = (int64_t)batch->max_new * group;
   int tiles = 0, slices = 0;
   CUtensorMap map{};
-  if (rows > 16 && padded <= 128 && !four_bit(spec->format)) {
+  Rows4 r4{};
+  if (rows > 16 && padded <= 128 && !four) {
     // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
     // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
     // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels stay with the row kernel: two jobs' sums and scores
@@ -125,14 +145,30 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     // rows streams a long 8-bit cache, whose narrow rows and scales are then read in pieces too small: by the caller's bounds, from 512 MB
     // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316).
     const int64_t stream = 2ll * batch->n_req * batch->max_tokens * a.c.row_bytes;
-    const bool whole = quantised(spec->format) && tiles == 1 && stream >= 512ll << 20;
+    const bool whole = quantised(spec->format) && tiles == 1 && (stream >= 512ll << 20 || (four && stream >= (getenv("KVR_W") ? atoll(getenv("KVR_W")) : 0ll) << 20));
     while (!whole && a.group_heads > 1 && (int64_t)batch->n_req * a.head_groups * 8 < sms) {
       a.group_heads = (a.group_heads + 1) / 2;
       a.head_groups = (spec->kv_heads + a.group_heads - 1) / a.group_heads;
     }
     slices = warps / a.group_heads;
-    const int turn = 16 * slices * chunks_at_once(spec->format, tiles);      // keys that the warps of a head take at a time
+    const int turn = 16 * slices * (four ? rows4_at_once(padded, tiles) : chunks_at_once(spec->format, tiles));      // keys that the warps of a head take at a time
     a.unit = FastDiv((64 + turn - 1) / turn * turn);
+    if (four) {
+      const int group_bytes = a.group_heads * a.c.head_bytes, stage_keys = 16 * slices, merge = (slices - 1) * a.group_heads * (padded * 8 + 16) * 4;
+      // Rows of many records stand 32 bytes behind a multiple of 128, for the banks; of few as they are, or the ring would hold too few keys.
+      r4.stride = group_bytes < 256 ? group_bytes : group_bytes + (160 - group_bytes % 128) % 128;
+      r4.slices = slices;
+      // tokens of a box: what divides a block and a stage
+      for (r4.box_rows = 128; r4.box_rows >= 8 && (spec->block_size % r4.box_rows || stage_keys % r4.box_rows); r4.box_rows /= 2) {}
+      if (r4.box_rows < 8 || r4.stride > 2048) {             // (a box is at most 256 x 8 bytes wide)
+        r4.box_rows = 0;
+      } else {
+        r4.box_bytes = r4.box_rows * r4.stride;
+        if (!record_map(spec, a.c, r4.stride, r4.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
+      }
+      const int fit = (kRows4Shared - (merge > 256 ? merge : 256)) / (2 * stage_keys * r4.stride);
+      r4.stages = fit < 8 ? fit : 8;
+    }
     // 64 or more: fewer pieces.  (us, units of 16 / 64 / 128 / 256 / 512 keys, one token, bf16: 32 requests of 333 tokens 21.4 / 18.5 / 18.8 /
     // 25.3 / 23.6, 16 of them 25.9 / 15.6 / 15.7 / 18.6 / 15.8.  Of few requests a turn is 128 keys anyway: one of 333 13.8 / 13.5 /
     // 13.7 / 14.4 / 9.5, of 1,000 15.1 / 15.1 / 15.1 / 15.1 / 16.0.)
@@ -151,7 +187,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   switch (spec->format) {
     case KVR_CACHE_BF16: e = launch_attend_bf16(a, tiles, slices, map, s); break;
     case KVR_CACHE_F16: e = launch_attend_f16(a, tiles, slices, map, s); break;
-    case KVR_CACHE_E2M1: e = launch_attend_e2m1(a, tiles, slices, map, s); break;
+    case KVR_CACHE_E2M1: e = launch_attend_e2m1(a, tiles, r4, map, s); break;
     case KVR_CACHE_E4M3: e = launch_attend_e4m3(a, tiles, slices, map, s); break;
     default: e = launch_attend_int8(a, tiles, slices, map, s);
   }

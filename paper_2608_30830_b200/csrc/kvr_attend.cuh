@@ -142,9 +142,19 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int 
 #endif
 
 // chunks of 16 keys that a warp of the row kernel takes at a time (tiles: of 8 rows); a unit holds a multiple of them
-__host__ __device__ constexpr int chunks_at_once(int format, int tiles) { return quantised(format) && !four_bit(format) && tiles == 1 ? 2 : 1; }
+__host__ __device__ constexpr int chunks_at_once(int format, int tiles) { return quantised(format) && tiles == 1 ? 2 : 1; }
 // warps of a CTA of the row kernel: KV heads of a group x slices of the keys
-__host__ __device__ constexpr int rows_warps(int format, int padded_dim) { return (padded_dim == 256 ? 4 : 8) * (four_bit(format) ? 2 : 1); }
+__host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim == 256 ? 4 : 8; }
+
+// Of the row kernel for 4-bit caches: warps that a CTA's heads share, chunks of 16 keys that each takes at a time (tiles: of 8 rows), shared
+// memory beside its barriers.
+__host__ __device__ constexpr int rows4_warps(int padded_dim) { return padded_dim == 256 ? 8 : 16; }
+__host__ __device__ constexpr int rows4_at_once(int padded_dim, int tiles) { return padded_dim <= 128 && tiles == 1 ? 1 : 1; }
+constexpr int kRows4Shared = 227 * 1024 - 4096;
+struct Rows4 {
+  int slices, stages, stride;          // warps of a head; stages of the ring; bytes from one key's records to the next's
+  int box_rows, box_bytes;             // tokens of a TMA box (0: copies by lanes), bytes of one
+};
 
 // By cache format, one translation unit each (kvr_attend_<format>.cu).  tiles: of the row kernel, query rows of a segment / 8,
 // 1 or 2; 0 is the tile kernel (at most 128 channels), for 128 or 256 rows a segment, with its map of
@@ -152,7 +162,7 @@ __host__ __device__ constexpr int rows_warps(int format, int padded_dim) { retur
 cudaError_t launch_attend_bf16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
 cudaError_t launch_attend_f16(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
 cudaError_t launch_attend_e4m3(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
-cudaError_t launch_attend_e2m1(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
+cudaError_t launch_attend_e2m1(const AttendArgs &a, int tiles, const Rows4 &r4, const CUtensorMap &map, cudaStream_t s);
 cudaError_t launch_attend_int8(const AttendArgs &a, int tiles, int slices, const CUtensorMap &map, cudaStream_t s);
 
 }  // namespace kvr

@@ -52,11 +52,10 @@ __device__ __forceinline__ void product(float (&c)[4], const unsigned (&a)[4], u
 }
 template <int FMT, int DP>
 struct Shape {
-  static constexpr bool kQuant = quantised(FMT), kFour = four_bit(FMT);
-  static constexpr int kWarps = rows_warps(FMT, DP);                     // heads and slices of a CTA
-  static constexpr int kRow = kFour ? DP / 2 : DP * (kQuant ? 1 : 2);    // bytes of a key's head
-  static constexpr int kTail = DP == 256 ? 32 : 16;                      // 4 bits: what lies behind a head's codes
-  static constexpr int kStageBytes = 2 * 16 * kRow + (kFour ? 32 * kTail : kQuant ? 128 : 0); // K, V, scales
+  static constexpr bool kQuant = quantised(FMT);
+  static constexpr int kWarps = rows_warps(DP);                          // heads and slices of a CTA
+  static constexpr int kRow = DP * (kQuant ? 1 : 2);                     // bytes of a key's head
+  static constexpr int kStageBytes = 2 * 16 * kRow + (kQuant ? 128 : 0); // K, V, scales
   static constexpr int kFit = 196608 / kWarps / kStageBytes;
   static constexpr int kStages = kFit > 6 ? 6 : kFit;                    // 3 to 6
 };
@@ -69,29 +68,15 @@ __device__ __forceinline__ int spread(int key, int chunk) {
   else return key * DP + ((chunk ^ (((key >> 2) << 1) ^ ((key & 1) << 2))) << 4);
 }
 
-// The same for 4-bit codes.  64-byte rows stand in the order key ^ bit 2 of it, so that the rows which the lanes of an 8-byte read look at lie
-// in both halves of 128 bytes; 32-byte rows likewise in its quarters.
-template <int DP>
-__device__ __forceinline__ int spread4(int key, int chunk) {
-  if constexpr (DP == 64) return (key ^ ((key >> 2 & 1) << 1 | key >> 3)) * 32 + (chunk << 4);
-  else if constexpr (DP == 128) return (key ^ (key >> 2 & 1)) * 64 + ((chunk ^ (key >> 3 << 1)) << 4);
-  else return key * 128 + ((chunk ^ (((key >> 2) << 1) ^ ((key & 1) << 2))) << 4);
-}
-__device__ __forceinline__ unsigned times(unsigned x, unsigned scale) {
-  const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&scale));
-  return *reinterpret_cast<const unsigned *>(&v);
-}
-
 template <int FMT, int DP, int NT>
 __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_kernel(const __grid_constant__ AttendArgs a, int slices) {
   using S = Shape<FMT, DP>;
-  constexpr bool kQuant = S::kQuant, kFour = S::kFour, kBf16 = FMT == KVR_CACHE_BF16;
+  constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
   constexpr int kStages = S::kStages, kRow = S::kRow, kChunks = kRow / 16, kTiles = DP / 16;
   // Chunks of 16 keys that a turn takes: two where registers allow it, so that one's chain of dependent steps runs beside the other's
   // and the maximum is looked for once.
   constexpr int kAtOnce = chunks_at_once(FMT, NT);
   static_assert(kStages >= 2 * kAtOnce, "");
-  constexpr int kOwn = kFour && DP >= 128 ? 32 : 16;     // codes: channels of a key that a lane has side by side
   constexpr float kLazy = 4.f;         // a row's maximum moves only when a score passes it by 2^4: fewer rescales,
                                        // probabilities up to 16 (room in f16, see the scale of V below)
   extern __shared__ __align__(128) unsigned char smem[];
@@ -149,24 +134,6 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
       const unsigned valid = __ballot_sync(0xffffffffu, in);
       unsigned char *st = ring + stage * S::kStageBytes;
       const unsigned k_at = shared_at(st);
-      if constexpr (kFour) {
-        // Lane r knows where record r lies: of key r & 15, K's or V's.  A record's 16-byte columns, codes and then scales, go to neighbouring lanes.
-        constexpr int kCodes = DP / 32, kColumns = kCodes + S::kTail / 16;
-        const long long record = in ? offset + (long long)head * a.c.head_bytes + (lane >= 16 ? a.c.v_offset : 0) : -1;
-#pragma unroll
-        for (int i = 0; i < kColumns; ++i) {
-          const int r = (i * 32 + lane) / kColumns, col = i * 32 + lane - r * kColumns, behind = (col - kCodes) * 16;
-          const long long off = __shfl_sync(0xffffffffu, record, r);
-          const bool v = off >= 0 && (col < kCodes ? col * 32 < a.c.head_dim : behind < a.c.head_bytes - a.c.scale_offset);
-          const char *src = a.c.base + (v ? off + (col < kCodes ? col * 16 : a.c.scale_offset + behind) : 0);
-          copy16(k_at + (col < kCodes ? (r >> 4) * (16 * kRow) + spread4<DP>(r & 15, col) : 32 * kRow + r * S::kTail + behind), src, v);
-        }
-        ++load_c;
-        settle();
-        fetch_id();
-        copy_commit();
-        return;
-      }
       const int column = head < a.c.kv_heads ? head * a.c.head_dim * (kQuant ? 1 : 2) : 0;
       const int used = a.c.head_dim * (kQuant ? 1 : 2) / 16;             // 16-byte columns of a head
       const char *base = a.c.base + column;
@@ -221,14 +188,14 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         }
         q_scale[n][0] = q_scale[n][1] = a.scale_log2;
       } else {
-        // k-step (group of 4 * kOwn channels, s): channels 4 * kOwn * group + kOwn * tig + 4 * s + 0..3
+        // k-step (group of 64 channels, s): channels 64 * group + 16 * tig + 4 * s + 0..3
         float top = 0.f;
-        float x[DP / (4 * kOwn)][kOwn];
+        float x[DP / 64][16];
 #pragma unroll
-        for (int w = 0; w < DP / (4 * kOwn); ++w) {
-          const int d = w * (4 * kOwn) + tig * kOwn;
+        for (int w = 0; w < DP / 64; ++w) {
+          const int d = w * 64 + tig * 16;
 #pragma unroll
-          for (int h = 0; h < kOwn / 8; ++h) {
+          for (int h = 0; h < 2; ++h) {
             float y[8] = {};
             if (have && d < a.c.head_dim) {
               if (a.q.type == KVR_BF16) load8<KVR_BF16>(src + (d + h * 8) * 2, y);
@@ -245,11 +212,11 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         const bool plain = e >= 1 && e <= 253;
         const float down = plain ? __uint_as_float((254u - e) << 23) : 1.f, up = plain ? __uint_as_float(e << 23) : 1.f;
 #pragma unroll
-        for (int w = 0; w < DP / (4 * kOwn); ++w)
+        for (int w = 0; w < DP / 64; ++w)
 #pragma unroll
-          for (int s = 0; s < kOwn / 4; ++s) {
-            q[n][w * (kOwn / 4) + s][0] = pack_f16(x[w][4 * s] * down, x[w][4 * s + 1] * down);
-            q[n][w * (kOwn / 4) + s][1] = pack_f16(x[w][4 * s + 2] * down, x[w][4 * s + 3] * down);
+          for (int s = 0; s < 4; ++s) {
+            q[n][w * 4 + s][0] = pack_f16(x[w][4 * s] * down, x[w][4 * s + 1] * down);
+            q[n][w * 4 + s][1] = pack_f16(x[w][4 * s + 2] * down, x[w][4 * s + 3] * down);
           }
 #pragma unroll
         for (int i = 0; i < 2; ++i) q_scale[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (tig * 2 + i) * 4);
@@ -313,40 +280,6 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
 #pragma unroll
             for (int n = 0; n < NT; ++n) product<kBf16>(s[u][n], f, q[n][k][0], q[n][k][1]);
           }
-      } else if constexpr (kFour) {
-#pragma unroll
-        for (int w = 0; w < DP / (4 * kOwn); ++w)
-#pragma unroll
-          for (int u = 0; u < kAtOnce; ++u) {
-            unsigned x[2][kOwn / 8], scale[2][kOwn / 16];                // of key_a, key_b
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int key = e ? key_b : key_a;
-              const unsigned char *tail = st_of[u] + 32 * kRow + key * S::kTail + 4;
-              if constexpr (kOwn == 32) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(st_of[u] + spread4<DP>(key, w * 4 + tig));
-                x[e][0] = v.x; x[e][1] = v.y; x[e][kOwn / 8 - 2] = v.z; x[e][kOwn / 8 - 1] = v.w;
-                const unsigned two = *reinterpret_cast<const unsigned short *>(tail + w * 8 + tig * 2);
-                scale[e][0] = group_scale(two & 0xffu) * 0x10001u;
-                scale[e][kOwn / 16 - 1] = group_scale(two >> 8) * 0x10001u;
-              } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(st_of[u] + spread4<DP>(key, tig >> 1) + (tig & 1) * 8);
-                x[e][0] = v.x; x[e][1] = v.y;
-                scale[e][0] = group_scale(tail[tig]) * 0x10001u;
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < kOwn / 8; ++k)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const unsigned sa = scale[0][k >> 1], sb = scale[1][k >> 1], xa = x[0][k], xb = x[1][k];
-                const unsigned f[4] = {times(half ? widen_e2m1<2>(xa) : widen_e2m1<0>(xa), sa), times(half ? widen_e2m1<2>(xb) : widen_e2m1<0>(xb), sb),
-                                       times(half ? widen_e2m1<3>(xa) : widen_e2m1<1>(xa), sa), times(half ? widen_e2m1<3>(xb) : widen_e2m1<1>(xb), sb)};
-                const int step = w * (kOwn / 4) + k * 2 + half;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) product<false>(s[u][n], f, q[n][step][0], q[n][step][1]);
-              }
-          }
       } else {
 #pragma unroll
         for (int w = 0; w < DP / 64; ++w) {
@@ -373,11 +306,7 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
         const int key0 = ((c + u) * slices + slice) * 16;
         float k_scale[2] = {1.f, 1.f};
         v_scale[u][0] = v_scale[u][1] = 1.f;
-        if constexpr (kFour) {
-          auto scale_of = [&](int record) { return *reinterpret_cast<const float *>(st + 32 * kRow + record * S::kTail) * kGroupUnit; };
-          k_scale[0] = scale_of(key_a); k_scale[1] = scale_of(key_b);
-          v_scale[u][0] = scale_of(16 + key_a); v_scale[u][1] = scale_of(16 + key_b);
-        } else if constexpr (kQuant) {
+        if constexpr (kQuant) {
           const float *sc = reinterpret_cast<const float *>(st + 32 * kRow);
           k_scale[0] = sc[key_a]; k_scale[1] = sc[key_b];
           v_scale[u][0] = sc[16 + key_a]; v_scale[u][1] = sc[16 + key_b];
@@ -549,47 +478,6 @@ __global__ void __launch_bounds__(Shape<FMT, DP>::kWarps * 32, 1) attend_rows_ke
             load_matrix4<true>(f, v_at + spread<false, DP>((lane & 7) + (lane >> 4) * 8, t * 2 + ((lane >> 3) & 1)));
 #pragma unroll
             for (int n = 0; n < NT; ++n) product<kBf16>(o[t][n], f, p[n][0], p[n][1]);
-          }
-        } else if constexpr (kFour) {
-          // The lane's keys are 4 * tig + 0..3, its channels gid * DP / 8 + 0 .. DP / 8 - 1.  Codes of two keys at one channel are brought into one
-          // byte: those of even channels of both, then the odd ones.
-          constexpr int kWords = DP / 64, kGroups = DP == 256 ? 2 : 1;
-          unsigned w[4][kWords], scale[2][kGroups];                        // of keys 0 and 1, 2 and 3
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = tig * 4 + j;
-            const unsigned char *v_row = st + 16 * kRow, *tail = st + 32 * kRow + (16 + key) * S::kTail + 4;
-            if constexpr (DP == 64) {
-              w[j][0] = *reinterpret_cast<const unsigned *>(v_row + spread4<DP>(key, gid >> 2) + (gid & 3) * 4);
-            } else if constexpr (DP == 128) {
-              const uint2 x = *reinterpret_cast<const uint2 *>(v_row + spread4<DP>(key, gid >> 1) + (gid & 1) * 8);
-              w[j][0] = x.x; w[j][1] = x.y;
-            } else {
-              const uint4 x = *reinterpret_cast<const uint4 *>(v_row + spread4<DP>(key, gid));
-              w[j][0] = x.x; w[j][1] = x.y; w[j][kWords - 2] = x.z; w[j][kWords - 1] = x.w;
-            }
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-              const unsigned one = group_scale(tail[DP == 64 ? gid >> 1 : gid * kGroups + g]);
-              if (j & 1) scale[j >> 1][g] |= one << 16; else scale[j >> 1][g] = one;
-            }
-          }
-#pragma unroll
-          for (int x = 0; x < kWords; ++x) {
-            unsigned even[2], odd[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              even[h] = (w[2 * h][x] & 0x0f0f0f0fu) | (w[2 * h + 1][x] << 4 & 0xf0f0f0f0u);
-              odd[h] = (w[2 * h][x] >> 4 & 0x0f0f0f0fu) | (w[2 * h + 1][x] & 0xf0f0f0f0u);
-            }
-            const unsigned s01 = scale[0][x >> 1 & (kGroups - 1)], s23 = scale[1][x >> 1 & (kGroups - 1)];
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              auto of = [&](unsigned word) { return b == 0 ? widen_e2m1<0>(word) : b == 1 ? widen_e2m1<1>(word) : b == 2 ? widen_e2m1<2>(word) : widen_e2m1<3>(word); };
-              const unsigned f[4] = {times(of(even[0]), s01), times(of(odd[0]), s01), times(of(even[1]), s23), times(of(odd[1]), s23)};
-#pragma unroll
-              for (int n = 0; n < NT; ++n) product<false>(o[x * 4 + b][n], f, p[n][0], p[n][1]);
-            }
           }
         } else {
           // the lane's keys are 4 * tig + 0..3, its channels gid * DP / 8 + 0 .. DP / 8 - 1

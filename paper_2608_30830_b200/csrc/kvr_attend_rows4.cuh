@@ -1,0 +1,577 @@
+// Attention for few query rows a KV head over a 4-bit cache.  The products, the key chunks and the joins are those of the row kernel
+// (kvr_attend_rows.cuh); what differs is how the cache gets to them, for 4 bits leave half as many cycles for a key.
+//
+// A warp of its own brings the keys of a stage for all heads of the CTA's group: TMA boxes of whole tokens (a group's records side by
+// side, K and V), or, for block sizes that are no multiple of 8, 16-byte copies.  The warps of the heads spend nothing on addresses.  A
+// stage's rows stand `stride` bytes apart, 32 more than a multiple of 128 where records are many (the boxes are wider than the rows):
+// then the rows that a read looks at (four keys, 32 bytes of each) fall into different banks, with keys 4 to 7 of each 8 swapped in pairs.
+//
+// An element is widened to code times its group's scale, exactly: a conversion of two codes and a product of two f16.  The head's
+// scale multiplies the score (K) or the probability (V).  No pattern of bits is widened to NaN or infinity (a NaN lies in the head's scale
+// alone), so what a row does not see needs no look at V.
+#pragma once
+#include "kvr_attend_common.cuh"
+
+namespace kvr {
+namespace {
+
+// ---- barriers and boxes
+__device__ __forceinline__ void bar4_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar4_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar4_expect(unsigned bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar4_try(unsigned bar, unsigned parity) {
+  unsigned ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// A warp's wait.  One that runs out (after `polls`) sets the flag and goes on like one that did not, on whatever is there, as do all later
+// ones at once: no role leaves its loops early, so that barriers between warps always meet.
+__device__ __forceinline__ void bar4_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned polls) {
+  unsigned spin = 0;
+  while (!bar4_try(bar, parity)) {
+    if (++spin >= polls) *gave_up = 1;
+    if ((spin & 15) == 0 && *gave_up) break;
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void box4_load(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int row, int block, int plane) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(row), "r"(block), "r"(plane) : "memory");
+}
+__device__ __forceinline__ void product4(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ unsigned transpose4(unsigned v) {
+  unsigned r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ unsigned times(unsigned x, unsigned scale) {
+  unsigned r;
+  asm("mul.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(scale));
+  return r;
+}
+template <int BYTE>
+__device__ __forceinline__ unsigned widen_times(unsigned w, unsigned scale) { return times(widen_e2m1<BYTE>(w), scale); }
+
+// Reads of shared memory, by address; volatile, so that they stay between the barriers.
+__device__ __forceinline__ unsigned lds1(unsigned at) { unsigned r; asm volatile("ld.shared.u8 %0, [%1];" : "=r"(r) : "r"(at)); return r; }
+__device__ __forceinline__ unsigned lds4(unsigned at) { unsigned r; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r) : "r"(at)); return r; }
+__device__ __forceinline__ uint2 lds8(unsigned at) { uint2 r; asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(at)); return r; }
+__device__ __forceinline__ uint4 lds16(unsigned at) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at));
+  return r;
+}
+
+constexpr int kMaxStages4 = 8;
+
+// EXACT: head_dim is DP, so that the scales' place is known.
+template <int DP, int NT, bool EXACT>
+__global__ void __launch_bounds__((rows4_warps(DP) + 1) * 32, 1)
+attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Rows4 r4, const __grid_constant__ CUtensorMap map) {
+  constexpr int kTiles = DP / 16, kAtOnce = rows4_at_once(DP, NT), kWide = DP / 64, kTails = DP == 256 ? 2 : 1;
+  constexpr float kLazy = 4.f;         // as in the row kernel
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ unsigned scratch[39];
+  __shared__ __align__(8) unsigned long long full[kMaxStages4], empty[kMaxStages4];
+  __shared__ int last_in, gave_up_word;
+  __shared__ Piece pieces[rows4_warps(DP)];     // of the heads' warps, whose registers are the products'
+  volatile int *gave_up = &gave_up_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const int slices = r4.slices, stride = r4.stride, warps = a.group_heads * slices, stage_keys = 16 * slices;
+  const int plane_bytes = stage_keys * stride, stage_bytes = 2 * plane_bytes;
+
+  Shares shares;
+  Piece start;
+  if (!find_share(a, scratch, shares, start.r, start.base, start.len)) return;
+  const unsigned first = shares.first(blockIdx.x), last = shares.first(blockIdx.x + 1);
+  start.unit = first;
+  if (!open_piece(a, start, last)) return;     // an opening alone
+  if (threadIdx.x == 0) {
+    gave_up_word = a.polls == 0;
+    for (int i = 0; i < r4.stages; ++i) { bar4_init(shared_at(&full[i]), r4.box_rows ? 1 : 32); bar4_init(shared_at(&empty[i]), warps); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp < warps && lane == 0) pieces[warp] = start;
+  __syncthreads();
+  // Stages of a piece, kAtOnce of which are a turn.  (The last one may lie behind the keys.)
+  const int unit_stages = (int)a.unit.d / stage_keys;
+  auto stage_end = [&](const Piece &p) { return min(p.end * unit_stages, (p.len.keys + kAtOnce * stage_keys - 1) / (kAtOnce * stage_keys) * kAtOnce); };
+
+  if (warp == warps) {
+    // ---- loads
+    int stage = 0, t = start.begin * unit_stages, end = stage_end(start);
+    unsigned round = 0;                // of the ring
+    bool more = true;
+    // the ids of a stage's first 32 boxes are fetched a stage ahead
+    int next_id = 0;
+    auto fetch_ids = [&]() {
+      const int token = t * stage_keys + lane * r4.box_rows;
+      if (more && lane * r4.box_rows < stage_keys && token < start.len.keys)
+        next_id = __ldg(a.b.tables + (long long)start.r * a.b.table_stride + a.bs.div((unsigned)token));
+    };
+    if (r4.box_rows) fetch_ids();
+    while (more) {
+      const int key0 = t * stage_keys, keys = min(stage_keys, start.len.keys - key0), x0 = start.head_group * a.group_heads * a.c.head_bytes;
+      unsigned char *st = smem + stage * stage_bytes;
+      const unsigned bar = shared_at(&full[stage]);
+      if (round) bar4_wait(shared_at(&empty[stage]), (round - 1) & 1, gave_up, a.polls);
+      if (r4.box_rows) {
+        // a lane a box of K and a box of V
+        const int boxes = keys > 0 ? (keys + r4.box_rows - 1) / r4.box_rows : 0;
+        if (boxes == 0 && lane == 0) bar4_arrive(bar);
+        for (int b0 = 0; b0 < boxes; b0 += 32) {
+          const int box = b0 + lane, token = key0 + box * r4.box_rows;
+          const bool in = box < boxes;
+          const unsigned block = a.bs.div((unsigned)token);
+          const int id = !in ? 0 : b0 == 0 ? next_id : __ldg(a.b.tables + (long long)start.r * a.b.table_stride + block);
+          const bool known = in && (unsigned)id < (unsigned)a.c.num_blocks;
+          unsigned char *to = st + box * r4.box_bytes;
+          if (in && !known) {          // a block that is not there
+            report(a.b.status, KVR_DEV_BAD_BLOCK);
+            for (int i = 0; i < r4.box_bytes; i += 16)
+              *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<uint4 *>(to + plane_bytes + i) = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
+          if (lane == 0) {
+            // all of the stage's bytes are expected by the one arrival, which comes with the last 32 boxes
+            if (b0 + 32 >= boxes) bar4_expect(bar, got * 2 * r4.box_bytes);
+            else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(got * 2 * r4.box_bytes) : "memory");
+          }
+          __syncwarp();
+          if (known) {
+            const int row = token - (int)block * (int)a.bs.d;
+            box4_load(shared_at(to), &map, bar, x0 >> 3, row, id, 0);
+            box4_load(shared_at(to + plane_bytes), &map, bar, x0 >> 3, row, id, 1);
+          }
+          __syncwarp();
+        }
+      } else {
+        const int columns = min(a.group_heads * a.c.head_bytes, a.c.kv_heads * a.c.head_bytes - x0) / 16;
+        for (int k0 = 0; k0 < keys; k0 += 32) {
+          // a lane finds a key
+          const int key = k0 + lane;
+          const long long found = key < keys ? token_offset(a.b, a.c, a.bs, start.r, key0 + key) : -1;
+          if (found < 0 && key < keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
+          const int n = min(32, keys - k0) * columns;
+          for (int i = lane; i - lane < n; i += 32) {
+            const int k = min(i / columns, 31), column = i - k * columns;
+            const long long off = __shfl_sync(0xffffffffu, found, k);
+            if (i >= n) continue;
+            const char *src = a.c.base + (off >= 0 ? off + x0 + column * 16 : 0);
+            const unsigned to = shared_at(st + (k0 + k) * stride) + column * 16;
+            copy16(to, src, off >= 0);
+            copy16(to + plane_bytes, src + (off >= 0 ? a.c.v_offset : 0), off >= 0);
+          }
+          __syncwarp();
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+      }
+      if (++stage == r4.stages) { stage = 0; ++round; }
+      if (++t == end) {
+        more = next_piece(a, start, last);
+        t = start.begin * unit_stages;
+        end = stage_end(start);
+      }
+      if (r4.box_rows) fetch_ids();
+    }
+    copy_wait<0>();
+  } else {
+    // ---- products and softmax
+    const Piece &piece = pieces[warp];
+    int stage = 0;                     // of the ring
+    unsigned round = 0;
+    auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory"); return true; };
+    const int local_head = warp / slices, slice = warp - local_head * slices;
+    float *merge = reinterpret_cast<float *>(smem + r4.stages * stage_bytes);
+    const int swapped = gid ^ (gid >> 2), first_key = (2 * tig) ^ (tig >> 1), codes = EXACT ? DP / 2 : a.c.scale_offset;
+    // what a lane reads: K's rows of key `swapped` and + 8, V's of four keys
+    const unsigned k_first = shared_at(smem) + (slice * 16 + swapped) * stride + local_head * a.c.head_bytes;
+    const unsigned v_first = shared_at(smem) + plane_bytes + (slice * 16 + first_key) * stride + local_head * a.c.head_bytes;
+    const int v_step = tig < 2 ? stride : -stride;
+    for (bool again = true; again;) {
+      const Lengths &len = piece.len;
+      const int context = len.context, head = piece.head_group * a.group_heads + local_head;
+      const int rows = min(a.row_tile, len.fresh * (int)a.group.d - piece.row0);     // of this tile
+      const bool live = head < a.c.kv_heads;
+      // Q^T fragments: k-step (group of 64 channels w, s) has channels 64 w + 16 tig + 4 s + 0..3
+      unsigned q[NT][kTiles][2];
+      float q_scale[NT][2];            // of the rows whose scores this lane holds (tig * 2, + 1)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int row = piece.row0 + n * 8 + gid;
+        const bool have = live && n * 8 + gid < rows;
+        const int t = have ? (int)a.group.div(row) : 0, g = have ? row - t * (int)a.group.d : 0;
+        const char *src = a.q.data + (long long)(len.first + t) * a.q.token_stride + (long long)((live ? head : 0) * (int)a.group.d + g) * a.q.head_stride;
+        float top = 0.f;
+        float x[kWide][16];
+#pragma unroll
+        for (int w = 0; w < kWide; ++w) {
+          const int d = w * 64 + tig * 16;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float y[8] = {};
+            if (have && d < a.c.head_dim) {
+              if (a.q.type == KVR_BF16) load8<KVR_BF16>(src + (d + h * 8) * 2, y);
+              else load8<KVR_F16>(src + (d + h * 8) * 2, y);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { x[w][h * 8 + i] = y[i]; top = fmaxf(top, fabsf(y[i])); }
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^-e with 2^e <= top < 2^(e+1), by the exponent's bits; rows of zeros, subnormals and infinities stay as they are
+        const unsigned e = __float_as_uint(top) >> 23;
+        const bool plain = e >= 1 && e <= 253;
+        const float down = plain ? __uint_as_float((254u - e) << 23) : 1.f, up = plain ? __uint_as_float(e << 23) : 1.f;
+#pragma unroll
+        for (int w = 0; w < kWide; ++w)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            q[n][w * 4 + s][0] = pack_f16(x[w][4 * s] * down, x[w][4 * s + 1] * down);
+            q[n][w * 4 + s][1] = pack_f16(x[w][4 * s + 2] * down, x[w][4 * s + 3] * down);
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) q_scale[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (tig * 2 + i) * 4);
+      }
+      float o[kTiles][NT][4] = {};
+      float top[NT][2], base[NT][2], sum[NT][2], unit[NT][2];        // base: top, 0 where that is -infinity; unit: of V's scales
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          top[n][e] = -INFINITY;
+          base[n][e] = sum[n][e] = 0.f;
+          unit[n][e] = unit_first(n * 8 + tig * 2 + e < rows);
+        }
+
+      const int end = stage_end(piece);
+      for (int t = piece.begin * unit_stages; t < end; t += kAtOnce) {
+        unsigned k_at[kAtOnce], v_at[kAtOnce];
+        int used[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          bar4_wait(shared_at(&full[stage]), round & 1, gave_up, a.polls);
+          k_at[u] = k_first + stage * stage_bytes;
+          v_at[u] = v_first + stage * stage_bytes;
+          used[u] = stage;
+          if (++stage == r4.stages) { stage = 0; ++round; }
+        }
+        const int key0 = (t * slices + slice) * 16;          // of the first chunk; the next starts 16 * slices further on
+        const bool edge = key0 + ((kAtOnce - 1) * slices + 1) * 16 > context;
+
+        // S^T = K Q^T; the chunks' products in turn, for a product waits for the one before it
+        float s[kAtOnce][NT][4] = {}, v_scale[kAtOnce][2], k_scale[kAtOnce][2];
+        uint4 tail[kAtOnce][2];        // of K's records: the head's scale, groups 0 to 11
+        unsigned more[kAtOnce][2];     // groups 12 to 15
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const unsigned row = k_at[u] + e * 8 * stride + codes;
+            tail[u][e] = lds16(row);
+            if constexpr (kTails == 2) more[u][e] = lds8(row + 16).x;
+            k_scale[u][e] = __uint_as_float(tail[u][e].x) * kGroupUnit;
+            v_scale[u][e] = __uint_as_float(lds4(row + plane_bytes)) * kGroupUnit;
+          }
+#pragma unroll
+        for (int w = 0; w < kWide; ++w) {
+          uint2 x[kAtOnce][2];
+          unsigned scale[kAtOnce][2];
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              x[u][e] = lds8(k_at[u] + e * 8 * stride + tig * 8 + w * 32);
+              const unsigned four = w == 0 ? tail[u][e].y : w == 1 ? tail[u][e].z : w == 2 ? tail[u][e].w : more[u][e];
+              scale[u][e] = (four >> (tig * 8) & 0x7fu) * 0x00800080u;
+            }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+              const unsigned xa = k < 2 ? x[u][0].x : x[u][0].y, xb = k < 2 ? x[u][1].x : x[u][1].y, sa = scale[u][0], sb = scale[u][1];
+              const unsigned f[4] = {k & 1 ? widen_times<2>(xa, sa) : widen_times<0>(xa, sa), k & 1 ? widen_times<2>(xb, sb) : widen_times<0>(xb, sb),
+                                     k & 1 ? widen_times<3>(xa, sa) : widen_times<1>(xa, sa), k & 1 ? widen_times<3>(xb, sb) : widen_times<1>(xb, sb)};
+#pragma unroll
+              for (int n = 0; n < NT; ++n) product4(s[u][n], f, q[n][w * 4 + k][0], q[n][w * 4 + k][1]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[u][n][i] *= q_scale[n][i & 1] * k_scale[u][i >> 1];
+        if (edge) {                    // what a row does not see
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int j = key0 + u * slices * 16 + swapped + i * 8 - context;      // among the new tokens
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const int row = n * 8 + tig * 2 + e;
+                  const bool seen = j < 0 || (j < len.fresh && row < rows && sees(a, len.first, (int)a.group.div(piece.row0 + row), j));
+                  if (!seen) s[u][n][i * 2 + e] = -INFINITY;
+                }
+            }
+        }
+
+        // running maximum of each row, over the 8 lanes that share it
+        float best[NT][2];
+        bool moved = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = fmaxf(s[0][n][e], s[0][n][2 + e]);
+            if constexpr (kAtOnce == 2) m = max3(m, s[kAtOnce - 1][n][e], s[kAtOnce - 1][n][2 + e]);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            best[n][e] = m;
+            moved = moved || m > top[n][e] + kLazy;                    // from -infinity: any score moves it
+          }
+        float big = fmaxf(v_scale[0][0], v_scale[0][1]);
+        if constexpr (kAtOnce == 2) big = max3(big, v_scale[kAtOnce - 1][0], v_scale[kAtOnce - 1][1]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) moved = moved || big * unit[n][e] >= kUnitLimit;
+        if (__builtin_expect(__any_sync(0xffffffffu, moved), 0)) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              // the largest of V's scales that the row sees
+              float own = 0.f;
+#pragma unroll
+              for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                  if (s[u][n][i * 2 + e] != -INFINITY) own = fmaxf(own, v_scale[u][i]);
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 4));
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 8));
+              own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 16));
+              float less = 1.f;
+              if (own * unit[n][e] >= kUnitLimit) {
+                less = unit_of(own) * unit_back(unit[n][e]);
+                unit[n][e] = unit_of(own);
+              }
+              const float was = top[n][e];
+              if (best[n][e] > was + kLazy) top[n][e] = best[n][e];
+              const float f = was == top[n][e] ? 1.f : exp2_fast(was - top[n][e]);     // was = -infinity: 0
+              base[n][e] = top[n][e] == -INFINITY ? 0.f : top[n][e];
+              sum[n][e] *= f;
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t) {
+                o[t][n][e] *= f * less;
+                o[t][n][2 + e] *= f * less;
+              }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          // P^T, as the right operand of the second product
+          unsigned p[NT][2];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float pf[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = exp2_fast(s[u][n][i] - base[n][i & 1]);
+              sum[n][i & 1] += x;
+              pf[i] = x * (v_scale[u][i >> 1] * unit[n][i & 1]);
+            }
+            if (edge) {                // a scale that is not finite, at a key that the row does not see
+#pragma unroll
+              for (int i = 0; i < 4; ++i) if (s[u][n][i] == -INFINITY) pf[i] = 0.f;
+            }
+            p[n][0] = transpose4(pack_f16(pf[0], pf[1]));
+            p[n][1] = transpose4(pack_f16(pf[2], pf[3]));
+          }
+          // O^T += V^T P^T.  The lane's keys are rows 2 tig, 2 tig + 1, + 8, + 9 of S^T, its channels gid * DP / 8 + 0 .. DP / 8 - 1.  Codes of two keys
+          // at one channel are brought into one byte: those of even channels, then of odd ones.
+          constexpr int kWords = DP / 64;
+          unsigned w[4][kWords], scale[2][kTails];                       // of keys 0 and 1, 2 and 3
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const unsigned row = v_at[u] + (j & 1 ? v_step : 0) + (j >> 1) * 8 * stride;
+            if constexpr (DP == 64) {
+              w[j][0] = lds4(row + gid * 4);
+            } else if constexpr (DP == 128) {
+              const uint2 x = lds8(row + gid * 8);
+              w[j][0] = x.x; w[j][kWords - 1] = x.y;
+            } else {
+              const uint4 x = lds16(row + gid * 16);
+              w[j][0] = x.x; w[j][1 % kWords] = x.y; w[j][2 % kWords] = x.z; w[j][3 % kWords] = x.w;
+            }
+#pragma unroll
+            for (int g = 0; g < kTails; ++g) {
+              const unsigned byte = lds1(row + (DP == 64 ? gid >> 1 : gid * kTails) + codes + 4 + g);
+              if (j & 1) scale[j >> 1][g] = ((scale[j >> 1][g] | byte << 16) << 7) & 0x3f803f80u; else scale[j >> 1][g] = byte;
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) {
+            unsigned even[2], odd[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              even[h] = (w[2 * h][x] & 0x0f0f0f0fu) | (w[2 * h + 1][x] << 4 & 0xf0f0f0f0u);
+              odd[h] = (w[2 * h][x] >> 4 & 0x0f0f0f0fu) | (w[2 * h + 1][x] & 0xf0f0f0f0u);
+            }
+            const unsigned s01 = scale[0][kTails == 2 ? x >> 1 & 1 : 0], s23 = scale[1][kTails == 2 ? x >> 1 & 1 : 0];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              auto of = [&](unsigned word) { return b == 0 ? widen_e2m1<0>(word) : b == 1 ? widen_e2m1<1>(word) : b == 2 ? widen_e2m1<2>(word) : widen_e2m1<3>(word); };
+              const unsigned f[4] = {times(of(even[0]), s01), times(of(odd[0]), s01), times(of(even[1]), s23), times(of(odd[1]), s23)};
+#pragma unroll
+              for (int n = 0; n < NT; ++n) product4(o[x * 4 + b][n], f, p[n][0], p[n][1]);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) bar4_arrive(shared_at(&empty[used[u]]));
+        }
+      }
+
+      // ---- the piece's result
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 4);
+          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 8);
+          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 16);
+        }
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][n][i] *= unit_back(unit[n][i & 1]);
+      if (slices > 1) {
+        // slices of a head are joined through shared memory, one n-tile at a time, in slice order
+        constexpr int kPer = DP * 8 + 16;                                // accumulators, then (maximum, sum) of 8 rows
+        const int heads = a.group_heads;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float *mine = merge + ((slice - 1) * heads + local_head) * kPer;
+          if (slice > 0) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mine[(t * 4 + i) * 32 + lane] = o[t][n][i];
+            if (gid == 0) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                mine[DP * 8 + (tig * 2 + e) * 2] = top[n][e];
+                mine[DP * 8 + (tig * 2 + e) * 2 + 1] = sum[n][e];
+              }
+            }
+          }
+          meet();
+          if (slice == 0) {
+            for (int s = 1; s < slices; ++s) {
+              const float *other = merge + ((s - 1) * heads + local_head) * kPer;
+              float f[2], g[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float m2 = other[DP * 8 + (tig * 2 + e) * 2], l2 = other[DP * 8 + (tig * 2 + e) * 2 + 1];
+                const float m = fmaxf(top[n][e], m2);
+                f[e] = top[n][e] == m ? 1.f : exp2_fast(top[n][e] - m);
+                g[e] = m2 == m ? 1.f : exp2_fast(m2 - m);
+                if (m == -INFINITY) g[e] = 0.f;
+                sum[n][e] = sum[n][e] * f[e] + l2 * g[e];
+                top[n][e] = m;
+              }
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[t][n][i] = o[t][n][i] * f[i & 1] + other[(t * 4 + i) * 32 + lane] * g[i & 1];
+            }
+          }
+          meet();
+        }
+      }
+      if (slice == 0 && live) {
+        const bool whole = piece.begin == 0 && piece.end == len.units;
+        const long long slot = ((long long)blockIdx.x * 2 + (piece.unit == first ? 0 : 1)) * a.group_heads + local_head;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int row = n * 8 + tig * 2 + e;
+            if (row >= rows) continue;
+            const int t_row = (int)a.group.div(piece.row0 + row);
+            const int q_head = head * (int)a.group.d + (piece.row0 + row - t_row * (int)a.group.d);
+            const float inv = !whole ? 1.f : sum[n][e] > 0.f ? 1.f / sum[n][e] : sum[n][e] == 0.f ? 0.f : NAN;
+            char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
+            float *part = a.part_o + (slot * a.row_tile + row) * a.c.head_dim;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int d = gid * (DP / 8) + t * 2 + h;
+                if (d >= a.c.head_dim) continue;
+                const float x = o[t][n][h * 2 + e] * inv;
+                if (!whole) part[d] = x;
+                else if (a.out.type == KVR_BF16) reinterpret_cast<__nv_bfloat16 *>(dst)[d] = __float2bfloat16_rn(x);
+                else reinterpret_cast<__half *>(dst)[d] = __float2half_rn(x);
+              }
+            if (gid == 0) {
+              if (!whole) a.part_ml[slot * a.row_tile + row] = make_float2(top[n][e], sum[n][e]);
+              else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum[n][e] == 0.f ? -INFINITY : top[n][e] * 0.69314718f + logf(sum[n][e]);
+            }
+          }
+      }
+      if (piece.begin != 0 || piece.end != len.units) {
+        const int heads = min(a.group_heads, a.c.kv_heads - piece.head_group * a.group_heads);
+        hand_in(a, piece, shares, meet, &last_in, warp, lane, [&](const Cut &cut, int c, int step, int n, bool fold) {
+          join_pieces<DP / 128 + DP % 128 / 64>(a, piece, cut, c, step, n, fold, rows, heads, warps, warp, lane);
+        });
+      }
+      __syncwarp();
+      if (lane == 0) {
+        Piece next = piece;
+        again = next_piece(a, next, last);
+        pieces[warp] = next;
+      }
+      again = __shfl_sync(0xffffffffu, again, 0);
+    }
+  }
+  __syncthreads();
+  if (gave_up_word) {
+    // boxes that were under way when a wait ran out still land in shared memory: a fifth of a millisecond is ample
+    for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
+    if (threadIdx.x == 0) report(a.b.status, KVR_DEV_GAVE_UP);
+    __syncthreads();
+  }
+}
+
+template <int DP, int NT, bool EXACT>
+cudaError_t launch_rows4(const AttendArgs &a, const Rows4 &r4, const CUtensorMap &map, cudaStream_t s) {
+  const int merge = r4.slices > 1 ? (r4.slices - 1) * a.group_heads * (DP * 8 + 16) * 4 : 0;
+  const int bytes = r4.stages * 32 * r4.slices * r4.stride + (merge > 256 ? merge : 256);    // 256: reads past a record's end
+  static OncePerDevice once;
+  if (const cudaError_t e = allow_shared(once, attend_rows4_kernel<DP, NT, EXACT>, kRows4Shared)) return e;
+  attend_rows4_kernel<DP, NT, EXACT><<<a.ctas, (a.group_heads * r4.slices + 1) * 32, bytes, s>>>(a, r4, map);
+  return cudaGetLastError();
+}
+template <int DP>
+cudaError_t launch_rows4(const AttendArgs &a, int tiles, const Rows4 &r4, const CUtensorMap &map, cudaStream_t s) {
+  if (a.c.head_dim == DP) return tiles == 1 ? launch_rows4<DP, 1, true>(a, r4, map, s) : launch_rows4<DP, 2, true>(a, r4, map, s);
+  return tiles == 1 ? launch_rows4<DP, 1, false>(a, r4, map, s) : launch_rows4<DP, 2, false>(a, r4, map, s);
+}
+
+}  // namespace
+}  // namespace kvr
