@@ -55,9 +55,10 @@ bool layer_map(const kvr_cache_spec *s, const CacheView &c, int padded, int box_
   if (!encode) return false;
   const bool quant = quantised(s->format);
   const cuuint64_t element = quant ? 1 : 2;
-  const cuuint64_t dims[5] = {(cuuint64_t)s->head_dim, (cuuint64_t)s->kv_heads, (cuuint64_t)s->block_size, (cuuint64_t)s->num_blocks, 2};
-  const cuuint64_t strides[4] = {s->head_dim * element, (cuuint64_t)c.row_bytes, (cuuint64_t)c.block_stride, (cuuint64_t)c.v_offset};
-  const cuuint32_t box[5] = {(cuuint32_t)(quant ? padded : 64), 1, (cuuint32_t)box_rows, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+  const int head = four_bit(s->format) ? c.head_bytes : s->head_dim;      // elements of a head: records by the byte
+  const cuuint64_t dims[5] = {(cuuint64_t)head, (cuuint64_t)s->kv_heads, (cuuint64_t)s->block_size, (cuuint64_t)s->num_blocks, 2};
+  const cuuint64_t strides[4] = {head * element, (cuuint64_t)c.row_bytes, (cuuint64_t)c.block_stride, (cuuint64_t)c.v_offset};
+  const cuuint32_t box[5] = {(cuuint32_t)(four_bit(s->format) ? head : quant ? padded : 64), 1, (cuuint32_t)box_rows, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
   return encode(map, quant ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, c.base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 quant ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -115,7 +116,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   int tiles = 0, slices = 0;
   CUtensorMap map{};
   Rows4 r4{};
-  if (rows > 16 && padded <= 128 && !four) {
+  if (rows > 16 && padded <= 128) {
     // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
     // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
     // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels stay with the row kernel: two jobs' sums and scores

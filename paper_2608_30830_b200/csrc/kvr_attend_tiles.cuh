@@ -125,7 +125,7 @@ __device__ __forceinline__ void box_load(unsigned dst, const CUtensorMap *map, u
 
 template <int FMT, int DP, bool TWO>
 struct TileShape {
-  static constexpr bool kQuant = quantised(FMT);
+  static constexpr bool kQuant = quantised(FMT), kFour = four_bit(FMT);
   static constexpr int kBlocks = DP / 64;                                // 128-byte columns of a row
   // Warps: 0..7 softmax, 8 issues the products, the others load.  Whole warpgroups: registers are dealt to those.
   static constexpr int kSteps = 3, kPerStep = kQuant ? 2 : 1;         // steps loaded at a time, warps of a step
@@ -140,7 +140,8 @@ struct TileShape {
   // having filled step s - kSteps, and a barrier's parity is clear only if step s - 2 kRing is known to be over.
   static constexpr int kRing = (kQuant ? 3 : 5) + (kQuant && !TWO ? 1 : 0);
   static_assert(kRing >= kSteps, "");
-  static constexpr int kRaw = kTileKeys * DP;                            // codes of K or V of a tile
+  static constexpr int kRaw = kTileKeys * DP;                            // codes (4 bits: records, which are no longer) of K or V of a tile
+  static_assert(!kFour || record_bytes(DP) <= DP, "");
   static constexpr int kScaleSlots = kQuant ? 4 : 0;                     // 128 scales of K, 128 of V
   static constexpr int kBytes = kQBytes + kRing * kBuffer + (kQuant ? kSteps * (kRaw + 2 * kTileKeys * 4) : 0) + kScaleSlots * 1024 + 1024;
 };
@@ -329,11 +330,20 @@ __device__ __noinline__ unsigned nan_channels(const AttendArgs &a, const Lengths
   return bits;
 }
 
+// 8 codes times their group's scale, as f16
+__device__ __forceinline__ uint4 widen_group(unsigned w, unsigned scale) {
+  auto times = [&](unsigned x) {
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&scale));
+    return *reinterpret_cast<const unsigned *>(&v);
+  };
+  return make_uint4(times(widen_e2m1<0>(w)), times(widen_e2m1<1>(w)), times(widen_e2m1<2>(w)), times(widen_e2m1<3>(w)));
+}
+
 template <int FMT, int DP, bool TWO>
 __global__ void __launch_bounds__(TileShape<FMT, DP, TWO>::kThreads, 1)
 attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
   using S = TileShape<FMT, DP, TWO>;
-  constexpr bool kQuant = S::kQuant, kBf16 = FMT == KVR_CACHE_BF16;
+  constexpr bool kQuant = S::kQuant, kFour = S::kFour, kBf16 = FMT == KVR_CACHE_BF16;
   constexpr int kAhead = TWO ? 1 : 2;            // key tiles whose scores are made before the first is used
   constexpr float kLazy = kQuant ? 4.f : 8.f;    // 8-bit: leaves room for V's scale, see the row kernel
   extern __shared__ unsigned char raw_smem[];
@@ -390,7 +400,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     const int me = warp - 9, group = me / S::kPerStep, span0 = (me % S::kPerStep) * S::kSpan;
     constexpr int kElement = kQuant ? 1 : 2, kChunks = DP * kElement / 16, kAtOnce = 32 / kChunks;
     const int chunk = lane % kChunks, sub = lane / kChunks;
-    const int used = a.c.head_dim * kElement / 16;
+    const int staged = kFour ? a.c.head_bytes : DP * kElement;   // of a key in the staging area
+    const int used = a.c.head_bytes / 16;
     TileWalk<kAhead> at;
     at.p = piece; at.step = at.tiles = 0; at.more = true;
     at.open(a, unit_tiles);
@@ -428,18 +439,18 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         const int box = lane / kWide, part = lane % kWide, boxes = per_tile / S::kPerStep;
         const int id = box < boxes ? ids[(key0 / a.box_rows + box) & 63] : 0;
         if (__all_sync(0xffffffffu, (unsigned)id < (unsigned)a.c.num_blocks)) {
-          if (lane == 0) bar_expect(shared_at(bar), S::kSpan * DP * kElement);
+          if (lane == 0) bar_expect(shared_at(bar), S::kSpan * staged);
           __syncwarp();
           if (box < boxes) {
             const int token = key0 + box * a.box_rows, row = token - (int)a.bs.div(token) * (int)a.bs.d;
-            unsigned char *to = kQuant ? dst + box * a.box_rows * DP : dst + part * (kTileKeys * 128) + box * a.box_rows * 128;
+            unsigned char *to = kQuant ? dst + box * a.box_rows * staged : dst + part * (kTileKeys * 128) + box * a.box_rows * 128;
             box_load(shared_at(to), &map, shared_at(bar), part * 64, at.p.head_group, row, id, v);
           }
           __syncwarp();
           return true;
         }
       }
-      const char *base = a.c.base + (v ? a.c.v_offset : 0) + at.p.head_group * a.c.head_dim * kElement;
+      const char *base = a.c.base + (v ? a.c.v_offset : 0) + at.p.head_group * a.c.head_bytes;
 #pragma unroll 1
       for (int k0 = 0; k0 < S::kSpan; k0 += 32) {
         // a lane finds a key; a wait for the table in every turn below came to 10 us a tile
@@ -452,7 +463,8 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           const long long off = __shfl_sync(0xffffffffu, found, i * kAtOnce + sub);
           const bool got = off >= 0 && chunk < used;
           const char *src = got ? base + off + chunk * 16 : a.c.base;
-          if constexpr (kQuant) copy16(shared_at(dst + key * DP + chunk * 16), src, got);
+          if constexpr (kFour) { if (chunk < used) copy16(shared_at(dst + key * staged + chunk * 16), src, got); }
+          else if constexpr (kQuant) copy16(shared_at(dst + key * DP + chunk * 16), src, got);
           else copy16(shared_at(dst + (chunk >> 3) * (kTileKeys * 128) + key * 128 + (((chunk & 7) ^ (key & 7)) << 4)), src, got);
         }
       }
@@ -529,7 +541,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             } else if (j < at.p.len.keys) {
               off = token_offset(a.b, a.c, a.bs, at.p.r, j);
             }
-            const char *src = a.c.base + (off >= 0 ? off + a.c.scale_offset + 4 * at.p.head_group : 0);
+            const char *src = a.c.base + (off >= 0 ? off + a.c.scale_offset + (kFour ? a.c.head_bytes : 4) * at.p.head_group : 0);
             copy4(shared_at(scale_stage + h + lane), src, off >= 0);
             copy4(shared_at(scale_stage + kTileKeys + h + lane), src + (off >= 0 ? a.c.v_offset : 0), off >= 0);
           }
@@ -554,6 +566,19 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           // softmax threads are told that there were some (append stores none).
           if (clear_nan<DP, S::kSpan>(stage, lane)) odd_codes = 1;
         }
+        if constexpr (kFour) {
+          // 16 channels are a group: 8 bytes of codes and one scale, which goes into the elements (exact)
+          const unsigned char *record = stage + sub * staged;
+#pragma unroll 4
+          for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
+            const int key = i * kAtOnce + sub;
+            const uint2 x = *reinterpret_cast<const uint2 *>(record + i * kAtOnce * staged + chunk * 8);
+            const unsigned scale = group_scale(record[i * kAtOnce * staged + a.c.scale_offset + 4 + chunk]) * 0x10001u;
+            unsigned char *to = row + i * (kAtOnce * 128);
+            *reinterpret_cast<uint4 *>(to + (((c0 + swap) ^ (key & 7)) << 4)) = widen_group(swap ? x.y : x.x, scale);
+            *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) = widen_group(swap ? x.x : x.y, scale);
+          }
+        } else {
 #pragma unroll 4
         for (int i = 0; i < S::kSpan / kAtOnce; ++i) {
           const int key = i * kAtOnce + sub;             // kAtOnce is even: the key's parity is sub's
@@ -564,11 +589,12 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           *reinterpret_cast<uint4 *>(to + (((c0 + 1 - swap) ^ (key & 7)) << 4)) =
               make_uint4(widen<FMT, false>(y.x), widen<FMT, true>(y.x), widen<FMT, false>(y.y), widen<FMT, true>(y.y));
         }
+        }
         if (!v) {
 #pragma unroll
           for (int h = 0; h < S::kSpan; h += 32) {
-            scales[scale_slot * 256 + span0 + h + lane] = scale_stage[h + lane];
-            scales[scale_slot * 256 + 128 + span0 + h + lane] = scale_stage[kTileKeys + h + lane];
+            scales[scale_slot * 256 + span0 + h + lane] = scale_stage[h + lane] * (kFour ? kGroupUnit : 1.f);
+            scales[scale_slot * 256 + 128 + span0 + h + lane] = scale_stage[kTileKeys + h + lane] * (kFour ? kGroupUnit : 1.f);
           }
         }
         fence_async();
