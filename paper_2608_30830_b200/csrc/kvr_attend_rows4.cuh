@@ -70,6 +70,82 @@ __device__ __forceinline__ uint4 lds16(unsigned at) {
 
 constexpr int kMaxStages4 = 8;
 
+// The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  A thread 4 channels of
+// a row, 8 pieces' loads under way at a time.  Out of line: the loop's registers are the products'.
+__device__ __noinline__ void join4(const AttendArgs &a, const Piece &p, const Cut &cut, int c, int step, int n, bool fold, int rows, int heads, int threads) {
+  constexpr int kAhead = 8;
+  const int quads = a.c.head_dim >> 2, items = rows * heads * quads;
+  const long long stride = (long long)step * 2 * a.group_heads * a.row_tile;     // rows from one piece to the next
+  // the first CTA of a segment may hold it as its second piece, all others as their first
+  const long long second = c == cut.c0 && cut.which0 ? (long long)a.group_heads * a.row_tile : 0;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < items; i += threads) {
+    const int both = i / quads, d = (i - both * quads) * 4, lh = both / rows, row = both - lh * rows;
+    const long long at = ((long long)c * 2 * a.group_heads + lh) * a.row_tile + row;
+    float m = -INFINITY, l = 0.f, o[4] = {};
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += kAhead) {
+      float2 ml[kAhead];
+      float4 x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + k < n) {
+          const long long from = at + (k0 + k) * stride + (k0 + k == 0 ? second : 0);
+          ml[k] = __ldcg(a.part_ml + from);
+          x[k] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + from * a.c.head_dim + d));
+        }
+      }
+      float best = m;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) best = fmaxf(best, ml[k].x);
+      const float was = m == best ? 1.f : exp2_fast(m - best);             // both -infinity: pieces of an empty row
+      l *= was;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= was;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float f = ml[k].x == best ? 1.f : exp2_fast(ml[k].x - best);
+        l += ml[k].y * f;
+        o[0] += x[k].x * f; o[1] += x[k].y * f; o[2] += x[k].z * f; o[3] += x[k].w * f;
+      }
+      m = best;
+    }
+    if (fold) {
+      *reinterpret_cast<float4 *>(a.part_o + (at + second) * a.c.head_dim + d) = make_float4(o[0], o[1], o[2], o[3]);
+      continue;                        // maximum and sum are read by other threads too: fold4
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+    const int t = (int)a.group.div(p.row0 + row), q_head = (p.head_group * a.group_heads + lh) * (int)a.group.d + (p.row0 + row - t * (int)a.group.d);
+    char *dst = a.out.data + (long long)(p.len.first + t) * a.out.token_stride + (long long)q_head * a.out.head_stride + d * 2;
+    uint2 w;
+    if (a.out.type == KVR_BF16) w = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    else w = make_uint2(pack_f16(o[0] * inv, o[1] * inv), pack_f16(o[2] * inv, o[3] * inv));
+    *reinterpret_cast<uint2 *>(dst) = w;
+    if (a.lse && d == 0) a.lse[(long long)(p.len.first + t) * a.q_heads + q_head] = l == 0.f ? -INFINITY : m * 0.69314718f + logf(l);
+  }
+}
+
+// Behind join4 (fold), when all its threads are through: the rows' maxima and sums.
+__device__ __noinline__ void fold4(const AttendArgs &a, const Cut &cut, int c, int step, int n, int rows, int heads, int threads) {
+  const long long stride = (long long)step * 2 * a.group_heads * a.row_tile;
+  const long long second = c == cut.c0 && cut.which0 ? (long long)a.group_heads * a.row_tile : 0;
+  for (int i = threadIdx.x; i < rows * heads; i += threads) {
+    const int lh = i / rows;
+    const long long at = ((long long)c * 2 * a.group_heads + lh) * a.row_tile + (i - lh * rows);
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      const float2 ml = __ldcg(a.part_ml + at + k * stride + (k == 0 ? second : 0));
+      const float best = fmaxf(m, ml.x);
+      l = l * (m == best ? 1.f : exp2_fast(m - best)) + ml.y * (ml.x == best ? 1.f : exp2_fast(ml.x - best));
+      m = best;
+    }
+    a.part_ml[at + second] = make_float2(m, l);
+  }
+}
+
 // EXACT: head_dim is DP, so that the scales' place is known.
 template <int DP, int NT, bool EXACT>
 __global__ void __launch_bounds__((rows4_warps(DP) + 1) * 32, 1)
@@ -517,17 +593,17 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             const float inv = !whole ? 1.f : sum[n][e] > 0.f ? 1.f / sum[n][e] : sum[n][e] == 0.f ? 0.f : NAN;
             char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
             float *part = a.part_o + (slot * a.row_tile + row) * a.c.head_dim;
+            // a lane's channels lie side by side, 8 at a time
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int d = gid * (DP / 8) + t * 2 + h;
-                if (d >= a.c.head_dim) continue;
-                const float x = o[t][n][h * 2 + e] * inv;
-                if (!whole) part[d] = x;
-                else if (a.out.type == KVR_BF16) reinterpret_cast<__nv_bfloat16 *>(dst)[d] = __float2bfloat16_rn(x);
-                else reinterpret_cast<__half *>(dst)[d] = __float2half_rn(x);
-              }
+            for (int t = 0; t < kTiles; t += 4) {
+              const int d = gid * (DP / 8) + t * 2;
+              if (d >= a.c.head_dim) continue;
+              const float y[8] = {o[t][n][e] * inv, o[t][n][2 + e] * inv, o[t + 1][n][e] * inv, o[t + 1][n][2 + e] * inv,
+                                  o[t + 2][n][e] * inv, o[t + 2][n][2 + e] * inv, o[t + 3][n][e] * inv, o[t + 3][n][2 + e] * inv};
+              if (!whole) store8<KVR_F32>(reinterpret_cast<char *>(part + d), y);
+              else if (a.out.type == KVR_BF16) store8<KVR_BF16>(dst + d * 2, y);
+              else store8<KVR_F16>(dst + d * 2, y);
+            }
             if (gid == 0) {
               if (!whole) a.part_ml[slot * a.row_tile + row] = make_float2(top[n][e], sum[n][e]);
               else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum[n][e] == 0.f ? -INFINITY : top[n][e] * 0.69314718f + logf(sum[n][e]);
@@ -537,7 +613,10 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       if (piece.begin != 0 || piece.end != len.units) {
         const int heads = min(a.group_heads, a.c.kv_heads - piece.head_group * a.group_heads);
         hand_in(a, piece, shares, meet, &last_in, warp, lane, [&](const Cut &cut, int c, int step, int n, bool fold) {
-          join_pieces<DP / 128 + DP % 128 / 64>(a, piece, cut, c, step, n, fold, rows, heads, warps, warp, lane);
+          join4(a, piece, cut, c, step, n, fold, rows, heads, warps * 32);
+          if (!fold) return;
+          meet();
+          fold4(a, cut, c, step, n, rows, heads, warps * 32);
         });
       }
       __syncwarp();
