@@ -3,7 +3,6 @@
 
 #include <atomic>
 #include <cmath>
-#include <cstdlib>
 
 #include "kvr_once.hpp"
 
@@ -44,8 +43,9 @@ bool record_map(const kvr_cache_spec *s, const CacheView &c, int width, int box_
   const cuuint64_t dims[4] = {(cuuint64_t)c.row_bytes / 8, (cuuint64_t)s->block_size, (cuuint64_t)s->num_blocks, 2};
   const cuuint64_t strides[3] = {(cuuint64_t)c.row_bytes, (cuuint64_t)c.block_stride, (cuuint64_t)c.v_offset};
   const cuuint32_t box[4] = {(cuuint32_t)width / 8, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
+  // (a group that is a part of the row must not bring the rest of it: 1.6 times the bytes for two heads of eight)
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 4, c.base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                width < c.row_bytes ? CU_TENSOR_MAP_L2_PROMOTION_NONE : CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The layer's planes as [plane][block][token][head][channel]: boxes are `box_rows` tokens of one head, 128 bytes wide (128-byte
@@ -144,21 +144,25 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     // a segment's pieces are joined by one CTA.  (us, 8 rows, 16-bit / int8, all heads in a CTA against this: 1 request of 4k 39 / 44,
     // 24 / 20; 2 of 16k 67 / 66, 39 / 33; 8 of 16k 111 / 100, 97 / 85; 4 pieces: 96 / 98, 16 pieces: 95 / 85.)  Not where one tile of
     // rows streams a long 8-bit cache, whose narrow rows and scales are then read in pieces too small: by the caller's bounds, from 512 MB
-    // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316).
+    // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316.  4 bits, whole / split: of 4k, 42 MB, 53 / 37,
+    // of 8k 59 / 51, of 16k 78 / 78, of 32k 115 / 129: from 128 MB on).
     const int64_t stream = 2ll * batch->n_req * batch->max_tokens * a.c.row_bytes;
-    const bool whole = quantised(spec->format) && tiles == 1 && (stream >= 512ll << 20 || (four && stream >= (getenv("KVR_W") ? atoll(getenv("KVR_W")) : 0ll) << 20));
+    const bool whole = quantised(spec->format) && tiles == 1 && stream >= (four ? 128ll : 512ll) << 20;
     while (!whole && a.group_heads > 1 && (int64_t)batch->n_req * a.head_groups * 8 < sms) {
       a.group_heads = (a.group_heads + 1) / 2;
       a.head_groups = (spec->kv_heads + a.group_heads - 1) / a.group_heads;
     }
     slices = warps / a.group_heads;
-    const int turn = 16 * slices * (four ? rows4_at_once(padded, tiles) : chunks_at_once(spec->format, tiles));      // keys that the warps of a head take at a time
+    const int turn = 16 * slices * (four ? rows4_chunks(padded, tiles) : chunks_at_once(spec->format, tiles));      // keys that the warps of a head take at a time
     a.unit = FastDiv((64 + turn - 1) / turn * turn);
     if (four) {
-      const int group_bytes = a.group_heads * a.c.head_bytes, stage_keys = 16 * slices, merge = (slices - 1) * a.group_heads * (padded * 8 + 16) * 4;
+      // A segment begun inside a CTA's share costs it another Q, the join of its warps and a piece to hand in.  (us, weight 0 / 1 / 2 / 3 / 4: 32 requests
+      // of 300 tokens 33 / 27 / 27 / 27 / 27, of 2k 51 / 49 / 47 / 45 / 45, of 8k 102 / 100 / 98 / 98 / 96; 8 of 4k 41 / 39 / 35 / 35 / 37.)
+      a.opening = 3;
+      r4.slices = slices;
+      const int group_bytes = a.group_heads * a.c.head_bytes, stage_keys = 16 * rows4_chunks(padded, tiles) * slices;
       // Rows of many records stand 32 bytes behind a multiple of 128, for the banks; of few as they are, or the ring would hold too few keys.
       r4.stride = group_bytes < 256 ? group_bytes : group_bytes + (160 - group_bytes % 128) % 128;
-      r4.slices = slices;
       // tokens of a box: what divides a block and a stage
       for (r4.box_rows = 128; r4.box_rows >= 8 && (spec->block_size % r4.box_rows || stage_keys % r4.box_rows); r4.box_rows /= 2) {}
       if (r4.box_rows < 8 || r4.stride > 2048) {             // (a box is at most 256 x 8 bytes wide)
@@ -167,8 +171,8 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
         r4.box_bytes = r4.box_rows * r4.stride;
         if (!record_map(spec, a.c, r4.stride, r4.box_rows, &map)) return fail_cache(KVR_ERR_CUDA, "no tensor map could be made of the layer");
       }
-      const int fit = (kRows4Shared - (merge > 256 ? merge : 256)) / (2 * stage_keys * r4.stride);
-      r4.stages = fit < 8 ? fit : 8;
+      const int fit = (kRows4Shared - rows4_beside(padded, tiles, a.group_heads, slices)) / (2 * stage_keys * r4.stride);
+      r4.stages = fit < 16 ? fit : 16;
     }
     // 64 or more: fewer pieces.  (us, units of 16 / 64 / 128 / 256 / 512 keys, one token, bf16: 32 requests of 333 tokens 21.4 / 18.5 / 18.8 /
     // 25.3 / 23.6, 16 of them 25.9 / 15.6 / 15.7 / 18.6 / 15.8.  Of few requests a turn is 128 keys anyway: one of 333 13.8 / 13.5 /

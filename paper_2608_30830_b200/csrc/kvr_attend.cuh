@@ -142,15 +142,18 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int first, int i, int 
 #endif
 
 // chunks of 16 keys that a warp of the row kernel takes at a time (tiles: of 8 rows); a unit holds a multiple of them
-__host__ __device__ constexpr int chunks_at_once(int format, int tiles) { return quantised(format) && tiles == 1 ? 2 : 1; }
+__host__ __device__ constexpr int chunks_at_once(int format, int tiles) { return quantised(format) && !four_bit(format) && tiles == 1 ? 2 : 1; }
 // warps of a CTA of the row kernel: KV heads of a group x slices of the keys
 __host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim == 256 ? 4 : 8; }
 
-// Of the row kernel for 4-bit caches: warps that a CTA's heads share, chunks of 16 keys that each takes at a time (tiles: of 8 rows), shared
-// memory beside its barriers.
+// Of the row kernel for 4-bit caches: warps that a CTA's heads share; shared memory beside its barriers, and what of it is not the ring's
+// (statistics and a quarter of the accumulators of all slices; what is read past the last record).
 __host__ __device__ constexpr int rows4_warps(int padded_dim) { return padded_dim == 256 ? 8 : 16; }
-__host__ __device__ constexpr int rows4_at_once(int padded_dim, int tiles) { return padded_dim <= 128 && tiles == 1 ? 1 : 1; }
-constexpr int kRows4Shared = 227 * 1024 - 4096;
+__host__ __device__ constexpr int rows4_chunks(int padded_dim, int tiles) { return tiles == 1 ? 2 : 1; }      // of 16 keys, that a warp takes at a time
+__host__ __device__ constexpr int rows4_beside(int padded_dim, int tiles, int heads, int slices) {
+  return (slices > 1 ? heads * slices * tiles * 64 + heads * (slices - 1) * (padded_dim / 64) * 512 : 0) + 256;
+}
+constexpr int kRows4Shared = 227 * 1024 - 2048;
 struct Rows4 {
   int slices, stages, stride;          // warps of a head; stages of the ring; bytes from one key's records to the next's
   int box_rows, box_bytes;             // tokens of a TMA box (0: copies by lanes), bytes of one

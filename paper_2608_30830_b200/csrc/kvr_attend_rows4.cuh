@@ -68,7 +68,7 @@ __device__ __forceinline__ uint4 lds16(unsigned at) {
   return r;
 }
 
-constexpr int kMaxStages4 = 8;
+constexpr int kMaxStages4 = 16;
 
 // The rows of a segment from its pieces of n CTAs c, c + step, ...: to the output, or (fold) to the first one's place.  A thread 4 channels of
 // a row, 8 pieces' loads under way at a time.  Out of line: the loop's registers are the products'.
@@ -150,7 +150,7 @@ __device__ __noinline__ void fold4(const AttendArgs &a, const Cut &cut, int c, i
 template <int DP, int NT, bool EXACT>
 __global__ void __launch_bounds__((rows4_warps(DP) + 1) * 32, 1)
 attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Rows4 r4, const __grid_constant__ CUtensorMap map) {
-  constexpr int kTiles = DP / 16, kAtOnce = rows4_at_once(DP, NT), kWide = DP / 64, kTails = DP == 256 ? 2 : 1;
+  constexpr int kTiles = DP / 16, kChunks = rows4_chunks(DP, NT), kWide = DP / 64, kTails = DP == 256 ? 2 : 1;
   constexpr float kLazy = 4.f;         // as in the row kernel
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ unsigned scratch[39];
@@ -159,7 +159,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ Piece pieces[rows4_warps(DP)];     // of the heads' warps, whose registers are the products'
   volatile int *gave_up = &gave_up_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
-  const int slices = r4.slices, stride = r4.stride, warps = a.group_heads * slices, stage_keys = 16 * slices;
+  const int slices = r4.slices, stride = r4.stride, warps = a.group_heads * slices, stage_keys = 16 * kChunks * slices;
   const int plane_bytes = stage_keys * stride, stage_bytes = 2 * plane_bytes;
 
   Shares shares;
@@ -175,38 +175,45 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   }
   if (warp < warps && lane == 0) pieces[warp] = start;
   __syncthreads();
-  // Stages of a piece, kAtOnce of which are a turn.  (The last one may lie behind the keys.)
+  // stages of a piece
   const int unit_stages = (int)a.unit.d / stage_keys;
-  auto stage_end = [&](const Piece &p) { return min(p.end * unit_stages, (p.len.keys + kAtOnce * stage_keys - 1) / (kAtOnce * stage_keys) * kAtOnce); };
+  auto stage_end = [&](const Piece &p) { return min(p.end * unit_stages, (p.len.keys + stage_keys - 1) / stage_keys); };
 
   if (warp == warps) {
     // ---- loads
     int stage = 0, t = start.begin * unit_stages, end = stage_end(start);
     unsigned round = 0;                // of the ring
     bool more = true;
-    // the ids of a stage's first 32 boxes are fetched a stage ahead
-    int next_id = 0;
-    auto fetch_ids = [&]() {
-      const int token = t * stage_keys + lane * r4.box_rows;
-      if (more && lane * r4.box_rows < stage_keys && token < start.len.keys)
-        next_id = __ldg(a.b.tables + (long long)start.r * a.b.table_stride + a.bs.div((unsigned)token));
+    // Ids of the blocks that the boxes of a piece lie in, a lane a box: of boxes id_base .. + 31, and of the 32 behind them, on their way while
+    // those are used.
+    int id_base = 0, ids = 0, later_ids = 0;
+    auto fetch_ids = [&](int box) {
+      const int token = (box + lane) * r4.box_rows;
+      return token < start.len.keys ? __ldg(a.b.tables + (long long)start.r * a.b.table_stride + a.bs.div((unsigned)token)) : 0;
     };
-    if (r4.box_rows) fetch_ids();
+    auto first_ids = [&]() {
+      id_base = t * stage_keys / r4.box_rows;
+      ids = fetch_ids(id_base);
+      later_ids = fetch_ids(id_base + 32);
+    };
+    if (r4.box_rows) first_ids();
     while (more) {
       const int key0 = t * stage_keys, keys = min(stage_keys, start.len.keys - key0), x0 = start.head_group * a.group_heads * a.c.head_bytes;
       unsigned char *st = smem + stage * stage_bytes;
       const unsigned bar = shared_at(&full[stage]);
       if (round) bar4_wait(shared_at(&empty[stage]), (round - 1) & 1, gave_up, a.polls);
       if (r4.box_rows) {
-        // a lane a box of K and a box of V
-        const int boxes = keys > 0 ? (keys + r4.box_rows - 1) / r4.box_rows : 0;
-        if (boxes == 0 && lane == 0) bar4_arrive(bar);
+        const int boxes = min(stage_keys, keys + r4.box_rows - 1) / r4.box_rows, box0 = key0 / r4.box_rows;
         for (int b0 = 0; b0 < boxes; b0 += 32) {
-          const int box = b0 + lane, token = key0 + box * r4.box_rows;
-          const bool in = box < boxes;
-          const unsigned block = a.bs.div((unsigned)token);
-          const int id = !in ? 0 : b0 == 0 ? next_id : __ldg(a.b.tables + (long long)start.r * a.b.table_stride + block);
-          const bool known = in && (unsigned)id < (unsigned)a.c.num_blocks;
+          // a lane a box of K and a box of V
+          if (box0 + b0 >= id_base + 32) {
+            id_base += 32;
+            ids = later_ids;
+            later_ids = fetch_ids(id_base + 32);
+          }
+          const int box = b0 + lane, at = box0 + box - id_base, token = key0 + box * r4.box_rows;
+          const int now = __shfl_sync(0xffffffffu, ids, at & 31), then = __shfl_sync(0xffffffffu, later_ids, at & 31), id = at < 32 ? now : then;
+          const bool in = box < boxes, known = in && (unsigned)id < (unsigned)a.c.num_blocks;
           unsigned char *to = st + box * r4.box_bytes;
           if (in && !known) {          // a block that is not there
             report(a.b.status, KVR_DEV_BAD_BLOCK);
@@ -216,13 +223,13 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
           const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
           if (lane == 0) {
-            // all of the stage's bytes are expected by the one arrival, which comes with the last 32 boxes
+            // all of the stage's bytes are expected by the one arrival, which comes with its last boxes
             if (b0 + 32 >= boxes) bar4_expect(bar, got * 2 * r4.box_bytes);
             else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(got * 2 * r4.box_bytes) : "memory");
           }
           __syncwarp();
           if (known) {
-            const int row = token - (int)block * (int)a.bs.d;
+            const int row = token - (int)a.bs.div((unsigned)token) * (int)a.bs.d;
             box4_load(shared_at(to), &map, bar, x0 >> 3, row, id, 0);
             box4_load(shared_at(to + plane_bytes), &map, bar, x0 >> 3, row, id, 1);
           }
@@ -254,22 +261,22 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         more = next_piece(a, start, last);
         t = start.begin * unit_stages;
         end = stage_end(start);
+        if (more && r4.box_rows) first_ids();
       }
-      if (r4.box_rows) fetch_ids();
     }
     copy_wait<0>();
   } else {
     // ---- products and softmax
     const Piece &piece = pieces[warp];
-    int stage = 0;                     // of the ring
+    int slot = 0;                      // of the ring
     unsigned round = 0;
     auto meet = [&]() { asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory"); return true; };
     const int local_head = warp / slices, slice = warp - local_head * slices;
     float *merge = reinterpret_cast<float *>(smem + r4.stages * stage_bytes);
     const int swapped = gid ^ (gid >> 2), first_key = (2 * tig) ^ (tig >> 1), codes = EXACT ? DP / 2 : a.c.scale_offset;
     // what a lane reads: K's rows of key `swapped` and + 8, V's of four keys
-    const unsigned k_first = shared_at(smem) + (slice * 16 + swapped) * stride + local_head * a.c.head_bytes;
-    const unsigned v_first = shared_at(smem) + plane_bytes + (slice * 16 + first_key) * stride + local_head * a.c.head_bytes;
+    const unsigned k_first = shared_at(smem) + (slice * 16 * kChunks + swapped) * stride + local_head * a.c.head_bytes;
+    const unsigned v_first = shared_at(smem) + plane_bytes + (slice * 16 * kChunks + first_key) * stride + local_head * a.c.head_bytes;
     const int v_step = tig < 2 ? stride : -stride;
     for (bool again = true; again;) {
       const Lengths &len = piece.len;
@@ -277,8 +284,8 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       const int rows = min(a.row_tile, len.fresh * (int)a.group.d - piece.row0);     // of this tile
       const bool live = head < a.c.kv_heads;
       // Q^T fragments: k-step (group of 64 channels w, s) has channels 64 w + 16 tig + 4 s + 0..3
-      unsigned q[NT][kTiles][2];
-      float q_scale[NT][2];            // of the rows whose scores this lane holds (tig * 2, + 1)
+      uint2 q[NT][kTiles];
+      Pair q_scale[NT];                // of the rows whose scores this lane holds (tig * 2, + 1)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int row = piece.row0 + n * 8 + gid;
@@ -303,95 +310,86 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^-e with 2^e <= top < 2^(e+1), by the exponent's bits; rows of zeros, subnormals and infinities stay as they are
-        const unsigned e = __float_as_uint(top) >> 23;
-        const bool plain = e >= 1 && e <= 253;
-        const float down = plain ? __uint_as_float((254u - e) << 23) : 1.f, up = plain ? __uint_as_float(e << 23) : 1.f;
+        // The row's largest element is brought to [2^8, 2^9) by a power of two, 2^(8 - e), and 2^e goes to the scores: 2^-8 of it meets the
+        // unit of K's groups.  (Not quite so far where 2^e is below 2^-118; rows of zeros, subnormals and infinities stay as they are.)
+        const unsigned e = __float_as_uint(top) >> 23, field = e >= 1 && e <= 253 ? min(262u - e, 253u) : 127u;
+        const float down = __uint_as_float(field << 23), up = __uint_as_float((262u - field) << 23);
 #pragma unroll
         for (int w = 0; w < kWide; ++w)
 #pragma unroll
           for (int s = 0; s < 4; ++s) {
-            q[n][w * 4 + s][0] = pack_f16(x[w][4 * s] * down, x[w][4 * s + 1] * down);
-            q[n][w * 4 + s][1] = pack_f16(x[w][4 * s + 2] * down, x[w][4 * s + 3] * down);
+            q[n][w * 4 + s] = make_uint2(pack_f16(x[w][4 * s] * down, x[w][4 * s + 1] * down), pack_f16(x[w][4 * s + 2] * down, x[w][4 * s + 3] * down));
           }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) q_scale[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (tig * 2 + i) * 4);
+        q_scale[n] = pair(a.scale_log2 * __shfl_sync(0xffffffffu, up, tig * 8), a.scale_log2 * __shfl_sync(0xffffffffu, up, tig * 8 + 4));
       }
       float o[kTiles][NT][4] = {};
-      float top[NT][2], base[NT][2], sum[NT][2], unit[NT][2];        // base: top, 0 where that is -infinity; unit: of V's scales
+      float top[NT][2], unit[NT][2];   // unit: of V's scales
+      Pair base[NT], sum[NT];          // base: -top, 0 where that is infinite
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        top[n][0] = top[n][1] = -INFINITY;
+        base[n] = sum[n] = pair(0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          top[n][e] = -INFINITY;
-          base[n][e] = sum[n][e] = 0.f;
-          unit[n][e] = unit_first(n * 8 + tig * 2 + e < rows);
-        }
+        for (int e = 0; e < 2; ++e) unit[n][e] = unit_first(n * 8 + tig * 2 + e < rows);
+      }
 
       const int end = stage_end(piece);
-      for (int t = piece.begin * unit_stages; t < end; t += kAtOnce) {
-        unsigned k_at[kAtOnce], v_at[kAtOnce];
-        int used[kAtOnce];
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-          bar4_wait(shared_at(&full[stage]), round & 1, gave_up, a.polls);
-          k_at[u] = k_first + stage * stage_bytes;
-          v_at[u] = v_first + stage * stage_bytes;
-          used[u] = stage;
-          if (++stage == r4.stages) { stage = 0; ++round; }
-        }
-        const int key0 = (t * slices + slice) * 16;          // of the first chunk; the next starts 16 * slices further on
-        const bool edge = key0 + ((kAtOnce - 1) * slices + 1) * 16 > context;
+#pragma unroll 1
+      for (int t = piece.begin * unit_stages; t < end; ++t) {
+        bar4_wait(shared_at(&full[slot]), round & 1, gave_up, a.polls);
+        unsigned k_at = k_first + slot * stage_bytes, v_at = v_first + slot * stage_bytes;
+        const int key0 = (t * slices + slice) * (16 * kChunks);
+        const bool edge = key0 + 16 * kChunks > context;
 
-        // S^T = K Q^T; the chunks' products in turn, for a product waits for the one before it
-        float s[kAtOnce][NT][4] = {}, v_scale[kAtOnce][2], k_scale[kAtOnce][2];
-        uint4 tail[kAtOnce][2];        // of K's records: the head's scale, groups 0 to 11
-        unsigned more[kAtOnce][2];     // groups 12 to 15
+        // S^T = K Q^T
+        float s[kChunks][NT][4] = {}, v_scale[kChunks][2];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
+        for (int u = 0; u < kChunks; ++u) {
+          uint4 tail[2];               // of K's records: the head's scale, groups 0 to 11
+          unsigned more[2] = {};       // groups 12 to 15
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const unsigned row = k_at[u] + e * 8 * stride + codes;
-            tail[u][e] = lds16(row);
-            if constexpr (kTails == 2) more[u][e] = lds8(row + 16).x;
-            k_scale[u][e] = __uint_as_float(tail[u][e].x) * kGroupUnit;
-            v_scale[u][e] = __uint_as_float(lds4(row + plane_bytes)) * kGroupUnit;
+            const unsigned row = k_at + (u * 16 + e * 8) * stride + codes;
+            tail[e] = lds16(row);
+            if constexpr (kTails == 2) more[e] = lds4(row + 16);
+            v_scale[u][e] = __uint_as_float(lds4(row + plane_bytes));
           }
 #pragma unroll
-        for (int w = 0; w < kWide; ++w) {
-          uint2 x[kAtOnce][2];
-          unsigned scale[kAtOnce][2];
-#pragma unroll
-          for (int u = 0; u < kAtOnce; ++u)
+          for (int w = 0; w < kWide; ++w) {
+            uint2 x[2];
+            unsigned scale[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              x[u][e] = lds8(k_at[u] + e * 8 * stride + tig * 8 + w * 32);
-              const unsigned four = w == 0 ? tail[u][e].y : w == 1 ? tail[u][e].z : w == 2 ? tail[u][e].w : more[u][e];
-              scale[u][e] = (four >> (tig * 8) & 0x7fu) * 0x00800080u;
+              x[e] = lds8(k_at + (u * 16 + e * 8) * stride + tig * 8 + w * 32);
+              const unsigned four = w == 0 ? tail[e].y : w == 1 ? tail[e].z : w == 2 ? tail[e].w : more[e];
+              scale[e] = (four >> (tig * 8) & 0x7fu) * 0x00800080u;
             }
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 4; ++k) {
+              const unsigned xa = k < 2 ? x[0].x : x[0].y, xb = k < 2 ? x[1].x : x[1].y;
+              const unsigned f[4] = {k & 1 ? widen_times<2>(xa, scale[0]) : widen_times<0>(xa, scale[0]), k & 1 ? widen_times<2>(xb, scale[1]) : widen_times<0>(xb, scale[1]),
+                                     k & 1 ? widen_times<3>(xa, scale[0]) : widen_times<1>(xa, scale[0]), k & 1 ? widen_times<3>(xb, scale[1]) : widen_times<1>(xb, scale[1])};
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-              const unsigned xa = k < 2 ? x[u][0].x : x[u][0].y, xb = k < 2 ? x[u][1].x : x[u][1].y, sa = scale[u][0], sb = scale[u][1];
-              const unsigned f[4] = {k & 1 ? widen_times<2>(xa, sa) : widen_times<0>(xa, sa), k & 1 ? widen_times<2>(xb, sb) : widen_times<0>(xb, sb),
-                                     k & 1 ? widen_times<3>(xa, sa) : widen_times<1>(xa, sa), k & 1 ? widen_times<3>(xb, sb) : widen_times<1>(xb, sb)};
-#pragma unroll
-              for (int n = 0; n < NT; ++n) product4(s[u][n], f, q[n][w * 4 + k][0], q[n][w * 4 + k][1]);
+              for (int n = 0; n < NT; ++n) {
+                product4(s[u][n], f, q[n][w * 4 + k].x, q[n][w * 4 + k].y);
+              }
             }
-        }
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
+          }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[u][n][i] *= q_scale[n][i & 1] * k_scale[u][i >> 1];
-        if (edge) {                    // what a row does not see
+            for (int i = 0; i < 2; ++i) {
+              const float k_scale = __uint_as_float(tail[i].x);
+              const float2 v = unpair(mul2(pair(s[u][n][2 * i], s[u][n][2 * i + 1]), mul2(q_scale[n], pair(k_scale, k_scale))));
+              s[u][n][2 * i] = v.x; s[u][n][2 * i + 1] = v.y;
+            }
+        }
+        if (__builtin_expect(edge, 0)) {                     // what a row does not see
 #pragma unroll
-          for (int u = 0; u < kAtOnce; ++u)
+          for (int u = 0; u < kChunks; ++u)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const int j = key0 + u * slices * 16 + swapped + i * 8 - context;      // among the new tokens
+              const int j = key0 + u * 16 + swapped + i * 8 - context;         // among the new tokens
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -406,83 +404,79 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         // running maximum of each row, over the 8 lanes that share it
         float best[NT][2];
         bool moved = false;
+        float big = fmaxf(v_scale[0][0], v_scale[0][1]);
+        if constexpr (kChunks == 2) big = max3(big, v_scale[kChunks - 1][0], v_scale[kChunks - 1][1]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float m = fmaxf(s[0][n][e], s[0][n][2 + e]);
-            if constexpr (kAtOnce == 2) m = max3(m, s[kAtOnce - 1][n][e], s[kAtOnce - 1][n][2 + e]);
+            if constexpr (kChunks == 2) m = max3(m, s[kChunks - 1][n][e], s[kChunks - 1][n][2 + e]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
             best[n][e] = m;
-            moved = moved || m > top[n][e] + kLazy;                    // from -infinity: any score moves it
+            moved = moved || m > top[n][e] + kLazy || big * unit[n][e] >= kUnitLimit;      // from -infinity: any score moves it
           }
-        float big = fmaxf(v_scale[0][0], v_scale[0][1]);
-        if constexpr (kAtOnce == 2) big = max3(big, v_scale[kAtOnce - 1][0], v_scale[kAtOnce - 1][1]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) moved = moved || big * unit[n][e] >= kUnitLimit;
         if (__builtin_expect(__any_sync(0xffffffffu, moved), 0)) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n) {
+            float f[2], less[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               // the largest of V's scales that the row sees
               float own = 0.f;
 #pragma unroll
-              for (int u = 0; u < kAtOnce; ++u)
+              for (int u = 0; u < kChunks; ++u)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                   if (s[u][n][i * 2 + e] != -INFINITY) own = fmaxf(own, v_scale[u][i]);
               own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 4));
               own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 8));
               own = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 16));
-              float less = 1.f;
+              less[e] = 1.f;
               if (own * unit[n][e] >= kUnitLimit) {
-                less = unit_of(own) * unit_back(unit[n][e]);
+                less[e] = unit_of(own) * unit_back(unit[n][e]);
                 unit[n][e] = unit_of(own);
               }
               const float was = top[n][e];
               if (best[n][e] > was + kLazy) top[n][e] = best[n][e];
-              const float f = was == top[n][e] ? 1.f : exp2_fast(was - top[n][e]);     // was = -infinity: 0
-              base[n][e] = top[n][e] == -INFINITY ? 0.f : top[n][e];
-              sum[n][e] *= f;
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t) {
-                o[t][n][e] *= f * less;
-                o[t][n][2 + e] *= f * less;
-              }
+              f[e] = was == top[n][e] ? 1.f : exp2_fast(was - top[n][e]);      // was = -infinity: 0
+              less[e] *= f[e];
             }
+            base[n] = pair(top[n][0] == -INFINITY ? 0.f : -top[n][0], top[n][1] == -INFINITY ? 0.f : -top[n][1]);
+            sum[n] = mul2(sum[n], pair(f[0], f[1]));
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[t][n][i] *= less[i & 1];
+          }
         }
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
+        for (int u = 0; u < kChunks; ++u) {
           // P^T, as the right operand of the second product
           unsigned p[NT][2];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float pf[4];
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x = exp2_fast(s[u][n][i] - base[n][i & 1]);
-              sum[n][i & 1] += x;
-              pf[i] = x * (v_scale[u][i >> 1] * unit[n][i & 1]);
+            for (int i = 0; i < 2; ++i) {
+              const float2 x = unpair(add2(pair(s[u][n][2 * i], s[u][n][2 * i + 1]), base[n]));
+              const Pair y = pair(exp2_fast(x.x), exp2_fast(x.y));
+              sum[n] = add2(sum[n], y);
+              float2 v = unpair(mul2(y, mul2(pair(unit[n][0], unit[n][1]), pair(v_scale[u][i], v_scale[u][i]))));
+              if (__builtin_expect(edge, 0)) {               // a scale that is not finite, at a key that the row does not see
+                if (s[u][n][2 * i] == -INFINITY) v.x = 0.f;
+                if (s[u][n][2 * i + 1] == -INFINITY) v.y = 0.f;
+              }
+              p[n][i] = transpose4(pack_f16(v.x, v.y));
             }
-            if (edge) {                // a scale that is not finite, at a key that the row does not see
-#pragma unroll
-              for (int i = 0; i < 4; ++i) if (s[u][n][i] == -INFINITY) pf[i] = 0.f;
-            }
-            p[n][0] = transpose4(pack_f16(pf[0], pf[1]));
-            p[n][1] = transpose4(pack_f16(pf[2], pf[3]));
-          }
-          // O^T += V^T P^T.  The lane's keys are rows 2 tig, 2 tig + 1, + 8, + 9 of S^T, its channels gid * DP / 8 + 0 .. DP / 8 - 1.  Codes of two keys
-          // at one channel are brought into one byte: those of even channels, then of odd ones.
+          // O^T += V^T P^T.  The lane's keys are rows 2 tig, 2 tig + 1, + 8, + 9 of S^T, its channels gid * DP / 8 + 0 .. DP / 8 - 1.  Codes of two
+          // keys at one channel are brought into one byte: those of even channels, then of odd ones.
           constexpr int kWords = DP / 64;
-          unsigned w[4][kWords], scale[2][kTails];                       // of keys 0 and 1, 2 and 3
+          unsigned w[4][kWords], scale[2][kTails];           // of keys 0 and 1, 2 and 3
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const unsigned row = v_at[u] + (j & 1 ? v_step : 0) + (j >> 1) * 8 * stride;
+            const unsigned row = v_at + (j & 1 ? v_step : 0) + (u * 16 + (j >> 1) * 8) * stride;
             if constexpr (DP == 64) {
               w[j][0] = lds4(row + gid * 4);
             } else if constexpr (DP == 128) {
@@ -515,69 +509,94 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
               for (int n = 0; n < NT; ++n) product4(o[x * 4 + b][n], f, p[n][0], p[n][1]);
             }
           }
-          __syncwarp();
-          if (lane == 0) bar4_arrive(shared_at(&empty[used[u]]));
         }
+        __syncwarp();
+        if (lane == 0) bar4_arrive(shared_at(&empty[slot]));
+        if (++slot == r4.stages) { slot = 0; ++round; }
       }
 
       // ---- the piece's result
+      float l[NT][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        const float2 both = unpair(sum[n]);
+        l[n][0] = both.x; l[n][1] = both.y;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 4);
-          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 8);
-          sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], 16);
+          l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 4);
+          l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 8);
+          l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], 16);
         }
+      }
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[t][n][i] *= unit_back(unit[n][i & 1]);
+          for (int i = 0; i < 4; ++i) o[t][n][i] = o[t][n][i] * unit_back(unit[n][i & 1]) * kGroupUnit;
       if (slices > 1) {
-        // slices of a head are joined through shared memory, one n-tile at a time, in slice order
-        constexpr int kPer = DP * 8 + 16;                                // accumulators, then (maximum, sum) of 8 rows
-        const int heads = a.group_heads;
+        // The slices of a head are joined through shared memory in slice order: first the maxima and sums of all, then the accumulators, a
+        // quarter of one n-tile at a time, scaled to the common maximum.
+        constexpr int kPart = kTiles / 4;
+        float2 *ml = reinterpret_cast<float2 *>(merge);      // [head][slice][n-tile][8 rows]
+        float *parts = merge + warps * NT * 16;              // [head][slice - 1][kPart * 4][32]
+        if (gid == 0) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float *mine = merge + ((slice - 1) * heads + local_head) * kPer;
-          if (slice > 0) {
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) mine[(t * 4 + i) * 32 + lane] = o[t][n][i];
-            if (gid == 0) {
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                mine[DP * 8 + (tig * 2 + e) * 2] = top[n][e];
-                mine[DP * 8 + (tig * 2 + e) * 2 + 1] = sum[n][e];
-              }
-            }
-          }
-          meet();
-          if (slice == 0) {
-            for (int s = 1; s < slices; ++s) {
-              const float *other = merge + ((s - 1) * heads + local_head) * kPer;
-              float f[2], g[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float m2 = other[DP * 8 + (tig * 2 + e) * 2], l2 = other[DP * 8 + (tig * 2 + e) * 2 + 1];
-                const float m = fmaxf(top[n][e], m2);
-                f[e] = top[n][e] == m ? 1.f : exp2_fast(top[n][e] - m);
-                g[e] = m2 == m ? 1.f : exp2_fast(m2 - m);
-                if (m == -INFINITY) g[e] = 0.f;
-                sum[n][e] = sum[n][e] * f[e] + l2 * g[e];
-                top[n][e] = m;
-              }
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[t][n][i] = o[t][n][i] * f[i & 1] + other[(t * 4 + i) * 32 + lane] * g[i & 1];
-            }
-          }
-          meet();
+            for (int e = 0; e < 2; ++e) ml[(warp * NT + n) * 8 + tig * 2 + e] = make_float2(top[n][e], l[n][e]);
         }
+        meet();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            // a lane takes slices gid and gid + 8 (of 16 at most); lanes of the same rows put theirs together
+            float2 x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              x[k] = gid + 8 * k < slices ? ml[((local_head * slices + gid + 8 * k) * NT + n) * 8 + tig * 2 + e] : make_float2(-INFINITY, 0.f);
+            float m = fmaxf(x[0].x, x[1].x);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            float all = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) all += x[k].y * (x[k].x == m ? 1.f : exp2_fast(x[k].x - m));
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+            const float f = top[n][e] == m ? 1.f : exp2_fast(top[n][e] - m);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+              o[t][n][e] *= f;
+              o[t][n][2 + e] *= f;
+            }
+            top[n][e] = m;
+            l[n][e] = all;
+          }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int t0 = 0; t0 < kTiles; t0 += kPart) {
+            float *mine = parts + (local_head * (slices - 1) + slice - 1) * (kPart * 128) + lane;
+            if (slice > 0) {
+#pragma unroll
+              for (int t = 0; t < kPart; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mine[(t * 4 + i) * 32] = o[t0 + t][n][i];
+            }
+            meet();
+            if (slice == 0) {
+#pragma unroll 4
+              for (int k = 1; k < slices; ++k) {
+                const float *other = parts + (local_head * (slices - 1) + k - 1) * (kPart * 128) + lane;
+#pragma unroll
+                for (int t = 0; t < kPart; ++t)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) o[t0 + t][n][i] += other[(t * 4 + i) * 32];
+              }
+            }
+            meet();
+          }
       }
       if (slice == 0 && live) {
         const bool whole = piece.begin == 0 && piece.end == len.units;
@@ -590,7 +609,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             if (row >= rows) continue;
             const int t_row = (int)a.group.div(piece.row0 + row);
             const int q_head = head * (int)a.group.d + (piece.row0 + row - t_row * (int)a.group.d);
-            const float inv = !whole ? 1.f : sum[n][e] > 0.f ? 1.f / sum[n][e] : sum[n][e] == 0.f ? 0.f : NAN;
+            const float inv = !whole ? 1.f : l[n][e] > 0.f ? 1.f / l[n][e] : l[n][e] == 0.f ? 0.f : NAN;
             char *dst = a.out.data + (long long)(len.first + t_row) * a.out.token_stride + (long long)q_head * a.out.head_stride;
             float *part = a.part_o + (slot * a.row_tile + row) * a.c.head_dim;
             // a lane's channels lie side by side, 8 at a time
@@ -605,8 +624,8 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
               else store8<KVR_F16>(dst + d * 2, y);
             }
             if (gid == 0) {
-              if (!whole) a.part_ml[slot * a.row_tile + row] = make_float2(top[n][e], sum[n][e]);
-              else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = sum[n][e] == 0.f ? -INFINITY : top[n][e] * 0.69314718f + logf(sum[n][e]);
+              if (!whole) a.part_ml[slot * a.row_tile + row] = make_float2(top[n][e], l[n][e]);
+              else if (a.lse) a.lse[(long long)(len.first + t_row) * a.q_heads + q_head] = l[n][e] == 0.f ? -INFINITY : top[n][e] * 0.69314718f + logf(l[n][e]);
             }
           }
       }
@@ -639,8 +658,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
 
 template <int DP, int NT, bool EXACT>
 cudaError_t launch_rows4(const AttendArgs &a, const Rows4 &r4, const CUtensorMap &map, cudaStream_t s) {
-  const int merge = r4.slices > 1 ? (r4.slices - 1) * a.group_heads * (DP * 8 + 16) * 4 : 0;
-  const int bytes = r4.stages * 32 * r4.slices * r4.stride + (merge > 256 ? merge : 256);    // 256: reads past a record's end
+  const int bytes = r4.stages * 32 * rows4_chunks(DP, NT) * r4.slices * r4.stride + rows4_beside(DP, NT, a.group_heads, r4.slices);
   static OncePerDevice once;
   if (const cudaError_t e = allow_shared(once, attend_rows4_kernel<DP, NT, EXACT>, kRows4Shared)) return e;
   attend_rows4_kernel<DP, NT, EXACT><<<a.ctas, (a.group_heads * r4.slices + 1) * 32, bytes, s>>>(a, r4, map);
