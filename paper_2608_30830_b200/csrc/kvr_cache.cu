@@ -198,37 +198,6 @@ template <int FMT, int LPH>
 __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_offset, int head, int head_dim, int d0, bool live) {
   if constexpr (!quantised(FMT)) {
     if (live) store8<FMT == KVR_CACHE_BF16 ? KVR_BF16 : KVR_F16>(row + ((long long)head * head_dim + d0) * 2, x);
-  } else if constexpr (four_bit(FMT)) {
-    // Two lanes hold a group.  Reciprocals and products are rounded one by one, as the header has them.
-    unsigned top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    if (!live) top = 0;
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1, LPH));
-    unsigned most = top;
-#pragma unroll
-    for (int m = 2; m < LPH; m <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, m, LPH));
-    const bool finite = most < 0x7f800000u;
-    const float scale = finite ? fmaxf(__fmul_rn(__uint_as_float(most), 1.f / 2688.f), 7.8886091e-31f) : __uint_as_float(0x7fc00000u);
-    const float largest = __fmul_rn(__uint_as_float(top), __fmul_rn(__frcp_rn(scale), 1.f / 6.f));
-    const unsigned byte = finite ? __nv_cvt_float_to_fp8(largest, __NV_SATFINITE, __NV_E4M3) : 0u;
-    const float step = __fmul_rn(__half2float(__ushort_as_half((unsigned short)group_scale(byte))) * kGroupUnit, scale);
-    const float back = byte ? __frcp_rn(step) : 0.f;
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(x[i], back);
-    const unsigned codes = finite ? narrow_e2m1(y) : 0u;
-    // the scales, 8 lanes' (4 groups') to a word, then a word to a lane: the head's scale, the groups', zeros
-    const int lane = d0 >> 3;
-    unsigned word = lane & 1 ? 0u : byte << ((lane & 6) * 4);
-    word |= __shfl_xor_sync(0xffffffffu, word, 2, LPH);
-    word |= __shfl_xor_sync(0xffffffffu, word, 4, LPH);
-    const unsigned groups = __shfl_sync(0xffffffffu, word, (lane - 1) * 8, LPH);
-    if (!live) return;
-    char *record = row + (long long)head * record_bytes(head_dim);
-    *reinterpret_cast<unsigned *>(record + (d0 >> 1)) = codes;
-    if (lane * 4 < record_bytes(head_dim) - head_dim / 2)
-      *reinterpret_cast<unsigned *>(record + head_dim / 2 + lane * 4) = lane == 0 ? __float_as_uint(scale) : lane <= LPH / 8 ? groups : 0u;
   } else {
     unsigned top = 0;
 #pragma unroll
@@ -275,6 +244,62 @@ __device__ __forceinline__ void put8(const float (&x)[8], char *row, int scale_o
     }
     *reinterpret_cast<uint2 *>(row + (long long)head * head_dim + d0) = make_uint2(w[0], w[1]);
     if (d0 == 0) *reinterpret_cast<float *>(row + scale_offset + 4 * head) = scale;
+  }
+}
+
+// The largest magnitude of three numbers; NaN if one is.
+__device__ __forceinline__ float top3(float a, float b, float c) { float r; asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// The same into a 4-bit cache, N heads at once (of the lanes' heads first, first + step, ...): step by step for all of them, for each is a chain of shuffles,
+// reciprocals and conversions.  Two lanes hold a group.  Reciprocals and products are rounded one by one, as the header has them.
+template <int LPH, int N>
+__device__ __forceinline__ void put4(const float (&x)[N][8], char *row, int first, int step, int heads, int head_dim, int d0, bool lane_live) {
+  const int lane = d0 >> 3;
+  float top[N], most[N], scale[N], back[N];
+  unsigned byte[N], codes[N], word[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) top[i] = top3(top3(top3(x[i][0], x[i][1], x[i][2]), x[i][3], x[i][4]), top3(x[i][5], x[i][6], x[i][7]), 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) most[i] = top[i] = top3(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1, LPH), 0.f);
+#pragma unroll
+  for (int m = 2; m < LPH; m <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) most[i] = top3(most[i], __shfl_xor_sync(0xffffffffu, most[i], m, LPH), 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    scale[i] = most[i] < INFINITY ? fmaxf(__fmul_rn(most[i], 1.f / 2688.f), 7.8886091e-31f) : __uint_as_float(0x7fc00000u);
+    back[i] = __fmul_rn(__frcp_rn(scale[i]), 1.f / 6.f);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) byte[i] = most[i] < INFINITY ? __nv_cvt_float_to_fp8(__fmul_rn(top[i], back[i]), __NV_SATFINITE, __NV_E4M3) : 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float unit = __fmul_rn(__half2float(__ushort_as_half((unsigned short)group_scale(byte[i]))) * kGroupUnit, scale[i]);
+    back[i] = byte[i] ? __frcp_rn(unit) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(x[i][e], back[i]);
+    codes[i] = most[i] < INFINITY ? narrow_e2m1(y) : 0u;
+    word[i] = lane & 1 ? 0u : byte[i] << ((lane & 6) * 4);
+  }
+  // the scales, 8 lanes' (4 groups') to a word, then a word to a lane: the head's scale, the groups', zeros
+#pragma unroll
+  for (int i = 0; i < N; ++i) word[i] |= __shfl_xor_sync(0xffffffffu, word[i], 2, LPH);
+#pragma unroll
+  for (int i = 0; i < N; ++i) word[i] |= __shfl_xor_sync(0xffffffffu, word[i], 4, LPH);
+#pragma unroll
+  for (int i = 0; i < N; ++i) word[i] = __shfl_sync(0xffffffffu, word[i], (lane - 1) * 8, LPH);
+  const int bytes = record_bytes(head_dim);
+  char *to = row + (long long)first * bytes;
+#pragma unroll
+  for (int i = 0; i < N; ++i, to += (long long)step * bytes) {
+    if (!lane_live || first + i * step >= heads) continue;
+    *reinterpret_cast<unsigned *>(to + (d0 >> 1)) = codes[i];
+    if (lane * 4 < bytes - head_dim / 2)
+      *reinterpret_cast<unsigned *>(to + head_dim / 2 + lane * 4) = lane == 0 ? __float_as_uint(scale[i]) : lane <= LPH / 8 ? word[i] : 0u;
   }
 }
 
@@ -379,6 +404,10 @@ __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_consta
         if (live && at0 + i * per_token + sub < heads) store8<XT>(to, x[i]);
     } else {
       char *row = a.c.base + (now == 2 ? a.c.v_offset : 0) + t.offset;
+      if constexpr (four_bit(FMT)) {
+        put4<LPH, kAhead>(x, row, at0 + sub, per_token, heads, a.c.head_dim, d0, live);
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int head = at0 + i * per_token + sub;
