@@ -2,7 +2,7 @@
 // (kvr_attend_rows.cuh); what differs is how the cache gets to them, for 4 bits leave half as many cycles for a key.
 //
 // A warp of its own brings the keys of a stage for all heads of the CTA's group: TMA boxes of whole tokens (a group's records side by
-// side, K and V), or, for block sizes that are no multiple of 8, 16-byte copies.  The warps of the heads spend nothing on addresses.  A
+// side, K and V), or, for block sizes that are no multiple of 8, a bulk copy for each token.  The warps of the heads spend nothing on addresses.  A
 // stage's rows stand `stride` bytes apart, 32 more than a multiple of 128 where records are many (the boxes are wider than the rows):
 // then the rows that a read looks at (four keys, 32 bytes of each) fall into different banks, with keys 4 to 7 of each 8 swapped in pairs.
 //
@@ -28,7 +28,7 @@ __device__ __forceinline__ bool bar4_try(unsigned bar, unsigned parity) {
   return ok != 0;
 }
 // A warp's wait.  One that runs out (after `polls`) sets the flag and goes on like one that did not, on whatever is there, as do all later
-// ones at once: no role leaves its loops early, so that barriers between warps always meet.
+// ones at once: the heads' warps do not leave their loops early, so that barriers between them always meet.
 __device__ __forceinline__ void bar4_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned polls) {
   unsigned spin = 0;
   while (!bar4_try(bar, parity)) {
@@ -40,6 +40,9 @@ __device__ __forceinline__ void bar4_wait(unsigned bar, unsigned parity, volatil
 __device__ __forceinline__ void box4_load(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int row, int block, int plane) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(row), "r"(block), "r"(plane) : "memory");
+}
+__device__ __forceinline__ void row4_load(unsigned dst, const char *src, int bytes, unsigned bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void product4(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -170,7 +173,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   if (!open_piece(a, start, last)) return;     // an opening alone
   if (threadIdx.x == 0) {
     gave_up_word = a.polls == 0;
-    for (int i = 0; i < r4.stages; ++i) { bar4_init(shared_at(&full[i]), r4.box_rows ? 1 : 32); bar4_init(shared_at(&empty[i]), warps); }
+    for (int i = 0; i < r4.stages; ++i) { bar4_init(shared_at(&full[i]), 1); bar4_init(shared_at(&empty[i]), warps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp < warps && lane == 0) pieces[warp] = start;
@@ -202,10 +205,28 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       unsigned char *st = smem + stage * stage_bytes;
       const unsigned bar = shared_at(&full[stage]);
       if (round) bar4_wait(shared_at(&empty[stage]), (round - 1) & 1, gave_up, a.polls);
+      if (__any_sync(0xffffffffu, *gave_up != 0)) break;     // nothing more is brought into places that may be in use
+      // K and V of `n` pieces of the stage, a lane a piece: brought by bring() where its block is known, zeros where not.  All of the stage's bytes
+      // are expected by the one arrival, which comes with its last pieces.
+      auto bring_all = [&](bool in, bool known, unsigned char *to, int bytes, bool last_ones, auto bring) {
+        if (in && !known) {
+          report(a.b.status, KVR_DEV_BAD_BLOCK);
+          for (int i = 0; i < bytes; i += 16)
+            *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<uint4 *>(to + plane_bytes + i) = make_uint4(0, 0, 0, 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
+        if (lane == 0) {
+          if (last_ones) bar4_expect(bar, got * 2 * bytes);
+          else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(got * 2 * bytes) : "memory");
+        }
+        __syncwarp();
+        if (known) bring();
+        __syncwarp();
+      };
       if (r4.box_rows) {
         const int boxes = min(stage_keys, keys + r4.box_rows - 1) / r4.box_rows, box0 = key0 / r4.box_rows;
         for (int b0 = 0; b0 < boxes; b0 += 32) {
-          // a lane a box of K and a box of V
           if (box0 + b0 >= id_base + 32) {
             id_base += 32;
             ids = later_ids;
@@ -213,48 +234,24 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
           const int box = b0 + lane, at = box0 + box - id_base, token = key0 + box * r4.box_rows;
           const int now = __shfl_sync(0xffffffffu, ids, at & 31), then = __shfl_sync(0xffffffffu, later_ids, at & 31), id = at < 32 ? now : then;
-          const bool in = box < boxes, known = in && (unsigned)id < (unsigned)a.c.num_blocks;
           unsigned char *to = st + box * r4.box_bytes;
-          if (in && !known) {          // a block that is not there
-            report(a.b.status, KVR_DEV_BAD_BLOCK);
-            for (int i = 0; i < r4.box_bytes; i += 16)
-              *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<uint4 *>(to + plane_bytes + i) = make_uint4(0, 0, 0, 0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          }
-          const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
-          if (lane == 0) {
-            // all of the stage's bytes are expected by the one arrival, which comes with its last boxes
-            if (b0 + 32 >= boxes) bar4_expect(bar, got * 2 * r4.box_bytes);
-            else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(got * 2 * r4.box_bytes) : "memory");
-          }
-          __syncwarp();
-          if (known) {
+          bring_all(box < boxes, box < boxes && (unsigned)id < (unsigned)a.c.num_blocks, to, r4.box_bytes, b0 + 32 >= boxes, [&] {
             const int row = token - (int)a.bs.div((unsigned)token) * (int)a.bs.d;
             box4_load(shared_at(to), &map, bar, x0 >> 3, row, id, 0);
             box4_load(shared_at(to + plane_bytes), &map, bar, x0 >> 3, row, id, 1);
-          }
-          __syncwarp();
+          });
         }
       } else {
-        const int columns = min(a.group_heads * a.c.head_bytes, a.c.kv_heads * a.c.head_bytes - x0) / 16;
+        const int bytes = min(a.group_heads * a.c.head_bytes, a.c.kv_heads * a.c.head_bytes - x0);
         for (int k0 = 0; k0 < keys; k0 += 32) {
-          // a lane finds a key
           const int key = k0 + lane;
-          const long long found = key < keys ? token_offset(a.b, a.c, a.bs, start.r, key0 + key) : -1;
-          if (found < 0 && key < keys) report(a.b.status, KVR_DEV_BAD_BLOCK);
-          const int n = min(32, keys - k0) * columns;
-          for (int i = lane; i - lane < n; i += 32) {
-            const int k = min(i / columns, 31), column = i - k * columns;
-            const long long off = __shfl_sync(0xffffffffu, found, k);
-            if (i >= n) continue;
-            const char *src = a.c.base + (off >= 0 ? off + x0 + column * 16 : 0);
-            const unsigned to = shared_at(st + (k0 + k) * stride) + column * 16;
-            copy16(to, src, off >= 0);
-            copy16(to + plane_bytes, src + (off >= 0 ? a.c.v_offset : 0), off >= 0);
-          }
-          __syncwarp();
+          const long long off = key < keys ? token_offset(a.b, a.c, a.bs, start.r, key0 + key) : -1;
+          unsigned char *to = st + key * stride;
+          bring_all(key < keys, off >= 0, to, bytes, k0 + 32 >= keys, [&] {
+            row4_load(shared_at(to), a.c.base + off + x0, bytes, bar);
+            row4_load(shared_at(to + plane_bytes), a.c.base + off + a.c.v_offset + x0, bytes, bar);
+          });
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
       }
       if (++stage == r4.stages) { stage = 0; ++round; }
       if (++t == end) {
@@ -264,7 +261,6 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         if (more && r4.box_rows) first_ids();
       }
     }
-    copy_wait<0>();
   } else {
     // ---- products and softmax
     const Piece &piece = pieces[warp];

@@ -549,3 +549,72 @@ def test_a_4_bit_request_is_forked_suspended_compacted_and_answers_the_same():
         assert p.resume_from_host([1], kvr.SYNC)[0] == kvr.OK and torch.equal(answer(1), first)
         assert p.info(1)[1]["blocks"].tolist() != blocks.tolist()
         assert len(p.compact()[1]) > 0 and torch.equal(answer(1), first) and torch.equal(answer(2), first)
+
+
+@pytest.mark.parametrize("heads,group,dim,bs,new", [(2, 4, 128, 16, 1), (8, 4, 128, 8, 1), (2, 8, 64, 5, 2), (1, 1, 256, 16, 3), (2, 4, 128, 16, 20), (2, 8, 64, 5, 10)])
+def test_a_call_that_gives_up_says_so_and_the_next_is_right(heads, group, dim, bs, new):
+    """Both kernels' waits have limits: lowered on the host, on barriers that do complete later."""
+    s = Setup("e2m1", heads, dim, bs, [900, 30, 0], [new] * 3, layers=1, seed=new)
+    s.fill()
+    mask, _ = base.tree(s, np.random.default_rng(new))
+    q = rand(s, s.tokens, heads * group, dim)
+
+    def attend():
+        out, ws = torch.zeros_like(q), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+        s.status.zero_()
+        s.cache.attend(s.pool, 0, s.batch, q, out, ws, mask=mask)
+        torch.cuda.synchronize()
+        return out, int(s.status)
+
+    want, status = attend()
+    assert status == 0
+    polls = kvr.lib().kvr_test_attend_polls
+    for limit in (0, 1, 8, 100):
+        was = polls(limit)
+        try:
+            out, status = attend()
+        finally:
+            polls(was)
+        assert status == kvr.DEV_GAVE_UP if limit == 0 else status in (0, kvr.DEV_GAVE_UP)
+        assert status or torch.equal(out, want)
+        out, status = attend()
+        assert status == 0 and torch.equal(out, want)
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own():
+    """On two streams, several times; each answer is the one that the call gives alone."""
+    a = Setup("e2m1", 8, 128, 16, [3000, 500, 70], [1, 1, 1], layers=1, seed=5)
+    b = Setup("e2m1", 2, 64, 8, [4000, 9], [30, 7], layers=1, seed=6)
+    both = []
+    for s, heads in ((a, 32), (b, 8)):
+        s.fill()
+        q = rand(s, s.tokens, heads, s.dim)
+        both.append((s, q, torch.zeros_like(q), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda"), torch.cuda.Stream()))
+    want = []
+    for s, q, out, ws, _ in both:
+        s.cache.attend(s.pool, 0, s.batch, q, out, ws)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+        out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, q, out, ws, stream in both:
+            with torch.cuda.stream(stream):
+                s.cache.attend(s.pool, 0, s.batch, q, out, ws)
+    torch.cuda.synchronize()
+    for (s, q, out, ws, _), x in zip(both, want):
+        assert torch.equal(out, x)
+        s.ok()
+
+
+def test_rows_behind_the_last_request_stay_as_they_were():
+    s = Setup("e2m1", 2, 128, 16, [40, 3], [1, 2], seed=8)
+    s.fill()
+    for grown in (1, 30):                        # the row kernel's tiles, and the tile kernel's
+        new = s.batch if grown == 1 else kvr.Batch(*s.arrays, 30, 70, s.status)
+        q = rand(s, 7, 8, 128)
+        out, lse = torch.full_like(q, 5.0), torch.full((7, 8), 5.0, device="cuda")
+        ws = torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+        s.cache.attend(s.pool, 0, new, q, out, ws, lse=lse)
+        s.ok()
+        assert (out[3:] == 5).all() and (lse[3:] == 5).all() and (out[:3] != 5).any()
