@@ -111,8 +111,8 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   a.q_heads = q->heads;
   const int padded = spec->head_dim <= 64 ? 64 : spec->head_dim <= 128 ? 128 : 256;
   const bool four = four_bit(spec->format);
-  const int warps = four ? rows4_warps(padded) : rows_warps(padded);
   const int64_t rows = (int64_t)batch->max_new * group;
+  const int warps = four ? kRows4Warps : rows_warps(padded);
   int tiles = 0, slices = 0;
   CUtensorMap map{};
   Rows4 r4{};
@@ -156,9 +156,9 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     const int turn = 16 * slices * (four ? rows4_chunks(padded, tiles) : chunks_at_once(spec->format, tiles));      // keys that the warps of a head take at a time
     a.unit = FastDiv((64 + turn - 1) / turn * turn);
     if (four) {
-      // A segment begun inside a CTA's share costs it another Q, the join of its warps and a piece to hand in.  (us, weight 0 / 1 / 2 / 3 / 4: 32 requests
-      // of 300 tokens 33 / 27 / 27 / 27 / 27, of 2k 51 / 49 / 47 / 45 / 45, of 8k 102 / 100 / 98 / 98 / 96; 8 of 4k 41 / 39 / 35 / 35 / 37.)
-      a.opening = 3;
+      // A segment begun inside a CTA's share costs it another Q and a piece to hand in.  (us, weight 1 / 2 / 3, units of 96 keys: 32 requests of 300 tokens
+      // 26 / 27 / 27, of 2k 41 / 40 / 41, of 8k 90 / 88 / 90; 8 of 4k 33 / 30 / 29.)
+      a.opening = 2;
       r4.slices = slices;
       const int group_bytes = a.group_heads * a.c.head_bytes, stage_keys = 16 * rows4_chunks(padded, tiles) * slices;
       // Rows of many records stand 32 bytes behind a multiple of 128, for the banks; of few as they are, or the ring would hold too few keys.

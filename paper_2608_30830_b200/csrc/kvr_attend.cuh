@@ -148,8 +148,8 @@ __host__ __device__ constexpr int rows_warps(int padded_dim) { return padded_dim
 
 // Of the row kernel for 4-bit caches: warps that a CTA's heads share; shared memory beside its barriers, and what of it is not the ring's
 // (statistics and a quarter of the accumulators of all slices; what is read past the last record).
-__host__ __device__ constexpr int rows4_warps(int padded_dim) { return padded_dim == 256 ? 8 : 16; }
-__host__ __device__ constexpr int rows4_chunks(int padded_dim, int tiles) { return tiles == 1 ? 2 : 1; }      // of 16 keys, that a warp takes at a time
+constexpr int kRows4Warps = 8;
+__host__ __device__ constexpr int rows4_chunks(int padded_dim, int tiles) { return padded_dim == 256 ? 3 - tiles : tiles == 2 ? 2 : padded_dim == 128 ? 3 : 4; }      // of 16 keys, that a warp takes at a time
 __host__ __device__ constexpr int rows4_beside(int padded_dim, int tiles, int heads, int slices) {
   return (slices > 1 ? heads * slices * tiles * 64 + heads * (slices - 1) * (padded_dim / 64) * 512 : 0) + 256;
 }

@@ -151,7 +151,7 @@ __device__ __noinline__ void fold4(const AttendArgs &a, const Cut &cut, int c, i
 
 // EXACT: head_dim is DP, so that the scales' place is known.
 template <int DP, int NT, bool EXACT>
-__global__ void __launch_bounds__((rows4_warps(DP) + 1) * 32, 1)
+__global__ void __launch_bounds__((kRows4Warps + 1) * 32, 1)
 attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Rows4 r4, const __grid_constant__ CUtensorMap map) {
   constexpr int kTiles = DP / 16, kChunks = rows4_chunks(DP, NT), kWide = DP / 64, kTails = DP == 256 ? 2 : 1;
   constexpr float kLazy = 4.f;         // as in the row kernel
@@ -159,7 +159,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ unsigned scratch[39];
   __shared__ __align__(8) unsigned long long full[kMaxStages4], empty[kMaxStages4];
   __shared__ int last_in, gave_up_word;
-  __shared__ Piece pieces[rows4_warps(DP)];     // of the heads' warps, whose registers are the products'
+  __shared__ Piece pieces[kRows4Warps];     // of the heads' warps, whose registers are the products'
   volatile int *gave_up = &gave_up_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
   const int slices = r4.slices, stride = r4.stride, warps = a.group_heads * slices, stage_keys = 16 * kChunks * slices;
@@ -401,13 +401,15 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         float best[NT][2];
         bool moved = false;
         float big = fmaxf(v_scale[0][0], v_scale[0][1]);
-        if constexpr (kChunks == 2) big = max3(big, v_scale[kChunks - 1][0], v_scale[kChunks - 1][1]);
+#pragma unroll
+        for (int u = 1; u < kChunks; ++u) big = max3(big, v_scale[u][0], v_scale[u][1]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float m = fmaxf(s[0][n][e], s[0][n][2 + e]);
-            if constexpr (kChunks == 2) m = max3(m, s[kChunks - 1][n][e], s[kChunks - 1][n][2 + e]);
+#pragma unroll
+            for (int u = 1; u < kChunks; ++u) m = max3(m, s[u][n][e], s[u][n][2 + e]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
