@@ -116,7 +116,8 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
   int tiles = 0, slices = 0;
   CUtensorMap map{};
   Rows4 r4{};
-  if (rows > 16 && padded <= 128) {
+  // (4 bits, us, row kernel / tile kernel: 16 requests of 8k, rows 20 / 32 / 36: 141 / 203, 150 / 201, 195 / 205; heads of 64 channels, 32 of 4k, 32 rows: 98 / 172.)
+  if (rows > (four ? 48 : 16) && padded <= 128) {
     // More rows than two tiles of the row kernel.  (us, 8 KV heads of 128, 2 requests of 16k / 32 of 4k.  16 rows: row kernel
     // 44 / 115, tile kernel 54 / 122; int8 44 / 121, 68 / 207.  32 rows, with four tiles of the row kernel, which there was: 198 / 190, tile
     // kernel 57 / 128; int8 228 / 256, 74 / 211.)  Heads of more than 128 channels stay with the row kernel: two jobs' sums and scores
@@ -144,8 +145,8 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
     // a segment's pieces are joined by one CTA.  (us, 8 rows, 16-bit / int8, all heads in a CTA against this: 1 request of 4k 39 / 44,
     // 24 / 20; 2 of 16k 67 / 66, 39 / 33; 8 of 16k 111 / 100, 97 / 85; 4 pieces: 96 / 98, 16 pieces: 95 / 85.)  Not where one tile of
     // rows streams a long 8-bit cache, whose narrow rows and scales are then read in pieces too small: by the caller's bounds, from 512 MB
-    // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316.  4 bits, whole / split: of 4k, 42 MB, 53 / 37,
-    // of 8k 59 / 51, of 16k 78 / 78, of 32k 115 / 129: from 128 MB on).
+    // on (int8, 4 rows, 8 requests: of 4k, 67 MB, 49 us whole, 34 split; of 16k 82, 87; of 64k 233, 316.  4 bits, whole / split: of 4k, 42 MB, 43 / 31,
+    // of 8k 51 / 43, of 16k 70 / 70, of 32k 100 / 115: from 128 MB on).
     const int64_t stream = 2ll * batch->n_req * batch->max_tokens * a.c.row_bytes;
     const bool whole = quantised(spec->format) && tiles == 1 && stream >= (four ? 128ll : 512ll) << 20;
     while (!whole && a.group_heads > 1 && (int64_t)batch->n_req * a.head_groups * 8 < sms) {
