@@ -1,6 +1,6 @@
 """One layer of a serving loop over a kvr pool: prefill, a step of drafted tokens, the wait for a human, and on.
 
-    python examples/drafted_decode.py [bf16 | f16 | e4m3 | int8]
+    python examples/drafted_decode.py [bf16 | f16 | e4m3 | int8 | e2m1]
 
 The pool's block tables and the cache operators work on the same memory: kvr.Pool hands out blocks and moves them to the
 host and back, kvr.Cache writes tokens into them and attends over them.  Random numbers stand in for the projections.

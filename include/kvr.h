@@ -490,8 +490,8 @@ kvr_status kvr_cache_read(const kvr_cache_spec *spec, const void *device_pool, i
  * whatever lies there (NaN included).  q and out: [n_tokens] rows of the same heads and type, 16-bit; for a 16-bit cache of
  * the cache's type.  Scores, sums and accumulators are fp32.  Rounded to fewer bits, besides out:
  *   probabilities, to the 16-bit type of the product with V: 8 bits for bf16 caches, 11 for f16 (or 2^-25 of the row's largest);
- *   for 8-bit caches probability times V's scale, to f16: 11 bits, or 2^-32 of the largest scale among the keys that the row sees;
- *   for 8-bit caches q, to f16: 11 bits (a bf16 element has 8), or 2^-25 of the row's largest element
+ *   for 8-bit and 4-bit caches probability times V's scale (of the head), to f16: 11 bits, or 2^-32 of the largest scale among the keys that the row sees;
+ *   for 8-bit and 4-bit caches q, to f16: 11 bits (a bf16 element has 8), or 2^-25 of the row's largest element
  * (whichever is more).
  * At most 2^30 tokens in one request, and n_req, max_new and max_tokens such that tiles of query rows times spans of 64 keys stay below
  * 2^31 (KVR_ERR_INVALID_ARG).  max_new chooses the kernel and max_tokens how heads are shared out, so bounds near the truth are

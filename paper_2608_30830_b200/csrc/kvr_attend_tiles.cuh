@@ -22,7 +22,8 @@
 // the row kernel.
 //
 // Measured, 8 KV heads of 128, 256 rows (TWO), 16 requests of 8k, bf16: 169 to 191 us by the GPU and its clock, for 581 MB and 144 GFLOP
-// (3.4 to 3.0 TB/s, 850 to 755 TFLOP/s; either alone would take 89 us); over an e4m3 cache 303.  In the fast case a tile of 128 keys takes 2.0 us, in which a warpgroup is busy for 1.3 with its exponentials and waits 0.7
+// (3.4 to 3.0 TB/s, 850 to 755 TFLOP/s; either alone would take 89 us); over an e4m3 cache 289 to 303, over a 4-bit one 287 to 300 (its records of 80 bytes come
+// whole, scales among them; without the widening 254, without the multiplications by scales too 193).  In the fast case a tile of 128 keys takes 2.0 us, in which a warpgroup is busy for 1.3 with its exponentials and waits 0.7
 // for its products, whose scores cannot be asked for before the probabilities in the same place are used up.  Around the stream:
 // 7 us until Q is in and the first scores are there, 5 for each epilogue, 12 to 15 for a join.  104 rows of an int8 cache, 2 KV heads, 32
 // requests of 8k: 121 to 124 us for 152 MB: 2.5 us a tile, of which a widening warp takes 1.4 for its half of K or V.

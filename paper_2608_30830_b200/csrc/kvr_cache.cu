@@ -310,7 +310,9 @@ __device__ __forceinline__ void put4(const float (&x)[N][8], char *row, int firs
 // 32k tokens of 32 query and 8 KV heads of 128 into an e4m3 cache: 734 MB in 156 to 160 us, 4.7 TB/s (int8 165).  Two CTAs an SM (128
 // registers) issue in half of the cycles and DRAM is busy for 54 %: neither is full, the warps wait on their loads; bytes alone would
 // take 112 us.  Into a bf16 cache 797 MB in 140 us, 5.7 TB/s.  Fewer heads ahead for more CTAs: 170 us (three), 179 us (four).  A step of 32
-// tokens takes 5.5 us replayed in a graph (dependent loads: token_start, block table, angles); a call from Python more than that.
+// tokens takes 5.5 us replayed in a graph (dependent loads: token_start, block table, angles); a call from Python more than that.  Into a 4-bit cache
+// 32k tokens take 160 us, 730 MB, 4.6 TB/s: q's half runs at the memory's rate (82 us), k and v wait on the chains of put4 (78 us for 193 MB; one
+// head after the other 90).  With positions of three axes 16k tokens take what they take with one (84 us, 4.9 TB/s).
 template <int XT, int FMT, int LPH, bool AXES>
 __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kGroups = kThreads / LPH, kSize = XT == KVR_F32 ? 4 : 2, kAhead = XT == KVR_F32 ? 2 : 4;
