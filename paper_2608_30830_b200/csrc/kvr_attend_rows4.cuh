@@ -15,8 +15,9 @@
 // 48 keys a turn (32 of 128 channels: 300 us; 64: 287), so that the maximum, the votes and the barriers come once for three chunks.
 //
 // Measured, 8 KV heads of 128.  8 requests of 128k, one token of 4 query heads: 1.34 GB in 279 to 285 us, 4.7 TB/s (72 % of a copy; the algorithm's
-// bytes without the padding 198 us).  The loads alone take 166 us a GB, the products and conversions alone 158 (with nothing in shared memory to wait
-// for): neither is full, ALU 43 %, 0.52 instructions a cycle and scheduler from two warps, 299 instructions for a chunk.  32 requests of 8k: 88 us, of which 20 to 25 are the start
+// bytes without the padding 198 us).  The same loads and waits without the arithmetic take 244 us, the arithmetic over
+// zeros with nothing brought 272: the arithmetic bounds it, and no pipe is full (ALU 43 %, 0.52 instructions a cycle and scheduler from two
+// warps, 299 instructions for a chunk).  32 requests of 8k: 88 us, of which 20 to 25 are the start
 // (lengths, table, first box: 5 us), pieces handed in and joined.  One request of 333 tokens from a cold cache: 14 us.
 #pragma once
 #include "kvr_attend_common.cuh"
@@ -215,7 +216,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       const unsigned bar = shared_at(&full[stage]);
       if (round) bar4_wait(shared_at(&empty[stage]), (round - 1) & 1, gave_up, a.polls);
       if (__any_sync(0xffffffffu, *gave_up != 0)) break;     // nothing more is brought into places that may be in use
-      // K and V of `n` pieces of the stage, a lane a piece: brought by bring() where its block is known, zeros where not.  All of the stage's bytes
+      // K and V of up to 32 pieces of the stage, a lane a piece: brought by bring() where its block is known, zeros where not.  All of the stage's bytes
       // are expected by the one arrival, which comes with its last pieces.
       auto bring_all = [&](bool in, bool known, unsigned char *to, int bytes, bool last_ones, auto bring) {
         if (in && !known) {

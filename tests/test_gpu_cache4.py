@@ -618,3 +618,27 @@ def test_rows_behind_the_last_request_stay_as_they_were():
         s.cache.attend(s.pool, 0, new, q, out, ws, lse=lse)
         s.ok()
         assert (out[3:] == 5).all() and (lse[3:] == 5).all() and (out[:3] != 5).any()
+
+
+@pytest.mark.parametrize("heads,group,dim,bs,new", [(1, 4, 64, 8, 1), (1, 1, 64, 64, 1), (2, 4, 128, 128, 1), (8, 4, 128, 256, 1), (8, 2, 128, 48, 3), (20, 1, 128, 16, 1),
+                                                    (7, 2, 256, 40, 2), (3, 4, 32, 9, 3), (4, 12, 96, 64, 4), (1, 16, 128, 2, 2)])
+def test_attend_any_block_size_and_number_of_heads(heads, group, dim, bs, new):
+    """Blocks that are smaller and larger than a stage of the loads, boxes of every size, groups of heads that do not divide; two layers, the second one read."""
+    s = Setup("e2m1", heads, dim, bs, [1500, 0, 47, 400, 1], [new] * 5, seed=heads + dim + bs, layout=bs % 2)
+    base.check_attend(s, heads * group, "bf16", layer=1)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_tables_cut_from_wider_ones(new):
+    """Rows of a table that are views into wider ones, with ids behind them that are no blocks."""
+    s = Setup("e2m1", 2, 128, 16, [100, 37], [new, new], seed=9)
+    k, v = s.fill()
+    q, ws = rand(s, s.tokens, 8, 128), torch.zeros(s.cache.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    width = -(-(100 + new) // 16)
+    wide = torch.full((2, 50), s.nb + 7, dtype=torch.int32, device="cuda")
+    wide[:, 10:10 + width] = s.arrays[2][:, :width]
+    out = [torch.zeros_like(q) for _ in range(2)]
+    s.cache.attend(s.pool, 0, s.batch, q, out[0], ws)
+    s.cache.attend(s.pool, 0, kvr.Batch(s.arrays[0], s.arrays[1], wide[:, 10:10 + width], new, 100 + new, s.status), q, out[1], ws)
+    s.ok()
+    assert torch.equal(*out)
