@@ -437,7 +437,10 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
         if (popped) tag = p->fq.pop(1, &own);
         else for (int32_t i = nb; i < r.nb && own < 0; ++i) if (p->fq.refs(r.blocks[i]) == 1) own = r.blocks[i];
         if (own < 0) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
+        if (!popped) tag = p->fq.tag(own);
         pairs.push_back(make_int2(r.blocks[nb - 1], own));
+      } else if (part && n_tokens < r.n_tokens) {
+        tag = p->fq.tag(r.blocks[nb - 1]);                   // nobody else refers to it, but the suspend of one that did may still read it
       }
       if (!p->meta_only && (nb < r.nb || own >= 0)) {        // blocks change hands: later moves come behind the caller's work on them
         if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag)) {
@@ -460,7 +463,8 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
   r.n_shared = std::min(r.n_shared, (int32_t)(n_tokens / p->BS));
   r.image_bytes = (uint64_t)private_tokens(p, r) * p->bpt;
   if (out_blocks && nb) memcpy(out_blocks, r.blocks.data(), (size_t)nb * 4);
-  if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);       // a gather may still be reading the added blocks
+  // a gather may still be reading the added blocks, or the last one
+  if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);
   return KVR_OK;
 }
 
