@@ -66,6 +66,9 @@ void free_host(kvr_pool *p, Request &r, uint64_t reader_seq) {
   r.arena_off = r.arena_len = 0;
 }
 
+// blocks of n_tokens >= 0 tokens; no sum that could pass 64 bits
+inline int64_t blocks_for(const kvr_pool *p, int64_t n_tokens) { return n_tokens / p->BS + (n_tokens % p->BS != 0); }
+
 inline int64_t private_tokens(const kvr_pool *p, const Request &r) { return r.n_tokens - (int64_t)r.n_shared * p->BS; }
 
 // shared body of the four bookkeeping-only outcomes and of the per-request loops
@@ -97,7 +100,7 @@ kvr_status check_donor(kvr_pool *p, uint64_t id, uint64_t donor_id, int32_t n_sh
 // the new request's table: donor prefix (one more reference each) followed by ids from the head of the queue
 kvr_status admit_common(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t id, int64_t n_tokens, const Request *donor,
                         int32_t n_shared, int32_t *out_blocks) {
-  const int64_t nb = (n_tokens + p->BS - 1) / p->BS;
+  const int64_t nb = blocks_for(p, n_tokens);
   if (nb - n_shared > p->fq.size()) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
   std::vector<int32_t> table((size_t)nb);
   for (int32_t i = 0; i < n_shared; ++i) table[i] = donor->blocks[i];
@@ -237,7 +240,7 @@ kvr_status kvr_request_admit(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_t
   if (kvr_status s = check_pool(p)) return s;
   Enter enter(p);
   if (n_tokens < 0) return fail(KVR_ERR_INVALID_ARG, "n_tokens < 0");
-  const int64_t nb = (n_tokens + p->BS - 1) / p->BS;
+  const int64_t nb = blocks_for(p, n_tokens);
   if (out_blocks && cap < nb) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
   auto it = p->reqs.find(id);
   if (it != p->reqs.end() && it->second.state != KVR_EXPIRED) return fail(KVR_ERR_BAD_STATE, "request exists");
@@ -253,7 +256,7 @@ kvr_status kvr_request_admit_sharing(kvr_pool *p, uint64_t id, int64_t n_tokens,
   if (kvr_status s = check_pool(p)) return s;
   Enter enter(p);
   if (n_tokens < 0 || n_shared < 0) return fail(KVR_ERR_INVALID_ARG, "negative size");
-  const int64_t nb = (n_tokens + p->BS - 1) / p->BS;
+  const int64_t nb = blocks_for(p, n_tokens);
   if ((int64_t)n_shared * p->BS > n_tokens) return fail(KVR_ERR_INVALID_ARG, "the shared prefix must be whole blocks inside the request");
   if (out_blocks && cap < nb) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
   auto it = p->reqs.find(id);
@@ -273,19 +276,18 @@ kvr_status kvr_request_admit_sharing_into(kvr_pool *p, uint64_t id, int64_t n_to
   Enter enter(p);
   if (n_tokens < 0 || n_shared < 0 || n_private < 0 || (n_private > 0 && !private_blocks)) return fail(KVR_ERR_INVALID_ARG, "bad size or block list");
   if ((int64_t)n_shared * p->BS > n_tokens) return fail(KVR_ERR_INVALID_ARG, "the shared prefix must be whole blocks inside the request");
-  if ((n_tokens + p->BS - 1) / p->BS != (int64_t)n_shared + (int64_t)n_private)
+  if (blocks_for(p, n_tokens) != (int64_t)n_shared + (int64_t)n_private)
     return fail(KVR_ERR_INVALID_ARG, "shared + private blocks must equal ceil(n_tokens / block_size)");
   auto it = p->reqs.find(id);
   if (it != p->reqs.end() && it->second.state != KVR_EXPIRED) return fail(KVR_ERR_BAD_STATE, "request exists");
   const bool existed = it != p->reqs.end();
+  const Request *donor = nullptr;
+  if (n_shared > 0) { if (kvr_status s = check_donor(p, id, donor_id, n_shared, &donor)) return s; }
+  if (n_private > p->NB - n_shared) return fail(KVR_ERR_INVALID_ARG, "more blocks than the pool has");
   try {
     const int32_t nb = n_shared + n_private;
     std::vector<int32_t> table((size_t)nb), prevs((size_t)n_private);
-    if (n_shared > 0) {
-      const Request *donor = nullptr;
-      if (kvr_status s = check_donor(p, id, donor_id, n_shared, &donor)) return s;
-      for (int32_t i = 0; i < n_shared; ++i) table[i] = donor->blocks[i];
-    }
+    for (int32_t i = 0; i < n_shared; ++i) table[i] = donor->blocks[i];
     Request &r = p->reqs[id];
     uint64_t tag = 0;
     int32_t bad = -1;
@@ -310,7 +312,7 @@ kvr_status kvr_request_admit_into(kvr_pool *p, uint64_t id, int64_t n_tokens, co
   if (kvr_status s = check_pool(p)) return s;
   Enter enter(p);
   if (n_tokens < 0 || nb < 0 || (nb > 0 && !blocks)) return fail(KVR_ERR_INVALID_ARG, "bad size or block list");
-  if ((n_tokens + p->BS - 1) / p->BS != (int64_t)nb) return fail(KVR_ERR_INVALID_ARG, "nb must equal ceil(n_tokens / block_size)");
+  if (blocks_for(p, n_tokens) != (int64_t)nb) return fail(KVR_ERR_INVALID_ARG, "nb must equal ceil(n_tokens / block_size)");
   auto it = p->reqs.find(id);
   if (it != p->reqs.end() && it->second.state != KVR_EXPIRED) return fail(KVR_ERR_BAD_STATE, "request exists");
   const bool existed = it != p->reqs.end();
@@ -408,7 +410,7 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
   if (kvr_status s = check_pool(p)) return s;
   Enter enter(p);
   if (n_tokens < 0) return fail(KVR_ERR_INVALID_ARG, "n_tokens < 0");
-  const int64_t blocks = (n_tokens + p->BS - 1) / p->BS;
+  const int64_t blocks = blocks_for(p, n_tokens);
   if (out_blocks && cap < blocks) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
   if (kvr_status s = check_copy_stream(p, (cudaStream_t)stream)) return s;
   for (;;) {
