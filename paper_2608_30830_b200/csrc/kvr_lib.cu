@@ -129,10 +129,13 @@ kvr_status check_copy_stream(kvr_pool *p, cudaStream_t s) {
 }
 
 // Enqueues copies of `rows` rows on the caller's stream (behind the gather `tag`, which may still read a destination), and orders the pool's
-// own streams behind what that stream holds by then.  On failure nothing of it is left in the stream.
-kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag) {
+// own streams behind what that stream holds by then.  On failure nothing of it is left in the stream.  live: the destination holds tokens of the
+// request until the call succeeds; once the copy has been launched they are gone, so what fails behind it must not undo the call: the stream has
+// come to rest by then, and nothing is left to be ordered.
+kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag, bool live) {
   const PoolView view{p->d_pool, p->plane_stride, p->block_stride, p->planes, p->NB, p->BS, p->row};
   cudaEvent_t reached = nullptr;
+  bool launched = false;
   try {
     p->event_pool.reserve(p->event_pool.size() + 1);         // nothing below allocates on the host
   } catch (const std::bad_alloc &) {
@@ -142,12 +145,13 @@ kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows,
     if (kvr_status st = get_event(p, &reached)) return st;
     if (kvr_status st = stream_after(p, s, tag, true)) return st;
     CUP(p, copy_blocks(view, pairs.data(), (int)pairs.size(), rows, s));
+    launched = true;
     CUP(p, cudaEventRecord(reached, s));
     for (cudaStream_t own : {p->s_gather, p->s_d2h, p->s_h2d, p->s_scatter}) CUP(p, cudaStreamWaitEvent(own, reached, 0));
     return KVR_OK;
   };
-  const kvr_status st = run();
-  if (st != KVR_OK) cudaStreamSynchronize(s);
+  kvr_status st = run();
+  if (st != KVR_OK && cudaStreamSynchronize(s) == cudaSuccess && launched && live) st = KVR_OK;
   put_event(p, reached);
   return st;
 }
@@ -384,7 +388,7 @@ kvr_status kvr_request_fork(kvr_pool *p, uint64_t id, uint64_t donor_id, int64_t
       if (!existed) p->reqs[id].state = KVR_EXPIRED;         // the node is there before anything is taken
       tag = p->fq.pop(1, &table[full]);
       pairs[0].y = table[full];
-      const kvr_status s = p->meta_only ? KVR_OK : enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag);
+      const kvr_status s = p->meta_only ? KVR_OK : enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, false);
       if (s != KVR_OK) {
         p->fq.unpop(&table[full], 1);
         if (!existed) p->reqs.erase(id);
@@ -445,7 +449,7 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
         tag = p->fq.tag(r.blocks[nb - 1]);                   // nobody else refers to it, but the suspend of one that did may still read it
       }
       if (!p->meta_only && (nb < r.nb || own >= 0)) {        // blocks change hands: later moves come behind the caller's work on them
-        if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag)) {
+        if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, own >= 0 && !popped)) {
           if (popped) p->fq.unpop(&own, 1);
           return s;
         }
@@ -488,7 +492,7 @@ kvr_status kvr_pool_compact(kvr_pool *p, int32_t max_moves, int32_t *moves, int3
     if (pairs.empty()) return KVR_OK;
     std::vector<int32_t> now((size_t)p->NB);
     for (int32_t b = 0; b < p->NB; ++b) now[b] = b;
-    if (!p->meta_only) { if (kvr_status s = enqueue_copies(p, pairs, p->BS, (cudaStream_t)stream, 0)) return s; }
+    if (!p->meta_only) { if (kvr_status s = enqueue_copies(p, pairs, p->BS, (cudaStream_t)stream, 0, false)) return s; }
     for (const int2 &m : pairs) { p->fq.move(m.x, m.y); now[m.x] = m.y; }
     for (auto &entry : p->reqs)
       for (int32_t &b : entry.second.blocks) b = now[b];
