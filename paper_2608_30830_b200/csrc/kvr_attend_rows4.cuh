@@ -225,6 +225,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
             *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<uint4 *>(to + plane_bytes + i) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
+        __syncwarp();                  // a vote orders no memory: the zeros go before lane 0's arrival
         const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
         if (lane == 0) {
           if (last_ones) bar4_expect(bar, got * 2 * bytes);
@@ -652,6 +653,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         again = next_piece(a, next, last);
         pieces[warp] = next;
       }
+      __syncwarp();                    // nor does a shuffle: the piece goes before what the other lanes read of it
       again = __shfl_sync(0xffffffffu, again, 0);
     }
   }
