@@ -26,22 +26,11 @@ namespace kvr {
 namespace {
 
 // ---- barriers and boxes
-__device__ __forceinline__ void bar4_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar4_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void bar4_expect(unsigned bar, unsigned bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar4_try(unsigned bar, unsigned parity) {
-  unsigned ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 // A warp's wait.  One that runs out (after `polls`) sets the flag and goes on like one that did not, on whatever is there, as do all later
 // ones at once: the heads' warps do not leave their loops early, so that barriers between them always meet.
 __device__ __forceinline__ void bar4_wait(unsigned bar, unsigned parity, volatile int *gave_up, unsigned polls) {
   unsigned spin = 0;
-  while (!bar4_try(bar, parity)) {
+  while (!bar_try(bar, parity)) {
     if (++spin >= polls) *gave_up = 1;
     if ((spin & 15) == 0 && *gave_up) break;
   }
@@ -183,7 +172,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   if (!open_piece(a, start, last)) return;     // an opening alone
   if (threadIdx.x == 0) {
     gave_up_word = a.polls == 0;
-    for (int i = 0; i < r4.stages; ++i) { bar4_init(shared_at(&full[i]), 1); bar4_init(shared_at(&empty[i]), warps); }
+    for (int i = 0; i < r4.stages; ++i) { bar_init(shared_at(&full[i]), 1); bar_init(shared_at(&empty[i]), warps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp < warps && lane == 0) pieces[warp] = start;
@@ -228,7 +217,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         __syncwarp();                  // a vote orders no memory: the zeros go before lane 0's arrival
         const unsigned got = __popc(__ballot_sync(0xffffffffu, known));
         if (lane == 0) {
-          if (last_ones) bar4_expect(bar, got * 2 * bytes);
+          if (last_ones) bar_expect(bar, got * 2 * bytes);
           else asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(got * 2 * bytes) : "memory");
         }
         __syncwarp();
@@ -271,6 +260,11 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
         end = stage_end(start);
         if (more && r4.box_rows) first_ids();
       }
+    }
+    // What has been asked for lands before the CTA ends, also where a wait has run out.
+    for (int i = 0; i < r4.stages; ++i) {
+      const unsigned asked = round + (i < stage);
+      if (asked && !bar_settle(shared_at(&full[i]), (asked - 1) & 1)) *gave_up = 1;
     }
   } else {
     // ---- products and softmax
@@ -520,7 +514,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           }
         }
         __syncwarp();
-        if (lane == 0) bar4_arrive(shared_at(&empty[slot]));
+        if (lane == 0) bar_arrive(shared_at(&empty[slot]));
         if (++slot == r4.stages) { slot = 0; ++round; }
       }
 
@@ -658,12 +652,7 @@ attend_rows4_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     }
   }
   __syncthreads();
-  if (gave_up_word) {
-    // boxes that were under way when a wait ran out still land in shared memory: a fifth of a millisecond is ample
-    for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
-    if (threadIdx.x == 0) report(a.b.status, KVR_DEV_GAVE_UP);
-    __syncthreads();
-  }
+  if (threadIdx.x == 0 && gave_up_word) report(a.b.status, KVR_DEV_GAVE_UP);
 }
 
 template <int DP, int NT, bool EXACT>

@@ -45,14 +45,6 @@ constexpr int kTileKeys = 128;
 constexpr int kSoftmax = 256;
 
 // ---- barriers, fences, tensor memory
-__device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity) {
-  unsigned ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 // A warp's wait.  All lanes ask and meet again behind it: what follows are instructions of the whole warp (tcgen05.ld, .mma, .commit) with
 // operands in uniform registers, and a loop that one lane ran while the others waited ahead of them led to wild addresses (it
 // was also slower, 170 clocks on a barrier that is complete against 95).  A wait that runs out (after `polls`), here or in another role,
@@ -116,9 +108,6 @@ __device__ __forceinline__ void tm_store1(unsigned at, unsigned x) { asm volatil
 __device__ __forceinline__ void tm_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void box_load(unsigned dst, const CUtensorMap *map, unsigned bar, int x, int head, int row, int block, int plane) {
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
                ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(head), "r"(row), "r"(block), "r"(plane) : "memory");
@@ -352,6 +341,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __shared__ __align__(8) TileBars bars;
   __shared__ unsigned tm_slot;
   __shared__ int gave_up_word, last_in;
+  __shared__ int brought[S::kSteps];             // 16-bit caches: a loader's last step
   __shared__ unsigned long long odd_keys[5][2];  // by ring slot: keys of a V tile with elements that are not finite
   __shared__ volatile int odd_codes;             // a loader has met codes of V that are NaN among a request's new tokens
   __shared__ float2 join_ml[2][128];
@@ -472,6 +462,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
       return false;
     };
     bool ok = true;
+    int done = -1;                       // this loader's last step
     auto slot_free = [&](int step) {     // has the buffer's previous tenant been used up?
       if (step >= S::kRing) bar_wait(shared_at(&bars.empty[step % S::kRing]), (step / S::kRing - 1) & 1, gave_up, a.polls);
       return __any_sync(0xffffffffu, *gave_up != 0) == 0;
@@ -518,9 +509,11 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           __syncwarp();
           if (lane == 0) bar_arrive(shared_at(&bars.full[slot]));
         }
+        done = at.step;
         at.advance(a, unit_tiles, last);
         mine();
       }
+      if (lane == 0) brought[group] = done;
     } else {
       // a step's codes and scales come to this warp's stage and are widened into the ring
       unsigned char *stage = raw + group * S::kRaw + span0 * DP;
@@ -556,7 +549,10 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
           phase ^= 1;
         }
         __syncwarp();
-        if (!ok) break;
+        if (!ok) {                       // the boxes land all the same before the CTA ends
+          if (boxes && !bar_settle(shared_at(&bars.raw_full[me]), phase ^ 1)) *gave_up = 1;
+          break;
+        }
         // 16 channels of a key are two neighbouring 16-byte columns.  Which goes first alternates with the half of the row and
         // with the key, so that 8-byte reads of 16 lanes and 16-byte writes of 8 lanes fall into different banks.
         const int c0 = (chunk & 3) * 2, swap = ((chunk >> 2) ^ sub) & 1;
@@ -668,7 +664,7 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
     }
     // all products have ended before tensor memory is given back
     tc_commit(shared_at(&bars.drained), leader);
-    bar_wait(shared_at(&bars.drained), 0, gave_up, a.polls);
+    if (!bar_settle(shared_at(&bars.drained), 0)) *gave_up = 1;
   } else if (warp < 8) {
     // ---- softmax: warpgroup w, thread = row
     const int w = warp >> 2, tid = threadIdx.x & 127;
@@ -1010,8 +1006,17 @@ attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant_
   __syncthreads();
   tc_after();
   if (gave_up_word) {
-    // boxes that were under way when a wait ran out still land in shared memory: a fifth of a millisecond is ample
-    for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
+    // Boxes under way when a wait ran out land before the CTA ends.  (Of 8-bit and 4-bit caches each loader has seen to its own.)  All roles have
+    // stopped: the last step that went to a buffer is the only one that may not have landed, for each took the place of one that had been used up.
+    if (!kQuant && threadIdx.x < S::kRing) {
+      int step = -1;
+      for (int g = 0; g < S::kSteps; ++g) {
+        int mine = brought[g];
+        while (mine >= 0 && mine % S::kRing != (int)threadIdx.x) mine -= S::kSteps;
+        step = max(step, mine);
+      }
+      if (step >= 0) bar_settle(shared_at(&bars.full[threadIdx.x]), (step / S::kRing) & 1);
+    }
     __syncthreads();
   }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
