@@ -208,8 +208,10 @@ kvr_status kvr_pool_destroy(kvr_pool *pool);
  * from the head of the free queue (in a server the engine's own allocator does
  * this; here it is what tests and benchmarks use).  out_blocks (cap entries,
  * may be NULL) receives the block table.  The blocks are safe to write when the
- * call returns: it waits for any gather still reading them.  Re-admitting an
- * EXPIRED id is allowed (the recompute happened).  n_tokens = 0 is legal.
+ * call returns: it waits for any gather still reading them, and for copies of
+ * kvr_request_fork, kvr_request_resize and kvr_pool_compact that use them (a
+ * block that a resize let go: for the work before it on that call's stream).
+ * Re-admitting an EXPIRED id is allowed (the recompute happened).  n_tokens = 0 is legal.
  * KVR_HBM_FULL, KVR_ERR_BAD_STATE (id exists), KVR_ERR_INVALID_ARG.
  */
 kvr_status kvr_request_admit(kvr_pool *pool, uint64_t req_id, int64_t n_tokens, int32_t *out_blocks, int32_t cap);
@@ -526,8 +528,9 @@ kvr_status kvr_cache_copy(const kvr_cache_spec *spec, void *device_pool, const i
 
 /*
  * Requests that share, grow and shrink, and a pool without holes.  Where these copy rows they enqueue the copies on `stream` (a cudaStream_t
- * of the pool's device, the one that the caller's kernels write the blocks from; NULL: the default stream), and later moves of this pool are ordered
- * behind them.  The stream must not be under capture (KVR_ERR_INVALID_ARG).  With KVR_METADATA_ONLY they keep the books alone.
+ * of the pool's device, the one that the caller's kernels write the blocks from; NULL: the default stream), and later moves of this pool, and calls of this
+ * kind on other streams that use the same blocks, are ordered behind them.  The blocks that a call hands out or leaves partly filled are safe to write on `stream`.
+ * The stream must not be under capture (KVR_ERR_INVALID_ARG).  With KVR_METADATA_ONLY they keep the books alone.
  *
  * kvr_request_fork: request new_id begins as the first n_tokens tokens of donor_id (ACTIVE or RETAINED): full blocks are shared, as in
  * kvr_request_admit_sharing, and the rows of a last block that is not full are copied into a block of its own, so either may go on writing.

@@ -112,6 +112,12 @@ kvr_status poll(kvr_pool *p) {
     else if (e == cudaErrorNotReady) ++it;
     else return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
   }
+  for (auto it = p->copies.begin(); it != p->copies.end();) {
+    cudaError_t e = cudaEventQuery(it->second);
+    if (e == cudaSuccess) { put_event(p, it->second); it = p->copies.erase(it); }
+    else if (e == cudaErrorNotReady) ++it;
+    else return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
+  }
   if (!p->pending_free.empty()) {
     size_t k = 0;
     for (auto &pf : p->pending_free) if (p->ops.count(pf.seq)) p->pending_free[k++] = pf;
@@ -155,6 +161,22 @@ kvr_status wait_unlocked(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64
   }
 }
 
+// the same wait for a copy on a caller's stream
+kvr_status wait_copy(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t number, int64_t timeout_ms) {
+  const auto t0 = Clock::now();
+  for (unsigned spin = 0;; ++spin) {
+    auto it = p->copies.find(number);
+    if (it == p->copies.end()) return KVR_OK;
+    cudaError_t e = cudaEventQuery(it->second);
+    if (e == cudaSuccess) return KVR_OK;
+    if (e != cudaErrorNotReady) return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
+    if (ms_since(t0) > (double)timeout_ms) return fail(KVR_ERR_TIMEOUT, "copy still in flight after %lld ms", (long long)timeout_ms);
+    lock.unlock();
+    if (spin > 2000) std::this_thread::sleep_for(std::chrono::microseconds(50)); else std::this_thread::yield();
+    lock.lock();
+  }
+}
+
 // the same wait with the lock held throughout (pool destruction, self-tests)
 kvr_status wait_locked(kvr_pool *p, uint64_t seq, int64_t timeout_ms) {
   if (p->meta_only) return KVR_OK;
@@ -173,6 +195,12 @@ kvr_status stream_after(kvr_pool *p, cudaStream_t s, uint64_t seq, bool read_onl
   auto it = p->ops.find(seq);
   if (it == p->ops.end()) return KVR_OK;
   CUP(p, cudaStreamWaitEvent(s, read_only ? it->second.read_done : it->second.done, 0));
+  return KVR_OK;
+}
+
+kvr_status stream_after_copy(kvr_pool *p, cudaStream_t s, uint64_t number) {
+  auto it = p->copies.find(number);
+  if (it != p->copies.end()) CUP(p, cudaStreamWaitEvent(s, it->second, 0));
   return KVR_OK;
 }
 
@@ -649,6 +677,7 @@ void destroy_engine(kvr_pool *p) {
   for (auto &d : p->descs) free_desc(d);
   for (Ring *r : {&p->out_ring, &p->in_ring})
     for (auto &s : r->slots) if (s.freed) cudaEventDestroy(s.freed);
+  for (auto &c : p->copies) cudaEventDestroy(c.second);
   for (auto e : p->event_pool) cudaEventDestroy(e);
   if (p->own_staging && p->staging) cudaFree(p->staging);
   if (p->status_word) cudaFreeHost(p->status_word);

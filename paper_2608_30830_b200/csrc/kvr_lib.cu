@@ -97,6 +97,27 @@ kvr_status check_donor(kvr_pool *p, uint64_t id, uint64_t donor_id, int32_t n_sh
   return KVR_OK;
 }
 
+// The caller will write a new request's blocks (those behind its shared prefix) from a stream of its own: lets any gather (`tag`) and any copy on a
+// caller's stream that still use them finish.
+kvr_status settle_blocks(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t id, uint64_t tag) {
+  if (p->meta_only) return KVR_OK;
+  if (tag) { if (kvr_status s = wait_unlocked(p, lock, tag, true, 60000)) return s; }
+  for (;;) {
+    if (p->copies.empty()) return KVR_OK;
+    auto it = p->reqs.find(id);                      // the lock is given up in the waits
+    if (it == p->reqs.end() || it->second.state != KVR_ACTIVE) return KVR_OK;
+    const Request &r = it->second;
+    uint64_t number = 0;
+    for (size_t i = (size_t)r.n_shared; i < r.blocks.size() && !number; ++i) {
+      const uint64_t c = p->fq.copy(r.blocks[i]);
+      if (c && p->copies.count(c)) number = c;
+    }
+    if (!number) return KVR_OK;
+    if (kvr_status s = wait_copy(p, lock, number, 60000)) return s;
+    if (kvr_status s = poll(p)) return s;            // a copy that is through leaves the table
+  }
+}
+
 // the new request's table: donor prefix (one more reference each) followed by ids from the head of the queue
 kvr_status admit_common(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t id, int64_t n_tokens, const Request *donor,
                         int32_t n_shared, int32_t *out_blocks) {
@@ -112,9 +133,7 @@ kvr_status admit_common(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_
   for (int32_t i = 0; i < n_shared; ++i) p->fq.add_ref(r.blocks[i]);
   const uint64_t tag = p->fq.pop((int32_t)nb - n_shared, r.blocks.data() + n_shared);
   if (out_blocks && nb) memcpy(out_blocks, r.blocks.data(), (size_t)nb * 4);
-  // the caller will write the new blocks from its own stream: let any gather still reading them finish
-  if (tag && !p->meta_only) return wait_unlocked(p, lock, tag, true, 60000);
-  return KVR_OK;
+  return settle_blocks(p, lock, id, tag);
 }
 
 // A stream that copies may be enqueued on.
@@ -128,32 +147,58 @@ kvr_status check_copy_stream(kvr_pool *p, cudaStream_t s) {
   return capture == cudaStreamCaptureStatusNone ? KVR_OK : fail(KVR_ERR_INVALID_ARG, "the stream is under capture");
 }
 
-// Enqueues copies of `rows` rows on the caller's stream (behind the gather `tag`, which may still read a destination), and orders the pool's
-// own streams behind what that stream holds by then.  On failure nothing of it is left in the stream.  live: the destination holds tokens of the
+// Enqueues copies of `rows` rows on the caller's stream, behind the gather `tag`, which may still read a destination, and behind copies on other streams
+// that use the same blocks; then orders the pool's own streams behind what that stream holds by then.  The blocks, and those let go, carry the
+// number of that point from now on.  On failure nothing of it is left in the stream.  live: the destination holds tokens of the
 // request until the call succeeds; once the copy has been launched they are gone, so what fails behind it must not undo the call: the stream has
 // come to rest by then, and nothing is left to be ordered.
-kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag, bool live) {
+kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag, bool live, const int32_t *let_go, int32_t n_let_go) {
   const PoolView view{p->d_pool, p->plane_stride, p->block_stride, p->planes, p->NB, p->BS, p->row};
   cudaEvent_t reached = nullptr;
   bool launched = false;
+  if (kvr_status st = poll(p)) return st;
+  const uint64_t number = p->next_copy++;
   try {
-    p->event_pool.reserve(p->event_pool.size() + 1);         // nothing below allocates on the host
+    p->event_pool.reserve(p->event_pool.size() + p->copies.size() + 1);
+    p->copies.emplace(number, nullptr);                      // nothing below allocates on the host
   } catch (const std::bad_alloc &) {
     return fail(KVR_ERR_NOMEM, "out of host memory");
   }
+  uint64_t last = 0;
+  auto behind = [&](int32_t block) -> kvr_status {
+    const uint64_t c = p->fq.copy(block);
+    if (!c || c == last) return KVR_OK;
+    last = c;
+    return stream_after_copy(p, s, c);
+  };
   auto run = [&]() -> kvr_status {
     if (kvr_status st = get_event(p, &reached)) return st;
     if (kvr_status st = stream_after(p, s, tag, true)) return st;
+    if (pairs.size() > 16) {                                 // many blocks: behind all there is
+      for (auto &c : p->copies) if (c.second) CUP(p, cudaStreamWaitEvent(s, c.second, 0));
+    } else if (p->copies.size() > 1) {
+      for (const int2 &m : pairs)
+        for (int32_t b : {m.x, m.y}) if (kvr_status st = behind(b)) return st;
+    }
+    if (p->copies.size() > 1)
+      for (int32_t i = 0; i < n_let_go; ++i) if (kvr_status st = behind(let_go[i])) return st;
     CUP(p, copy_blocks(view, pairs.data(), (int)pairs.size(), rows, s));
     launched = true;
     CUP(p, cudaEventRecord(reached, s));
     for (cudaStream_t own : {p->s_gather, p->s_d2h, p->s_h2d, p->s_scatter}) CUP(p, cudaStreamWaitEvent(own, reached, 0));
     return KVR_OK;
   };
-  kvr_status st = run();
-  if (st != KVR_OK && cudaStreamSynchronize(s) == cudaSuccess && launched && live) st = KVR_OK;
-  put_event(p, reached);
-  return st;
+  const kvr_status st = run();
+  if (st != KVR_OK) {
+    const bool rests = cudaStreamSynchronize(s) == cudaSuccess;
+    p->copies.erase(number);
+    put_event(p, reached);
+    return rests && launched && live ? KVR_OK : st;
+  }
+  p->copies[number] = reached;
+  for (const int2 &m : pairs) { p->fq.note_copy(m.x, number); p->fq.note_copy(m.y, number); }
+  for (int32_t i = 0; i < n_let_go; ++i) p->fq.note_copy(let_go[i], number);
+  return KVR_OK;
 }
 
 }  // namespace
@@ -305,8 +350,7 @@ kvr_status kvr_request_admit_sharing_into(kvr_pool *p, uint64_t id, int64_t n_to
     r.image_bytes = (uint64_t)(n_tokens - (int64_t)n_shared * p->BS) * p->bpt;
     r.blocks.swap(table);
     for (int32_t i = 0; i < n_shared; ++i) p->fq.add_ref(r.blocks[i]);
-    if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);     // a gather may still be reading the named blocks
-    return KVR_OK;
+    return settle_blocks(p, enter.lock, id, tag);
   } catch (const std::bad_alloc &) {
     return fail(KVR_ERR_NOMEM, "out of host memory");
   }
@@ -333,8 +377,7 @@ kvr_status kvr_request_admit_into(kvr_pool *p, uint64_t id, int64_t n_tokens, co
     r.state = KVR_ACTIVE; r.n_tokens = n_tokens; r.nb = nb;
     r.image_bytes = (uint64_t)n_tokens * p->bpt;
     r.blocks.swap(table);
-    if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);     // a gather may still be reading these blocks
-    return KVR_OK;
+    return settle_blocks(p, enter.lock, id, tag);
   } catch (const std::bad_alloc &) {
     return fail(KVR_ERR_NOMEM, "out of host memory");
   }
@@ -388,7 +431,7 @@ kvr_status kvr_request_fork(kvr_pool *p, uint64_t id, uint64_t donor_id, int64_t
       if (!existed) p->reqs[id].state = KVR_EXPIRED;         // the node is there before anything is taken
       tag = p->fq.pop(1, &table[full]);
       pairs[0].y = table[full];
-      const kvr_status s = p->meta_only ? KVR_OK : enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, false);
+      const kvr_status s = p->meta_only ? KVR_OK : enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, false, nullptr, 0);
       if (s != KVR_OK) {
         p->fq.unpop(&table[full], 1);
         if (!existed) p->reqs.erase(id);
@@ -432,6 +475,15 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
     if (nb > r.nb) {
       r.blocks.resize((size_t)nb);
       tag = p->fq.pop(nb - r.nb, r.blocks.data() + r.nb);
+      // copies on other streams may still use the added blocks, which the caller writes on this one
+      kvr_status s = KVR_OK;
+      for (int32_t i = r.nb; i < nb && !s && !p->copies.empty(); ++i)
+        if (const uint64_t c = p->fq.copy(r.blocks[i])) s = stream_after_copy(p, (cudaStream_t)stream, c);
+      if (s) {
+        p->fq.unpop(r.blocks.data() + r.nb, nb - r.nb);
+        r.blocks.resize((size_t)r.nb);
+        return s;
+      }
     } else {
       // A last block that others refer to must not be written on: its rows go to a block of the free queue, or to one that this call lets go.
       std::vector<int2> pairs;
@@ -446,10 +498,12 @@ kvr_status kvr_request_resize(kvr_pool *p, uint64_t id, int64_t n_tokens, int32_
         if (!popped) tag = p->fq.tag(own);
         pairs.push_back(make_int2(r.blocks[nb - 1], own));
       } else if (part && n_tokens < r.n_tokens) {
-        tag = p->fq.tag(r.blocks[nb - 1]);                   // nobody else refers to it, but the suspend of one that did may still read it
+        // nobody else refers to it, but the suspend of one that did may still read it, or a copy on another stream
+        tag = p->fq.tag(r.blocks[nb - 1]);
+        if (kvr_status s = stream_after_copy(p, (cudaStream_t)stream, p->fq.copy(r.blocks[nb - 1]))) return s;
       }
       if (!p->meta_only && (nb < r.nb || own >= 0)) {        // blocks change hands: later moves come behind the caller's work on them
-        if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, own >= 0 && !popped)) {
+        if (kvr_status s = enqueue_copies(p, pairs, part, (cudaStream_t)stream, tag, own >= 0 && !popped, r.blocks.data() + nb, r.nb - nb)) {
           if (popped) p->fq.unpop(&own, 1);
           return s;
         }
@@ -492,7 +546,7 @@ kvr_status kvr_pool_compact(kvr_pool *p, int32_t max_moves, int32_t *moves, int3
     if (pairs.empty()) return KVR_OK;
     std::vector<int32_t> now((size_t)p->NB);
     for (int32_t b = 0; b < p->NB; ++b) now[b] = b;
-    if (!p->meta_only) { if (kvr_status s = enqueue_copies(p, pairs, p->BS, (cudaStream_t)stream, 0, false)) return s; }
+    if (!p->meta_only) { if (kvr_status s = enqueue_copies(p, pairs, p->BS, (cudaStream_t)stream, 0, false, nullptr, 0)) return s; }
     for (const int2 &m : pairs) { p->fq.move(m.x, m.y); now[m.x] = m.y; }
     for (auto &entry : p->reqs)
       for (int32_t &b : entry.second.blocks) b = now[b];

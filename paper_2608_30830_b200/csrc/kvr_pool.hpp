@@ -146,6 +146,10 @@ struct kvr_pool {
   std::vector<cudaEvent_t> event_pool;
   std::map<uint64_t, kvr::Op> ops;
   uint64_t next_seq = 1;
+  // Points on callers' streams behind which copies of fork, resize and compact are through, by number.  Whoever uses a block that names one
+  // (FreeQueue::copy) comes behind it, so a block's last one stands for all before it.
+  std::map<uint64_t, cudaEvent_t> copies;
+  uint64_t next_copy = 1;
   std::vector<kvr::DescBuf> descs;
   std::vector<kvr::PendingFree> pending_free;
   std::mutex mu;                          // every entry point holds it: calls on one pool are serialised
@@ -191,6 +195,9 @@ kvr_status look(kvr_pool *p, uint64_t seq, bool read_only);
 kvr_status wait_unlocked(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t seq, bool read_only, int64_t timeout_ms);
 kvr_status wait_locked(kvr_pool *p, uint64_t seq, int64_t timeout_ms);
 kvr_status stream_after(kvr_pool *p, cudaStream_t s, uint64_t seq, bool read_only);
+// the same for a copy on a caller's stream
+kvr_status stream_after_copy(kvr_pool *p, cudaStream_t s, uint64_t number);
+kvr_status wait_copy(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t number, int64_t timeout_ms);
 void plan_staged(kvr_pool *p, const std::vector<Item> &items, Ring &ring, bool ramp_down_too, const char *desc_dev, Plan &pl);
 // Queues the byte movement of one move.  On failure nothing of it is left in the streams and no record of it remains.
 kvr_status enqueue(kvr_pool *p, int kind, std::vector<Item> &items, int route, char *lin_dev, uint64_t block_tag,

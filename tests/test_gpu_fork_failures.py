@@ -38,3 +38,27 @@ def test_a_shrink_in_a_full_pool_happens_or_changes_nothing():
             break
         n += 1
     assert n > 3 and (False, kvr.OK) in outcomes and (True, kvr.ERR_CUDA) in outcomes
+
+
+def test_a_growth_that_cannot_be_ordered_behind_a_copy_changes_nothing():
+    late, n = torch.cuda.Stream(), 1
+    while True:
+        p, dev, _ = make(5)
+        with p:
+            assert p.admit(1, 20)[0] == p.admit(2, 20)[0] == kvr.OK
+            torch.cuda.synchronize()
+            with torch.cuda.stream(late):
+                torch.cuda._sleep(40_000_000)
+            assert p.fork(3, 1, 20, stream=late.cuda_stream)[0] == p.release(3) == kvr.OK
+            before = books(p, 5)
+            assert p.test_fail_nth(kvr.FAIL_CUDA, n) == kvr.OK
+            st, table = p.resize(2, 48)
+            reached = p.test_points(kvr.FAIL_CUDA) >= n
+            p.test_fail_nth(kvr.FAIL_CUDA, 0)
+            torch.cuda.synchronize()
+            if not reached:
+                assert st == kvr.OK and table.tolist() == [2, 3, 4]
+                break
+            assert st == kvr.ERR_CUDA and books(p, 5) == before
+            n += 1
+    assert n > 1

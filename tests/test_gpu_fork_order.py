@@ -71,3 +71,146 @@ def test_a_copy_into_the_requests_own_tail_waits_for_the_suspend_that_still_read
         assert torch.equal(rows(p, dev, 5, 2), was[:, :, :20]) and torch.equal(rows(p, dev, 5, 3), was[:, :, :32])
         assert p.release(2) == p.release(3) == kvr.OK
         assert p.resume_from_host([1], kvr.SYNC)[0] == kvr.OK and torch.equal(rows(p, dev, 5, 1), was)
+
+
+# ---- copies that are late: their stream is busy, and whoever takes one of their blocks comes from elsewhere
+
+def write(dev, nb, blocks, value, stream, rows=slice(None)):
+    with torch.cuda.stream(stream):
+        for b in blocks:
+            tiles(dev, 0, GEOM, nb)[:, :, int(b), rows] = value
+
+
+def test_admit_waits_for_a_copy_that_reads_or_writes_its_blocks():
+    p, dev, _ = make(4)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        for call in ("admit", "admit_into", "admit_sharing", "admit_sharing_into"):
+            for gone in (1, 2):                              # the source's owner, the destination's
+                assert p.admit(1, 20)[0] == kvr.OK
+                was = rows(p, dev, 4, 1)
+                torch.cuda.synchronize()
+                busy(late)
+                assert p.fork(2, 1, 20, stream=late.cuda_stream)[0] == kvr.OK
+                last = int(p.info(gone)[1]["blocks"][1])
+                assert p.release(gone) == kvr.OK
+                free = p.free_queue()
+                assert last in free
+                if call == "admit":
+                    assert p.admit(3, 32)[0] == kvr.OK
+                elif call == "admit_into":
+                    assert p.admit_into(3, 32, free) == kvr.OK
+                elif call == "admit_sharing":
+                    assert p.admit_sharing(3, 48, 3 - gone, 1)[0] == kvr.OK
+                else:
+                    assert p.admit_sharing_into(3, 48, 3 - gone, 1, free) == kvr.OK
+                write(dev, 4, free, 9, other)
+                torch.cuda.synchronize()
+                assert torch.equal(rows(p, dev, 4, 3 - gone), was)
+                assert all((tiles(dev, 0, GEOM, 4)[:, :, int(b)] == 9).all() for b in free)
+                assert p.release(3) == p.release(3 - gone) == kvr.OK
+
+
+def test_copies_on_two_streams_that_use_one_block_come_one_after_the_other():
+    p, dev, _ = make(5)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 20)[0] == p.admit(5, 20)[0] == kvr.OK
+        was = rows(p, dev, 5, 1), rows(p, dev, 5, 5)
+        torch.cuda.synchronize()
+        busy(late)
+        assert p.fork(2, 1, 20, stream=late.cuda_stream)[1].tolist() == [0, 4]
+        assert p.release(2) == kvr.OK
+        assert p.fork(6, 5, 20, stream=other.cuda_stream)[1].tolist() == [2, 4]                  # the same destination
+        assert p.fork(7, 6, 16, stream=late.cuda_stream)[0] == kvr.OK
+        torch.cuda.synchronize()
+        assert torch.equal(rows(p, dev, 5, 6), was[1]) and torch.equal(rows(p, dev, 5, 5), was[1]) and torch.equal(rows(p, dev, 5, 1), was[0])
+        # a fork of what is still being copied
+        assert p.release(6) == p.release(7) == p.release(1) == kvr.OK
+        torch.cuda.synchronize()
+        busy(late)
+        assert p.fork(8, 5, 20, stream=late.cuda_stream)[0] == kvr.OK
+        assert p.fork(9, 8, 19, stream=other.cuda_stream)[0] == kvr.OK
+        torch.cuda.synchronize()
+        assert torch.equal(rows(p, dev, 5, 8), was[1]) and torch.equal(rows(p, dev, 5, 9), was[1][:, :, :19])
+
+
+def test_a_growing_request_comes_behind_a_late_copy_into_its_new_block():
+    p, dev, _ = make(5)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 20)[0] == p.admit(5, 20)[0] == kvr.OK
+        torch.cuda.synchronize()
+        busy(late)
+        assert p.fork(2, 1, 20, stream=late.cuda_stream)[0] == p.release(2) == kvr.OK
+        assert p.resize(5, 48, stream=other.cuda_stream)[1].tolist() == [2, 3, 4]
+        write(dev, 5, [4], 9, other)
+        torch.cuda.synchronize()
+        assert (tiles(dev, 0, GEOM, 5)[:, :, 4] == 9).all()
+
+
+def test_a_shrink_comes_behind_a_late_copy_of_the_rows_it_takes_back():
+    p, dev, _ = make(5)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 20)[0] == kvr.OK
+        was = rows(p, dev, 5, 1)
+        torch.cuda.synchronize()
+        busy(late)
+        assert p.fork(2, 1, 20, stream=late.cuda_stream)[0] == kvr.OK
+        assert p.resize(1, 17, stream=other.cuda_stream)[1].tolist() == [0, 1]
+        write(dev, 5, [1], 9, other, slice(1, None))
+        torch.cuda.synchronize()
+        assert torch.equal(rows(p, dev, 5, 2), was) and torch.equal(rows(p, dev, 5, 1), was[:, :, :17])
+
+
+def test_a_block_that_a_shrink_let_go_is_copied_into_behind_the_work_on_it():
+    p, dev, _ = make(5)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 20)[0] == p.admit(2, 48)[0] == kvr.OK
+        was = rows(p, dev, 5, 1), rows(p, dev, 5, 2)
+        torch.cuda.synchronize()
+        busy(late)
+        with torch.cuda.stream(late):
+            seen = rows(p, dev, 5, 2)                        # the caller's own reading, late
+        assert p.resize(2, 32, stream=late.cuda_stream)[0] == kvr.OK
+        assert p.fork(3, 1, 20, stream=other.cuda_stream)[1].tolist() == [0, 4]
+        torch.cuda.synchronize()
+        assert torch.equal(seen, was[1]) and torch.equal(rows(p, dev, 5, 3), was[0])
+
+
+def test_blocks_that_a_compaction_moved_away_from_are_handed_out_behind_it():
+    p, dev, _ = make(3)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 16)[0] == p.admit(2, 16)[0] == kvr.OK
+        was = rows(p, dev, 3, 2)
+        torch.cuda.synchronize()
+        assert p.release(1) == kvr.OK
+        busy(late)
+        assert p.compact(stream=late.cuda_stream)[1].tolist() == [[1, 0]]
+        assert p.admit(3, 32)[1].tolist() == [2, 1]
+        write(dev, 3, [1, 2], 9, other)
+        torch.cuda.synchronize()
+        assert torch.equal(rows(p, dev, 3, 2), was)
+
+
+def test_a_compaction_comes_behind_late_copies_on_other_streams():
+    p, dev, _ = make(40)
+    late, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with p:
+        for many in (1, 30):                                 # a few pairs, and more than are looked at one by one
+            for rid in range(many):
+                assert p.admit(100 + rid, 1)[0] == kvr.OK
+            assert p.admit(1, 20)[0] == kvr.OK
+            was = rows(p, dev, 40, 1)
+            torch.cuda.synchronize()
+            busy(late)
+            assert p.fork(2, 1, 20, stream=late.cuda_stream)[0] == kvr.OK
+            for rid in range(many):
+                assert p.release(100 + rid) == kvr.OK
+            assert len(p.compact(stream=other.cuda_stream)[1]) > 0
+            torch.cuda.synchronize()
+            assert torch.equal(rows(p, dev, 40, 1), was) and torch.equal(rows(p, dev, 40, 2), was)
+            assert p.release(1) == p.release(2) == kvr.OK
