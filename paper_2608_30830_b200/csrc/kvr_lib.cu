@@ -147,8 +147,25 @@ kvr_status check_copy_stream(kvr_pool *p, cudaStream_t s) {
   return capture == cudaStreamCaptureStatusNone ? KVR_OK : fail(KVR_ERR_INVALID_ARG, "the stream is under capture");
 }
 
-// Enqueues copies of `rows` rows on the caller's stream, behind the gather `tag`, which may still read a destination, and behind copies on other streams
-// that use the same blocks; then orders the pool's own streams behind what that stream holds by then.  The blocks, and those let go, carry the
+// Orders stream s behind what still fills a request's blocks: a resume or an import in flight (also one of another request, which shares them),
+// and copies on other streams.
+kvr_status stream_after_fillers(kvr_pool *p, cudaStream_t s, const int32_t *blocks, int32_t n) {
+  uint64_t copy = 0, writer = 0;
+  for (int32_t i = 0; i < n && !(p->copies.empty() && p->ops.empty()); ++i) {
+    if (const uint64_t c = p->fq.copy(blocks[i])) {
+      if (c != copy) { if (kvr_status st = stream_after_copy(p, s, c)) return st; }
+      copy = c;
+    }
+    if (const uint64_t w = p->fq.writer(blocks[i])) {
+      if (w != writer) { if (kvr_status st = stream_after(p, s, w, false)) return st; }
+      writer = w;
+    }
+  }
+  return KVR_OK;
+}
+
+// Enqueues copies of `rows` rows on the caller's stream, behind the gather `tag`, which may still read a destination, and behind the moves and the copies on
+// other streams that still fill or use the same blocks; then orders the pool's own streams behind what that stream holds by then.  The blocks, and those let go, carry the
 // number of that point from now on.  On failure nothing of it is left in the stream.  live: the destination holds tokens of the
 // request until the call succeeds; once the copy has been launched they are gone, so what fails behind it must not undo the call: the stream has
 // come to rest by then, and nothing is left to be ordered.
@@ -164,24 +181,15 @@ kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows,
   } catch (const std::bad_alloc &) {
     return fail(KVR_ERR_NOMEM, "out of host memory");
   }
-  uint64_t last = 0;
-  auto behind = [&](int32_t block) -> kvr_status {
-    const uint64_t c = p->fq.copy(block);
-    if (!c || c == last) return KVR_OK;
-    last = c;
-    return stream_after_copy(p, s, c);
-  };
   auto run = [&]() -> kvr_status {
     if (kvr_status st = get_event(p, &reached)) return st;
     if (kvr_status st = stream_after(p, s, tag, true)) return st;
-    if (pairs.size() > 16) {                                 // many blocks: behind all there is
+    if (pairs.size() > 16) {                                 // many blocks (a compaction: no move is in flight): behind all there is
       for (auto &c : p->copies) if (c.second) CUP(p, cudaStreamWaitEvent(s, c.second, 0));
-    } else if (p->copies.size() > 1) {
-      for (const int2 &m : pairs)
-        for (int32_t b : {m.x, m.y}) if (kvr_status st = behind(b)) return st;
+    } else {
+      for (const int2 &m : pairs) if (kvr_status st = stream_after_fillers(p, s, &m.x, 2)) return st;
     }
-    if (p->copies.size() > 1)
-      for (int32_t i = 0; i < n_let_go; ++i) if (kvr_status st = behind(let_go[i])) return st;
+    if (kvr_status st = stream_after_fillers(p, s, let_go, n_let_go)) return st;
     CUP(p, copy_blocks(view, pairs.data(), (int)pairs.size(), rows, s));
     launched = true;
     CUP(p, cudaEventRecord(reached, s));
@@ -422,6 +430,8 @@ kvr_status kvr_request_fork(kvr_pool *p, uint64_t id, uint64_t donor_id, int64_t
   const int32_t full = (int32_t)(n_tokens / p->BS), part = (int32_t)(n_tokens % p->BS), nb = full + (part > 0);
   if (out_blocks && cap < nb) return fail(KVR_ERR_INVALID_ARG, "out_blocks too small");
   if (nb - full > p->fq.size()) { p->st.hbm_full_rejects++; return KVR_HBM_FULL; }
+  // the donor may itself share blocks that another request's resume still fills
+  if (!p->meta_only) { if (kvr_status s = stream_after_fillers(p, (cudaStream_t)stream, donor.blocks.data(), nb)) return s; }
   try {
     std::vector<int32_t> table(donor.blocks.begin(), donor.blocks.begin() + nb);
     std::vector<int2> pairs;
@@ -703,7 +713,10 @@ static kvr_status resume_commit_or_rollback(kvr_pool *p, std::unique_lock<std::m
     *rolled_back = true;
     return err;
   }
-  for (auto &it : items) free_host(p, *it.r, seq);
+  for (auto &it : items) {
+    p->fq.note_writer(it.blocks, it.nb, seq);
+    free_host(p, *it.r, seq);
+  }
   if (seq && (flags & KVR_SYNC)) return wait_unlocked(p, lock, seq, false, 60000);
   return KVR_OK;
 }
@@ -823,6 +836,7 @@ static kvr_status device_copy(kvr_pool *p, int kind, const uint64_t *req, int32_
     std::vector<uint64_t> none;
     if (!items.empty())
       if (kvr_status s = enqueue(p, kind, items, 0, dev, 0, none, t_call, lease.idx, &seq)) return s;
+    if (kind == OP_IMPORT) for (auto &it : items) p->fq.note_writer(it.blocks, it.nb, seq);
     if (seq && (flags & KVR_SYNC)) return wait_unlocked(p, enter.lock, seq, false, 60000);
     return KVR_OK;
   } catch (const std::bad_alloc &) {

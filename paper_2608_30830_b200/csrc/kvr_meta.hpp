@@ -19,12 +19,13 @@ inline uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 //   - a reference count: how many (request, position) pairs name it; it is in the queue iff the count is 0;
 //   - the sequence number of the last move whose gather read it (0 = none), so a later writer can order itself
 //     after that gather on the device;
+//   - the sequence number of the last move that wrote it (a resume or an import; 0 = none);
 //   - the number of the last copy on a caller's stream that read or wrote it, or of the last resize that let it go (0 = none).
 class FreeQueue {
  public:
   void init(int32_t nb, const int32_t *order) {
     cap_ = nb;
-    next_.assign(nb, -1); prev_.assign(nb, -1); tag_.assign(nb, 0); copy_.assign(nb, 0); refs_.assign(nb, 0); mark_.assign(nb, 0);
+    next_.assign(nb, -1); prev_.assign(nb, -1); tag_.assign(nb, 0); copy_.assign(nb, 0); writer_.assign(nb, 0); refs_.assign(nb, 0); mark_.assign(nb, 0);
     head_ = tail_ = -1; size_ = 0;
     for (int32_t i = 0; i < nb; ++i) link_tail(order ? order[i] : i);
   }
@@ -33,6 +34,7 @@ class FreeQueue {
   bool is_free(int32_t b) const { return b >= 0 && b < cap_ && refs_[b] == 0; }
   int32_t refs(int32_t b) const { return refs_[b]; }
   uint64_t tag(int32_t b) const { return tag_[b]; }
+  uint64_t writer(int32_t b) const { return writer_[b]; }
   uint64_t copy(int32_t b) const { return copy_[b]; }
   void note_copy(int32_t b, uint64_t number) { copy_[b] = number; }
 
@@ -99,6 +101,10 @@ class FreeQueue {
     for (int32_t i = 0; i < n; ++i) if (tag_[ids[i]] < seq) tag_[ids[i]] = seq;
   }
 
+  void note_writer(const int32_t *ids, int32_t n, uint64_t seq) {
+    for (int32_t i = 0; i < n; ++i) writer_[ids[i]] = seq;
+  }
+
   // iteration, head first: for (b = first(); b >= 0; b = after(b))
   int32_t first() const { return head_; }
   int32_t after(int32_t b) const { return next_[b]; }
@@ -121,7 +127,7 @@ class FreeQueue {
   void link_tail(int32_t b) { link_after(b, tail_); }
 
   std::vector<int32_t> next_, prev_, refs_;
-  std::vector<uint64_t> tag_, copy_;
+  std::vector<uint64_t> tag_, writer_, copy_;
   std::vector<uint8_t> mark_;
   int64_t cap_ = 0, size_ = 0;
   int32_t head_ = -1, tail_ = -1;

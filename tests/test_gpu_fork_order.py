@@ -214,3 +214,38 @@ def test_a_compaction_comes_behind_late_copies_on_other_streams():
             torch.cuda.synchronize()
             assert torch.equal(rows(p, dev, 40, 1), was) and torch.equal(rows(p, dev, 40, 2), was)
             assert p.release(1) == p.release(2) == kvr.OK
+
+
+# ---- resumes that are late: the stream that writes the blocks is busy
+
+@pytest.mark.parametrize("what", ["resume", "import"])
+@pytest.mark.parametrize("route", ROUTES)
+def test_a_copy_out_of_a_prefix_that_another_requests_move_still_fills(route, what):
+    p, dev, streams = make(16, route)
+    side = torch.cuda.Stream()
+    with p:
+        assert p.admit(1, 40)[0] == kvr.OK
+        was = rows(p, dev, 16, 1)
+        buffer = torch.zeros(40 * 2 * GEOM[0] * was.shape[-1] + 256, dtype=torch.uint8, device="cuda")
+        if what == "import":
+            assert p.export_to_device([1], buffer.data_ptr(), buffer.numel(), kvr.SYNC)[0] == kvr.OK
+        else:
+            assert p.suspend_to_host([1], kvr.SYNC)[0] == kvr.OK
+        dev.random_(0, 256)
+        torch.cuda.synchronize()
+        busy(streams[2 if route == "dma2d" and what == "resume" else 3])
+        if what == "import":
+            assert p.import_from_device([1], buffer.data_ptr(), buffer.numel())[0] == kvr.OK
+        else:
+            assert p.resume_from_host([1])[0] == kvr.OK
+        assert p.admit_sharing(2, 32, 1, 2)[0] == p.admit_sharing(5, 32, 1, 2)[0] == kvr.OK
+        assert p.fork(3, 2, 21, stream=side.cuda_stream)[0] == p.fork(4, 2, 32, stream=side.cuda_stream)[0] == kvr.OK
+        with torch.cuda.stream(side):
+            shared = rows(p, dev, 16, 4)                     # what a kernel on the fork's stream sees
+        assert p.resize(2, 19, stream=side.cuda_stream)[0] == kvr.OK
+        table = p.resize(5, 30, stream=torch.cuda.Stream().cuda_stream)[1]
+        assert table[1] != p.info(1)[1]["blocks"][1]
+        torch.cuda.synchronize()
+        for rid, n in ((1, 40), (2, 19), (3, 21), (4, 32), (5, 30)):
+            assert torch.equal(rows(p, dev, 16, rid), was[:, :, :n]), rid
+        assert torch.equal(shared, was[:, :, :32])
