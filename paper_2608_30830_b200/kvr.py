@@ -2,6 +2,7 @@
 import ctypes as C
 import math
 import os
+import sys
 
 import numpy as np
 
@@ -435,7 +436,7 @@ class Pool:
                  suspend_single_bytes=0, resume_single_bytes=0, copy_piece_bytes=0, max_moves_in_flight=0,
                  bulk_shape=None):
         self.geom = (layers, kv_heads, head_dim, dtype_bytes, block_size)
-        self.NB = num_blocks
+        self.NB, self.device = num_blocks, device
         cfg = Config()
         cfg.g = Geometry(*self.geom)
         cfg.num_blocks, cfg.device = num_blocks, device
@@ -515,19 +516,26 @@ class Pool:
         st = fn(self._h, *args[:-1], n_tokens, _i32p(out), nb, args[-1])
         return st, (out[:nb].copy() if st == OK else None)
 
+    def _stream(self, stream):
+        """A cudaStream_t; None is torch's current stream on the pool's device, as for Cache (the default one where torch has not been used)."""
+        if stream is not None:
+            return stream
+        torch = sys.modules.get("torch")
+        return torch._C._cuda_getCurrentRawStream(self.device) if torch is not None and torch.cuda.is_initialized() else None
+
     def fork(self, rid, donor, n_tokens, stream=None):
-        """kvr_request_fork: (status, block table of the new request).  stream: a cudaStream_t; None is the default stream."""
-        return self._resized(lib().kvr_request_fork, n_tokens, rid, donor, stream)
+        """kvr_request_fork: (status, block table of the new request).  stream: a cudaStream_t; None is torch's current stream."""
+        return self._resized(lib().kvr_request_fork, n_tokens, rid, donor, self._stream(stream))
 
     def resize(self, rid, n_tokens, stream=None):
-        """kvr_request_resize: (status, the request's whole block table)."""
-        return self._resized(lib().kvr_request_resize, n_tokens, rid, stream)
+        """kvr_request_resize: (status, the request's whole block table).  stream as in fork()."""
+        return self._resized(lib().kvr_request_resize, n_tokens, rid, self._stream(stream))
 
     def compact(self, max_moves=None, stream=None):
-        """kvr_pool_compact: (status, [[from, to], ...] in order)."""
+        """kvr_pool_compact: (status, [[from, to], ...] in order).  stream as in fork()."""
         most = self.NB if max_moves is None else max_moves
         moves, n = np.zeros((max(most, 1), 2), dtype=np.int32), C.c_int32()
-        st = lib().kvr_pool_compact(self._h, most, _i32p(moves), C.byref(n), stream)
+        st = lib().kvr_pool_compact(self._h, most, _i32p(moves), C.byref(n), self._stream(stream))
         return st, moves[:n.value].copy()
 
     def sharing(self, rid):

@@ -27,6 +27,25 @@ def busy(stream):
         torch.cuda._sleep(40_000_000)
 
 
+def write(dev, nb, blocks, value, stream, rows=slice(None)):
+    with torch.cuda.stream(stream):
+        for b in blocks:
+            tiles(dev, 0, GEOM, nb)[:, :, int(b), rows] = value
+
+
+@pytest.fixture(autouse=True, scope="module")
+def loaded():
+    """Every kernel has run once: the first launch of one waits for the device."""
+    for route in ROUTES:
+        p, dev, streams = make(8, route)
+        with p:
+            assert p.admit(1, 20)[0] == p.fork(2, 1, 20)[0] == p.suspend_to_host([1])[0] == p.resume_from_host([1], kvr.SYNC)[0] == kvr.OK
+            write(dev, 8, [7], 1, streams[0])
+            rows(p, dev, 8, 1)
+            busy(streams[0])
+            torch.cuda.synchronize()
+
+
 def reader(streams, route):
     """The stream that reads the blocks of a suspend."""
     return streams[1 if route == "dma2d" else 0]
@@ -74,12 +93,6 @@ def test_a_copy_into_the_requests_own_tail_waits_for_the_suspend_that_still_read
 
 
 # ---- copies that are late: their stream is busy, and whoever takes one of their blocks comes from elsewhere
-
-def write(dev, nb, blocks, value, stream, rows=slice(None)):
-    with torch.cuda.stream(stream):
-        for b in blocks:
-            tiles(dev, 0, GEOM, nb)[:, :, int(b), rows] = value
-
 
 def test_admit_waits_for_a_copy_that_reads_or_writes_its_blocks():
     p, dev, _ = make(4)
@@ -249,3 +262,35 @@ def test_a_copy_out_of_a_prefix_that_another_requests_move_still_fills(route, wh
         for rid, n in ((1, 40), (2, 19), (3, 21), (4, 32), (5, 30)):
             assert torch.equal(rows(p, dev, 16, rid), was[:, :, :n]), rid
         assert torch.equal(shared, was[:, :, :32])
+
+
+def test_no_stream_is_the_current_one():
+    """As for Cache: what the current stream is about to write is what a fork, a shrink and a compaction copy."""
+    p, dev, _ = make(8)
+    side = torch.cuda.Stream()
+    with p:
+        assert p.admit(9, 16)[0] == p.admit(1, 48)[0] == p.fork(5, 1, 48)[0] == kvr.OK
+        torch.cuda.synchronize()
+        busy(side)
+        write(dev, 8, [1, 2, 3], 9, side)
+        with torch.cuda.stream(side):
+            assert p.fork(2, 1, 40)[0] == kvr.OK
+            assert p.resize(5, 20)[0] == kvr.OK
+            assert p.release(9) == kvr.OK
+            assert len(p.compact()[1]) == 1
+        torch.cuda.synchronize()
+        for rid in (1, 2, 5):
+            assert (rows(p, dev, 8, rid) == 9).all(), rid
+
+
+def test_a_current_stream_under_capture_is_refused():
+    p, dev, _ = make(8)
+    with p:
+        assert p.admit(1, 20)[0] == kvr.OK
+        graph, x = torch.cuda.CUDAGraph(), torch.zeros(8, device="cuda")
+        with torch.cuda.graph(graph):
+            x += 1
+            assert p.fork(3, 1, 20)[0] == p.resize(1, 5)[0] == p.compact()[0] == kvr.ERR_INVALID_ARG
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (x == 1).all() and p.info(1)[1]["n_tokens"] == 20
