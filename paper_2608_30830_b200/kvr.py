@@ -511,9 +511,9 @@ class Pool:
         return lib().kvr_request_admit_sharing_into(self._h, rid, n_tokens, donor, n_shared, _i32p(blocks), len(blocks))
 
     def _resized(self, fn, n_tokens, *args):
-        nb = max(0, -(-n_tokens // self.geom[4]))
-        out = np.zeros(max(nb, 1), dtype=np.int32)
-        st = fn(self._h, *args[:-1], n_tokens, _i32p(out), nb, args[-1])
+        nb = max(0, -(-_int64(n_tokens, "n_tokens") // self.geom[4]))
+        out = np.zeros(max(nb, 1), dtype=np.int32) if nb <= self.NB else None          # (more than the pool has: refused)
+        st = fn(self._h, *args[:-1], n_tokens, None if out is None else _i32p(out), 0 if out is None else nb, args[-1])
         return st, (out[:nb].copy() if st == OK else None)
 
     def _stream(self, stream):
@@ -533,7 +533,7 @@ class Pool:
 
     def compact(self, max_moves=None, stream=None):
         """kvr_pool_compact: (status, [[from, to], ...] in order).  stream as in fork()."""
-        most = self.NB if max_moves is None else max_moves
+        most = self.NB if max_moves is None else max(-1, min(_int64(max_moves, "max_moves"), self.NB))
         moves, n = np.zeros((max(most, 1), 2), dtype=np.int32), C.c_int32()
         st = lib().kvr_pool_compact(self._h, most, _i32p(moves), C.byref(n), self._stream(stream))
         return st, moves[:n.value].copy()
@@ -694,6 +694,12 @@ def _int32(x, what):
     """x, if the library's 32 bits hold it (ctypes would drop the rest)."""
     if not -2**31 <= x < 2**31:
         raise ValueError("%s does not fit 32 bits" % what)
+    return x
+
+
+def _int64(x, what):
+    if not -2**63 <= x < 2**63:
+        raise ValueError("%s does not fit 64 bits" % what)
     return x
 
 

@@ -49,3 +49,26 @@ def test_a_request_longer_than_any_pool_is_not_admitted(n):
             assert L.kvr_request_admit_sharing_into(p._h, 2, 2**31 * BS, 1, shared, kvr._i32p(ids), private) == kvr.ERR_INVALID_ARG
         assert L.kvr_request_fork(p._h, 2, 1, n, None, 0, None) == kvr.ERR_INVALID_ARG
         assert books(p) == was and p.info(2)[0] == kvr.ERR_UNKNOWN_REQUEST
+
+
+@pytest.mark.parametrize("n", [2**64, 2**64 + 5, 2**63, -2**63 - 1])
+def test_the_binding_drops_no_bits_of_a_length(n):
+    with pool() as p:
+        assert p.admit(1, 40)[0] == kvr.OK
+        was = books(p)
+        for call in (lambda: p.resize(1, n), lambda: p.fork(2, 1, n), lambda: p.compact(n)):
+            with pytest.raises(ValueError):
+                call()
+        assert books(p) == was and p.info(1)[1]["n_tokens"] == 40 and p.info(2)[0] == kvr.ERR_UNKNOWN_REQUEST
+
+
+def test_the_binding_takes_any_length_that_fits():
+    with pool() as p:
+        assert p.admit(1, 40)[0] == kvr.OK
+        for n in LONG:
+            assert p.resize(1, n) == (kvr.HBM_FULL, None) and p.fork(2, 1, n) == (kvr.ERR_INVALID_ARG, None)
+        assert p.resize(1, -2**63) == (kvr.ERR_INVALID_ARG, None)
+        assert p.admit(2, 10)[0] == p.release(1) == kvr.OK                       # block 3 is in use, 0 to 2 are free
+        for most in (-1, -2**31, -2**63):
+            assert p.compact(most)[0] == kvr.ERR_INVALID_ARG
+        assert p.compact(2**63 - 1)[1].tolist() == [[3, 0]]
