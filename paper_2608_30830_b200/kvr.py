@@ -1,6 +1,7 @@
 """ctypes binding of libkvr.so: same names as the C ABI (include/kvr.h), argument marshalling only."""
 import ctypes as C
 import math
+import operator
 import os
 import sys
 
@@ -757,7 +758,7 @@ class Rope:
         self.table = table          # kept alive
         self.axes = None
         if axes is not None:
-            axes = bytes(axes)       # refuses what is not in [0, 255]
+            axes = bytes([operator.index(a) for a in axes])       # the numbers, not an array's memory; refuses what is not in [0, 255]
             if 2 * len(axes) != rot_dim or len(axes) > 128 or max(axes) > 3:
                 raise ValueError("axes must have rot_dim / 2 entries from 0 to 3")
             self.axes = RopeAxes()
