@@ -104,17 +104,34 @@ static void retire(kvr_pool *p, Op &op) {
   }
 }
 
+// A query costs more than all else that a copy's point does on the host (1.3 us), so it is not asked at every call: beyond a number that
+// doubles with what is still under way, newest first, and what lies before a point that is through, on its stream, is through.
+kvr_status poll_copies(kvr_pool *p) {
+  if (p->copies.size() < p->copies_limit) return KVR_OK;
+  unsigned long long through[16];
+  int n = 0;
+  for (auto it = p->copies.end(); it != p->copies.begin();) {
+    --it;
+    bool gone = false;
+    for (int i = 0; i < n; ++i) gone = gone || through[i] == it->second.stream;
+    if (!gone) {
+      cudaError_t e = cudaEventQuery(it->second.event);
+      if (e == cudaErrorNotReady) continue;
+      if (e != cudaSuccess) return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
+      if (n < 16) through[n++] = it->second.stream;
+    }
+    p->copy_events.push_back(it->second.event);              // reserved when the point was made
+    it = p->copies.erase(it);
+  }
+  p->copies_limit = 2 * p->copies.size() + 32;
+  return KVR_OK;
+}
+
 // retire every move whose last event has fired
 kvr_status poll(kvr_pool *p) {
   for (auto it = p->ops.begin(); it != p->ops.end();) {
     cudaError_t e = cudaEventQuery(it->second.done);
     if (e == cudaSuccess) { retire(p, it->second); it = p->ops.erase(it); }
-    else if (e == cudaErrorNotReady) ++it;
-    else return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
-  }
-  for (auto it = p->copies.begin(); it != p->copies.end();) {
-    cudaError_t e = cudaEventQuery(it->second);
-    if (e == cudaSuccess) { put_event(p, it->second); it = p->copies.erase(it); }
     else if (e == cudaErrorNotReady) ++it;
     else return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
   }
@@ -167,8 +184,12 @@ kvr_status wait_copy(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t n
   for (unsigned spin = 0;; ++spin) {
     auto it = p->copies.find(number);
     if (it == p->copies.end()) return KVR_OK;
-    cudaError_t e = cudaEventQuery(it->second);
-    if (e == cudaSuccess) return KVR_OK;
+    cudaError_t e = cudaEventQuery(it->second.event);
+    if (e == cudaSuccess) {
+      p->copy_events.push_back(it->second.event);
+      p->copies.erase(it);
+      return KVR_OK;
+    }
     if (e != cudaErrorNotReady) return fail(KVR_ERR_CUDA, "cudaEventQuery: %s", cudaGetErrorString(e));
     if (ms_since(t0) > (double)timeout_ms) return fail(KVR_ERR_TIMEOUT, "copy still in flight after %lld ms", (long long)timeout_ms);
     lock.unlock();
@@ -200,7 +221,7 @@ kvr_status stream_after(kvr_pool *p, cudaStream_t s, uint64_t seq, bool read_onl
 
 kvr_status stream_after_copy(kvr_pool *p, cudaStream_t s, uint64_t number) {
   auto it = p->copies.find(number);
-  if (it != p->copies.end()) CUP(p, cudaStreamWaitEvent(s, it->second, 0));
+  if (it != p->copies.end()) CUP(p, cudaStreamWaitEvent(s, it->second.event, 0));
   return KVR_OK;
 }
 
@@ -677,7 +698,8 @@ void destroy_engine(kvr_pool *p) {
   for (auto &d : p->descs) free_desc(d);
   for (Ring *r : {&p->out_ring, &p->in_ring})
     for (auto &s : r->slots) if (s.freed) cudaEventDestroy(s.freed);
-  for (auto &c : p->copies) cudaEventDestroy(c.second);
+  for (auto &c : p->copies) cudaEventDestroy(c.second.event);
+  for (auto e : p->copy_events) cudaEventDestroy(e);
   for (auto e : p->event_pool) cudaEventDestroy(e);
   if (p->own_staging && p->staging) cudaFree(p->staging);
   if (p->status_word) cudaFreeHost(p->status_word);

@@ -102,19 +102,18 @@ kvr_status check_donor(kvr_pool *p, uint64_t id, uint64_t donor_id, int32_t n_sh
 kvr_status settle_blocks(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t id, uint64_t tag) {
   if (p->meta_only) return KVR_OK;
   if (tag) { if (kvr_status s = wait_unlocked(p, lock, tag, true, 60000)) return s; }
-  for (;;) {
+  for (size_t i = 0;;) {
     if (p->copies.empty()) return KVR_OK;
     auto it = p->reqs.find(id);                      // the lock is given up in the waits
     if (it == p->reqs.end() || it->second.state != KVR_ACTIVE) return KVR_OK;
     const Request &r = it->second;
     uint64_t number = 0;
-    for (size_t i = (size_t)r.n_shared; i < r.blocks.size() && !number; ++i) {
+    for (i = std::max(i, (size_t)r.n_shared); i < r.blocks.size() && !number; ++i) {
       const uint64_t c = p->fq.copy(r.blocks[i]);
       if (c && p->copies.count(c)) number = c;
     }
     if (!number) return KVR_OK;
     if (kvr_status s = wait_copy(p, lock, number, 60000)) return s;
-    if (kvr_status s = poll(p)) return s;            // a copy that is through leaves the table
   }
 }
 
@@ -171,39 +170,45 @@ kvr_status stream_after_fillers(kvr_pool *p, cudaStream_t s, const int32_t *bloc
 // come to rest by then, and nothing is left to be ordered.
 kvr_status enqueue_copies(kvr_pool *p, const std::vector<int2> &pairs, int rows, cudaStream_t s, uint64_t tag, bool live, const int32_t *let_go, int32_t n_let_go) {
   const PoolView view{p->d_pool, p->plane_stride, p->block_stride, p->planes, p->NB, p->BS, p->row};
-  cudaEvent_t reached = nullptr;
   bool launched = false;
-  if (kvr_status st = poll(p)) return st;
+  if (kvr_status st = poll_copies(p)) return st;
   const uint64_t number = p->next_copy++;
+  CopyPoint *point = nullptr;
   try {
-    p->event_pool.reserve(p->event_pool.size() + p->copies.size() + 1);
-    p->copies.emplace(number, nullptr);                      // nothing below allocates on the host
+    const size_t events = p->copy_events.size() + p->copies.size() + 1;      // all that there will be
+    if (p->copy_events.capacity() < events) p->copy_events.reserve(2 * events);
+    point = &p->copies[number];                              // nothing below allocates on the host
   } catch (const std::bad_alloc &) {
     return fail(KVR_ERR_NOMEM, "out of host memory");
   }
   auto run = [&]() -> kvr_status {
-    if (kvr_status st = get_event(p, &reached)) return st;
+    if (p->copy_events.empty()) {
+      CUP(p, cudaEventCreateWithFlags(&point->event, cudaEventDisableTiming));
+    } else {
+      point->event = p->copy_events.back();
+      p->copy_events.pop_back();
+    }
+    CUP(p, cudaStreamGetId(s, &point->stream));
     if (kvr_status st = stream_after(p, s, tag, true)) return st;
     if (pairs.size() > 16) {                                 // many blocks (a compaction: no move is in flight): behind all there is
-      for (auto &c : p->copies) if (c.second) CUP(p, cudaStreamWaitEvent(s, c.second, 0));
+      for (auto &c : p->copies) if (&c.second != point) CUP(p, cudaStreamWaitEvent(s, c.second.event, 0));
     } else {
       for (const int2 &m : pairs) if (kvr_status st = stream_after_fillers(p, s, &m.x, 2)) return st;
     }
     if (kvr_status st = stream_after_fillers(p, s, let_go, n_let_go)) return st;
     CUP(p, copy_blocks(view, pairs.data(), (int)pairs.size(), rows, s));
     launched = true;
-    CUP(p, cudaEventRecord(reached, s));
-    for (cudaStream_t own : {p->s_gather, p->s_d2h, p->s_h2d, p->s_scatter}) CUP(p, cudaStreamWaitEvent(own, reached, 0));
+    CUP(p, cudaEventRecord(point->event, s));
+    for (cudaStream_t own : {p->s_gather, p->s_d2h, p->s_h2d, p->s_scatter}) CUP(p, cudaStreamWaitEvent(own, point->event, 0));
     return KVR_OK;
   };
   const kvr_status st = run();
   if (st != KVR_OK) {
     const bool rests = cudaStreamSynchronize(s) == cudaSuccess;
+    if (point->event) p->copy_events.push_back(point->event);
     p->copies.erase(number);
-    put_event(p, reached);
     return rests && launched && live ? KVR_OK : st;
   }
-  p->copies[number] = reached;
   for (const int2 &m : pairs) { p->fq.note_copy(m.x, number); p->fq.note_copy(m.y, number); }
   for (int32_t i = 0; i < n_let_go; ++i) p->fq.note_copy(let_go[i], number);
   return KVR_OK;

@@ -80,6 +80,8 @@ struct DescBuf { char *h = nullptr; char *d = nullptr; size_t cap = 0; uint64_t 
 // (all on one stream), so waiting for the largest `seq` among a set of slots covers the whole set.
 struct Slot { cudaEvent_t freed = nullptr; bool used = false; uint64_t seq = 0; int owner = 0; };
 struct Ring { char *base = nullptr; std::vector<Slot> slots; int next = 0; uint64_t seq = 0; };
+// A point on a caller's stream, behind which a copy of fork, resize or compact is through.
+struct CopyPoint { cudaEvent_t event = nullptr; unsigned long long stream = 0; };    // (the stream's id, which no later stream gets)
 struct PendingFree { uint64_t off, len, seq; };
 
 // one request's part of a move
@@ -146,10 +148,11 @@ struct kvr_pool {
   std::vector<cudaEvent_t> event_pool;
   std::map<uint64_t, kvr::Op> ops;
   uint64_t next_seq = 1;
-  // Points on callers' streams behind which copies of fork, resize and compact are through, by number.  Whoever uses a block that names one
-  // (FreeQueue::copy) comes behind it, so a block's last one stands for all before it.
-  std::map<uint64_t, cudaEvent_t> copies;
+  // By number.  Whoever uses a block that names one (FreeQueue::copy) comes behind it, so a block's last one stands for all before it.
+  std::map<uint64_t, kvr::CopyPoint> copies;
   uint64_t next_copy = 1;
+  size_t copies_limit = 32;               // how many there may be before those that are through are looked for
+  std::vector<cudaEvent_t> copy_events;   // to be used again; without time stamps, whose recording costs five times as much
   std::vector<kvr::DescBuf> descs;
   std::vector<kvr::PendingFree> pending_free;
   std::mutex mu;                          // every entry point holds it: calls on one pool are serialised
@@ -195,6 +198,8 @@ kvr_status look(kvr_pool *p, uint64_t seq, bool read_only);
 kvr_status wait_unlocked(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t seq, bool read_only, int64_t timeout_ms);
 kvr_status wait_locked(kvr_pool *p, uint64_t seq, int64_t timeout_ms);
 kvr_status stream_after(kvr_pool *p, cudaStream_t s, uint64_t seq, bool read_only);
+// drops copies on callers' streams that are through; if many are kept, looks
+kvr_status poll_copies(kvr_pool *p);
 // the same for a copy on a caller's stream
 kvr_status stream_after_copy(kvr_pool *p, cudaStream_t s, uint64_t number);
 kvr_status wait_copy(kvr_pool *p, std::unique_lock<std::mutex> &lock, uint64_t number, int64_t timeout_ms);
