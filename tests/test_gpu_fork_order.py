@@ -21,10 +21,10 @@ def make(nb, route="staged"):
     return p, dev, streams
 
 
-def busy(stream):
+def busy(stream, cycles=40_000_000):
     """About 20 ms of work."""
     with torch.cuda.stream(stream):
-        torch.cuda._sleep(40_000_000)
+        torch.cuda._sleep(cycles)
 
 
 def write(dev, nb, blocks, value, stream, rows=slice(None)):
