@@ -533,13 +533,15 @@ kvr_status kvr_cache_copy(const kvr_cache_spec *spec, void *device_pool, const i
  * The stream must not be under capture (KVR_ERR_INVALID_ARG).  With KVR_METADATA_ONLY they keep the books alone.
  *
  * kvr_request_fork: request new_id begins as the first n_tokens tokens of donor_id (ACTIVE or RETAINED): full blocks are shared, as in
- * kvr_request_admit_sharing, and the rows of a last block that is not full are copied into a block of its own, so either may go on writing.
- * A donor whose resume is in flight is waited for.  out_blocks as in kvr_request_admit.
+ * kvr_request_admit_sharing, and the rows of a last block that is not full are copied into a block of its own, so either may go on writing behind
+ * n_tokens.  Rows of shared blocks are both requests': n_tokens should not count drafted tokens that kvr_cache_keep may still move, on either side.
+ * A donor whose resume is in flight is waited for.  The tokens are there for kernels on `stream`.  out_blocks as in kvr_request_admit.
  *
  * kvr_request_resize: an ACTIVE request gets n_tokens tokens.  More: blocks from the head of the free queue are added.  Fewer (drafted tokens that
  * were not accepted): blocks behind the last are let go, in logical order; a last block that is then partly the request's, and that others refer
- * to, is replaced by a copy of its own.  A resume in flight is waited for.  out_blocks receives the whole table.
- *   both: KVR_HBM_FULL (nothing changes), KVR_ERR_UNKNOWN_REQUEST, KVR_ERR_BAD_STATE, KVR_ERR_INVALID_ARG
+ * to, is replaced by a copy of its own.  A resume in flight is waited for, and a suspend that still reads a block to be written.  out_blocks receives
+ * the whole table.
+ *   both: KVR_HBM_FULL, KVR_ERR_UNKNOWN_REQUEST, KVR_ERR_BAD_STATE, KVR_ERR_INVALID_ARG, KVR_ERR_CUDA (nothing changes)
  *
  * kvr_pool_compact: while a block that somebody refers to lies above a free one, the highest such block moves to the lowest free one, at most
  * max_moves times; every table that names it follows, the prefixes of requests on the host too, and it joins the free tail.  moves (HOST, 2 *

@@ -166,7 +166,7 @@ extern "C" kvr_status kvr_cache_attend(const kvr_cache_spec *spec, const void *d
       r4.stride = group_bytes < 256 ? group_bytes : group_bytes + (160 - group_bytes % 128) % 128;
       // tokens of a box: what divides a block and a stage
       for (r4.box_rows = 128; r4.box_rows >= 8 && (spec->block_size % r4.box_rows || stage_keys % r4.box_rows); r4.box_rows /= 2) {}
-      if (r4.box_rows < 8 || r4.stride > 2048) {             // (a box is at most 256 x 8 bytes wide)
+      if (r4.box_rows < 8) {                                 // (a box may be 256 x 8 bytes wide; 8 heads are at most 1,312)
         r4.box_rows = 0;
       } else {
         r4.box_bytes = r4.box_rows * r4.stride;

@@ -8,7 +8,10 @@
 // then the rows that a read looks at (four keys, 32 bytes of each) fall into different banks, with keys 4 to 7 of each 8 swapped in pairs.
 //
 // An element is widened to code times its group's scale, exactly: a conversion of two codes and a product of two f16.  The head's
-// scale multiplies the score (K) or the probability (V).  No pattern of bits is widened to NaN or infinity (a NaN lies in the head's scale
+// scale multiplies the score (K) or the probability (V).  Probability times scale is rounded to f16, for the matrix instructions take no more: by up to
+// 2^-11 of it, which comes to 2.0e-4 of an output over 8k random keys, a twentieth of a bf16 step.  So one bf16 output in ten, the small ones most, falls on the
+// other side of a rounding (8.6e-4 over all, against fp32 probabilities; from 64 bits 1.66e-3 instead of 1.65e-3).  Two products, with the upper and the
+// lower half of the bits, would have them all at twice the instructions of the second product.  No pattern of bits is widened to NaN or infinity (a NaN lies in the head's scale
 // alone), so what a row does not see needs no look at V.
 //
 // Eight warps share the heads, at 168 registers each (16 warps of 96 spill in the loop: 290 against 280 us, two tiles of rows 150 against 100), and take

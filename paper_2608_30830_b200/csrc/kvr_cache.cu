@@ -408,12 +408,12 @@ __global__ void __launch_bounds__(kThreads, 2) append_kernel(const __grid_consta
       char *row = a.c.base + (now == 2 ? a.c.v_offset : 0) + t.offset;
       if constexpr (four_bit(FMT)) {
         put4<LPH, kAhead>(x, row, at0 + sub, per_token, heads, a.c.head_dim, d0, live);
-        continue;
-      }
+      } else {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int head = at0 + i * per_token + sub;
-        put8<FMT, LPH>(x[i], row, a.c.scale_offset, head, a.c.head_dim, d0, live && head < heads);
+        for (int i = 0; i < kAhead; ++i) {
+          const int head = at0 + i * per_token + sub;
+          put8<FMT, LPH>(x[i], row, a.c.scale_offset, head, a.c.head_dim, d0, live && head < heads);
+        }
       }
     }
   }

@@ -460,7 +460,7 @@ kvr_status kvr_request_fork(kvr_pool *p, uint64_t id, uint64_t donor_id, int64_t
     r.blocks.swap(table);
     for (int32_t i = 0; i < full; ++i) p->fq.add_ref(r.blocks[i]);
     if (out_blocks && nb) memcpy(out_blocks, r.blocks.data(), (size_t)nb * 4);
-    // safe to write when the call returns, from any stream, but for what this one still copies
+    // a gather may still be reading the new block, which may be written on `stream` when the call returns
     if (tag && !p->meta_only) return wait_unlocked(p, enter.lock, tag, true, 60000);
     return KVR_OK;
   } catch (const std::bad_alloc &) {

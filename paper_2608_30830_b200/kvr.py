@@ -525,7 +525,8 @@ class Pool:
         return torch._C._cuda_getCurrentRawStream(self.device) if torch is not None and torch.cuda.is_initialized() else None
 
     def fork(self, rid, donor, n_tokens, stream=None):
-        """kvr_request_fork: (status, block table of the new request).  stream: a cudaStream_t; None is torch's current stream."""
+        """kvr_request_fork: (status, block table of the new request).  Full blocks are shared: n_tokens should not count drafted tokens that
+        keep() may still move.  stream: a cudaStream_t; None is torch's current stream."""
         return self._resized(lib().kvr_request_fork, n_tokens, rid, donor, self._stream(stream))
 
     def resize(self, rid, n_tokens, stream=None):
