@@ -235,6 +235,7 @@ kvr_status kvr_request_release(kvr_pool *pool, uint64_t req_id);
  * Sharing is by whole blocks: n_shared_blocks * block_size tokens must lie inside the new request and inside the
  * donor.  The donor may be ACTIVE or RETAINED (any of its full blocks) or on the HOST (its own shared prefix);
  * with n_shared_blocks = 0 the donor is ignored and the call equals kvr_request_admit.
+ * (While a donor's resume is in flight the prefix is still being filled: kvr_wait() on the donor before it is read.)
  * KVR_HBM_FULL, KVR_ERR_BAD_STATE (id exists, donor EXPIRED), KVR_ERR_UNKNOWN_REQUEST (donor), KVR_ERR_INVALID_ARG.
  */
 kvr_status kvr_request_admit_sharing(kvr_pool *pool, uint64_t req_id, int64_t n_tokens, uint64_t donor_id,

@@ -294,3 +294,32 @@ def test_a_current_stream_under_capture_is_refused():
         graph.replay()
         torch.cuda.synchronize()
         assert (x == 1).all() and p.info(1)[1]["n_tokens"] == 20
+
+
+def test_many_copies_under_way_on_several_streams():
+    """More than are kept before those that are through are looked for; then all of their blocks change hands."""
+    p, dev, _ = make(200)
+    streams = [torch.cuda.Stream() for _ in range(20)]       # more than one look tells apart
+    with p:
+        assert p.admit(1, 40)[0] == kvr.OK
+        was = rows(p, dev, 200, 1)
+        for turn in range(3):
+            torch.cuda.synchronize()
+            for s in streams[::2]:
+                busy(s, 4_000_000)
+            for i in range(190):
+                assert p.fork(10 + i, 1, 35 + i % 5, stream=streams[(i * 7 + turn) % 20].cuda_stream)[0] == kvr.OK
+            if turn == 1:
+                torch.cuda.synchronize()
+            if turn == 2:
+                for i in range(190):
+                    assert p.release(10 + i) == kvr.OK
+                st, table = p.admit(2, 190 * 16)
+                write(dev, 200, table, 9, streams[1])
+                torch.cuda.synchronize()
+                assert st == kvr.OK and (rows(p, dev, 200, 2) == 9).all() and torch.equal(rows(p, dev, 200, 1), was)
+                break
+            torch.cuda.synchronize()
+            for i in range(190):
+                assert torch.equal(rows(p, dev, 200, 10 + i), was[:, :, :35 + i % 5])
+                assert p.release(10 + i) == kvr.OK
